@@ -9,10 +9,10 @@ layer normalisation of the Transformer-shaped workloads).  Gradients of paramete
 where ``own`` is true, by the library.  ``exact`` has the definitions in 64 bits, written apart from the plain form.
 
     linear          z = x W^T + b,  y = residual + drop(act(z));  z is kept for the gradient where ``pre`` says so
-    input_grad      dx = residual + (dz W) * drop'(act'(pre))     (pre: the input of the activation that made x)
+    input_grad      dx = residual + drop((dz W) * act'(pre))      (pre: the input of the activation that made x)
     weight_grad     dW = dz^T x,  db = the sum of dz's rows
     dropout         y = residual + drop(act(x))
-    dropout_grad    dz = drop'(dy) * act'(pre)
+    dropout_grad    dz = drop(dy * act'(pre))
     norm            h = (v - mean) * rstd * w + b,  y = act(h), mean and rstd per sample and group
     norm_grad       dx (+ residual), dw, db
 
@@ -261,8 +261,9 @@ def _plain(st):
         y = y if res is None else res.float() + y
         return {"y": y.to(dt), "pre": z.to(dt)} if case["pre"] else {"y": y.to(dt)}
     if op == "input_grad":
-        dx = _drop(st["dz"].float() @ st["w"].float(), case["p"], st["seed"], st["offset"])
+        dx = st["dz"].float() @ st["w"].float()
         dx = dx if st["pre"] is None else dx * _act_slope(st["pre"].float(), case["act"])
+        dx = _drop(dx, case["p"], st["seed"], st["offset"])
         return {"dx": (dx if res is None else res.float() + dx).to(dt)}
     if op == "weight_grad":
         dz = st["dz"].float()
@@ -271,8 +272,9 @@ def _plain(st):
         y = _drop(_act(st["x"].float(), case["act"]), case["p"], st["seed"], st["offset"])
         return {"y": (y if res is None else res.float() + y).to(dt)}
     if op == "dropout_grad":
-        dz = _drop(st["dy"].float(), case["p"], st["seed"], st["offset"])
-        return {"dz": (dz if st["pre"] is None else dz * _act_slope(st["pre"].float(), case["act"])).to(dt)}
+        dz = st["dy"].float()
+        dz = dz if st["pre"] is None else dz * _act_slope(st["pre"].float(), case["act"])
+        return {"dz": _drop(dz, case["p"], st["seed"], st["offset"]).to(dt)}
     n, s, c, g = case["samples"], case["positions"], case["channels"], case["groups"]
     x = st["x"].float().view(n, s, g, c // g)
     w, b = st["w"].view(g, c // g), st["b"].view(g, c // g)
