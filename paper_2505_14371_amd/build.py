@@ -8,7 +8,8 @@ import sysconfig
 import warnings
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
-SOURCES = [os.path.join(_HERE, "csrc", f) for f in ("qoda_kernels.hip", "qoda_api.hip")]
+SOURCES = [os.path.join(_HERE, "csrc", f) for f in ("qoda_kernels.hip", "qoda_api.hip", "qoda_linear.hip", "qoda_dropout.hip",
+                                                     "qoda_group_norm.hip", "qoda_operators_api.hip")]
 LIB = os.path.join(_HERE, "libqoda.so")
 PROBE_SRC = os.path.join(_HERE, "harness", "qoda_probe.hip")
 TORCH_SRC = os.path.join(_HERE, "csrc", "qoda_torch.cpp")

@@ -1,0 +1,110 @@
+// Device code that the operators' kernels share: entries of the two types, activations and their derivatives, dropout's lots.
+#pragma once
+
+#include "qoda_operators.h"
+#include "qoda_philox.h"
+
+namespace qoda {
+
+typedef unsigned short u16;
+typedef unsigned int u32;
+
+struct bf16 { u16 bits; };
+
+__device__ __forceinline__ float to_float(float v) { return v; }
+__device__ __forceinline__ float to_float(bf16 v) { return __uint_as_float((u32)v.bits << 16); }
+// to nearest even; a NaN stays one
+__device__ __forceinline__ u32 bf16_bits(float v) {
+  const __bf16 b = (__bf16)v;
+  return __builtin_bit_cast(u16, b);
+}
+template <class T> __device__ __forceinline__ T from_float(float v);
+template <> __device__ __forceinline__ float from_float<float>(float v) { return v; }
+template <> __device__ __forceinline__ bf16 from_float<bf16>(float v) { return bf16{(u16)bf16_bits(v)}; }
+
+constexpr float kSlope = 0.2f;   // of leaky_relu
+constexpr float kLog2E = 1.4426950408889634f;
+
+// 1 - Phi(|z|) = erfc(|z| / sqrt 2) / 2 and exp(-z^2 / 2): formula 7.1.26 of Abramowitz and Stegun, erfc(x) = (a1 t + ... + a5 t^5) exp(-x^2)
+// with t = 1 / (1 + p x), whose error is at most 1.5e-7 -- that of 1 + erf in fp32.  The exponential is the density's too, so
+// the function and its derivative take one exponential and one reciprocal.
+__device__ __forceinline__ void normal_tail(float z, float &tail, float &e) {
+  const float x = fabsf(z) * 0.70710678118654752f;
+  const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3275911f, x, 1.0f));
+  e = __builtin_amdgcn_exp2f(z * z * (-0.5f * kLog2E));
+  float q = __builtin_fmaf(1.061405429f, t, -1.453152027f);
+  q = __builtin_fmaf(q, t, 1.421413741f);
+  q = __builtin_fmaf(q, t, -0.284496736f);
+  q = __builtin_fmaf(q, t, 0.254829592f);
+  tail = 0.5f * q * t * e;
+}
+
+template <int ACT>
+__device__ __forceinline__ float act(float z) {
+  if constexpr (ACT == kActRelu) return z < 0.0f ? 0.0f : z;   // a NaN stays one
+  if constexpr (ACT == kActLeakyRelu) return z > 0.0f ? z : kSlope * z;
+  if constexpr (ACT == kActGelu) {
+    float tail, e;
+    normal_tail(z, tail, e);
+    return z * (z < 0.0f ? tail : 1.0f - tail);
+  }
+  if constexpr (ACT == kActSilu) return z * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2E * z));
+  return z;
+}
+
+template <int ACT>
+__device__ __forceinline__ float act_slope(float z) {
+  if constexpr (ACT == kActRelu) return z > 0.0f ? 1.0f : 0.0f;
+  if constexpr (ACT == kActLeakyRelu) return z > 0.0f ? 1.0f : kSlope;
+  if constexpr (ACT == kActGelu) {
+    float tail, e;
+    normal_tail(z, tail, e);
+    return __builtin_fmaf(z * 0.39894228040143268f, e, z < 0.0f ? tail : 1.0f - tail);
+  }
+  if constexpr (ACT == kActSilu) {
+    const float s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2E * z));
+    return s * __builtin_fmaf(z, 1.0f - s, 1.0f);
+  }
+  return 1.0f;
+}
+
+// The same by an activation that is known at run time; the branch is one for the whole launch.
+__device__ __forceinline__ float act_of(int a, float z) {
+  switch (a) {
+    case kActRelu: return act<kActRelu>(z);
+    case kActLeakyRelu: return act<kActLeakyRelu>(z);
+    case kActGelu: return act<kActGelu>(z);
+    case kActSilu: return act<kActSilu>(z);
+    default: return z;
+  }
+}
+__device__ __forceinline__ float act_slope_of(int a, float z) {
+  switch (a) {
+    case kActRelu: return act_slope<kActRelu>(z);
+    case kActLeakyRelu: return act_slope<kActLeakyRelu>(z);
+    case kActGelu: return act_slope<kActGelu>(z);
+    case kActSilu: return act_slope<kActSilu>(z);
+    default: return 1.0f;
+  }
+}
+
+// The eight lots of entries 8 block .. 8 block + 7 of a row, as bits: bit j set where entry j is kept.
+__device__ __forceinline__ u32 kept_bits(const Drop &d, u32 row, u32 block) {
+  u32 w[4];
+  philox4x32_10(block, row, d.o0, d.o1, d.k0, d.k1, w);
+  u32 bits = 0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const u32 lot = j < 4 ? w[j & 3] & 0xFFFFu : w[j & 3] >> 16;
+    bits |= lot >= d.threshold ? 1u << j : 0u;
+  }
+  return bits;
+}
+
+// Entry `col` of a row after dropout.
+__device__ __forceinline__ float dropped(const Drop &d, u32 row, u32 col, float v) {
+  if (d.threshold == 0) return v;
+  return kept_bits(d, row, col >> 3) >> (col & 7) & 1 ? v * d.scale : 0.0f;
+}
+
+}  // namespace qoda
