@@ -1,4 +1,16 @@
 // Matrix products with what follows them fused into their stores: x w^T, dz w and dz^T x of include/qoda_operators.h.
+//
+// One kernel for the three forms and both types, on the matrix cores (16 x 16 sums by 32 bf16 products or 4 times 4 fp32 products an
+// entry).  A workgroup computes a tile of BM x BN sums, in steps of 128 bytes along l (64 bf16, 32 fp32): the step's two operand tiles
+// lie in shared memory twice, and while one pair is multiplied the next is on its way.  A lane's piece of an operand is 16 bytes: 8
+// bf16 (one matrix instruction) or 4 fp32 (four).
+//
+// Operands whose entries are adjacent along l ("rows") lie in shared memory as rows of 128 bytes; the others ("columns") as they are, a
+// row for each l, and are transposed as they are read (bf16: by the transposing read, which hands each lane four entries of a column).
+// In both the 16-byte chunks of a row are permuted by an exclusive or with bits of the row's number, so that the lanes of a read hit different banks.
+//
+// The matrix instruction's first operand is b's piece: a lane then holds four sums adjacent in a row of c, and b's entries are dealt
+// to the instructions so that those of two instructions are eight adjacent ones: 16 bytes of bf16 to store, and one block of lots.
 
 #include "qoda_operators_device.h"
 
@@ -6,61 +18,337 @@ namespace qoda {
 
 namespace {
 
-constexpr int kTile = 64, kDepth = 16;
+typedef u32 v4u __attribute__((ext_vector_type(4)));
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
+typedef short v4s __attribute__((ext_vector_type(4)));
 
-// c[i][j], after the sum over l, to where the call wants it.
-template <class T>
-__device__ __forceinline__ void finish(const Product &p, int i, int j, float c) {
-  if (p.form == kProductColumns) {
-    float *o = static_cast<float *>(p.out) + (long long)i * p.ldo + j;
-    *o = p.accumulate ? *o + c : c;
-    return;
-  }
-  if (p.form == kProductRows) {
-    if (p.bias) c = c + p.bias[j];
-    if (p.pre) static_cast<T *>(p.pre)[(long long)i * p.ldp + j] = from_float<T>(c);
-    c = act_of(p.activation, c);
-  } else if (p.pre) {
-    c = c * act_slope_of(p.activation, to_float(static_cast<const T *>(p.pre)[(long long)i * p.ldp + j]));
-  }
-  c = dropped(p.drop, i, j, c);
-  if (p.extra) c = to_float(static_cast<const T *>(p.extra)[(long long)i * p.lde + j]) + c;
-  static_cast<T *>(p.out)[(long long)i * p.ldo + j] = from_float<T>(c);
+constexpr int kStepBytes = 128;
+
+#define LDS(type, p) (reinterpret_cast<__attribute__((address_space(3))) type *>(p))
+typedef __attribute__((address_space(3))) char *lds_ptr;
+
+// The chunk's place in its row of a "rows" tile.  SIDE 1 (b): the 16 rows that a read touches are 8 q + 4 t + r; SIDE 0: 16 adjacent ones.
+template <int SIDE>
+__device__ __forceinline__ int row_swizzle(int row) {
+  return SIDE == 0 ? (row >> 1) & 7 : ((row >> 1) & 1) | ((row >> 2) & 6);
+}
+// ... and in row l of a "columns" tile.  bf16: a read touches rows 8 g + r and 32 (SIDE 0) or every other 8 of 64 bytes of each; fp32: rows
+// 4 g and 64 bytes, or every other 16 of 128.
+template <class T, int SIDE>
+__device__ __forceinline__ int column_swizzle(int l) {
+  if constexpr (sizeof(T) == 2) return SIDE == 0 ? ((l & 3) << 1) | (l & 8) : (l & 3) << 2;
+  else return SIDE == 0 ? l & 12 : ((l & 4) << 1) | ((l >> 3) & 1);
 }
 
-// A tile of 64 x 64 sums by 256 threads of 4 x 4, 16 deep through shared memory.
+// A chunk of 16 bytes of which the first `valid` entries (any number) exist; the others come as 0.
 template <class T>
-__global__ void __launch_bounds__(256) k_product(Product p) {
-  __shared__ float as[kDepth][kTile + 4], bs[kDepth][kTile + 4];
-  const int tiles_n = (p.n + kTile - 1) / kTile;
-  const int i0 = (int)(blockIdx.x / tiles_n) * kTile, j0 = (int)(blockIdx.x % tiles_n) * kTile;
-  const int t = threadIdx.x, ti = t / 16, tj = t % 16;
-  const T *a = static_cast<const T *>(p.a), *b = static_cast<const T *>(p.b);
-  float c[4][4] = {};
-  for (int l0 = 0; l0 < p.k; l0 += kDepth) {
-    for (int e = t; e < kTile * kDepth; e += 256) {
-      const bool rows = p.form != kProductColumns;
-      const int i = rows ? e / kDepth : e % kTile, l = rows ? e % kDepth : e / kTile;
-      as[l][i] = i0 + i < p.m && l0 + l < p.k ? to_float(a[rows ? (i0 + i) * p.lda + l0 + l : (l0 + l) * p.lda + i0 + i]) : 0.0f;
-    }
-    for (int e = t; e < kTile * kDepth; e += 256) {
-      const bool rows = p.form == kProductRows;
-      const int j = rows ? e / kDepth : e % kTile, l = rows ? e % kDepth : e / kTile;
-      bs[l][j] = j0 + j < p.n && l0 + l < p.k ? to_float(b[rows ? (j0 + j) * p.ldb + l0 + l : (l0 + l) * p.ldb + j0 + j]) : 0.0f;
-    }
-    __syncthreads();
-    for (int l = 0; l < kDepth; ++l)
+__device__ __forceinline__ v4u load_chunk(const T *p, int valid) {
+  constexpr int E = 16 / (int)sizeof(T);
+  v4u v = {0, 0, 0, 0};
+  if (valid >= E) {
+    __builtin_memcpy(&v, p, 16);
+  } else if constexpr (sizeof(T) == 4) {
 #pragma unroll
-      for (int x = 0; x < 4; ++x)
+    for (int j = 0; j < 4; ++j)
+      if (j < valid) v[j] = __builtin_bit_cast(u32, p[j]);
+  } else {
 #pragma unroll
-        for (int y = 0; y < 4; ++y) c[x][y] = __builtin_fmaf(as[l][4 * ti + x], bs[l][4 * tj + y], c[x][y]);
-    __syncthreads();
+    for (int j = 0; j < 8; ++j)
+      if (j < valid) v[j / 2] |= (u32)p[j].bits << (16 * (j & 1));
   }
-  for (int x = 0; x < 4; ++x)
-    for (int y = 0; y < 4; ++y) {
-      const int i = i0 + 4 * ti + x, j = j0 + 4 * tj + y;
-      if (i < p.m && j < p.n) finish<T>(p, i, j, c[x][y]);
+  return v;
+}
+
+// One operand's tile: N entries across (rows of c for SIDE 0, columns for SIDE 1) by a step of l, moved by the WG threads.
+template <class T, bool ROWS, int SIDE, int N, int WG>
+struct Operand {
+  static constexpr int E = 16 / (int)sizeof(T);                 // entries of a chunk
+  static constexpr int kStep = kStepBytes / (int)sizeof(T);     // l of a step
+  static constexpr int kRowChunks = ROWS ? 8 : N / E;           // chunks of a row in shared memory
+  static constexpr int kMine = N * 8 / WG;                      // chunks that a thread moves
+  static_assert(N * 8 % WG == 0, "whole chunks a thread");
+
+  const T *base;     // entry (first, 0)
+  long long ld;
+  int across, k;     // entries that exist across from the tile's first on, and along l
+  u32 offset[kMine]; // of the thread's chunks from the step's first entry, in bytes (direct loads)
+
+  // place q of the thread: row and (permuted) chunk in shared memory; the chunk it holds
+  static __device__ __forceinline__ void place(int q, int &row, int &chunk) {
+    const int at = q * WG + (int)threadIdx.x;
+    row = at / kRowChunks;
+    chunk = (at % kRowChunks) ^ (ROWS ? row_swizzle<SIDE>(row) : column_swizzle<T, SIDE>(row));
+  }
+  __device__ __forceinline__ void start(const void *p, long long ld_, int first, int end, int k0, int k_) {
+    ld = ld_;
+    across = end - first;
+    k = k_;
+    base = static_cast<const T *>(p) + (ROWS ? (long long)first * ld + k0 : (long long)k0 * ld + first);
+#pragma unroll
+    for (int q = 0; q < kMine; ++q) {
+      int row, chunk;
+      place(q, row, chunk);
+      // beyond the edge: what is loaded there is multiplied into sums that are not stored
+      if (ROWS) offset[q] = (u32)((row < across ? row : across - 1) * ld * (int)sizeof(T)) + chunk * 16;
+      else offset[q] = (u32)(row * ld * (int)sizeof(T)) + (chunk * E < across ? chunk * 16 : 0);
     }
+  }
+  // A whole step straight into shared memory: 16-byte aligned rows only.
+  __device__ __forceinline__ void direct(int l, lds_ptr to) const {
+    const char *p = reinterpret_cast<const char *>(base + (ROWS ? (long long)l : (long long)l * ld));
+#pragma unroll
+    for (int q = 0; q < kMine; ++q)
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(p + offset[q]),
+                                       (__attribute__((address_space(3))) void *)(to + (q * WG + (int)(threadIdx.x & ~63u)) * 16), 16, 0, 0);
+  }
+  // Any step by way of registers, entries beyond an edge 0.
+  __device__ __forceinline__ void fetch(int l, v4u (&v)[kMine]) const {
+#pragma unroll
+    for (int q = 0; q < kMine; ++q) {
+      int row, chunk;
+      place(q, row, chunk);
+      const int a = ROWS ? row : chunk * E, b = l + (ROWS ? chunk * E : row);
+      const int valid = ROWS ? (a < across ? k - b : 0) : (b < k ? across - a : 0);
+      v[q] = load_chunk<T>(base + (ROWS ? a * ld + b : b * ld + a), valid);
+    }
+  }
+  static __device__ __forceinline__ void store(const v4u (&v)[kMine], lds_ptr to) {
+#pragma unroll
+    for (int q = 0; q < kMine; ++q) *LDS(v4u, to + (q * WG + threadIdx.x) * 16) = v[q];
+  }
+  // The lane's piece of 16 entries across (from `first` on; SIDE 1: every other four from first + 4 t on), half s of the step.
+  static __device__ __forceinline__ v4u piece(lds_ptr tile, int first, int t, int s) {
+    const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+    const int a = first + (SIDE == 0 ? i : (i >> 2) * 8 + t * 4 + (i & 3));
+    if constexpr (ROWS) {
+      return *LDS(v4u, tile + a * 128 + (((s * 4 + g) ^ row_swizzle<SIDE>(a)) * 16));
+    } else if constexpr (sizeof(T) == 2) {
+      // the lane names four adjacent entries of row 8 g + i / 4 (and of the row four further on), and receives one column's four
+      const int c4 = first + (SIDE == 0 ? (i & 3) * 4 : (i & 3) * 8 + t * 4);   // its four entries
+      v4u v;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int l = s * 32 + g * 8 + h * 4 + (i >> 2);
+        const v4s r = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            LDS(v4s, tile + l * (N * 2) + (((c4 >> 3) ^ column_swizzle<T, SIDE>(l)) * 16) + (c4 & 4) * 2));
+        const uint2 w = __builtin_bit_cast(uint2, r);
+        v[2 * h] = w.x, v[2 * h + 1] = w.y;
+      }
+      return v;
+    } else {
+      v4u v;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int l = s * 16 + g * 4 + j;
+        v[j] = *LDS(u32, tile + l * (N * 4) + (((a >> 2) ^ column_swizzle<T, SIDE>(l)) * 16) + (a & 3) * 4);
+      }
+      return v;
+    }
+  }
+};
+
+template <class T>
+__device__ __forceinline__ v4f multiply(v4u b, v4u a, v4f c) {
+  if constexpr (sizeof(T) == 2) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, b), __builtin_bit_cast(v8bf, a), c, 0, 0, 0);
+  } else {
+    const v4f x = __builtin_bit_cast(v4f, b), y = __builtin_bit_cast(v4f, a);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[j], y[j], c, 0, 0, 0);
+    return c;
+  }
+}
+
+// Eight adjacent entries, of which the first n exist.
+template <class T>
+__device__ __forceinline__ void load8(const T *p, int n, float (&v)[8]) {
+  T e[8];
+  if (n >= 8) {
+    __builtin_memcpy(e, p, sizeof e);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) e[j] = j < n ? p[j] : from_float<T>(0.0f);
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = to_float(e[j]);
+}
+template <class T>
+__device__ __forceinline__ void store8(T *p, int n, const float (&v)[8]) {
+  T e[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) e[j] = from_float<T>(v[j]);
+  if (n >= 8) {
+    __builtin_memcpy(p, e, sizeof e);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (j < n) p[j] = e[j];
+  }
+}
+
+// c[i][j .. j + 7] (n of them exist; j a multiple of 8), after the sum over l, to where the call wants them.
+template <class T, int FORM>
+__device__ __forceinline__ void finish(const Product &p, int i, int j, int n, float (&c)[8]) {
+  if constexpr (FORM == kProductColumns) {
+    float *o = static_cast<float *>(p.out) + (long long)i * p.ldo + j;
+    if (p.accumulate) {
+      float was[8];
+      load8(o, n, was);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) c[e] = was[e] + c[e];
+    }
+    store8(o, n, c);
+  } else {
+    float other[8];
+    if constexpr (FORM == kProductRows) {
+      if (p.bias) {
+        load8(p.bias + j, n, other);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) c[e] = c[e] + other[e];
+      }
+      if (p.pre) store8(static_cast<T *>(p.pre) + (long long)i * p.ldp + j, n, c);
+      if (p.activation != kActNone)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) c[e] = act_of(p.activation, c[e]);
+    } else if (p.pre) {
+      load8(static_cast<const T *>(p.pre) + (long long)i * p.ldp + j, n, other);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) c[e] = c[e] * act_slope_of(p.activation, other[e]);
+    }
+    if (p.drop.threshold) {
+      const u32 kept = kept_bits(p.drop, (u32)i, (u32)j >> 3);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) c[e] = kept >> e & 1 ? c[e] * p.drop.scale : 0.0f;
+    }
+    if (p.extra) {
+      load8(static_cast<const T *>(p.extra) + (long long)i * p.lde + j, n, other);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) c[e] = other[e] + c[e];
+    }
+    store8(static_cast<T *>(p.out) + (long long)i * p.ldo + j, n, c);
+  }
+}
+
+// Workgroups go to the eight XCDs in turn, and each XCD has a cache of its own: an XCD gets a run of tiles that are adjacent in c, column by
+// column in bands of kBand rows of tiles, so that what its workgroups load at one time are few rows of a and few of b.
+constexpr int kXcds = 8, kBand = 8;
+__device__ __forceinline__ void tile_of(int id, int tiles_m, int tiles_n, int &tm, int &tn) {
+  const int total = tiles_m * tiles_n, x = id % kXcds, q = id / kXcds;
+  const int each = total / kXcds, more = total % kXcds;
+  const int at = x * each + (x < more ? x : more) + q;
+  const int band = at / (kBand * tiles_n), in = at - band * kBand * tiles_n;
+  const int rows = tiles_m - band * kBand < kBand ? tiles_m - band * kBand : kBand;
+  tm = band * kBand + in % rows;
+  tn = in / rows;
+}
+
+template <class T, int FORM, int BM, int BN, int WM, int WN, bool DIRECT>
+__global__ void __launch_bounds__(64 * WM * WN) k_product(Product p, int tiles_m, int tiles_n, int steps_each) {
+  constexpr int WG = 64 * WM * WN, FM = BM / WM / 16, FN = BN / WN / 32;
+  typedef Operand<T, FORM != kProductColumns, 0, BM, WG> A;
+  typedef Operand<T, FORM == kProductRows, 1, BN, WG> B;
+  constexpr int kStep = A::kStep;
+  __shared__ __align__(16) char a0[BM * kStepBytes], b0[BN * kStepBytes], a1[BM * kStepBytes], b1[BN * kStepBytes];
+
+  int tm, tn;
+  tile_of((int)blockIdx.x, tiles_m, tiles_n, tm, tn);
+  const int i0 = tm * BM, j0 = tn * BN;
+  const int k0 = (int)blockIdx.y * steps_each * kStep;
+  const int k = (long long)p.k - k0 < (long long)steps_each * kStep ? p.k - k0 : steps_each * kStep;   // of this split
+  const int steps = (k + kStep - 1) / kStep;
+  A a;
+  B b;
+  a.start(p.a, p.lda, i0, p.m, k0, k);
+  b.start(p.b, p.ldb, j0, p.n, k0, k);
+  const int wave = threadIdx.x / 64, wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
+
+  v4f c[FM][2 * FN];
+#pragma unroll
+  for (int x = 0; x < FM; ++x)
+#pragma unroll
+    for (int y = 0; y < 2 * FN; ++y) c[x][y] = v4f{0, 0, 0, 0};
+
+  v4u ra[A::kMine], rb[B::kMine];
+  const auto whole = [&](int t) { return DIRECT && (t + 1) * kStep <= k; };
+  const auto request = [&](int t, lds_ptr ta, lds_ptr tb) {
+    if (whole(t)) {
+      a.direct(t * kStep, ta);
+      b.direct(t * kStep, tb);
+    } else {
+      a.fetch(t * kStep, ra);
+      b.fetch(t * kStep, rb);
+    }
+  };
+  const auto arrive = [&](int t, lds_ptr ta, lds_ptr tb) {
+    if (!whole(t)) {
+      A::store(ra, ta);
+      B::store(rb, tb);
+    }
+  };
+  const auto compute = [&](lds_ptr ta, lds_ptr tb) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      v4u fa[FM], fb[2 * FN];
+#pragma unroll
+      for (int x = 0; x < FM; ++x) fa[x] = A::piece(ta, wm + x * 16, 0, s);
+#pragma unroll
+      for (int y = 0; y < 2 * FN; ++y) fb[y] = B::piece(tb, wn + y / 2 * 32, y & 1, s);
+#pragma unroll
+      for (int x = 0; x < FM; ++x)
+#pragma unroll
+        for (int y = 0; y < 2 * FN; ++y) c[x][y] = multiply<T>(fb[y], fa[x], c[x][y]);
+    }
+  };
+  const lds_ptr ta[2] = {(lds_ptr)a0, (lds_ptr)a1}, tb[2] = {(lds_ptr)b0, (lds_ptr)b1};
+  if (steps > 0) {
+    request(0, ta[0], tb[0]);
+    arrive(0, ta[0], tb[0]);
+  }
+  for (int t = 0; t < steps; t += 2) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      if (t + h < steps) {
+        __syncthreads();   // step t + h is there, and nobody reads the other pair any more
+        if (t + h + 1 < steps) request(t + h + 1, ta[1 - h], tb[1 - h]);
+        compute(ta[h], tb[h]);
+        if (t + h + 1 < steps) arrive(t + h + 1, ta[1 - h], tb[1 - h]);
+      }
+  }
+
+  const int lane = threadIdx.x & 63, g = lane >> 4;
+#pragma unroll
+  for (int x = 0; x < FM; ++x) {
+    const int i = i0 + wm + x * 16 + (lane & 15);
+    if (i < p.m)
+#pragma unroll
+      for (int y = 0; y < FN; ++y) {
+        const int j = j0 + wn + y * 32 + g * 8;
+        if (j < p.n) {
+          float v[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = c[x][2 * y + e / 4][e & 3];
+          if (p.partial) store8(p.partial + ((long long)blockIdx.y * p.m + i) * p.n + j, p.n - j, v);
+          else finish<T, FORM>(p, i, j, p.n - j, v);
+        }
+      }
+  }
+}
+
+// The splits' sums added up in their order, and finished.
+template <class T, int FORM>
+__global__ void __launch_bounds__(256) k_join(Product p, int splits) {
+  const long long blocks = (p.n + 7) / 8, total = (long long)p.m * blocks;
+  for (long long q = (long long)blockIdx.x * 256 + threadIdx.x; q < total; q += (long long)gridDim.x * 256) {
+    const int i = (int)(q / blocks), j = (int)(q - i * blocks) * 8, n = p.n - j;
+    float c[8] = {}, v[8];
+    for (int s = 0; s < splits; ++s) {
+      load8(p.partial + ((long long)s * p.m + i) * p.n + j, n, v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) c[e] = c[e] + v[e];
+    }
+    finish<T, FORM>(p, i, j, n, c);
+  }
 }
 
 // The sums of a's columns (a[l][i]): 64 columns a workgroup, its four waves take rows in turn.
@@ -81,16 +369,56 @@ __global__ void __launch_bounds__(256) k_column_sums(Product p) {
   }
 }
 
+struct Plan {
+  int tiles_m, tiles_n, splits, steps_each;
+  bool large, direct;
+};
+
+int step_of(const Product &p) { return kStepBytes / (p.type == kF32 ? 4 : 2); }
+
+Plan plan_of(const Product &p) {
+  Plan q = {};
+  const int e = p.type == kF32 ? 4 : 2;
+  const auto ok = [&](const void *v, long long ld, bool rows, int n) {
+    return reinterpret_cast<uintptr_t>(v) % 16 == 0 && ld * e % 16 == 0 && (rows ? n : step_of(p)) * ld * e < (1ll << 31);
+  };
+  q.direct = ok(p.a, p.lda, p.form != kProductColumns, 256) && ok(p.b, p.ldb, p.form == kProductRows, 256);
+  q.large = q.direct && (long long)((p.m + 255) / 256) * ((p.n + 255) / 256) >= 128;
+  const int side = q.large ? 256 : 128;
+  q.tiles_m = (p.m + side - 1) / side, q.tiles_n = (p.n + side - 1) / side;
+  const int steps = (p.k + step_of(p) - 1) / step_of(p);
+  q.splits = 1;
+  q.steps_each = steps > 0 ? steps : 1;
+  return q;
+}
+
+template <class T, int FORM>
+void launch(const Product &p, const Plan &q, hipStream_t s) {
+  const dim3 grid((unsigned)(q.tiles_m * q.tiles_n), (unsigned)q.splits);
+  if (q.large) k_product<T, FORM, 256, 256, 2, 4, true><<<grid, 512, 0, s>>>(p, q.tiles_m, q.tiles_n, q.steps_each);
+  else if (q.direct) k_product<T, FORM, 128, 128, 2, 2, true><<<grid, 256, 0, s>>>(p, q.tiles_m, q.tiles_n, q.steps_each);
+  else k_product<T, FORM, 128, 128, 2, 2, false><<<grid, 256, 0, s>>>(p, q.tiles_m, q.tiles_n, q.steps_each);
+}
+
+template <class T>
+void launch(const Product &p, const Plan &q, hipStream_t s) {
+  switch (p.form) {
+    case kProductRows: return launch<T, kProductRows>(p, q, s);
+    case kProductMixed: return launch<T, kProductMixed>(p, q, s);
+    default: return launch<T, kProductColumns>(p, q, s);
+  }
+}
+
 }  // namespace
 
 size_t product_scratch(const Product &) { return 0; }
 
 hipError_t launch_product(const Product &p, hipStream_t s) {
-  const long long tiles = (long long)((p.m + kTile - 1) / kTile) * ((p.n + kTile - 1) / kTile);
-  if (tiles > 0x7fffffffll) return hipErrorInvalidValue;
-  if (tiles > 0) {
-    if (p.type == kF32) k_product<float><<<dim3((unsigned)tiles), 256, 0, s>>>(p);
-    else k_product<bf16><<<dim3((unsigned)tiles), 256, 0, s>>>(p);
+  if (p.m && p.n) {
+    const Plan q = plan_of(p);
+    if ((long long)q.tiles_m * q.tiles_n > 0x7fffffffll) return hipErrorInvalidValue;
+    if (p.type == kF32) launch<float>(p, q, s);
+    else launch<bf16>(p, q, s);
   }
   if (p.sums) {
     if (p.type == kF32) k_column_sums<float><<<dim3((p.m + 63) / 64), 256, 0, s>>>(p);
