@@ -12,6 +12,8 @@
 // The matrix instruction's first operand is b's piece: a lane then holds four sums adjacent in a row of c, and b's entries are dealt
 // to the instructions so that those of two instructions are eight adjacent ones: 16 bytes of bf16 to store, and one block of lots.
 
+#include <type_traits>
+
 #include "qoda_operators_device.h"
 
 namespace qoda {
@@ -160,6 +162,20 @@ __device__ __forceinline__ v4f multiply(v4u b, v4u a, v4f c) {
   }
 }
 
+// The sum of a chunk's entries.
+template <class T>
+__device__ __forceinline__ float chunk_sum(v4u v) {
+  if constexpr (sizeof(T) == 2) {
+    float s[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) s[j] = __uint_as_float(v[j] << 16) + __uint_as_float(v[j] & 0xFFFF0000u);
+    return (s[0] + s[1]) + (s[2] + s[3]);
+  } else {
+    const v4f f = __builtin_bit_cast(v4f, v);
+    return (f[0] + f[1]) + (f[2] + f[3]);
+  }
+}
+
 // Eight adjacent entries, of which the first n exist.
 template <class T>
 __device__ __forceinline__ void load8(const T *p, int n, float (&v)[8]) {
@@ -188,7 +204,7 @@ __device__ __forceinline__ void store8(T *p, int n, const float (&v)[8]) {
 }
 
 // c[i][j .. j + 7] (n of them exist; j a multiple of 8), after the sum over l, to where the call wants them.
-template <class T, int FORM>
+template <class T, int FORM, int ACT>
 __device__ __forceinline__ void finish(const Product &p, int i, int j, int n, float (&c)[8]) {
   if constexpr (FORM == kProductColumns) {
     float *o = static_cast<float *>(p.out) + (long long)i * p.ldo + j;
@@ -208,13 +224,12 @@ __device__ __forceinline__ void finish(const Product &p, int i, int j, int n, fl
         for (int e = 0; e < 8; ++e) c[e] = c[e] + other[e];
       }
       if (p.pre) store8(static_cast<T *>(p.pre) + (long long)i * p.ldp + j, n, c);
-      if (p.activation != kActNone)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) c[e] = act_of(p.activation, c[e]);
-    } else if (p.pre) {
+      for (int e = 0; e < 8; ++e) c[e] = act<ACT>(c[e]);
+    } else if constexpr (ACT != kActNone) {
       load8(static_cast<const T *>(p.pre) + (long long)i * p.ldp + j, n, other);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) c[e] = c[e] * act_slope_of(p.activation, other[e]);
+      for (int e = 0; e < 8; ++e) c[e] = c[e] * act_slope<ACT>(other[e]);
     }
     if (p.drop.threshold) {
       const u32 kept = kept_bits(p.drop, (u32)i, (u32)j >> 3);
@@ -227,6 +242,19 @@ __device__ __forceinline__ void finish(const Product &p, int i, int j, int n, fl
       for (int e = 0; e < 8; ++e) c[e] = other[e] + c[e];
     }
     store8(static_cast<T *>(p.out) + (long long)i * p.ldo + j, n, c);
+  }
+}
+
+// Calls f with the activation as a constant: the choice is made once for all of a thread's sums.
+template <int FORM, class F>
+__device__ __forceinline__ void by_activation(int a, F &&f) {
+  if constexpr (FORM == kProductColumns) return f(std::integral_constant<int, kActNone>());
+  switch (a) {
+    case kActRelu: return f(std::integral_constant<int, kActRelu>());
+    case kActLeakyRelu: return f(std::integral_constant<int, kActLeakyRelu>());
+    case kActGelu: return f(std::integral_constant<int, kActGelu>());
+    case kActSilu: return f(std::integral_constant<int, kActSilu>());
+    default: return f(std::integral_constant<int, kActNone>());
   }
 }
 
@@ -269,104 +297,134 @@ __global__ void __launch_bounds__(64 * WM * WN) k_product(Product p, int tiles_m
 #pragma unroll
     for (int y = 0; y < 2 * FN; ++y) c[x][y] = v4f{0, 0, 0, 0};
 
-  v4u ra[A::kMine], rb[B::kMine];
-  const auto whole = [&](int t) { return DIRECT && (t + 1) * kStep <= k; };
-  const auto request = [&](int t, lds_ptr ta, lds_ptr tb) {
-    if (whole(t)) {
-      a.direct(t * kStep, ta);
-      b.direct(t * kStep, tb);
-    } else {
-      a.fetch(t * kStep, ra);
-      b.fetch(t * kStep, rb);
-    }
-  };
-  const auto arrive = [&](int t, lds_ptr ta, lds_ptr tb) {
-    if (!whole(t)) {
-      A::store(ra, ta);
-      B::store(rb, tb);
-    }
-  };
+  // the sums of a's columns: the waves of the first column of tiles share them, each for some of its rows of c
+  constexpr int FS = FM / WN > 0 ? FM / WN : 1;
+  const bool with_sums = FORM == kProductColumns && p.sums && tn == 0 && wave % WN * FS < FM;
+  float sum[FS] = {};
+
   const auto compute = [&](lds_ptr ta, lds_ptr tb) {
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
       v4u fa[FM], fb[2 * FN];
 #pragma unroll
-      for (int x = 0; x < FM; ++x) fa[x] = A::piece(ta, wm + x * 16, 0, s);
-#pragma unroll
       for (int y = 0; y < 2 * FN; ++y) fb[y] = B::piece(tb, wn + y / 2 * 32, y & 1, s);
+#pragma unroll
+      for (int x = 0; x < FM; ++x) fa[x] = A::piece(ta, wm + x * 16, 0, s);
 #pragma unroll
       for (int x = 0; x < FM; ++x)
 #pragma unroll
         for (int y = 0; y < 2 * FN; ++y) c[x][y] = multiply<T>(fb[y], fa[x], c[x][y]);
+      if constexpr (FORM == kProductColumns)
+        if (with_sums)
+#pragma unroll
+          for (int x = 0; x < FS; ++x) sum[x] = sum[x] + chunk_sum<T>(A::piece(ta, wm + (wave % WN * FS + x) * 16, 0, s));
     }
   };
   const lds_ptr ta[2] = {(lds_ptr)a0, (lds_ptr)a1}, tb[2] = {(lds_ptr)b0, (lds_ptr)b1};
-  if (steps > 0) {
-    request(0, ta[0], tb[0]);
-    arrive(0, ta[0], tb[0]);
-  }
-  for (int t = 0; t < steps; t += 2) {
+  int rest = 0;   // the first step that direct loads cannot move: all, or a last one that ends inside
+  if constexpr (DIRECT) {
+    const int whole = k / kStep;
+    rest = whole;
+    if (whole > 0) {
+      a.direct(0, ta[0]);
+      b.direct(0, tb[0]);
+    }
+    for (int t = 0; t < whole; t += 2) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-      if (t + h < steps) {
-        __syncthreads();   // step t + h is there, and nobody reads the other pair any more
-        if (t + h + 1 < steps) request(t + h + 1, ta[1 - h], tb[1 - h]);
-        compute(ta[h], tb[h]);
-        if (t + h + 1 < steps) arrive(t + h + 1, ta[1 - h], tb[1 - h]);
-      }
+      for (int h = 0; h < 2; ++h)
+        if (t + h < whole) {
+          __syncthreads();   // step t + h is there, and nobody reads the other pair any more
+          if (t + h + 1 < whole) {
+            a.direct((t + h + 1) * kStep, ta[1 - h]);
+            b.direct((t + h + 1) * kStep, tb[1 - h]);
+          }
+          compute(ta[h], tb[h]);
+        }
+    }
+  }
+  if (rest < steps) {
+    v4u ra[A::kMine], rb[B::kMine];
+    a.fetch(rest * kStep, ra);
+    b.fetch(rest * kStep, rb);
+    if (DIRECT) __syncthreads();   // nobody reads the first pair any more
+    A::store(ra, ta[0]);
+    B::store(rb, tb[0]);
+    for (int t = rest; t < steps; t += 2) {
+#pragma unroll
+      for (int h = 0; h < (DIRECT ? 1 : 2); ++h)
+        if (t + h < steps) {
+          __syncthreads();
+          if (!DIRECT && t + h + 1 < steps) {
+            a.fetch((t + h + 1) * kStep, ra);
+            b.fetch((t + h + 1) * kStep, rb);
+          }
+          compute(ta[h], tb[h]);
+          if (!DIRECT && t + h + 1 < steps) {
+            A::store(ra, ta[1 - h]);
+            B::store(rb, tb[1 - h]);
+          }
+        }
+    }
   }
 
   const int lane = threadIdx.x & 63, g = lane >> 4;
+  if constexpr (FORM == kProductColumns)
+    if (with_sums)
 #pragma unroll
-  for (int x = 0; x < FM; ++x) {
-    const int i = i0 + wm + x * 16 + (lane & 15);
-    if (i < p.m)
-#pragma unroll
-      for (int y = 0; y < FN; ++y) {
-        const int j = j0 + wn + y * 32 + g * 8;
-        if (j < p.n) {
-          float v[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = c[x][2 * y + e / 4][e & 3];
-          if (p.partial) store8(p.partial + ((long long)blockIdx.y * p.m + i) * p.n + j, p.n - j, v);
-          else finish<T, FORM>(p, i, j, p.n - j, v);
+      for (int x = 0; x < FS; ++x) {
+        float v = sum[x];   // of a quarter of every step's l
+        v = v + __shfl_xor(v, 16);
+        v = v + __shfl_xor(v, 32);
+        const int i = i0 + wm + (wave % WN * FS + x) * 16 + lane;
+        if (lane < 16 && i < p.m) {
+          if (p.partial) p.partial[(long long)gridDim.y * p.m * p.n + (long long)blockIdx.y * p.m + i] = v;
+          else p.sums[i] = p.accumulate ? p.sums[i] + v : v;
         }
       }
-  }
+  const auto each = [&](auto &&f) {
+#pragma unroll
+    for (int x = 0; x < FM; ++x) {
+      const int i = i0 + wm + x * 16 + (lane & 15);
+      if (i < p.m)
+#pragma unroll
+        for (int y = 0; y < FN; ++y) {
+          const int j = j0 + wn + y * 32 + g * 8;
+          if (j < p.n) {
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = c[x][2 * y + e / 4][e & 3];
+            f(i, j, p.n - j, v);
+          }
+        }
+    }
+  };
+  if (p.partial) each([&](int i, int j, int n, float (&v)[8]) { store8(p.partial + ((long long)blockIdx.y * p.m + i) * p.n + j, n, v); });
+  else by_activation<FORM>(p.activation, [&](auto a) { each([&](int i, int j, int n, float (&v)[8]) { finish<T, FORM, decltype(a)::value>(p, i, j, n, v); }); });
 }
 
 // The splits' sums added up in their order, and finished.
 template <class T, int FORM>
 __global__ void __launch_bounds__(256) k_join(Product p, int splits) {
-  const long long blocks = (p.n + 7) / 8, total = (long long)p.m * blocks;
-  for (long long q = (long long)blockIdx.x * 256 + threadIdx.x; q < total; q += (long long)gridDim.x * 256) {
-    const int i = (int)(q / blocks), j = (int)(q - i * blocks) * 8, n = p.n - j;
-    float c[8] = {}, v[8];
-    for (int s = 0; s < splits; ++s) {
-      load8(p.partial + ((long long)s * p.m + i) * p.n + j, n, v);
+  const long long blocks = (p.n + 7) / 8, total = (long long)p.m * blocks, first = (long long)blockIdx.x * 256 + threadIdx.x, stride = (long long)gridDim.x * 256;
+  by_activation<FORM>(p.activation, [&](auto a) {
+    for (long long q = first; q < total; q += stride) {
+      const int i = (int)(q / blocks), j = (int)(q - i * blocks) * 8, n = p.n - j;
+      float c[8] = {}, v[8];
+      for (int s = 0; s < splits; ++s) {
+        load8(p.partial + ((long long)s * p.m + i) * p.n + j, n, v);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) c[e] = c[e] + v[e];
+        for (int e = 0; e < 8; ++e) c[e] = c[e] + v[e];
+      }
+      finish<T, FORM, decltype(a)::value>(p, i, j, n, c);
     }
-    finish<T, FORM>(p, i, j, n, c);
-  }
-}
-
-// The sums of a's columns (a[l][i]): 64 columns a workgroup, its four waves take rows in turn.
-template <class T>
-__global__ void __launch_bounds__(256) k_column_sums(Product p) {
-  __shared__ float part[4][64];
-  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-  const long long i = (long long)blockIdx.x * 64 + lane;
-  const T *a = static_cast<const T *>(p.a);
-  float s = 0.0f;
-  if (i < p.m)
-    for (int l = wave; l < p.k; l += 4) s = s + to_float(a[l * p.lda + i]);
-  part[wave][lane] = s;
-  __syncthreads();
-  if (wave == 0 && i < p.m) {
-    s = (part[0][lane] + part[1][lane]) + (part[2][lane] + part[3][lane]);
-    p.sums[i] = p.accumulate ? p.sums[i] + s : s;
-  }
+  });
+  if constexpr (FORM == kProductColumns)
+    if (p.sums)
+      for (long long i = first; i < p.m; i += stride) {
+        float v = 0.0f;
+        for (int s = 0; s < splits; ++s) v = v + p.partial[(long long)splits * p.m * p.n + (long long)s * p.m + i];
+        p.sums[i] = p.accumulate ? p.sums[i] + v : v;
+      }
 }
 
 struct Plan {
@@ -382,10 +440,10 @@ Plan plan_of(const Product &p) {
   const auto ok = [&](const void *v, long long ld, bool rows, int n) {
     return reinterpret_cast<uintptr_t>(v) % 16 == 0 && ld * e % 16 == 0 && (rows ? n : step_of(p)) * ld * e < (1ll << 31);
   };
-  q.direct = ok(p.a, p.lda, p.form != kProductColumns, 256) && ok(p.b, p.ldb, p.form == kProductRows, 256);
+  q.direct = p.n > 0 && ok(p.a, p.lda, p.form != kProductColumns, 256) && ok(p.b, p.ldb, p.form == kProductRows, 256);
   q.large = q.direct && (long long)((p.m + 255) / 256) * ((p.n + 255) / 256) >= 128;
   const int side = q.large ? 256 : 128;
-  q.tiles_m = (p.m + side - 1) / side, q.tiles_n = (p.n + side - 1) / side;
+  q.tiles_m = (p.m + side - 1) / side, q.tiles_n = p.n > 0 ? (p.n + side - 1) / side : 1;
   const int steps = (p.k + step_of(p) - 1) / step_of(p);
   q.splits = 1;
   q.steps_each = steps > 0 ? steps : 1;
@@ -413,17 +471,14 @@ void launch(const Product &p, const Plan &q, hipStream_t s) {
 
 size_t product_scratch(const Product &) { return 0; }
 
-hipError_t launch_product(const Product &p, hipStream_t s) {
-  if (p.m && p.n) {
-    const Plan q = plan_of(p);
-    if ((long long)q.tiles_m * q.tiles_n > 0x7fffffffll) return hipErrorInvalidValue;
-    if (p.type == kF32) launch<float>(p, q, s);
-    else launch<bf16>(p, q, s);
-  }
-  if (p.sums) {
-    if (p.type == kF32) k_column_sums<float><<<dim3((p.m + 63) / 64), 256, 0, s>>>(p);
-    else k_column_sums<bf16><<<dim3((p.m + 63) / 64), 256, 0, s>>>(p);
-  }
+hipError_t launch_product(const Product &call, hipStream_t s) {
+  Product p = call;
+  // without columns of c there is still one of tiles, for the sums of a's columns
+  const Plan q = plan_of(p);
+  if ((long long)q.tiles_m * q.tiles_n > 0x7fffffffll) return hipErrorInvalidValue;
+  if (q.splits == 1) p.partial = nullptr;
+  if (p.type == kF32) launch<float>(p, q, s);
+  else launch<bf16>(p, q, s);
   return hipGetLastError();
 }
 
