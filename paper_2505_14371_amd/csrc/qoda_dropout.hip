@@ -6,52 +6,93 @@ namespace qoda {
 
 namespace {
 
-// A thread takes the eight entries of one block of lots at a time.
-template <class T, int ACT, bool GRAD>
-__global__ void __launch_bounds__(256) k_entries(Entries e) {
-  const long long blocks = (e.cols + 7) / 8, total = e.rows * blocks;
+// Whole-number division of 32-bit numbers by one that a launch knows, as a product (Granlund and Montgomery 1994).
+struct Divisor {
+  u32 d, magic, shift1, shift2;
+};
+Divisor divisor(u32 d) {
+  int l = 0;
+  while (l < 32 && (1ull << l) < d) ++l;
+  return {d, (u32)(((1ull << l) - d) * (1ull << 32) / d + 1), l > 0 ? 1u : 0u, l > 0 ? (u32)(l - 1) : 0u};
+}
+__device__ __forceinline__ u32 divide(u32 v, const Divisor &d) {
+  const u32 t = __umulhi(d.magic, v);
+  return (t + ((v - t) >> d.shift1)) >> d.shift2;
+}
+
+constexpr int kEach = 4;   // blocks of eight entries a thread: so many loads on their way while the first block's lots are drawn
+
+// A thread takes blocks of eight entries, which share one draw of lots: 16 bytes of bf16.
+template <class T, int ACT, bool GRAD, bool EXTRA, bool DROP>
+__global__ void __launch_bounds__(256) k_entries(Entries e, Divisor blocks) {
+  // the workgroup's first block by a 64-bit division, the others from it in 32 bits
+  const long long total = e.rows * blocks.d, q0 = (long long)blockIdx.x * (256 * kEach);
+  const long long row0 = q0 / blocks.d;
+  const u32 col0 = (u32)(q0 - row0 * blocks.d);
   const T *x = static_cast<const T *>(e.x), *extra = static_cast<const T *>(e.extra);
-  T *y = static_cast<T *>(e.y);
-  for (long long q = (long long)blockIdx.x * 256 + threadIdx.x; q < total; q += (long long)gridDim.x * 256) {
-    const long long row = q / blocks, c0 = (q - row * blocks) * 8;
-    const u32 kept = e.drop.threshold ? kept_bits(e.drop, (u32)row, (u32)(c0 / 8)) : 0xFFu;
-    const float scale = e.drop.threshold ? e.drop.scale : 1.0f;
-    for (int j = 0; j < 8 && c0 + j < e.cols; ++j) {
-      float v = to_float(x[row * e.ldx + c0 + j]);
-      const float o = extra ? to_float(extra[row * e.lde + c0 + j]) : 0.0f;
-      if (GRAD) v = ACT == kActNone ? v : v * act_slope<ACT>(o);
-      else v = act<ACT>(v);
-      v = kept >> j & 1 ? v * scale : 0.0f;
-      if (!GRAD && extra) v = o + v;
-      y[row * e.ldy + c0 + j] = from_float<T>(v);
+  Eight<T> mine[kEach], other[kEach];
+  long long row[kEach];
+  u32 block[kEach];
+  int n[kEach];
+#pragma unroll
+  for (int u = 0; u < kEach; ++u) {
+    const u32 at = col0 + u * 256 + threadIdx.x, r = divide(at, blocks);
+    row[u] = row0 + r;
+    block[u] = at - r * blocks.d;
+    n[u] = q0 + u * 256 + threadIdx.x < total ? (int)(e.cols - (long long)block[u] * 8) : 0;
+    if (n[u] > 0) {
+      mine[u].load(x + row[u] * e.ldx + (long long)block[u] * 8, n[u]);
+      if (EXTRA) other[u].load(extra + row[u] * e.lde + (long long)block[u] * 8, n[u]);
     }
   }
+#pragma unroll
+  for (int u = 0; u < kEach; ++u)
+    if (n[u] > 0) {
+      float v[8], o[8];
+      mine[u].get(v);
+      if (EXTRA) other[u].get(o);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = !GRAD ? act<ACT>(v[j]) : EXTRA ? v[j] * act_slope<ACT>(o[j]) : v[j];
+      if (DROP) drop8(e.drop, (u32)row[u], block[u], v);
+      if (!GRAD && EXTRA)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = o[j] + v[j];
+      store8(static_cast<T *>(e.y) + row[u] * e.ldy + (long long)block[u] * 8, n[u], v);
+    }
+}
+
+template <class T, int ACT, bool GRAD, bool EXTRA>
+void launch(const Entries &e, unsigned grid, const Divisor &d, hipStream_t s) {
+  if (e.drop.threshold) k_entries<T, ACT, GRAD, EXTRA, true><<<dim3(grid), 256, 0, s>>>(e, d);
+  else k_entries<T, ACT, GRAD, EXTRA, false><<<dim3(grid), 256, 0, s>>>(e, d);
 }
 
 template <class T, int ACT>
-void launch(const Entries &e, unsigned grid, hipStream_t s) {
-  if (e.gradient) k_entries<T, ACT, true><<<dim3(grid), 256, 0, s>>>(e);
-  else k_entries<T, ACT, false><<<dim3(grid), 256, 0, s>>>(e);
+void launch(const Entries &e, unsigned grid, const Divisor &d, hipStream_t s) {
+  if (e.gradient) launch<T, ACT, true, ACT != kActNone>(e, grid, d, s);
+  else if (e.extra) launch<T, ACT, false, true>(e, grid, d, s);
+  else launch<T, ACT, false, false>(e, grid, d, s);
 }
 
 template <class T>
-void launch(const Entries &e, unsigned grid, hipStream_t s) {
+void launch(const Entries &e, unsigned grid, const Divisor &d, hipStream_t s) {
   switch (e.activation) {
-    case kActRelu: return launch<T, kActRelu>(e, grid, s);
-    case kActLeakyRelu: return launch<T, kActLeakyRelu>(e, grid, s);
-    case kActGelu: return launch<T, kActGelu>(e, grid, s);
-    case kActSilu: return launch<T, kActSilu>(e, grid, s);
-    default: return launch<T, kActNone>(e, grid, s);
+    case kActRelu: return launch<T, kActRelu>(e, grid, d, s);
+    case kActLeakyRelu: return launch<T, kActLeakyRelu>(e, grid, d, s);
+    case kActGelu: return launch<T, kActGelu>(e, grid, d, s);
+    case kActSilu: return launch<T, kActSilu>(e, grid, d, s);
+    default: return launch<T, kActNone>(e, grid, d, s);
   }
 }
 
 }  // namespace
 
 hipError_t launch_entries(const Entries &e, hipStream_t s) {
-  const long long blocks = e.rows * ((e.cols + 7) / 8), groups = (blocks + 255) / 256;
-  const unsigned grid = (unsigned)(groups < 65536 ? groups : 65536);
-  if (e.type == kF32) launch<float>(e, grid, s);
-  else launch<bf16>(e, grid, s);
+  const u32 blocks = (u32)((e.cols + 7) / 8);
+  const long long groups = (e.rows * blocks + 256 * kEach - 1) / (256 * kEach);
+  if (groups > 0x7fffffffll) return hipErrorInvalidValue;
+  if (e.type == kF32) launch<float>(e, (unsigned)groups, divisor(blocks), s);
+  else launch<bf16>(e, (unsigned)groups, divisor(blocks), s);
   return hipGetLastError();
 }
 

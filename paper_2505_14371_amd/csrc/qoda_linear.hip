@@ -176,33 +176,6 @@ __device__ __forceinline__ float chunk_sum(v4u v) {
   }
 }
 
-// Eight adjacent entries, of which the first n exist.
-template <class T>
-__device__ __forceinline__ void load8(const T *p, int n, float (&v)[8]) {
-  T e[8];
-  if (n >= 8) {
-    __builtin_memcpy(e, p, sizeof e);
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) e[j] = j < n ? p[j] : from_float<T>(0.0f);
-  }
-#pragma unroll
-  for (int j = 0; j < 8; ++j) v[j] = to_float(e[j]);
-}
-template <class T>
-__device__ __forceinline__ void store8(T *p, int n, const float (&v)[8]) {
-  T e[8];
-#pragma unroll
-  for (int j = 0; j < 8; ++j) e[j] = from_float<T>(v[j]);
-  if (n >= 8) {
-    __builtin_memcpy(p, e, sizeof e);
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (j < n) p[j] = e[j];
-  }
-}
-
 // c[i][j .. j + 7] (n of them exist; j a multiple of 8), after the sum over l, to where the call wants them.
 template <class T, int FORM, int ACT>
 __device__ __forceinline__ void finish(const Product &p, int i, int j, int n, float (&c)[8]) {
@@ -231,11 +204,7 @@ __device__ __forceinline__ void finish(const Product &p, int i, int j, int n, fl
 #pragma unroll
       for (int e = 0; e < 8; ++e) c[e] = c[e] * act_slope<ACT>(other[e]);
     }
-    if (p.drop.threshold) {
-      const u32 kept = kept_bits(p.drop, (u32)i, (u32)j >> 3);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) c[e] = kept >> e & 1 ? c[e] * p.drop.scale : 0.0f;
-    }
+    if (p.drop.threshold) drop8(p.drop, (u32)i, (u32)j >> 3, c);
     if (p.extra) {
       load8(static_cast<const T *>(p.extra) + (long long)i * p.lde + j, n, other);
 #pragma unroll

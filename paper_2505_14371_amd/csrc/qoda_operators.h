@@ -10,9 +10,10 @@ enum EntryType { kF32 = 0, kBf16 = 1 };
 enum Activation { kActNone = 0, kActRelu = 1, kActLeakyRelu = 2, kActGelu = 3, kActSilu = 4 };
 constexpr int kNumActivations = 5;
 
-// Dropout of a call: entries whose lot is below the threshold are dropped, the others multiplied by the scale.  threshold 0: none.
+// Dropout of a call: entries whose lot is below the threshold are dropped, the others multiplied by the scale.  limit: 2^16 threshold - 1,
+// modulo 2^32 (of no use with threshold 0, which drops nothing).
 struct Drop {
-  unsigned int threshold;
+  unsigned int threshold, limit;
   float scale;
   unsigned int k0, k1, o0, o1;   // the generator's key and the upper half of its counter
 };

@@ -61,7 +61,7 @@ int make_drop(const char *call, double p, uint64_t seed, uint64_t offset, Drop *
   if (!(p >= 0.0 && p <= 1.0)) return fail(QODA_EINVAL, "%s: p = %g is not in [0, 1]", call, p);
   const unsigned int t = (unsigned int)std::floor(p * 65536.0 + 0.5);
   const uint64_t key = seed ^ QODA_DROPOUT_KEY;
-  *d = {t, t < 65536u ? (float)(65536.0 / (65536u - t)) : 0.0f, (unsigned int)key, (unsigned int)(key >> 32), (unsigned int)offset,
+  *d = {t, (t << 16) - 1u, t < 65536u ? (float)(65536.0 / (65536u - t)) : 0.0f, (unsigned int)key, (unsigned int)(key >> 32), (unsigned int)offset,
         (unsigned int)(offset >> 32)};
   return QODA_OK;
 }

@@ -88,23 +88,50 @@ __device__ __forceinline__ float act_slope_of(int a, float z) {
   }
 }
 
-// The eight lots of entries 8 block .. 8 block + 7 of a row, as bits: bit j set where entry j is kept.
-__device__ __forceinline__ u32 kept_bits(const Drop &d, u32 row, u32 block) {
+// Dropout of the eight entries 8 block .. 8 block + 7 of a row.  A lot is compared where it lies, in the upper half of a word: lot >= threshold
+// is lot << 16 > (threshold << 16) - 1, and what is below the lot does not change that.
+__device__ __forceinline__ void drop8(const Drop &d, u32 row, u32 block, float (&v)[8]) {
   u32 w[4];
   philox4x32_10(block, row, d.o0, d.o1, d.k0, d.k1, w);
-  u32 bits = 0;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const u32 lot = j < 4 ? w[j & 3] & 0xFFFFu : w[j & 3] >> 16;
-    bits |= lot >= d.threshold ? 1u << j : 0u;
-  }
-  return bits;
+  for (int j = 0; j < 8; ++j) v[j] = (j < 4 ? w[j & 3] << 16 : w[j & 3]) > d.limit ? v[j] * d.scale : 0.0f;
 }
 
-// Entry `col` of a row after dropout.
-__device__ __forceinline__ float dropped(const Drop &d, u32 row, u32 col, float v) {
-  if (d.threshold == 0) return v;
-  return kept_bits(d, row, col >> 3) >> (col & 7) & 1 ? v * d.scale : 0.0f;
+// Eight adjacent entries as they lie in memory, of which the first n exist (the others are read as 0 and not stored).
+template <class T>
+struct Eight {
+  T e[8];
+  __device__ __forceinline__ void load(const T *p, int n) {
+    if (n >= 8) {
+      __builtin_memcpy(e, p, sizeof e);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) e[j] = j < n ? p[j] : from_float<T>(0.0f);
+    }
+  }
+  __device__ __forceinline__ void get(float (&v)[8]) const {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = to_float(e[j]);
+  }
+};
+template <class T>
+__device__ __forceinline__ void load8(const T *p, int n, float (&v)[8]) {
+  Eight<T> r;
+  r.load(p, n);
+  r.get(v);
+}
+template <class T>
+__device__ __forceinline__ void store8(T *p, int n, const float (&v)[8]) {
+  T e[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) e[j] = from_float<T>(v[j]);
+  if (n >= 8) {
+    __builtin_memcpy(p, e, sizeof e);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (j < n) p[j] = e[j];
+  }
 }
 
 }  // namespace qoda
