@@ -97,21 +97,56 @@ __device__ __forceinline__ void drop8(const Drop &d, u32 row, u32 block, float (
   for (int j = 0; j < 8; ++j) v[j] = (j < 4 ? w[j & 3] << 16 : w[j & 3]) > d.limit ? v[j] * d.scale : 0.0f;
 }
 
-// Eight adjacent entries as they lie in memory, of which the first n exist (the others are read as 0 and not stored).
+// Eight adjacent entries as they lie in memory, of which the first n exist (the others are read as 0 and not stored).  Words, so that
+// they move 16 bytes at a time at any alignment.
+typedef u32 v4u __attribute__((ext_vector_type(4)));
 template <class T>
 struct Eight {
-  T e[8];
+  static constexpr int kWords = sizeof(T) * 2;
+  v4u w[kWords / 4];
   __device__ __forceinline__ void load(const T *p, int n) {
     if (n >= 8) {
-      __builtin_memcpy(e, p, sizeof e);
-    } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) e[j] = j < n ? p[j] : from_float<T>(0.0f);
+      for (int q = 0; q < kWords / 4; ++q) __builtin_memcpy(&w[q], reinterpret_cast<const char *>(p) + 16 * q, 16);
+    } else {
+      u32 e[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if constexpr (sizeof(T) == 4) e[j] = j < n ? __builtin_bit_cast(u32, p[j]) : 0u;
+        else e[j] = j < n ? p[j].bits : 0u;
+      }
+#pragma unroll
+      for (int j = 0; j < kWords; ++j) w[j / 4][j % 4] = sizeof(T) == 4 ? e[j] : e[2 * j % 8] | e[(2 * j + 1) % 8] << 16;
     }
   }
   __device__ __forceinline__ void get(float (&v)[8]) const {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = to_float(e[j]);
+    for (int j = 0; j < 8; ++j) {
+      if constexpr (sizeof(T) == 4) v[j] = __uint_as_float(w[j / 4][j % 4]);
+      else v[j] = __uint_as_float(j & 1 ? w[0][j / 2] & 0xFFFF0000u : w[0][j / 2] << 16);
+    }
+  }
+  __device__ __forceinline__ void set(const float (&v)[8]) {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) w[j / 4][j % 4] = __float_as_uint(v[j]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[0][j] = bf16_bits(v[2 * j]) | bf16_bits(v[2 * j + 1]) << 16;
+    }
+  }
+  __device__ __forceinline__ void store(T *p, int n) const {
+    if (n >= 8) {
+#pragma unroll
+      for (int q = 0; q < kWords / 4; ++q) __builtin_memcpy(reinterpret_cast<char *>(p) + 16 * q, &w[q], 16);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (j < n) {
+          if constexpr (sizeof(T) == 4) p[j] = __uint_as_float(w[j / 4][j % 4]);
+          else p[j].bits = (u16)(w[0][j / 2] >> (16 * (j & 1)));
+        }
+    }
   }
 };
 template <class T>
@@ -122,16 +157,9 @@ __device__ __forceinline__ void load8(const T *p, int n, float (&v)[8]) {
 }
 template <class T>
 __device__ __forceinline__ void store8(T *p, int n, const float (&v)[8]) {
-  T e[8];
-#pragma unroll
-  for (int j = 0; j < 8; ++j) e[j] = from_float<T>(v[j]);
-  if (n >= 8) {
-    __builtin_memcpy(p, e, sizeof e);
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (j < n) p[j] = e[j];
-  }
+  Eight<T> r;
+  r.set(v);
+  r.store(p, n);
 }
 
 }  // namespace qoda
