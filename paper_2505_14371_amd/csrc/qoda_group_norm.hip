@@ -1,4 +1,14 @@
 // Group normalisation with an activation, channels last, and its gradient (include/qoda_operators.h).
+//
+// Every value is read once where a group's values fit the registers of a workgroup: the mean, the squares about it and the result all
+// come from there, so that the variance is no difference of large sums.  Two shapes of work:
+//   rows   one position: a group is one run of adjacent channels.  A team of lanes takes a row, eight entries a lane at a time.
+//   maps   several positions: a workgroup takes a block of channels that holds whole groups (or a part of one large group) at some or
+//          all positions; a thread owns eight channels at every so many positions.  Sums run per channel first, because that is what the
+//          gradients of weight and bias are, and a group's are sums of its channels'.  Where a block has more values than a workgroup holds, its
+//          positions are split: one launch for the pieces' sums, one that joins them and makes the result.
+
+#include <type_traits>
 
 #include "qoda_operators_device.h"
 
@@ -6,128 +16,895 @@ namespace qoda {
 
 namespace {
 
-// The sum over the workgroup's 256 threads, in all of them.
-__device__ float block_sum(float v, float *red) {
-  __syncthreads();
-  red[threadIdx.x] = v;
-  __syncthreads();
-  for (int h = 128; h > 0; h /= 2) {
-    if (threadIdx.x < h) red[threadIdx.x] = red[threadIdx.x] + red[threadIdx.x + h];
+constexpr int kThreads = 256;
+
+// Sums over teams of 16 or 64 adjacent lanes, the same in every lane.
+template <int TEAM>
+__device__ __forceinline__ float lanes_sum(float v) {
+  const auto move = [](float x, auto ctrl) {
+    return __uint_as_float((u32)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), decltype(ctrl)::value, 0xF, 0xF, true));
+  };
+  v = v + move(v, std::integral_constant<int, 0xB1>());    // lane ^ 1
+  v = v + move(v, std::integral_constant<int, 0x4E>());    // lane ^ 2
+  v = v + move(v, std::integral_constant<int, 0x141>());   // the other four of eight
+  v = v + move(v, std::integral_constant<int, 0x140>());   // the other eight of sixteen
+  if constexpr (TEAM == 64) {
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(b[0]) + __uint_as_float(b[1]);
+  }
+  return v;
+}
+// ... of a team that may be the whole workgroup.  red: a float for each wave, free again after the next barrier.
+template <int TEAM>
+__device__ __forceinline__ float team_sum(float v, float *red) {
+  if constexpr (TEAM <= 64) {
+    return lanes_sum<TEAM>(v);
+  } else {
+    v = lanes_sum<64>(v);
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x / 64] = v;
     __syncthreads();
+    float s = 0.0f;
+#pragma unroll
+    for (int w = 0; w < TEAM / 64; ++w) s = s + red[w];
+    return s;
   }
-  return red[0];
 }
 
-// A workgroup for each (sample, group): the mean, then the squares about it, then the values.
-template <class T>
-__global__ void __launch_bounds__(256) k_norm(GroupNorm g) {
-  __shared__ float red[256];
-  const long long n = blockIdx.x / g.groups, gr = blockIdx.x % g.groups, per = g.channels / g.groups, total = per * g.positions;
-  const T *x = static_cast<const T *>(g.x) + n * g.x_sample + gr * per;
-  T *y = static_cast<T *>(g.out) + n * g.out_sample + gr * per;
+__device__ __forceinline__ void vector8(const float *p, float otherwise, int n, float (&v)[8]) {
+  if (p) {
+    load8(p, n, v);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = otherwise;
+  }
+}
+
+__device__ __forceinline__ void act8(int a, float (&v)[8]) {
+  const auto all = [&](auto c) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = act<decltype(c)::value>(v[j]);
+  };
+  switch (a) {
+    case kActRelu: return all(std::integral_constant<int, kActRelu>());
+    case kActLeakyRelu: return all(std::integral_constant<int, kActLeakyRelu>());
+    case kActGelu: return all(std::integral_constant<int, kActGelu>());
+    case kActSilu: return all(std::integral_constant<int, kActSilu>());
+    default: return;
+  }
+}
+// v times the slope at z
+__device__ __forceinline__ void slope8(int a, const float (&z)[8], float (&v)[8]) {
+  const auto all = [&](auto c) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = v[j] * act_slope<decltype(c)::value>(z[j]);
+  };
+  switch (a) {
+    case kActRelu: return all(std::integral_constant<int, kActRelu>());
+    case kActLeakyRelu: return all(std::integral_constant<int, kActLeakyRelu>());
+    case kActGelu: return all(std::integral_constant<int, kActGelu>());
+    case kActSilu: return all(std::integral_constant<int, kActSilu>());
+    default: return;
+  }
+}
+
+// Eight normalised values times weight plus bias, through the activation.
+__device__ __forceinline__ void normalised8(const GroupNorm &g, long long c, int n, float mean, float rstd, float (&v)[8]) {
+  float w[8], b[8];
+  vector8(g.weight ? g.weight + c : nullptr, 1.0f, n, w);
+  vector8(g.bias ? g.bias + c : nullptr, 0.0f, n, b);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = __builtin_fmaf((v[j] - mean) * rstd, w[j], b[j]);
+  act8(g.activation, v);
+}
+
+// h: the normalised values of x; d: dy through the activation; w: the weights.
+__device__ __forceinline__ void back8(const GroupNorm &g, long long c, int n, float mean, float rstd, float (&h)[8], float (&d)[8], float (&w)[8]) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) h[j] = (h[j] - mean) * rstd;
+  vector8(g.weight ? g.weight + c : nullptr, 1.0f, n, w);
+  if (g.activation != kActNone) {
+    float z[8];
+    vector8(g.bias ? g.bias + c : nullptr, 0.0f, n, z);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) z[j] = __builtin_fmaf(h[j], w[j], z[j]);
+    slope8(g.activation, z, d);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ rows
+// Row r is group r % groups of sample r / groups: `len` channels.
+struct Row {
+  long long n, c0;   // sample, first channel
+  __device__ __forceinline__ Row(const GroupNorm &g, long long r, long long len) {
+    if (g.groups == 1) n = r, c0 = 0;
+    else n = r / g.groups, c0 = (r - n * g.groups) * len;
+  }
+};
+
+// A team a row, V times eight entries a lane.
+template <class T, int TEAM, int V>
+__global__ void __launch_bounds__(kThreads) k_norm_rows(GroupNorm g) {
+  __shared__ float red[2][kThreads / 64];
+  const int lane = threadIdx.x % TEAM;
+  const int len = (int)(g.channels / g.groups);
+  const long long rows = g.samples * g.groups;
+  long long r = (long long)blockIdx.x * (kThreads / TEAM) + threadIdx.x / TEAM;
+  const bool real = r < rows;
+  if (!real) r = rows - 1;   // a team without a row goes along with the last one's, and stores nothing
+  const Row row(g, r, len);
+  const T *x = static_cast<const T *>(g.x) + row.n * g.x_sample + row.c0;
+  Eight<T> raw[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) raw[v].load(x + (lane + v * TEAM) * 8, len - (lane + v * TEAM) * 8);
   float s = 0.0f;
-  for (long long q = threadIdx.x; q < total; q += 256) s = s + to_float(x[q / per * g.x_pos + q % per]);
-  const float mean = block_sum(s, red) / (float)total;
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    float e[8];
+    raw[v].get(e);   // 0 beyond the row
+    s = s + (((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7])));
+  }
+  const float mean = team_sum<TEAM>(s, red[0]) / (float)len;
   s = 0.0f;
-  for (long long q = threadIdx.x; q < total; q += 256) {
-    const float d = to_float(x[q / per * g.x_pos + q % per]) - mean;
-    s = __builtin_fmaf(d, d, s);
-  }
-  const float rstd = 1.0f / sqrtf(block_sum(s, red) / (float)total + g.eps);
-  if (threadIdx.x == 0) g.mean[blockIdx.x] = mean, g.rstd[blockIdx.x] = rstd;
-  for (long long q = threadIdx.x; q < total; q += 256) {
-    const long long c = q % per, at = gr * per + c;
-    const float h = (to_float(x[q / per * g.x_pos + c]) - mean) * rstd;
-    const float v = __builtin_fmaf(h, g.weight ? g.weight[at] : 1.0f, g.bias ? g.bias[at] : 0.0f);
-    y[q / per * g.out_pos + c] = from_float<T>(act_of(g.activation, v));
-  }
-}
-
-// The gradient before the activation, and the normalised value, of entry c of a group's position.
-template <class T>
-__device__ __forceinline__ void through(const GroupNorm &g, long long n, long long p, long long c, float mean, float rstd, float &dh, float &h) {
-  h = (to_float(static_cast<const T *>(g.x)[n * g.x_sample + p * g.x_pos + c]) - mean) * rstd;
-  dh = to_float(static_cast<const T *>(g.dy)[n * g.dy_sample + p * g.dy_pos + c]);
-  if (g.activation != kActNone)
-    dh = dh * act_slope_of(g.activation, __builtin_fmaf(h, g.weight ? g.weight[c] : 1.0f, g.bias ? g.bias[c] : 0.0f));
-}
-
-template <class T>
-__global__ void __launch_bounds__(256) k_norm_grad(GroupNorm g) {
-  __shared__ float red[256];
-  const long long n = blockIdx.x / g.groups, gr = blockIdx.x % g.groups, per = g.channels / g.groups, total = per * g.positions;
-  const float mean = g.mean[blockIdx.x], rstd = g.rstd[blockIdx.x];
-  float s1 = 0.0f, s2 = 0.0f;
-  for (long long q = threadIdx.x; q < total; q += 256) {
-    const long long c = gr * per + q % per;
-    float dh, h;
-    through<T>(g, n, q / per, c, mean, rstd, dh, h);
-    const float u = g.weight ? dh * g.weight[c] : dh;
-    s1 = s1 + u;
-    s2 = __builtin_fmaf(u, h, s2);
-  }
-  const float m1 = block_sum(s1, red) / (float)total, m2 = block_sum(s2, red) / (float)total;
-  for (long long q = threadIdx.x; q < total; q += 256) {
-    const long long c = gr * per + q % per, p = q / per;
-    float dh, h;
-    through<T>(g, n, p, c, mean, rstd, dh, h);
-    const float u = g.weight ? dh * g.weight[c] : dh;
-    float v = __builtin_fmaf(-h, m2, u - m1) * rstd;
-    if (g.extra) v = to_float(static_cast<const T *>(g.extra)[n * g.extra_sample + p * g.extra_pos + c]) + v;
-    static_cast<T *>(g.out)[n * g.out_sample + p * g.out_pos + c] = from_float<T>(v);
-  }
-}
-
-// dweight and dbias: 64 channels a workgroup, its four waves take positions in turn.  Before k_norm_grad, which may write where
-// the residual is but leaves x and dy alone.
-template <class T>
-__global__ void __launch_bounds__(256) k_norm_channels(GroupNorm g) {
-  __shared__ float part[2][4][64];
-  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-  const long long c = (long long)blockIdx.x * 64 + lane;
-  float sw = 0.0f, sb = 0.0f;
-  if (c < g.channels) {
-    const long long gr = c / (g.channels / g.groups);
-    for (long long q = wave; q < g.samples * g.positions; q += 4) {
-      const long long n = q / g.positions;
-      float dh, h;
-      through<T>(g, n, q % g.positions, c, g.mean[n * g.groups + gr], g.rstd[n * g.groups + gr], dh, h);
-      sw = __builtin_fmaf(dh, h, sw);
-      sb = sb + dh;
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    float e[8];
+    raw[v].get(e);
+    const int n = len - (lane + v * TEAM) * 8;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float d = j < n ? e[j] - mean : 0.0f;
+      s = __builtin_fmaf(d, d, s);
     }
   }
-  part[0][wave][lane] = sw, part[1][wave][lane] = sb;
-  __syncthreads();
-  if (wave < 2 && c < g.channels) {
-    const float v = (part[wave][0][lane] + part[wave][1][lane]) + (part[wave][2][lane] + part[wave][3][lane]);
-    float *o = wave == 0 ? g.dweight : g.dbias;
-    if (o) o[c] = g.accumulate ? o[c] + v : v;
+  const float rstd = 1.0f / sqrtf(team_sum<TEAM>(s, red[1]) / (float)len + g.eps);
+  if (!real) return;
+  if (lane == 0) g.mean[r] = mean, g.rstd[r] = rstd;
+  T *y = static_cast<T *>(g.out) + row.n * g.out_sample + row.c0;
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    const int at = (lane + v * TEAM) * 8, n = len - at;
+    if (n > 0) {
+      float e[8];
+      raw[v].get(e);
+      normalised8(g, row.c0 + at, n, mean, rstd, e);
+      store8(y + at, n, e);
+    }
   }
+}
+
+// Rows longer than the registers hold: a workgroup a row, read three times.
+template <class T>
+__global__ void __launch_bounds__(1024) k_norm_long_rows(GroupNorm g) {
+  __shared__ float red[2][16];
+  const long long r = blockIdx.x, len = g.channels / g.groups;
+  const Row row(g, r, len);
+  const T *x = static_cast<const T *>(g.x) + row.n * g.x_sample + row.c0;
+  T *y = static_cast<T *>(g.out) + row.n * g.out_sample + row.c0;
+  const auto clip = [](long long n) { return n < 8 ? (int)n : 8; };
+  float s = 0.0f, e[8];
+  for (long long at = threadIdx.x * 8; at < len; at += 8192) {
+    load8(x + at, clip(len - at), e);
+    s = s + (((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7])));
+  }
+  const float mean = team_sum<1024>(s, red[0]) / (float)len;
+  s = 0.0f;
+  for (long long at = threadIdx.x * 8; at < len; at += 8192) {
+    const int n = clip(len - at);
+    load8(x + at, n, e);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float d = j < n ? e[j] - mean : 0.0f;
+      s = __builtin_fmaf(d, d, s);
+    }
+  }
+  const float rstd = 1.0f / sqrtf(team_sum<1024>(s, red[1]) / (float)len + g.eps);
+  if (threadIdx.x == 0) g.mean[r] = mean, g.rstd[r] = rstd;
+  for (long long at = threadIdx.x * 8; at < len; at += 8192) {
+    const int n = clip(len - at);
+    load8(x + at, n, e);
+    normalised8(g, row.c0 + at, n, mean, rstd, e);
+    store8(y + at, n, e);
+  }
+}
+
+// The gradient of rows.  A team takes rows of one group, `step` samples apart, and keeps its channels' sums for dweight and dbias in
+// registers; the workgroup's teams join theirs in shared memory and store one row of partial sums.  grid: (groups, workgroups a group).
+template <class T, int TEAM, int V>
+__global__ void __launch_bounds__(kThreads) k_norm_rows_grad(GroupNorm g) {
+  constexpr int kTeams = kThreads / TEAM;
+  __shared__ float red[2][2][kThreads / 64];
+  __shared__ float join[kTeams > 1 ? TEAM * V * 8 : 1];
+  const int lane = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
+  const int len = (int)(g.channels / g.groups);
+  const long long c0 = (long long)blockIdx.x * len;
+  float sw[V][8] = {}, sb[V][8] = {};
+  const float inv = 1.0f / (float)len;
+  int turn = 0;
+  for (long long first = (long long)blockIdx.y * kTeams; first < g.samples; first += (long long)gridDim.y * kTeams, turn ^= 1) {
+    const long long n = first + team < g.samples ? first + team : g.samples - 1;
+    const bool real = first + team < g.samples;
+    const T *x = static_cast<const T *>(g.x) + n * g.x_sample + c0, *dy = static_cast<const T *>(g.dy) + n * g.dy_sample + c0;
+    Eight<T> rx[V], rd[V], re[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const int at = (lane + v * TEAM) * 8;
+      rx[v].load(x + at, len - at);
+      rd[v].load(dy + at, len - at);
+      if (g.extra) re[v].load(static_cast<const T *>(g.extra) + n * g.extra_sample + c0 + at, len - at);
+    }
+    const float mean = g.mean[n * g.groups + blockIdx.x], rstd = g.rstd[n * g.groups + blockIdx.x];
+    float s1 = 0.0f, s2 = 0.0f;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const int at = (lane + v * TEAM) * 8;
+      if (at < len) {
+        float h[8], d[8], w[8];
+        rx[v].get(h);
+        rd[v].get(d);   // 0 beyond the row
+        back8(g, c0 + at, len - at, mean, rstd, h, d, w);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          if (len - at <= j) d[j] = 0.0f, h[j] = 0.0f;
+          if (real) sw[v][j] = __builtin_fmaf(d[j], h[j], sw[v][j]), sb[v][j] = sb[v][j] + d[j];
+          const float u = d[j] * w[j];
+          s1 = s1 + u;
+          s2 = __builtin_fmaf(u, h[j], s2);
+        }
+      }
+    }
+    // two sums a turn, in places that the last turn's readers have left
+    const float m1 = team_sum<TEAM>(s1, red[turn][0]) * inv, m2 = team_sum<TEAM>(s2, red[turn][1]) * inv;
+    if (real) {
+      T *dx = static_cast<T *>(g.out) + n * g.out_sample + c0;
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        const int at = (lane + v * TEAM) * 8;
+        if (at < len) {
+          float h[8], d[8], w[8], o[8];
+          rx[v].get(h);
+          rd[v].get(d);
+          back8(g, c0 + at, len - at, mean, rstd, h, d, w);
+          if (g.extra) re[v].get(o);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const float q = __builtin_fmaf(-h[j], m2, __builtin_fmaf(d[j], w[j], -m1)) * rstd;
+            d[j] = g.extra ? o[j] + q : q;
+          }
+          store8(dx + at, len - at, d);
+        }
+      }
+    }
+  }
+  if (!g.scratch) return;
+  // partial sums of this workgroup: [2][channels]
+  float *part = g.scratch + (long long)blockIdx.y * 2 * g.channels + c0;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    if constexpr (kTeams > 1) {
+      for (int t = 0; t < kTeams; ++t) {   // the teams in their order
+        __syncthreads();
+        if (team == t)
+#pragma unroll
+          for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              float *o = &join[(v * 8 + j) * TEAM + lane];
+              const float mine = k == 0 ? sw[v][j] : sb[v][j];
+              *o = t == 0 ? mine : *o + mine;
+            }
+      }
+      if (team == kTeams - 1)   // this team's own writes
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          const int at = (lane + v * TEAM) * 8;
+          float e[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) e[j] = join[(v * 8 + j) * TEAM + lane];
+          if (at < len) store8(part + k * g.channels + at, len - at, e);
+        }
+    } else {
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        const int at = (lane + v * TEAM) * 8;
+        if (at < len) store8(part + k * g.channels + at, len - at, k == 0 ? sw[v] : sb[v]);
+      }
+    }
+  }
+}
+
+// Rows longer than the registers hold: a workgroup a row.  dweight and dbias come from k_norm_long_channels.
+template <class T>
+__global__ void __launch_bounds__(1024) k_norm_long_rows_grad(GroupNorm g) {
+  __shared__ float red[2][16];
+  const long long r = blockIdx.x, len = g.channels / g.groups;
+  const Row row(g, r, len);
+  const float mean = g.mean[r], rstd = g.rstd[r];
+  const T *x = static_cast<const T *>(g.x) + row.n * g.x_sample + row.c0, *dy = static_cast<const T *>(g.dy) + row.n * g.dy_sample + row.c0;
+  const auto clip = [](long long n) { return n < 8 ? (int)n : 8; };
+  float s1 = 0.0f, s2 = 0.0f, h[8], d[8], w[8];
+  for (long long at = threadIdx.x * 8; at < len; at += 8192) {
+    const int n = clip(len - at);
+    load8(x + at, n, h);
+    load8(dy + at, n, d);
+    back8(g, row.c0 + at, n, mean, rstd, h, d, w);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float u = j < n ? d[j] * w[j] : 0.0f;
+      s1 = s1 + u;
+      s2 = j < n ? __builtin_fmaf(u, h[j], s2) : s2;
+    }
+  }
+  const float m1 = team_sum<1024>(s1, red[0]) / (float)len, m2 = team_sum<1024>(s2, red[1]) / (float)len;
+  for (long long at = threadIdx.x * 8; at < len; at += 8192) {
+    const int n = clip(len - at);
+    load8(x + at, n, h);
+    load8(dy + at, n, d);
+    back8(g, row.c0 + at, n, mean, rstd, h, d, w);
+    float o[8] = {};
+    if (g.extra) load8(static_cast<const T *>(g.extra) + row.n * g.extra_sample + row.c0 + at, n, o);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float q = __builtin_fmaf(-h[j], m2, __builtin_fmaf(d[j], w[j], -m1)) * rstd;
+      d[j] = g.extra ? o[j] + q : q;
+    }
+    store8(static_cast<T *>(g.out) + row.n * g.out_sample + row.c0 + at, n, d);
+  }
+}
+// ... the partial sums over samples blockIdx.y, blockIdx.y + gridDim.y, ... of a thread's eight channels.
+template <class T>
+__global__ void __launch_bounds__(kThreads) k_norm_long_channels(GroupNorm g) {
+  const long long len = g.channels / g.groups;
+  const long long per_group = (len + 7) / 8, q = (long long)blockIdx.x * kThreads + threadIdx.x;
+  if (q >= per_group * g.groups) return;
+  const long long gr = q / per_group, at = (q - gr * per_group) * 8, c = gr * len + at;
+  const int n = len - at < 8 ? (int)(len - at) : 8;
+  float sw[8] = {}, sb[8] = {};
+  for (long long s = blockIdx.y; s < g.samples; s += gridDim.y) {
+    float h[8], d[8], w[8];
+    load8(static_cast<const T *>(g.x) + s * g.x_sample + c, n, h);
+    load8(static_cast<const T *>(g.dy) + s * g.dy_sample + c, n, d);
+    back8(g, c, n, g.mean[s * g.groups + gr], g.rstd[s * g.groups + gr], h, d, w);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sw[j] = __builtin_fmaf(d[j], h[j], sw[j]), sb[j] = sb[j] + d[j];
+  }
+  float *part = g.scratch + (long long)blockIdx.y * 2 * g.channels + c;
+  store8(part, n, sw);
+  store8(part + g.channels, n, sb);
+}
+
+// dweight and dbias from `count` rows of partial sums [2][channels]: 64 columns a workgroup, its waves take rows in turn.
+__global__ void __launch_bounds__(1024) k_norm_join(GroupNorm g, const float *part, long long count) {
+  __shared__ float red[16][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
+  const long long c = (long long)blockIdx.x * 64 + lane, total = 2 * g.channels;
+  float s = 0.0f;
+  if (c < total)
+    for (long long r = wave; r < count; r += 16) s = s + part[r * total + c];
+  red[wave][lane] = s;
+  __syncthreads();
+  if (wave == 0 && c < total) {
+    s = 0.0f;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) s = s + red[w][lane];
+    float *o = c < g.channels ? g.dweight : g.dbias;
+    const long long at = c < g.channels ? c : c - g.channels;
+    if (o) o[at] = g.accumulate ? o[at] + s : s;
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ maps
+// How a launch cuts [samples][positions][channels].  A block is `width` channels (the last may be shorter): whole groups, or, with
+// blocks_a_group > 1, a part of one.  A piece is `chunk` positions of a block.
+struct Maps {
+  int per;               // channels of a group
+  int width, blocks;     // channels of a block, blocks
+  int blocks_a_group;
+  int vectors;           // ceil(width / 8): threads across
+  int rows;              // positions at a time
+  int chunk, chunks;     // positions of a piece, pieces
+  int pieces_a_group;    // chunks, times blocks_a_group
+};
+
+// What a workgroup works on, and its thread's channels.
+template <int NT>
+struct Place {
+  long long n;
+  int block, chunk;
+  long long c0;       // the block's first channel
+  int width;          // its channels
+  u32 p0, p1;         // its positions
+  int vec, row;       // the thread's
+  int own;            // channels that it owns (<= 0: none), from c0 + 8 vec on
+  __device__ __forceinline__ Place(const GroupNorm &g, const Maps &m) {
+    n = blockIdx.x / (u32)(m.blocks * m.chunks);
+    const int piece = (int)(blockIdx.x - (u32)n * (u32)(m.blocks * m.chunks));
+    chunk = piece / m.blocks;
+    block = piece - chunk * m.blocks;
+    if (m.blocks_a_group > 1) {
+      const int gr = block / m.blocks_a_group, in = block - gr * m.blocks_a_group;
+      c0 = (long long)gr * m.per + in * m.width;
+      width = m.per - in * m.width < m.width ? m.per - in * m.width : m.width;
+    } else {
+      c0 = (long long)block * m.width;
+      width = g.channels - c0 < m.width ? (int)(g.channels - c0) : m.width;
+    }
+    p0 = (u32)chunk * m.chunk;
+    p1 = g.positions - p0 < m.chunk ? (u32)g.positions : p0 + m.chunk;
+    row = threadIdx.x / m.vectors;
+    vec = threadIdx.x - row * m.vectors;
+    own = row < m.rows ? width - vec * 8 : 0;
+  }
+};
+
+// v[j] of every thread summed per channel over the rows of the workgroup: into sums[0 .. width).  lanes: NT * 8 floats.
+template <int NT>
+__device__ __forceinline__ void channel_sums(const Maps &m, const Place<NT> &at, const float (&v)[8], float *lanes, float *sums) {
+  __syncthreads();
+  if (at.own > 0)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) lanes[(at.row * 8 + j) * m.vectors + at.vec] = v[j];
+  __syncthreads();
+  const int across = m.vectors * 8;
+  // several threads a channel, a power of two, adjacent in the rows that they take
+  int share = 1;
+  while (share * 2 * across <= NT && share * 2 <= m.rows) share *= 2;
+  float s = 0.0f;
+  const int t = threadIdx.x, q = t % across, r0 = t / across;
+  for (int c = q; c < across && r0 < share; c += NT)   // one turn, but for blocks wider than the workgroup
+  {
+    s = 0.0f;
+    for (int r = r0; r < m.rows; r += share) s = s + lanes[r * across + c];
+    const int j = c / m.vectors, vec = c - j * m.vectors;
+    if (share == 1 && vec * 8 + j < at.width) sums[vec * 8 + j] = s;
+  }
+  if (share > 1) {
+    __syncthreads();
+    if (r0 < share) lanes[r0 * across + q] = s;
+    __syncthreads();
+    if (t < across) {
+      s = 0.0f;
+      for (int r = 0; r < share; ++r) s = s + lanes[r * across + t];
+      const int j = t / m.vectors, vec = t - j * m.vectors;
+      if (vec * 8 + j < at.width) sums[vec * 8 + j] = s;
+    }
+  }
+  __syncthreads();
+}
+
+// Sums of each group's channels: out[g] for the groups of the block (one, where the block is a part of a group).
+template <int NT>
+__device__ __forceinline__ void group_sums(const Maps &m, const Place<NT> &at, const float *channels, float *out) {
+  const int per = m.blocks_a_group > 1 ? at.width : m.per, groups = at.width / per;
+  if (per <= 16) {
+    for (int q = threadIdx.x; q < groups; q += NT) {
+      float s = 0.0f;
+      for (int c = 0; c < per; ++c) s = s + channels[q * per + c];
+      out[q] = s;
+    }
+  } else {
+    for (int q = threadIdx.x / 64; q < groups; q += NT / 64) {
+      float s = 0.0f;
+      for (int c = threadIdx.x & 63; c < per; c += 64) s = s + channels[q * per + c];
+      s = lanes_sum<64>(s);
+      if ((threadIdx.x & 63) == 0) out[q] = s;
+    }
+  }
+  __syncthreads();
+}
+
+constexpr int kWidest = 2048;   // channels of a block
+
+// The group of each of a thread's channels, within the block.
+__device__ __forceinline__ void groups8(const Maps &m, int c, int (&q)[8]) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) q[j] = m.blocks_a_group > 1 ? 0 : (c + j) / m.per;
+}
+
+enum MapsPass { kWhole = 0, kPieces = 1, kJoined = 2 };
+
+// kWhole: a block's values are in registers from the mean to the result.  kPieces: mean and squares of a piece, per group, to
+// scratch[n][group][piece][2].  kJoined: those of the group's pieces joined (Chan et al.: squares about the common mean), and the result.
+template <class T, int NT, int U, int PASS>
+__global__ void __launch_bounds__(NT) k_norm_maps(GroupNorm g, Maps m) {
+  __shared__ float lanes[PASS == kJoined ? 1 : NT * 8];
+  __shared__ float channels[PASS == kJoined ? 1 : kWidest];
+  __shared__ float means[kWidest], rstds[kWidest];   // per group of the block
+  const Place<NT> at(g, m);
+  const T *x = static_cast<const T *>(g.x) + at.n * g.x_sample + at.c0 + at.vec * 8;
+  Eight<T> raw[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const u32 p = at.p0 + at.row + u * m.rows;
+    raw[u].load(x + (long long)p * g.x_pos, p < at.p1 ? at.own : 0);
+  }
+  int q[8];
+  groups8(m, at.vec * 8, q);
+  const int per = m.blocks_a_group > 1 ? at.width : m.per, groups = at.width / per;
+  const long long first = m.blocks_a_group > 1 ? at.block / m.blocks_a_group : at.c0 / m.per;   // the block's first group
+  if constexpr (PASS != kJoined) {
+    const float count = (float)per * (float)(at.p1 - at.p0);
+    float v[8] = {};
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float e[8];
+      raw[u].get(e);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = v[j] + e[j];
+    }
+    channel_sums<NT>(m, at, v, lanes, channels);
+    group_sums<NT>(m, at, channels, means);
+    for (int k = threadIdx.x; k < groups; k += NT) means[k] = means[k] / count;
+    __syncthreads();
+    float mean[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      mean[j] = j < at.own ? means[q[j]] : 0.0f;
+      v[j] = 0.0f;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float e[8];
+      raw[u].get(e);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float d = at.p0 + at.row + u * m.rows < at.p1 && j < at.own ? e[j] - mean[j] : 0.0f;
+        v[j] = __builtin_fmaf(d, d, v[j]);
+      }
+    }
+    channel_sums<NT>(m, at, v, lanes, channels);
+    group_sums<NT>(m, at, channels, rstds);
+    if constexpr (PASS == kPieces) {
+      const int piece = m.blocks_a_group > 1 ? at.chunk * m.blocks_a_group + at.block % m.blocks_a_group : at.chunk;
+      for (int k = threadIdx.x; k < groups; k += NT) {
+        float *o = g.scratch + ((at.n * g.groups + first + k) * m.pieces_a_group + piece) * 2;
+        o[0] = means[k], o[1] = rstds[k];
+      }
+      return;
+    }
+    for (int k = threadIdx.x; k < groups; k += NT) rstds[k] = 1.0f / sqrtf(rstds[k] / count + g.eps);
+  } else {
+    // the pieces' values: `per` channels, or a block's share of them, at `chunk` positions, or what is left
+    const auto values = [&](int piece) {
+      const int in = m.blocks_a_group > 1 ? piece % m.blocks_a_group : 0, ch = m.blocks_a_group > 1 ? piece / m.blocks_a_group : piece;
+      const int w = m.blocks_a_group > 1 ? (m.per - in * m.width < m.width ? m.per - in * m.width : m.width) : m.per;
+      const int p = g.positions - ch * m.chunk < m.chunk ? (int)(g.positions - ch * m.chunk) : m.chunk;
+      return (float)w * (float)p;
+    };
+    const float total = (float)m.per * (float)g.positions;
+    for (int k = threadIdx.x / 64; k < groups; k += NT / 64) {   // a wave a group
+      const float *s = g.scratch + (at.n * g.groups + first + k) * m.pieces_a_group * 2;
+      float mean = 0.0f;
+      for (int i = threadIdx.x & 63; i < m.pieces_a_group; i += 64) mean = __builtin_fmaf(s[2 * i], values(i) / total, mean);
+      mean = lanes_sum<64>(mean);
+      float sq = 0.0f;
+      for (int i = threadIdx.x & 63; i < m.pieces_a_group; i += 64) {
+        const float d = s[2 * i] - mean;
+        sq = sq + __builtin_fmaf(d * d, values(i), s[2 * i + 1]);
+      }
+      sq = lanes_sum<64>(sq);
+      if ((threadIdx.x & 63) == 0) means[k] = mean, rstds[k] = 1.0f / sqrtf(sq / total + g.eps);
+    }
+  }
+  __syncthreads();
+  if (at.chunk == 0 && (m.blocks_a_group == 1 || at.block % m.blocks_a_group == 0))
+    for (int k = threadIdx.x; k < groups; k += NT) {
+      g.mean[at.n * g.groups + first + k] = means[k];
+      g.rstd[at.n * g.groups + first + k] = rstds[k];
+    }
+  if (at.own <= 0) return;
+  float w[8], b[8];
+  vector8(g.weight ? g.weight + at.c0 + at.vec * 8 : nullptr, 1.0f, at.own, w);
+  vector8(g.bias ? g.bias + at.c0 + at.vec * 8 : nullptr, 0.0f, at.own, b);
+  float mean[8], rstd[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) mean[j] = j < at.own ? means[q[j]] : 0.0f, rstd[j] = j < at.own ? rstds[q[j]] : 0.0f;
+  T *y = static_cast<T *>(g.out) + at.n * g.out_sample + at.c0 + at.vec * 8;
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const u32 p = at.p0 + at.row + u * m.rows;
+    if (p < at.p1) {
+      float e[8];
+      raw[u].get(e);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) e[j] = __builtin_fmaf((e[j] - mean[j]) * rstd[j], w[j], b[j]);
+      act8(g.activation, e);
+      store8(y + (long long)p * g.out_pos, at.own, e);
+    }
+  }
+}
+
+// The gradient.  Per channel of a piece: the sums of d (dy through the activation) and of d h, to scratch[n][chunk][2][channels];
+// from them come dweight and dbias, and, weighted and summed over a group, what dx needs.
+template <class T, int NT, int U, int PASS>
+__global__ void __launch_bounds__(NT) k_norm_maps_grad(GroupNorm g, Maps m) {
+  __shared__ float lanes[PASS == kJoined ? 1 : NT * 8];
+  __shared__ float cw[kWidest], cb[kWidest];   // per channel: the sums of d h and of d
+  const Place<NT> at(g, m);
+  const long long c = at.c0 + at.vec * 8;
+  const T *x = static_cast<const T *>(g.x) + at.n * g.x_sample + c, *dy = static_cast<const T *>(g.dy) + at.n * g.dy_sample + c;
+  Eight<T> rx[U], rd[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const u32 p = at.p0 + at.row + u * m.rows;
+    const int n = p < at.p1 ? at.own : 0;
+    rx[u].load(x + (long long)p * g.x_pos, n);
+    rd[u].load(dy + (long long)p * g.dy_pos, n);
+  }
+  int q[8];
+  groups8(m, at.vec * 8, q);
+  const int per = m.blocks_a_group > 1 ? at.width : m.per, groups = at.width / per;
+  const long long first = m.blocks_a_group > 1 ? at.block / m.blocks_a_group : at.c0 / m.per;
+  float mean[8], rstd[8], w[8], b[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    mean[j] = j < at.own ? g.mean[at.n * g.groups + first + q[j]] : 0.0f;
+    rstd[j] = j < at.own ? g.rstd[at.n * g.groups + first + q[j]] : 0.0f;
+    w[j] = b[j] = 0.0f;
+  }
+  if (at.own > 0) {
+    vector8(g.weight ? g.weight + c : nullptr, 1.0f, at.own, w);
+    vector8(g.bias ? g.bias + c : nullptr, 0.0f, at.own, b);
+  }
+  const auto back = [&](int u, float (&h)[8], float (&d)[8]) {
+    rx[u].get(h);
+    rd[u].get(d);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) h[j] = (h[j] - mean[j]) * rstd[j];
+    if (g.activation != kActNone) {
+      float z[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) z[j] = __builtin_fmaf(h[j], w[j], b[j]);
+      slope8(g.activation, z, d);
+    }
+  };
+  if constexpr (PASS != kJoined) {
+    float vw[8] = {}, vb[8] = {};
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (at.p0 + at.row + u * m.rows < at.p1) {
+        float h[8], d[8];
+        back(u, h, d);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) vw[j] = __builtin_fmaf(d[j], h[j], vw[j]), vb[j] = vb[j] + d[j];
+      }
+    channel_sums<NT>(m, at, vw, lanes, cw);
+    channel_sums<NT>(m, at, vb, lanes, cb);
+    float *o = g.scratch + ((at.n * m.chunks + at.chunk) * 2) * g.channels + at.c0;
+    for (int k = threadIdx.x; k < at.width; k += NT) o[k] = cw[k], o[g.channels + k] = cb[k];
+    if constexpr (PASS == kPieces) return;
+  } else {
+    // over all of the group, which may be wider than the block
+    const long long from = m.blocks_a_group > 1 ? first * m.per : at.c0;
+    const int width = m.blocks_a_group > 1 ? m.per : at.width;
+    if (m.blocks_a_group > 1) {   // one group: sums over its channels, kept in one place
+      float s1 = 0.0f, s2 = 0.0f;
+      for (int k = threadIdx.x; k < width; k += NT) {
+        const float wk = g.weight ? g.weight[from + k] : 1.0f;
+        for (int ch = 0; ch < m.chunks; ++ch) {
+          const float *s = g.scratch + ((at.n * m.chunks + ch) * 2) * g.channels + from + k;
+          s2 = __builtin_fmaf(s[0], wk, s2);
+          s1 = __builtin_fmaf(s[g.channels], wk, s1);
+        }
+      }
+      __shared__ float red[2][NT / 64];
+      s1 = team_sum<NT>(s1, red[0]);
+      s2 = team_sum<NT>(s2, red[1]);
+      if (threadIdx.x == 0) cb[0] = s1, cw[0] = s2;
+    } else {
+      for (int k = threadIdx.x; k < width; k += NT) {
+        float s1 = 0.0f, s2 = 0.0f;
+        for (int ch = 0; ch < m.chunks; ++ch) {
+          const float *s = g.scratch + ((at.n * m.chunks + ch) * 2) * g.channels + from + k;
+          s2 = s2 + s[0];
+          s1 = s1 + s[g.channels];
+        }
+        cw[k] = s2, cb[k] = s1;
+      }
+    }
+  }
+  __syncthreads();
+  __shared__ float m1[kWidest], m2[kWidest];
+  const float total = (float)m.per * (float)g.positions;
+  if (m.blocks_a_group > 1) {
+    if (threadIdx.x == 0) m1[0] = cb[0] / total, m2[0] = cw[0] / total;
+    __syncthreads();
+  } else {
+    for (int k = threadIdx.x; k < at.width; k += NT) {
+      const float wk = g.weight ? g.weight[at.c0 + k] : 1.0f;
+      cw[k] = cw[k] * wk, cb[k] = cb[k] * wk;
+    }
+    __syncthreads();
+    group_sums<NT>(m, at, cb, m1);
+    group_sums<NT>(m, at, cw, m2);
+    for (int k = threadIdx.x; k < groups; k += NT) m1[k] = m1[k] / total, m2[k] = m2[k] / total;
+    __syncthreads();
+  }
+  if (at.own <= 0) return;
+  float e1[8], e2[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) e1[j] = j < at.own ? m1[q[j]] : 0.0f, e2[j] = j < at.own ? m2[q[j]] : 0.0f;
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const u32 p = at.p0 + at.row + u * m.rows;
+    if (p < at.p1) {
+      float h[8], d[8], o[8];
+      if (g.extra) load8(static_cast<const T *>(g.extra) + at.n * g.extra_sample + p * g.extra_pos + c, at.own, o);
+      back(u, h, d);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float v = __builtin_fmaf(-h[j], e2[j], __builtin_fmaf(d[j], w[j], -e1[j])) * rstd[j];
+        d[j] = g.extra ? o[j] + v : v;
+      }
+      store8(static_cast<T *>(g.out) + at.n * g.out_sample + p * g.out_pos + c, at.own, d);
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ launches
+long long gcd(long long a, long long b) { return b == 0 ? a : gcd(b, a % b); }
+
+// A block: whole groups and whole vectors of eight, so that no thread's channels cross a block's edge more often than at the end; at least 64
+// channels (128 bytes of bf16 in a row), more where few positions would leave threads idle; at most 256 vectors.
+Maps maps_of(const GroupNorm &g, int threads, int each) {
+  Maps m = {};
+  m.per = (int)(g.channels / g.groups);
+  m.blocks_a_group = 1;
+  if (m.per > kWidest) {
+    m.blocks_a_group = (m.per + kWidest - 1) / kWidest;
+    m.width = kWidest;
+    m.blocks = m.blocks_a_group * (int)g.groups;
+  } else {
+    long long unit = m.per / gcd(m.per, 8) * 8;
+    if (unit > 512 || unit > g.channels) unit = m.per;
+    long long w = unit;
+    while (w < g.channels && w + unit <= kWidest && (w < 64 || (w + 7) / 8 * g.positions < kThreads)) w += unit;
+    if (w > g.channels) w = g.channels;
+    m.width = (int)w;
+    m.blocks = (int)((g.channels + w - 1) / w);
+  }
+  m.vectors = (m.width + 7) / 8;
+  m.rows = threads / m.vectors;
+  m.chunk = m.rows * each;
+  m.chunks = (int)((g.positions + m.chunk - 1) / m.chunk);
+  m.pieces_a_group = m.chunks * m.blocks_a_group;
+  return m;
+}
+constexpr long long kMostWorkgroups = 0x7fffffff;
+long long workgroups(const GroupNorm &g, const Maps &m) { return (long long)m.blocks * m.chunks * g.samples; }
+bool whole(const GroupNorm &g, const Maps &m) { return m.chunks == 1 && m.blocks_a_group == 1 && workgroups(g, m) <= kMostWorkgroups; }
+
+// The rows' cut: lanes of a team and eights a lane, or neither: longer.
+struct Rows {
+  int team, each;
+};
+Rows rows_of(const GroupNorm &g) {
+  const long long v = (g.channels / g.groups + 7) / 8;
+  if (v <= 16) return {16, 1};
+  if (v <= 64) return {64, 1};
+  if (v <= 256) return {64, 4};
+  if (v <= 1024) return {256, 4};
+  return {0, 0};
+}
+// Workgroups that share a group's rows: enough to fill the device a few times, few enough that their partial sums are little beside the rows.
+long long rows_workgroups(const GroupNorm &g, const Rows &r) {
+  const long long teams = kThreads / r.team, most = (g.samples + teams - 1) / teams;
+  long long want = 1024 / g.groups;
+  if (want < 1) want = 1;
+  return most < want ? most : want;
+}
+constexpr long long kLongSplits = 64;
+
+template <class T>
+hipError_t norm(const GroupNorm &g, hipStream_t s) {
+  if (g.positions == 1) {
+    const long long rows = g.samples * g.groups;
+    const Rows r = rows_of(g);
+    if (r.team == 0) {
+      k_norm_long_rows<T><<<dim3((unsigned)rows), 1024, 0, s>>>(g);
+      return hipGetLastError();
+    }
+    const unsigned grid = (unsigned)((rows + kThreads / r.team - 1) / (kThreads / r.team));
+    if (r.team == 16) k_norm_rows<T, 16, 1><<<dim3(grid), kThreads, 0, s>>>(g);
+    else if (r.team == 64 && r.each == 1) k_norm_rows<T, 64, 1><<<dim3(grid), kThreads, 0, s>>>(g);
+    else if (r.team == 64) k_norm_rows<T, 64, 4><<<dim3(grid), kThreads, 0, s>>>(g);
+    else k_norm_rows<T, 256, 4><<<dim3(grid), kThreads, 0, s>>>(g);
+    return hipGetLastError();
+  }
+  Maps m;
+  const auto grid = [&] { return dim3((unsigned)workgroups(g, m)); };
+  if (m = maps_of(g, 256, 2), whole(g, m)) k_norm_maps<T, 256, 2, kWhole><<<grid(), 256, 0, s>>>(g, m);
+  else if (m = maps_of(g, 256, 8), whole(g, m)) k_norm_maps<T, 256, 8, kWhole><<<grid(), 256, 0, s>>>(g, m);
+  else if (m = maps_of(g, 1024, 8), whole(g, m)) k_norm_maps<T, 1024, 8, kWhole><<<grid(), 1024, 0, s>>>(g, m);
+  else {
+    m = maps_of(g, 256, 8);
+    if (workgroups(g, m) > kMostWorkgroups) return hipErrorInvalidValue;
+    k_norm_maps<T, 256, 8, kPieces><<<grid(), 256, 0, s>>>(g, m);
+    k_norm_maps<T, 256, 8, kJoined><<<grid(), 256, 0, s>>>(g, m);
+  }
+  return hipGetLastError();
+}
+
+// The gradient's cut of maps, and whether one launch does it.
+struct GradMaps {
+  Maps m;
+  int threads, each;
+  bool whole;
+};
+GradMaps grad_maps(const GroupNorm &g) {
+  const int most = g.type == kF32 ? 4 : 8;   // eights of two tensors in registers
+  GradMaps q = {maps_of(g, 256, 2), 256, 2, true};
+  if (whole(g, q.m)) return q;
+  q = {maps_of(g, 256, 4), 256, 4, true};
+  if (whole(g, q.m)) return q;
+  q = {maps_of(g, 1024, most), 1024, most, true};
+  if (whole(g, q.m)) return q;
+  return {maps_of(g, 256, 4), 256, 4, false};
+}
+
+template <class T>
+hipError_t norm_grad(const GroupNorm &call, hipStream_t s) {
+  GroupNorm g = call;
+  const bool sums = g.dweight || g.dbias;
+  long long count = 0;   // rows of partial sums
+  if (g.samples > 0 && g.positions == 1) {
+    const Rows r = rows_of(g);
+    if (!sums) g.scratch = nullptr;
+    if (r.team == 0) {
+      if (sums) {
+        count = g.samples < kLongSplits ? g.samples : kLongSplits;
+        const long long eights = ((g.channels / g.groups + 7) / 8) * g.groups;
+        k_norm_long_channels<T><<<dim3((unsigned)((eights + kThreads - 1) / kThreads), (unsigned)count), kThreads, 0, s>>>(g);
+      }
+      k_norm_long_rows_grad<T><<<dim3((unsigned)(g.samples * g.groups)), 1024, 0, s>>>(g);
+    } else {
+      count = rows_workgroups(g, r);
+      const dim3 grid((unsigned)g.groups, (unsigned)count);
+      if (r.team == 16) k_norm_rows_grad<T, 16, 1><<<grid, kThreads, 0, s>>>(g);
+      else if (r.team == 64 && r.each == 1) k_norm_rows_grad<T, 64, 1><<<grid, kThreads, 0, s>>>(g);
+      else if (r.team == 64) k_norm_rows_grad<T, 64, 4><<<grid, kThreads, 0, s>>>(g);
+      else k_norm_rows_grad<T, 256, 4><<<grid, kThreads, 0, s>>>(g);
+    }
+  } else if (g.samples > 0 && g.positions > 0) {
+    const GradMaps q = grad_maps(g);
+    if (workgroups(g, q.m) > kMostWorkgroups) return hipErrorInvalidValue;
+    const dim3 grid((unsigned)workgroups(g, q.m));
+    count = g.samples * q.m.chunks;
+    if (!q.whole) {
+      k_norm_maps_grad<T, 256, 4, kPieces><<<grid, 256, 0, s>>>(g, q.m);
+      k_norm_maps_grad<T, 256, 4, kJoined><<<grid, 256, 0, s>>>(g, q.m);
+    } else if (q.threads == 256) {
+      if (q.each == 2) k_norm_maps_grad<T, 256, 2, kWhole><<<grid, 256, 0, s>>>(g, q.m);
+      else k_norm_maps_grad<T, 256, 4, kWhole><<<grid, 256, 0, s>>>(g, q.m);
+    } else {
+      k_norm_maps_grad<T, 1024, sizeof(T) == 4 ? 4 : 8, kWhole><<<grid, 1024, 0, s>>>(g, q.m);
+    }
+  }
+  if (sums) k_norm_join<<<dim3((unsigned)((2 * g.channels + 63) / 64)), 1024, 0, s>>>(g, g.scratch, count);
+  return hipGetLastError();
 }
 
 }  // namespace
 
-size_t group_norm_scratch(const GroupNorm &, bool) { return 0; }
-
-hipError_t launch_group_norm(const GroupNorm &g, hipStream_t s) {
-  const dim3 grid((unsigned)(g.samples * g.groups));
-  if (g.type == kF32) k_norm<float><<<grid, 256, 0, s>>>(g);
-  else k_norm<bf16><<<grid, 256, 0, s>>>(g);
-  return hipGetLastError();
+size_t group_norm_scratch(const GroupNorm &g, bool gradient) {
+  if (g.samples == 0 || g.positions == 0 || g.channels == 0) return 0;
+  if (!gradient) {
+    if (g.positions == 1 || whole(g, maps_of(g, 256, 2)) || whole(g, maps_of(g, 256, 8)) || whole(g, maps_of(g, 1024, 8))) return 0;
+    return (size_t)(g.samples * g.groups * maps_of(g, 256, 8).pieces_a_group) * 2 * sizeof(float);
+  }
+  long long count;
+  if (g.positions == 1) {
+    if (!g.dweight && !g.dbias) return 0;
+    const Rows r = rows_of(g);
+    count = r.team == 0 ? (g.samples < kLongSplits ? g.samples : kLongSplits) : rows_workgroups(g, r);
+  } else {
+    count = g.samples * grad_maps(g).m.chunks;
+  }
+  return (size_t)(count * 2 * g.channels) * sizeof(float);
 }
 
-hipError_t launch_group_norm_grad(const GroupNorm &g, hipStream_t s) {
-  if (g.dweight || g.dbias) {
-    const dim3 grid((unsigned)((g.channels + 63) / 64));
-    if (g.type == kF32) k_norm_channels<float><<<grid, 256, 0, s>>>(g);
-    else k_norm_channels<bf16><<<grid, 256, 0, s>>>(g);
-  }
-  const dim3 grid((unsigned)(g.samples * g.groups));
-  if (grid.x && g.positions) {
-    if (g.type == kF32) k_norm_grad<float><<<grid, 256, 0, s>>>(g);
-    else k_norm_grad<bf16><<<grid, 256, 0, s>>>(g);
-  }
-  return hipGetLastError();
-}
+hipError_t launch_group_norm(const GroupNorm &g, hipStream_t s) { return g.type == kF32 ? norm<float>(g, s) : norm<bf16>(g, s); }
+hipError_t launch_group_norm_grad(const GroupNorm &g, hipStream_t s) { return g.type == kF32 ? norm_grad<float>(g, s) : norm_grad<bf16>(g, s); }
 
 }  // namespace qoda
