@@ -13,7 +13,8 @@
  *     thread's last error).  Arguments are checked before anything is launched; nothing throws across this boundary.
  *   - A matrix is row-major: `data` points at entry (0, 0) in device memory, entries of a row are adjacent, rows are `stride`
  *     entries apart (stride >= columns where there is more than one row).  Any alignment that the type itself has will do;
- *     16-byte rows are fastest.  Offsets are 64-bit throughout; a matrix has fewer than 2^31 rows and 2^31 columns.
+ *     rows that start at multiples of 16 bytes are fastest.  Offsets are 64-bit throughout; rows, columns, samples, positions and
+ *     channels number at most QODA_MAX_SIDE each, and samples times groups are fewer than 2^31.
  *   - Outputs may be no input's memory, except where a call says so.  A size of zero is no error: an empty output is left alone, and
  *     a sum over nothing is 0.
  *   - Entries are fp32 (QODA_F32) or bfloat16 (QODA_BF16); biases, scales, statistics and gradients of parameters are fp32.
@@ -38,6 +39,8 @@
 #ifdef __cplusplus
 extern "C" {
 #endif
+
+#define QODA_MAX_SIDE 0x7fff0000
 
 #define QODA_F32 0
 #define QODA_BF16 1

@@ -34,12 +34,13 @@ template <int SIDE>
 __device__ __forceinline__ int row_swizzle(int row) {
   return SIDE == 0 ? (row >> 1) & 7 : ((row >> 1) & 1) | ((row >> 2) & 6);
 }
-// ... and in row l of a "columns" tile.  bf16: a read touches rows 8 g + r and 32 (SIDE 0) or every other 8 of 64 bytes of each; fp32: rows
-// 4 g and 64 bytes, or every other 16 of 128.
-template <class T, int SIDE>
+// ... and in row l of a "columns" tile of N entries.  bf16: a read touches rows 8 g + r and 32 (SIDE 0) or every other 8 of 64 bytes of each;
+// fp32: rows 4 g and 64 bytes, or every other 16 of 128.
+template <class T, int SIDE, int N>
 __device__ __forceinline__ int column_swizzle(int l) {
-  if constexpr (sizeof(T) == 2) return SIDE == 0 ? ((l & 3) << 1) | (l & 8) : (l & 3) << 2;
-  else return SIDE == 0 ? l & 12 : ((l & 4) << 1) | ((l >> 3) & 1);
+  constexpr int kMask = N * (int)sizeof(T) / 16 - 1;   // of the row's chunks
+  if constexpr (sizeof(T) == 2) return (SIDE == 0 ? ((l & 3) << 1) | (l & 8) : (l & 3) << 2) & kMask;
+  else return (SIDE == 0 ? l & 12 : ((l & 4) << 1) | ((l >> 3) & 1)) & kMask;
 }
 
 // A chunk of 16 bytes of which the first `valid` entries (any number) exist; the others come as 0.
@@ -49,14 +50,18 @@ __device__ __forceinline__ v4u load_chunk(const T *p, int valid) {
   v4u v = {0, 0, 0, 0};
   if (valid >= E) {
     __builtin_memcpy(&v, p, 16);
-  } else if constexpr (sizeof(T) == 4) {
+  } else if (valid > 0) {   // all at once, those beyond the end from the last one's place: a branch for each would wait for each
+    u32 e[E];
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (j < valid) v[j] = __builtin_bit_cast(u32, p[j]);
-  } else {
+    for (int j = 0; j < E; ++j) {
+      const T *q = p + (j < valid ? j : valid - 1);
+      if constexpr (sizeof(T) == 4) e[j] = __float_as_uint(*q);
+      else e[j] = q->bits;
+    }
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (j < valid) v[j / 2] |= (u32)p[j].bits << (16 * (j & 1));
+    for (int j = 0; j < E; ++j) e[j] = j < valid ? e[j] : 0u;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = sizeof(T) == 4 ? e[j] : e[2 * j % E] | e[(2 * j + 1) % E] << 16;
   }
   return v;
 }
@@ -69,6 +74,7 @@ struct Operand {
   static constexpr int kRowChunks = ROWS ? 8 : N / E;           // chunks of a row in shared memory
   static constexpr int kMine = N * 8 / WG;                      // chunks that a thread moves
   static_assert(N * 8 % WG == 0, "whole chunks a thread");
+  static_assert((N & (N - 1)) == 0, "chunks are permuted inside a row");
 
   const T *base;     // entry (first, 0)
   long long ld;
@@ -79,7 +85,7 @@ struct Operand {
   static __device__ __forceinline__ void place(int q, int &row, int &chunk) {
     const int at = q * WG + (int)threadIdx.x;
     row = at / kRowChunks;
-    chunk = (at % kRowChunks) ^ (ROWS ? row_swizzle<SIDE>(row) : column_swizzle<T, SIDE>(row));
+    chunk = (at % kRowChunks) ^ (ROWS ? row_swizzle<SIDE>(row) : column_swizzle<T, SIDE, N>(row));
   }
   __device__ __forceinline__ void start(const void *p, long long ld_, int first, int end, int k0, int k_) {
     ld = ld_;
@@ -132,7 +138,7 @@ struct Operand {
       for (int h = 0; h < 2; ++h) {
         const int l = s * 32 + g * 8 + h * 4 + (i >> 2);
         const v4s r = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            LDS(v4s, tile + l * (N * 2) + (((c4 >> 3) ^ column_swizzle<T, SIDE>(l)) * 16) + (c4 & 4) * 2));
+            LDS(v4s, tile + l * (N * 2) + (((c4 >> 3) ^ column_swizzle<T, SIDE, N>(l)) * 16) + (c4 & 4) * 2));
         const uint2 w = __builtin_bit_cast(uint2, r);
         v[2 * h] = w.x, v[2 * h + 1] = w.y;
       }
@@ -142,7 +148,7 @@ struct Operand {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int l = s * 16 + g * 4 + j;
-        v[j] = *LDS(u32, tile + l * (N * 4) + (((a >> 2) ^ column_swizzle<T, SIDE>(l)) * 16) + (a & 3) * 4);
+        v[j] = *LDS(u32, tile + l * (N * 4) + (((a >> 2) ^ column_swizzle<T, SIDE, N>(l)) * 16) + (a & 3) * 4);
       }
       return v;
     }
@@ -370,6 +376,49 @@ __global__ void __launch_bounds__(64 * WM * WN) k_product(Product p, int tiles_m
   else by_activation<FORM>(p.activation, [&](auto a) { each([&](int i, int j, int n, float (&v)[8]) { finish<T, FORM, decltype(a)::value>(p, i, j, n, v); }); });
 }
 
+// x w^T for up to 16 rows of x: w is read once and that is the time.  A workgroup takes 16 rows of w, its NW waves the runs of 128 bytes along l in
+// turn, straight into the matrix instruction's registers: a lane's 32 bytes of a run are its pieces of two instructions (the
+// order along l is the same for both operands, and of no matter).  The waves' sums are joined in shared memory.
+template <class T, int NW>
+__global__ void __launch_bounds__(64 * NW) k_few_rows(Product p) {
+  constexpr int E = 16 / (int)sizeof(T), kRun = 8 * E, kAhead = 4;
+  __shared__ v4f part[NW][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, i = lane & 15, g = lane >> 4;
+  const int j0 = (int)blockIdx.x * 16;
+  const T *b = static_cast<const T *>(p.b) + (long long)(j0 + i < p.n ? j0 + i : p.n - 1) * p.ldb;
+  const T *a = static_cast<const T *>(p.a) + (long long)(i < p.m ? i : 0) * p.lda;
+  v4f c = {0, 0, 0, 0};
+  for (int l0 = wave * kRun; l0 < p.k; l0 += NW * kRun * kAhead) {
+    v4u fb[kAhead][2], fa[kAhead][2];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int l = l0 + u * NW * kRun + (2 * g + h) * E;
+        fb[u][h] = load_chunk<T>(b + l, p.k - l);
+        fa[u][h] = load_chunk<T>(a + l, i < p.m ? p.k - l : 0);
+      }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) c = multiply<T>(fb[u][h], fa[u][h], c);
+  }
+  part[wave][lane] = c;
+  __syncthreads();
+  // sums of column 4 g + r of the 16 and row i lie in lane 16 g + i, place r
+  const int row = (int)threadIdx.x / 2, j = (int)(threadIdx.x & 1) * 8;
+  if (row < p.m && j0 + j < p.n) {
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      v[e] = part[0][(j + e) / 4 * 16 + row][e & 3];
+#pragma unroll
+      for (int w = 1; w < NW; ++w) v[e] = v[e] + part[w][(j + e) / 4 * 16 + row][e & 3];
+    }
+    by_activation<kProductRows>(p.activation, [&](auto x) { finish<T, kProductRows, decltype(x)::value>(p, row, j0 + j, p.n - j0 - j, v); });
+  }
+}
+
 // The splits' sums added up in their order, and finished.
 template <class T, int FORM>
 __global__ void __launch_bounds__(256) k_join(Product p, int splits) {
@@ -395,35 +444,74 @@ __global__ void __launch_bounds__(256) k_join(Product p, int splits) {
       }
 }
 
+// How a product is cut.
+enum Tile { kFewRows, kTile32, kTile64, kTile128, kTile256 };
 struct Plan {
+  Tile tile;
+  bool direct;
   int tiles_m, tiles_n, splits, steps_each;
-  bool large, direct;
 };
 
-int step_of(const Product &p) { return kStepBytes / (p.type == kF32 ? 4 : 2); }
+constexpr int kCus = 256;
 
 Plan plan_of(const Product &p) {
   Plan q = {};
-  const int e = p.type == kF32 ? 4 : 2;
-  const auto ok = [&](const void *v, long long ld, bool rows, int n) {
-    return reinterpret_cast<uintptr_t>(v) % 16 == 0 && ld * e % 16 == 0 && (rows ? n : step_of(p)) * ld * e < (1ll << 31);
-  };
-  q.direct = p.n > 0 && ok(p.a, p.lda, p.form != kProductColumns, 256) && ok(p.b, p.ldb, p.form == kProductRows, 256);
-  q.large = q.direct && (long long)((p.m + 255) / 256) * ((p.n + 255) / 256) >= 128;
-  const int side = q.large ? 256 : 128;
-  q.tiles_m = (p.m + side - 1) / side, q.tiles_n = p.n > 0 ? (p.n + side - 1) / side : 1;
-  const int steps = (p.k + step_of(p) - 1) / step_of(p);
+  const int e = p.type == kF32 ? 4 : 2, step = kStepBytes / e;
   q.splits = 1;
-  q.steps_each = steps > 0 ? steps : 1;
+  if (p.m == 0 || (p.n == 0 && !p.sums)) return q;   // nothing to launch
+  if (p.form == kProductRows && p.m <= 16) {
+    q.tile = kFewRows;
+    q.tiles_m = 1, q.tiles_n = (p.n + 15) / 16;
+    return q;
+  }
+  // direct loads move aligned chunks of 16 bytes, by 32-bit offsets inside a tile
+  const auto fits = [&](const void *v, long long ld, bool rows) {
+    return reinterpret_cast<uintptr_t>(v) % 16 == 0 && ld * e % 16 == 0 && (rows ? 256 : step) * ld * e < (1ll << 31);
+  };
+  q.direct = p.n > 0 && fits(p.a, p.lda, p.form != kProductColumns) && fits(p.b, p.ldb, p.form == kProductRows);
+  const auto tiles = [&](int bm, int bn) { return (long long)((p.m + bm - 1) / bm) * (p.n > 0 ? (p.n + bn - 1) / bn : 1); };
+  const int steps = p.k > 0 ? (p.k + step - 1) / step : 1;
+  int bm, bn, slots;
+  if (p.m <= 32) q.tile = kTile32, bm = 32, bn = 128, slots = 4 * kCus;
+  else if (q.direct && tiles(256, 256) >= kCus * 3 / 4) q.tile = kTile256, bm = bn = 256, slots = kCus;
+  else if (tiles(128, 128) * (steps < 16 ? 1 : steps / 8) >= kCus) q.tile = kTile128, bm = bn = 128, slots = 2 * kCus;
+  else q.tile = kTile64, bm = bn = 64, slots = 4 * kCus;
+  q.tiles_m = (p.m + bm - 1) / bm, q.tiles_n = p.n > 0 ? (p.n + bn - 1) / bn : 1;
+  // few tiles: the sum over l is split, into parts of at least four steps, until the device is full once
+  const long long want = slots / tiles(bm, bn), most = steps / 4;
+  q.splits = (int)(want < most ? want : most);
+  if (q.tile == kTile256 || q.splits < 2) q.splits = 1;
+  q.steps_each = (steps + q.splits - 1) / q.splits;
+  q.splits = (steps + q.steps_each - 1) / q.steps_each;
   return q;
+}
+
+template <class T, int FORM, int BM, int BN, int WM, int WN>
+void launch(const Product &p, const Plan &q, hipStream_t s) {
+  const dim3 grid((unsigned)(q.tiles_m * q.tiles_n), (unsigned)q.splits);
+  if (q.direct) k_product<T, FORM, BM, BN, WM, WN, true><<<grid, 64 * WM * WN, 0, s>>>(p, q.tiles_m, q.tiles_n, q.steps_each);
+  else if constexpr (BM < 256) k_product<T, FORM, BM, BN, WM, WN, false><<<grid, 64 * WM * WN, 0, s>>>(p, q.tiles_m, q.tiles_n, q.steps_each);
 }
 
 template <class T, int FORM>
 void launch(const Product &p, const Plan &q, hipStream_t s) {
-  const dim3 grid((unsigned)(q.tiles_m * q.tiles_n), (unsigned)q.splits);
-  if (q.large) k_product<T, FORM, 256, 256, 2, 4, true><<<grid, 512, 0, s>>>(p, q.tiles_m, q.tiles_n, q.steps_each);
-  else if (q.direct) k_product<T, FORM, 128, 128, 2, 2, true><<<grid, 256, 0, s>>>(p, q.tiles_m, q.tiles_n, q.steps_each);
-  else k_product<T, FORM, 128, 128, 2, 2, false><<<grid, 256, 0, s>>>(p, q.tiles_m, q.tiles_n, q.steps_each);
+  switch (q.tile) {
+    case kFewRows:
+      if constexpr (FORM == kProductRows) {
+        // with few workgroups more waves each
+        if (q.tiles_n >= kCus) k_few_rows<T, 4><<<dim3((unsigned)q.tiles_n), 256, 0, s>>>(p);
+        else k_few_rows<T, 16><<<dim3((unsigned)q.tiles_n), 1024, 0, s>>>(p);
+      }
+      return;
+    case kTile32: launch<T, FORM, 32, 128, 1, 4>(p, q, s); break;
+    case kTile64: launch<T, FORM, 64, 64, 2, 2>(p, q, s); break;
+    case kTile128: launch<T, FORM, 128, 128, 2, 2>(p, q, s); break;
+    case kTile256: launch<T, FORM, 256, 256, 2, 4>(p, q, s); break;
+  }
+  if (q.splits > 1) {
+    const long long blocks = (long long)p.m * ((p.n + 7) / 8), groups = (blocks + 255) / 256;
+    k_join<T, FORM><<<dim3((unsigned)(groups < 4 * kCus ? (groups > 0 ? groups : 1) : 4 * kCus)), 256, 0, s>>>(p, q.splits);
+  }
 }
 
 template <class T>
@@ -437,14 +525,16 @@ void launch(const Product &p, const Plan &q, hipStream_t s) {
 
 }  // namespace
 
-size_t product_scratch(const Product &) { return 0; }
+size_t product_scratch(const Product &p) {
+  const Plan q = plan_of(p);
+  return q.splits < 2 ? 0 : sizeof(float) * (size_t)q.splits * ((size_t)p.m * p.n + (p.sums ? p.m : 0));
+}
 
 hipError_t launch_product(const Product &call, hipStream_t s) {
   Product p = call;
-  // without columns of c there is still one of tiles, for the sums of a's columns
   const Plan q = plan_of(p);
   if ((long long)q.tiles_m * q.tiles_n > 0x7fffffffll) return hipErrorInvalidValue;
-  if (q.splits == 1) p.partial = nullptr;
+  if (q.splits < 2) p.partial = nullptr;
   if (p.type == kF32) launch<float>(p, q, s);
   else launch<bf16>(p, q, s);
   return hipGetLastError();

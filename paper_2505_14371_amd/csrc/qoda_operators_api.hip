@@ -28,7 +28,7 @@ int done(const char *call, hipError_t e) {
   return fail(e == hipErrorOutOfMemory ? QODA_ENOMEM : QODA_EHIP, "%s: %s", call, hipGetErrorString(e));
 }
 
-constexpr int64_t kMostSide = (int64_t)1 << 31;   // rows and columns stay below it
+constexpr int64_t kMostSide = QODA_MAX_SIDE;   // rows and columns: the kernels' 32-bit indexes go a tile beyond them
 constexpr int64_t kMostStride = (int64_t)1 << 40;
 
 size_t entry_bytes(int type) { return type == kF32 ? 4 : 2; }
@@ -53,7 +53,7 @@ int check_common(const char *call, int32_t dtype, int32_t activation) {
 
 int check_sides(const char *call, int64_t a, int64_t b, int64_t c) {
   for (const int64_t v : {a, b, c})
-    if (v < 0 || v >= kMostSide) return fail(QODA_EINVAL, "%s: a size of %lld is not in [0, 2^31)", call, (long long)v);
+    if (v < 0 || v > kMostSide) return fail(QODA_EINVAL, "%s: a size of %lld is not in [0, %lld]", call, (long long)v, (long long)kMostSide);
   return QODA_OK;
 }
 
@@ -209,9 +209,9 @@ int check_values(const char *call, const char *name, const qoda_channels_last &v
 
 int check_groups(const char *call, int64_t samples, int64_t positions, int64_t channels, int64_t groups) {
   TRY(check_sides(call, samples, positions, channels));
-  if (groups < 1 || channels % groups != 0 || groups > kMostSide - 1)
+  if (groups < 1 || channels % groups != 0 || groups > kMostSide)
     return fail(QODA_EINVAL, "%s: %lld groups do not divide %lld channels", call, (long long)groups, (long long)channels);
-  if (samples * groups >= kMostSide) return fail(QODA_EINVAL, "%s: %lld samples of %lld groups are 2^31 statistics or more", call, (long long)samples, (long long)groups);
+  if (samples * groups >= (int64_t)1 << 31) return fail(QODA_EINVAL, "%s: %lld samples of %lld groups are 2^31 statistics or more", call, (long long)samples, (long long)groups);
   return QODA_OK;
 }
 

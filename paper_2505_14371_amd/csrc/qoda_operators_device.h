@@ -109,12 +109,17 @@ struct Eight {
 #pragma unroll
       for (int q = 0; q < kWords / 4; ++q) __builtin_memcpy(&w[q], reinterpret_cast<const char *>(p) + 16 * q, 16);
     } else {
-      u32 e[8];
+      u32 e[8] = {};
+      if (n > 0) {   // all at once, those beyond the end from the last one's place: a branch for each would wait for each
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        if constexpr (sizeof(T) == 4) e[j] = j < n ? __builtin_bit_cast(u32, p[j]) : 0u;
-        else e[j] = j < n ? p[j].bits : 0u;
+        for (int j = 0; j < 8; ++j) {
+          const T *q = p + (j < n ? j : n - 1);
+          if constexpr (sizeof(T) == 4) e[j] = __float_as_uint(*q);
+          else e[j] = q->bits;
+        }
       }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) e[j] = j < n ? e[j] : 0u;
 #pragma unroll
       for (int j = 0; j < kWords; ++j) w[j / 4][j % 4] = sizeof(T) == 4 ? e[j] : e[2 * j % 8] | e[(2 * j + 1) % 8] << 16;
     }

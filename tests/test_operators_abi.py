@@ -86,6 +86,10 @@ def test_refusals_launch_nothing(lib):
 def test_empty_outputs_are_no_error(lib):
     assert lib.qoda_linear(linear(rows=0, x=0, y=0), None, 0, None) == qoda.OK
     assert lib.qoda_linear(linear(cout=0, w=0, y=0), None, 0, None) == qoda.OK
+    for rows, cin, cout in ((0, 5, 7), (5, 0, 7), (5, 7, 0), (0, 0, 0)):
+        assert lib.qoda_linear_workspace_bytes(linear(rows=rows, cin=cin, cout=cout, ys=8)) >= 0
+        assert lib.qoda_linear_input_grad_workspace_bytes(ops._INPUT_GRAD.pack(0, 0, rows, cin, cout, 4096, 8, 4096, 8, 0, 8, 0, 8, 8192, 8, 0.0, 0, 0)) >= 0
+        assert lib.qoda_linear_weight_grad_workspace_bytes(ops._WEIGHT_GRAD.pack(0, 0, rows, cin, cout, 4096, 8, 4096, 8, 8192, 8, 4096)) >= 0
     assert lib.qoda_dropout(ops._DROPOUT.pack(0, 0, 0, 8, 0, 0, 0, 0, 0, 0, 0.5, 0, 0), None) == qoda.OK
     assert lib.qoda_group_norm(ops._NORM.pack(0, 0, 0, 3, 8, 2, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 1e-5), None, 0, None) == qoda.OK
 
