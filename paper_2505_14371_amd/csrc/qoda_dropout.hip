@@ -1,5 +1,7 @@
 // Dropout and its gradient, with the activation and the residual beside it (include/qoda_operators.h).
 
+#include <type_traits>
+
 #include "qoda_operators_device.h"
 
 namespace qoda {
@@ -23,7 +25,7 @@ __device__ __forceinline__ u32 divide(u32 v, const Divisor &d) {
 constexpr int kEach = 4;   // blocks of eight entries a thread: so many loads on their way while the first block's lots are drawn
 
 // A thread takes blocks of eight entries, which share one draw of lots: 16 bytes of bf16.
-template <class T, int ACT, bool GRAD, bool EXTRA, bool DROP>
+template <class T, int ACT, bool GRAD, bool EXTRA, bool DROP, bool EVEN>
 __global__ void __launch_bounds__(256) k_entries(Entries e, Divisor blocks) {
   // the workgroup's first block by a 64-bit division, the others from it in 32 bits
   const long long total = e.rows * blocks.d, q0 = (long long)blockIdx.x * (256 * kEach);
@@ -41,8 +43,8 @@ __global__ void __launch_bounds__(256) k_entries(Entries e, Divisor blocks) {
     block[u] = at - r * blocks.d;
     n[u] = q0 + u * 256 + threadIdx.x < total ? (int)(e.cols - (long long)block[u] * 8) : 0;
     if (n[u] > 0) {
-      mine[u].load(x + row[u] * e.ldx + (long long)block[u] * 8, n[u]);
-      if (EXTRA) other[u].load(extra + row[u] * e.lde + (long long)block[u] * 8, n[u]);
+      mine[u].template load<EVEN>(x + row[u] * e.ldx + (long long)block[u] * 8, n[u]);
+      if (EXTRA) other[u].template load<EVEN>(extra + row[u] * e.lde + (long long)block[u] * 8, n[u]);
     }
   }
 #pragma unroll
@@ -57,14 +59,18 @@ __global__ void __launch_bounds__(256) k_entries(Entries e, Divisor blocks) {
       if (!GRAD && EXTRA)
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = o[j] + v[j];
-      store8(static_cast<T *>(e.y) + row[u] * e.ldy + (long long)block[u] * 8, n[u], v);
+      store8<EVEN>(static_cast<T *>(e.y) + row[u] * e.ldy + (long long)block[u] * 8, n[u], v);
     }
 }
 
 template <class T, int ACT, bool GRAD, bool EXTRA>
 void launch(const Entries &e, unsigned grid, const Divisor &d, hipStream_t s) {
-  if (e.drop.threshold) k_entries<T, ACT, GRAD, EXTRA, true><<<dim3(grid), 256, 0, s>>>(e, d);
-  else k_entries<T, ACT, GRAD, EXTRA, false><<<dim3(grid), 256, 0, s>>>(e, d);
+  const auto run = [&](auto even) {
+    if (e.drop.threshold) k_entries<T, ACT, GRAD, EXTRA, true, decltype(even)::value><<<dim3(grid), 256, 0, s>>>(e, d);
+    else k_entries<T, ACT, GRAD, EXTRA, false, decltype(even)::value><<<dim3(grid), 256, 0, s>>>(e, d);
+  };
+  if (e.cols % 8 == 0) run(std::true_type());
+  else run(std::false_type());
 }
 
 template <class T, int ACT>

@@ -52,9 +52,25 @@ __device__ __forceinline__ float team_sum(float v, float *red) {
   }
 }
 
+// Two at once, with one barrier.  red: two floats for each wave.
+template <int TEAM>
+__device__ __forceinline__ void team_sums(float &a, float &b, float2 *red) {
+  if constexpr (TEAM <= 64) {
+    a = lanes_sum<TEAM>(a), b = lanes_sum<TEAM>(b);
+  } else {
+    a = lanes_sum<64>(a), b = lanes_sum<64>(b);
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x / 64] = {a, b};
+    __syncthreads();
+    a = b = 0.0f;
+#pragma unroll
+    for (int w = 0; w < TEAM / 64; ++w) a = a + red[w].x, b = b + red[w].y;
+  }
+}
+
+template <bool EVEN = false>
 __device__ __forceinline__ void vector8(const float *p, float otherwise, int n, float (&v)[8]) {
   if (p) {
-    load8(p, n, v);
+    load8<EVEN>(p, n, v);
   } else {
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = otherwise;
@@ -90,23 +106,25 @@ __device__ __forceinline__ void slope8(int a, const float (&z)[8], float (&v)[8]
 }
 
 // Eight normalised values times weight plus bias, through the activation.
+template <bool EVEN = false>
 __device__ __forceinline__ void normalised8(const GroupNorm &g, long long c, int n, float mean, float rstd, float (&v)[8]) {
   float w[8], b[8];
-  vector8(g.weight ? g.weight + c : nullptr, 1.0f, n, w);
-  vector8(g.bias ? g.bias + c : nullptr, 0.0f, n, b);
+  vector8<EVEN>(g.weight ? g.weight + c : nullptr, 1.0f, n, w);
+  vector8<EVEN>(g.bias ? g.bias + c : nullptr, 0.0f, n, b);
 #pragma unroll
   for (int j = 0; j < 8; ++j) v[j] = __builtin_fmaf((v[j] - mean) * rstd, w[j], b[j]);
   act8(g.activation, v);
 }
 
 // h: the normalised values of x; d: dy through the activation; w: the weights.
+template <bool EVEN = false>
 __device__ __forceinline__ void back8(const GroupNorm &g, long long c, int n, float mean, float rstd, float (&h)[8], float (&d)[8], float (&w)[8]) {
 #pragma unroll
   for (int j = 0; j < 8; ++j) h[j] = (h[j] - mean) * rstd;
-  vector8(g.weight ? g.weight + c : nullptr, 1.0f, n, w);
+  vector8<EVEN>(g.weight ? g.weight + c : nullptr, 1.0f, n, w);
   if (g.activation != kActNone) {
     float z[8];
-    vector8(g.bias ? g.bias + c : nullptr, 0.0f, n, z);
+    vector8<EVEN>(g.bias ? g.bias + c : nullptr, 0.0f, n, z);
 #pragma unroll
     for (int j = 0; j < 8; ++j) z[j] = __builtin_fmaf(h[j], w[j], z[j]);
     slope8(g.activation, z, d);
@@ -124,7 +142,7 @@ struct Row {
 };
 
 // A team a row, V times eight entries a lane.
-template <class T, int TEAM, int V>
+template <class T, int TEAM, int V, bool EVEN>
 __global__ void __launch_bounds__(kThreads) k_norm_rows(GroupNorm g) {
   __shared__ float red[2][kThreads / 64];
   const int lane = threadIdx.x % TEAM;
@@ -137,7 +155,7 @@ __global__ void __launch_bounds__(kThreads) k_norm_rows(GroupNorm g) {
   const T *x = static_cast<const T *>(g.x) + row.n * g.x_sample + row.c0;
   Eight<T> raw[V];
 #pragma unroll
-  for (int v = 0; v < V; ++v) raw[v].load(x + (lane + v * TEAM) * 8, len - (lane + v * TEAM) * 8);
+  for (int v = 0; v < V; ++v) raw[v].template load<EVEN>(x + (lane + v * TEAM) * 8, len - (lane + v * TEAM) * 8);
   float s = 0.0f;
 #pragma unroll
   for (int v = 0; v < V; ++v) {
@@ -154,7 +172,7 @@ __global__ void __launch_bounds__(kThreads) k_norm_rows(GroupNorm g) {
     const int n = len - (lane + v * TEAM) * 8;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const float d = j < n ? e[j] - mean : 0.0f;
+      const float d = (EVEN ? n > 0 : j < n) ? e[j] - mean : 0.0f;
       s = __builtin_fmaf(d, d, s);
     }
   }
@@ -168,8 +186,8 @@ __global__ void __launch_bounds__(kThreads) k_norm_rows(GroupNorm g) {
     if (n > 0) {
       float e[8];
       raw[v].get(e);
-      normalised8(g, row.c0 + at, n, mean, rstd, e);
-      store8(y + at, n, e);
+      normalised8<EVEN>(g, row.c0 + at, n, mean, rstd, e);
+      store8<EVEN>(y + at, n, e);
     }
   }
 }
@@ -211,10 +229,10 @@ __global__ void __launch_bounds__(1024) k_norm_long_rows(GroupNorm g) {
 
 // The gradient of rows.  A team takes rows of one group, `step` samples apart, and keeps its channels' sums for dweight and dbias in
 // registers; the workgroup's teams join theirs in shared memory and store one row of partial sums.  grid: (groups, workgroups a group).
-template <class T, int TEAM, int V>
+template <class T, int TEAM, int V, bool EVEN>
 __global__ void __launch_bounds__(kThreads) k_norm_rows_grad(GroupNorm g) {
   constexpr int kTeams = kThreads / TEAM;
-  __shared__ float red[2][2][kThreads / 64];
+  __shared__ float2 red[2][kThreads / 64];
   __shared__ float join[kTeams > 1 ? TEAM * V * 8 : 1];
   const int lane = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
   const int len = (int)(g.channels / g.groups);
@@ -230,9 +248,9 @@ __global__ void __launch_bounds__(kThreads) k_norm_rows_grad(GroupNorm g) {
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       const int at = (lane + v * TEAM) * 8;
-      rx[v].load(x + at, len - at);
-      rd[v].load(dy + at, len - at);
-      if (g.extra) re[v].load(static_cast<const T *>(g.extra) + n * g.extra_sample + c0 + at, len - at);
+      rx[v].template load<EVEN>(x + at, len - at);
+      rd[v].template load<EVEN>(dy + at, len - at);
+      if (g.extra) re[v].template load<EVEN>(static_cast<const T *>(g.extra) + n * g.extra_sample + c0 + at, len - at);
     }
     const float mean = g.mean[n * g.groups + blockIdx.x], rstd = g.rstd[n * g.groups + blockIdx.x];
     float s1 = 0.0f, s2 = 0.0f;
@@ -243,10 +261,10 @@ __global__ void __launch_bounds__(kThreads) k_norm_rows_grad(GroupNorm g) {
         float h[8], d[8], w[8];
         rx[v].get(h);
         rd[v].get(d);   // 0 beyond the row
-        back8(g, c0 + at, len - at, mean, rstd, h, d, w);
+        back8<EVEN>(g, c0 + at, len - at, mean, rstd, h, d, w);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          if (len - at <= j) d[j] = 0.0f, h[j] = 0.0f;
+          if (!EVEN && len - at <= j) d[j] = 0.0f, h[j] = 0.0f;
           if (real) sw[v][j] = __builtin_fmaf(d[j], h[j], sw[v][j]), sb[v][j] = sb[v][j] + d[j];
           const float u = d[j] * w[j];
           s1 = s1 + u;
@@ -254,8 +272,8 @@ __global__ void __launch_bounds__(kThreads) k_norm_rows_grad(GroupNorm g) {
         }
       }
     }
-    // two sums a turn, in places that the last turn's readers have left
-    const float m1 = team_sum<TEAM>(s1, red[turn][0]) * inv, m2 = team_sum<TEAM>(s2, red[turn][1]) * inv;
+    team_sums<TEAM>(s1, s2, red[turn]);   // by turns: the readers of one place are done before the next barrier but one
+    const float m1 = s1 * inv, m2 = s2 * inv;
     if (real) {
       T *dx = static_cast<T *>(g.out) + n * g.out_sample + c0;
 #pragma unroll
@@ -265,14 +283,14 @@ __global__ void __launch_bounds__(kThreads) k_norm_rows_grad(GroupNorm g) {
           float h[8], d[8], w[8], o[8];
           rx[v].get(h);
           rd[v].get(d);
-          back8(g, c0 + at, len - at, mean, rstd, h, d, w);
+          back8<EVEN>(g, c0 + at, len - at, mean, rstd, h, d, w);
           if (g.extra) re[v].get(o);
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
             const float q = __builtin_fmaf(-h[j], m2, __builtin_fmaf(d[j], w[j], -m1)) * rstd;
             d[j] = g.extra ? o[j] + q : q;
           }
-          store8(dx + at, len - at, d);
+          store8<EVEN>(dx + at, len - at, d);
         }
       }
     }
@@ -302,13 +320,13 @@ __global__ void __launch_bounds__(kThreads) k_norm_rows_grad(GroupNorm g) {
           float e[8];
 #pragma unroll
           for (int j = 0; j < 8; ++j) e[j] = join[(v * 8 + j) * TEAM + lane];
-          if (at < len) store8(part + k * g.channels + at, len - at, e);
+          if (at < len) store8<EVEN>(part + k * g.channels + at, len - at, e);
         }
     } else {
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         const int at = (lane + v * TEAM) * 8;
-        if (at < len) store8(part + k * g.channels + at, len - at, k == 0 ? sw[v] : sb[v]);
+        if (at < len) store8<EVEN>(part + k * g.channels + at, len - at, k == 0 ? sw[v] : sb[v]);
       }
     }
   }
@@ -374,23 +392,32 @@ __global__ void __launch_bounds__(kThreads) k_norm_long_channels(GroupNorm g) {
   store8(part + g.channels, n, sb);
 }
 
-// dweight and dbias from `count` rows of partial sums [2][channels]: 64 columns a workgroup, its waves take rows in turn.
+// dweight and dbias from `count` rows of partial sums [2][channels]: 16 columns a workgroup, its 64 teams of 16 lanes take rows in turn.
 __global__ void __launch_bounds__(1024) k_norm_join(GroupNorm g, const float *part, long long count) {
-  __shared__ float red[16][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
-  const long long c = (long long)blockIdx.x * 64 + lane, total = 2 * g.channels;
+  __shared__ float red[64][16 + 1];
+  const int lane = threadIdx.x & 15, team = threadIdx.x / 16;
+  const long long c = (long long)blockIdx.x * 16 + lane, total = 2 * g.channels;
   float s = 0.0f;
-  if (c < total)
-    for (long long r = wave; r < count; r += 16) s = s + part[r * total + c];
-  red[wave][lane] = s;
-  __syncthreads();
-  if (wave == 0 && c < total) {
-    s = 0.0f;
+  if (c < total) {
+    long long r = team;
+    for (; r + 3 * 64 < count; r += 4 * 64) {   // four on their way
+      float v[4];
 #pragma unroll
-    for (int w = 0; w < 16; ++w) s = s + red[w][lane];
-    float *o = c < g.channels ? g.dweight : g.dbias;
-    const long long at = c < g.channels ? c : c - g.channels;
-    if (o) o[at] = g.accumulate ? o[at] + s : s;
+      for (int q = 0; q < 4; ++q) v[q] = part[(r + q * 64) * total + c];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) s = s + v[q];
+    }
+    for (; r < count; r += 64) s = s + part[r * total + c];
+  }
+  red[team][lane] = s;
+  __syncthreads();
+  const int column = threadIdx.x / 64;   // a wave adds up a column's
+  s = lanes_sum<64>(red[threadIdx.x & 63][column]);
+  const long long o = (long long)blockIdx.x * 16 + column;
+  if ((threadIdx.x & 63) == 0 && o < total) {
+    float *to = o < g.channels ? g.dweight : g.dbias;
+    const long long at = o < g.channels ? o : o - g.channels;
+    if (to) to[at] = g.accumulate ? to[at] + s : s;
   }
 }
 
@@ -506,7 +533,7 @@ enum MapsPass { kWhole = 0, kPieces = 1, kJoined = 2 };
 
 // kWhole: a block's values are in registers from the mean to the result.  kPieces: mean and squares of a piece, per group, to
 // scratch[n][group][piece][2].  kJoined: those of the group's pieces joined (Chan et al.: squares about the common mean), and the result.
-template <class T, int NT, int U, int PASS>
+template <class T, int NT, int U, int PASS, bool EVEN>
 __global__ void __launch_bounds__(NT) k_norm_maps(GroupNorm g, Maps m) {
   __shared__ float lanes[PASS == kJoined ? 1 : NT * 8];
   __shared__ float channels[PASS == kJoined ? 1 : kWidest];
@@ -517,7 +544,7 @@ __global__ void __launch_bounds__(NT) k_norm_maps(GroupNorm g, Maps m) {
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const u32 p = at.p0 + at.row + u * m.rows;
-    raw[u].load(x + (long long)p * g.x_pos, p < at.p1 ? at.own : 0);
+    raw[u].template load<EVEN>(x + (long long)p * g.x_pos, p < at.p1 ? at.own : 0);
   }
   int q[8];
   groups8(m, at.vec * 8, q);
@@ -540,7 +567,7 @@ __global__ void __launch_bounds__(NT) k_norm_maps(GroupNorm g, Maps m) {
     float mean[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      mean[j] = j < at.own ? means[q[j]] : 0.0f;
+      mean[j] = (EVEN ? at.own > 0 : j < at.own) ? means[q[j]] : 0.0f;
       v[j] = 0.0f;
     }
 #pragma unroll
@@ -549,7 +576,7 @@ __global__ void __launch_bounds__(NT) k_norm_maps(GroupNorm g, Maps m) {
       raw[u].get(e);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const float d = at.p0 + at.row + u * m.rows < at.p1 && j < at.own ? e[j] - mean[j] : 0.0f;
+        const float d = at.p0 + at.row + u * m.rows < at.p1 && (EVEN ? at.own > 0 : j < at.own) ? e[j] - mean[j] : 0.0f;
         v[j] = __builtin_fmaf(d, d, v[j]);
       }
     }
@@ -595,11 +622,11 @@ __global__ void __launch_bounds__(NT) k_norm_maps(GroupNorm g, Maps m) {
     }
   if (at.own <= 0) return;
   float w[8], b[8];
-  vector8(g.weight ? g.weight + at.c0 + at.vec * 8 : nullptr, 1.0f, at.own, w);
-  vector8(g.bias ? g.bias + at.c0 + at.vec * 8 : nullptr, 0.0f, at.own, b);
+  vector8<EVEN>(g.weight ? g.weight + at.c0 + at.vec * 8 : nullptr, 1.0f, at.own, w);
+  vector8<EVEN>(g.bias ? g.bias + at.c0 + at.vec * 8 : nullptr, 0.0f, at.own, b);
   float mean[8], rstd[8];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) mean[j] = j < at.own ? means[q[j]] : 0.0f, rstd[j] = j < at.own ? rstds[q[j]] : 0.0f;
+  for (int j = 0; j < 8; ++j) mean[j] = (EVEN ? at.own > 0 : j < at.own) ? means[q[j]] : 0.0f, rstd[j] = (EVEN ? at.own > 0 : j < at.own) ? rstds[q[j]] : 0.0f;
   T *y = static_cast<T *>(g.out) + at.n * g.out_sample + at.c0 + at.vec * 8;
 #pragma unroll
   for (int u = 0; u < U; ++u) {
@@ -610,14 +637,14 @@ __global__ void __launch_bounds__(NT) k_norm_maps(GroupNorm g, Maps m) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) e[j] = __builtin_fmaf((e[j] - mean[j]) * rstd[j], w[j], b[j]);
       act8(g.activation, e);
-      store8(y + (long long)p * g.out_pos, at.own, e);
+      store8<EVEN>(y + (long long)p * g.out_pos, at.own, e);
     }
   }
 }
 
 // The gradient.  Per channel of a piece: the sums of d (dy through the activation) and of d h, to scratch[n][chunk][2][channels];
 // from them come dweight and dbias, and, weighted and summed over a group, what dx needs.
-template <class T, int NT, int U, int PASS>
+template <class T, int NT, int U, int PASS, bool EVEN>
 __global__ void __launch_bounds__(NT) k_norm_maps_grad(GroupNorm g, Maps m) {
   __shared__ float lanes[PASS == kJoined ? 1 : NT * 8];
   __shared__ float cw[kWidest], cb[kWidest];   // per channel: the sums of d h and of d
@@ -629,8 +656,8 @@ __global__ void __launch_bounds__(NT) k_norm_maps_grad(GroupNorm g, Maps m) {
   for (int u = 0; u < U; ++u) {
     const u32 p = at.p0 + at.row + u * m.rows;
     const int n = p < at.p1 ? at.own : 0;
-    rx[u].load(x + (long long)p * g.x_pos, n);
-    rd[u].load(dy + (long long)p * g.dy_pos, n);
+    rx[u].template load<EVEN>(x + (long long)p * g.x_pos, n);
+    rd[u].template load<EVEN>(dy + (long long)p * g.dy_pos, n);
   }
   int q[8];
   groups8(m, at.vec * 8, q);
@@ -639,13 +666,13 @@ __global__ void __launch_bounds__(NT) k_norm_maps_grad(GroupNorm g, Maps m) {
   float mean[8], rstd[8], w[8], b[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    mean[j] = j < at.own ? g.mean[at.n * g.groups + first + q[j]] : 0.0f;
-    rstd[j] = j < at.own ? g.rstd[at.n * g.groups + first + q[j]] : 0.0f;
+    mean[j] = (EVEN ? at.own > 0 : j < at.own) ? g.mean[at.n * g.groups + first + q[j]] : 0.0f;
+    rstd[j] = (EVEN ? at.own > 0 : j < at.own) ? g.rstd[at.n * g.groups + first + q[j]] : 0.0f;
     w[j] = b[j] = 0.0f;
   }
   if (at.own > 0) {
-    vector8(g.weight ? g.weight + c : nullptr, 1.0f, at.own, w);
-    vector8(g.bias ? g.bias + c : nullptr, 0.0f, at.own, b);
+    vector8<EVEN>(g.weight ? g.weight + c : nullptr, 1.0f, at.own, w);
+    vector8<EVEN>(g.bias ? g.bias + c : nullptr, 0.0f, at.own, b);
   }
   const auto back = [&](int u, float (&h)[8], float (&d)[8]) {
     rx[u].get(h);
@@ -724,20 +751,20 @@ __global__ void __launch_bounds__(NT) k_norm_maps_grad(GroupNorm g, Maps m) {
   if (at.own <= 0) return;
   float e1[8], e2[8];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) e1[j] = j < at.own ? m1[q[j]] : 0.0f, e2[j] = j < at.own ? m2[q[j]] : 0.0f;
+  for (int j = 0; j < 8; ++j) e1[j] = (EVEN ? at.own > 0 : j < at.own) ? m1[q[j]] : 0.0f, e2[j] = (EVEN ? at.own > 0 : j < at.own) ? m2[q[j]] : 0.0f;
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const u32 p = at.p0 + at.row + u * m.rows;
     if (p < at.p1) {
       float h[8], d[8], o[8];
-      if (g.extra) load8(static_cast<const T *>(g.extra) + at.n * g.extra_sample + p * g.extra_pos + c, at.own, o);
+      if (g.extra) load8<EVEN>(static_cast<const T *>(g.extra) + at.n * g.extra_sample + p * g.extra_pos + c, at.own, o);
       back(u, h, d);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const float v = __builtin_fmaf(-h[j], e2[j], __builtin_fmaf(d[j], w[j], -e1[j])) * rstd[j];
         d[j] = g.extra ? o[j] + v : v;
       }
-      store8(static_cast<T *>(g.out) + at.n * g.out_sample + p * g.out_pos + c, at.own, d);
+      store8<EVEN>(static_cast<T *>(g.out) + at.n * g.out_sample + p * g.out_pos + c, at.own, d);
     }
   }
 }
@@ -775,14 +802,16 @@ constexpr long long kMostWorkgroups = 0x7fffffff;
 long long workgroups(const GroupNorm &g, const Maps &m) { return (long long)m.blocks * m.chunks * g.samples; }
 bool whole(const GroupNorm &g, const Maps &m) { return m.chunks == 1 && m.blocks_a_group == 1 && workgroups(g, m) <= kMostWorkgroups; }
 
-// The rows' cut: lanes of a team and eights a lane, or neither: longer.
+// The rows' cut: lanes of a team and eights a lane, or neither: longer.  The gradient keeps two sums for each of its entries: fewer a lane.
 struct Rows {
   int team, each;
 };
-Rows rows_of(const GroupNorm &g) {
+Rows rows_of(const GroupNorm &g, bool gradient) {
   const long long v = (g.channels / g.groups + 7) / 8;
   if (v <= 16) return {16, 1};
   if (v <= 64) return {64, 1};
+  if (gradient && v <= 128) return {64, 2};
+  if (gradient && v <= 256) return {256, 1};
   if (v <= 256) return {64, 4};
   if (v <= 1024) return {256, 4};
   return {0, 0};
@@ -796,51 +825,67 @@ long long rows_workgroups(const GroupNorm &g, const Rows &r) {
 }
 constexpr long long kLongSplits = 64;
 
+// Calls f with whether every eight entries exist together or not at all.
+template <class F>
+void by_even(const GroupNorm &g, F &&f) {
+  bool even = g.channels / g.groups % 8 == 0;
+  if (!even && g.positions > 1) {   // small groups side by side in blocks of whole eights
+    const Maps m = maps_of(g, kThreads, 1);
+    even = m.blocks_a_group == 1 && m.width % 8 == 0 && g.channels % 8 == 0;
+  }
+  if (even) f(std::true_type());
+  else f(std::false_type());
+}
+
 template <class T>
 hipError_t norm(const GroupNorm &g, hipStream_t s) {
-  if (g.positions == 1) {
-    const long long rows = g.samples * g.groups;
-    const Rows r = rows_of(g);
-    if (r.team == 0) {
-      k_norm_long_rows<T><<<dim3((unsigned)rows), 1024, 0, s>>>(g);
-      return hipGetLastError();
+  hipError_t rc = hipSuccess;
+  by_even(g, [&](auto even) {
+    constexpr bool kEven = decltype(even)::value;
+    if (g.positions == 1) {
+      const long long rows = g.samples * g.groups;
+      const Rows r = rows_of(g, false);
+      if (r.team == 0) {
+        k_norm_long_rows<T><<<dim3((unsigned)rows), 1024, 0, s>>>(g);
+        return;
+      }
+      const unsigned grid = (unsigned)((rows + kThreads / r.team - 1) / (kThreads / r.team));
+      if (r.team == 16) k_norm_rows<T, 16, 1, kEven><<<dim3(grid), kThreads, 0, s>>>(g);
+      else if (r.team == 64 && r.each == 1) k_norm_rows<T, 64, 1, kEven><<<dim3(grid), kThreads, 0, s>>>(g);
+      else if (r.team == 64) k_norm_rows<T, 64, 4, kEven><<<dim3(grid), kThreads, 0, s>>>(g);
+      else k_norm_rows<T, 256, 4, kEven><<<dim3(grid), kThreads, 0, s>>>(g);
+      return;
     }
-    const unsigned grid = (unsigned)((rows + kThreads / r.team - 1) / (kThreads / r.team));
-    if (r.team == 16) k_norm_rows<T, 16, 1><<<dim3(grid), kThreads, 0, s>>>(g);
-    else if (r.team == 64 && r.each == 1) k_norm_rows<T, 64, 1><<<dim3(grid), kThreads, 0, s>>>(g);
-    else if (r.team == 64) k_norm_rows<T, 64, 4><<<dim3(grid), kThreads, 0, s>>>(g);
-    else k_norm_rows<T, 256, 4><<<dim3(grid), kThreads, 0, s>>>(g);
-    return hipGetLastError();
-  }
-  Maps m;
-  const auto grid = [&] { return dim3((unsigned)workgroups(g, m)); };
-  if (m = maps_of(g, 256, 2), whole(g, m)) k_norm_maps<T, 256, 2, kWhole><<<grid(), 256, 0, s>>>(g, m);
-  else if (m = maps_of(g, 256, 8), whole(g, m)) k_norm_maps<T, 256, 8, kWhole><<<grid(), 256, 0, s>>>(g, m);
-  else if (m = maps_of(g, 1024, 8), whole(g, m)) k_norm_maps<T, 1024, 8, kWhole><<<grid(), 1024, 0, s>>>(g, m);
-  else {
-    m = maps_of(g, 256, 8);
-    if (workgroups(g, m) > kMostWorkgroups) return hipErrorInvalidValue;
-    k_norm_maps<T, 256, 8, kPieces><<<grid(), 256, 0, s>>>(g, m);
-    k_norm_maps<T, 256, 8, kJoined><<<grid(), 256, 0, s>>>(g, m);
-  }
-  return hipGetLastError();
+    Maps m;
+    const auto grid = [&] { return dim3((unsigned)workgroups(g, m)); };
+    if (m = maps_of(g, 256, 2), whole(g, m)) k_norm_maps<T, 256, 2, kWhole, kEven><<<grid(), 256, 0, s>>>(g, m);
+    else if (m = maps_of(g, 256, 8), whole(g, m)) k_norm_maps<T, 256, 8, kWhole, kEven><<<grid(), 256, 0, s>>>(g, m);
+    else if (m = maps_of(g, 1024, 8), whole(g, m)) k_norm_maps<T, 1024, 8, kWhole, kEven><<<grid(), 1024, 0, s>>>(g, m);
+    else {
+      m = maps_of(g, 256, 8);
+      if (workgroups(g, m) > kMostWorkgroups) {
+        rc = hipErrorInvalidValue;
+        return;
+      }
+      k_norm_maps<T, 256, 8, kPieces, kEven><<<grid(), 256, 0, s>>>(g, m);
+      k_norm_maps<T, 256, 8, kJoined, kEven><<<grid(), 256, 0, s>>>(g, m);
+    }
+  });
+  return rc != hipSuccess ? rc : hipGetLastError();
 }
 
 // The gradient's cut of maps, and whether one launch does it.
 struct GradMaps {
   Maps m;
-  int threads, each;
+  int each;
   bool whole;
 };
 GradMaps grad_maps(const GroupNorm &g) {
-  const int most = g.type == kF32 ? 4 : 8;   // eights of two tensors in registers
-  GradMaps q = {maps_of(g, 256, 2), 256, 2, true};
+  GradMaps q = {maps_of(g, 256, 2), 2, true};
   if (whole(g, q.m)) return q;
-  q = {maps_of(g, 256, 4), 256, 4, true};
-  if (whole(g, q.m)) return q;
-  q = {maps_of(g, 1024, most), 1024, most, true};
-  if (whole(g, q.m)) return q;
-  return {maps_of(g, 256, 4), 256, 4, false};
+  q = {maps_of(g, 256, 4), 4, true};
+  if (!whole(g, q.m)) q.whole = false;
+  return q;
 }
 
 template <class T>
@@ -848,40 +893,48 @@ hipError_t norm_grad(const GroupNorm &call, hipStream_t s) {
   GroupNorm g = call;
   const bool sums = g.dweight || g.dbias;
   long long count = 0;   // rows of partial sums
-  if (g.samples > 0 && g.positions == 1) {
-    const Rows r = rows_of(g);
-    if (!sums) g.scratch = nullptr;
-    if (r.team == 0) {
-      if (sums) {
-        count = g.samples < kLongSplits ? g.samples : kLongSplits;
-        const long long eights = ((g.channels / g.groups + 7) / 8) * g.groups;
-        k_norm_long_channels<T><<<dim3((unsigned)((eights + kThreads - 1) / kThreads), (unsigned)count), kThreads, 0, s>>>(g);
+  hipError_t rc = hipSuccess;
+  by_even(g, [&](auto even) {
+    constexpr bool kEven = decltype(even)::value;
+    if (g.samples > 0 && g.positions == 1) {
+      const Rows r = rows_of(g, true);
+      if (!sums) g.scratch = nullptr;
+      if (r.team == 0) {
+        if (sums) {
+          count = g.samples < kLongSplits ? g.samples : kLongSplits;
+          const long long eights = ((g.channels / g.groups + 7) / 8) * g.groups;
+          k_norm_long_channels<T><<<dim3((unsigned)((eights + kThreads - 1) / kThreads), (unsigned)count), kThreads, 0, s>>>(g);
+        }
+        k_norm_long_rows_grad<T><<<dim3((unsigned)(g.samples * g.groups)), 1024, 0, s>>>(g);
+        return;
       }
-      k_norm_long_rows_grad<T><<<dim3((unsigned)(g.samples * g.groups)), 1024, 0, s>>>(g);
-    } else {
       count = rows_workgroups(g, r);
       const dim3 grid((unsigned)g.groups, (unsigned)count);
-      if (r.team == 16) k_norm_rows_grad<T, 16, 1><<<grid, kThreads, 0, s>>>(g);
-      else if (r.team == 64 && r.each == 1) k_norm_rows_grad<T, 64, 1><<<grid, kThreads, 0, s>>>(g);
-      else if (r.team == 64) k_norm_rows_grad<T, 64, 4><<<grid, kThreads, 0, s>>>(g);
-      else k_norm_rows_grad<T, 256, 4><<<grid, kThreads, 0, s>>>(g);
+      if (r.team == 16) k_norm_rows_grad<T, 16, 1, kEven><<<grid, kThreads, 0, s>>>(g);
+      else if (r.team == 64 && r.each == 1) k_norm_rows_grad<T, 64, 1, kEven><<<grid, kThreads, 0, s>>>(g);
+      else if (r.team == 64) k_norm_rows_grad<T, 64, 2, kEven><<<grid, kThreads, 0, s>>>(g);
+      else if (r.each == 1) k_norm_rows_grad<T, 256, 1, kEven><<<grid, kThreads, 0, s>>>(g);
+      else k_norm_rows_grad<T, 256, 4, kEven><<<grid, kThreads, 0, s>>>(g);
+    } else if (g.samples > 0 && g.positions > 0) {
+      const GradMaps q = grad_maps(g);
+      if (workgroups(g, q.m) > kMostWorkgroups) {
+        rc = hipErrorInvalidValue;
+        return;
+      }
+      const dim3 grid((unsigned)workgroups(g, q.m));
+      count = g.samples * q.m.chunks;
+      if (!q.whole) {
+        k_norm_maps_grad<T, 256, 4, kPieces, kEven><<<grid, 256, 0, s>>>(g, q.m);
+        k_norm_maps_grad<T, 256, 4, kJoined, kEven><<<grid, 256, 0, s>>>(g, q.m);
+      } else if (q.each == 2) {
+        k_norm_maps_grad<T, 256, 2, kWhole, kEven><<<grid, 256, 0, s>>>(g, q.m);
+      } else {
+        k_norm_maps_grad<T, 256, 4, kWhole, kEven><<<grid, 256, 0, s>>>(g, q.m);
+      }
     }
-  } else if (g.samples > 0 && g.positions > 0) {
-    const GradMaps q = grad_maps(g);
-    if (workgroups(g, q.m) > kMostWorkgroups) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)workgroups(g, q.m));
-    count = g.samples * q.m.chunks;
-    if (!q.whole) {
-      k_norm_maps_grad<T, 256, 4, kPieces><<<grid, 256, 0, s>>>(g, q.m);
-      k_norm_maps_grad<T, 256, 4, kJoined><<<grid, 256, 0, s>>>(g, q.m);
-    } else if (q.threads == 256) {
-      if (q.each == 2) k_norm_maps_grad<T, 256, 2, kWhole><<<grid, 256, 0, s>>>(g, q.m);
-      else k_norm_maps_grad<T, 256, 4, kWhole><<<grid, 256, 0, s>>>(g, q.m);
-    } else {
-      k_norm_maps_grad<T, 1024, sizeof(T) == 4 ? 4 : 8, kWhole><<<grid, 1024, 0, s>>>(g, q.m);
-    }
-  }
-  if (sums) k_norm_join<<<dim3((unsigned)((2 * g.channels + 63) / 64)), 1024, 0, s>>>(g, g.scratch, count);
+  });
+  if (rc != hipSuccess) return rc;
+  if (sums) k_norm_join<<<dim3((unsigned)((2 * g.channels + 15) / 16)), 1024, 0, s>>>(g, g.scratch, count);
   return hipGetLastError();
 }
 
@@ -896,7 +949,7 @@ size_t group_norm_scratch(const GroupNorm &g, bool gradient) {
   long long count;
   if (g.positions == 1) {
     if (!g.dweight && !g.dbias) return 0;
-    const Rows r = rows_of(g);
+    const Rows r = rows_of(g, true);
     count = r.team == 0 ? (g.samples < kLongSplits ? g.samples : kLongSplits) : rows_workgroups(g, r);
   } else {
     count = g.samples * grad_maps(g).m.chunks;

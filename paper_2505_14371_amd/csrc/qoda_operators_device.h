@@ -104,10 +104,15 @@ template <class T>
 struct Eight {
   static constexpr int kWords = sizeof(T) * 2;
   v4u w[kWords / 4];
+  // EVEN: n is at least 8 or not positive.  What handles the others costs registers even where it is not taken.
+  template <bool EVEN = false>
   __device__ __forceinline__ void load(const T *p, int n) {
-    if (n >= 8) {
+    if (EVEN ? n > 0 : n >= 8) {
 #pragma unroll
       for (int q = 0; q < kWords / 4; ++q) __builtin_memcpy(&w[q], reinterpret_cast<const char *>(p) + 16 * q, 16);
+    } else if constexpr (EVEN) {
+#pragma unroll
+      for (int q = 0; q < kWords / 4; ++q) w[q] = v4u{0, 0, 0, 0};
     } else {
       u32 e[8] = {};
       if (n > 0) {   // all at once, those beyond the end from the last one's place: a branch for each would wait for each
@@ -140,11 +145,12 @@ struct Eight {
       for (int j = 0; j < 4; ++j) w[0][j] = bf16_bits(v[2 * j]) | bf16_bits(v[2 * j + 1]) << 16;
     }
   }
+  template <bool EVEN = false>
   __device__ __forceinline__ void store(T *p, int n) const {
-    if (n >= 8) {
+    if (EVEN ? n > 0 : n >= 8) {
 #pragma unroll
       for (int q = 0; q < kWords / 4; ++q) __builtin_memcpy(reinterpret_cast<char *>(p) + 16 * q, &w[q], 16);
-    } else {
+    } else if constexpr (!EVEN) {
 #pragma unroll
       for (int j = 0; j < 8; ++j)
         if (j < n) {
@@ -154,17 +160,17 @@ struct Eight {
     }
   }
 };
-template <class T>
+template <bool EVEN = false, class T>
 __device__ __forceinline__ void load8(const T *p, int n, float (&v)[8]) {
   Eight<T> r;
-  r.load(p, n);
+  r.template load<EVEN>(p, n);
   r.get(v);
 }
-template <class T>
+template <bool EVEN = false, class T>
 __device__ __forceinline__ void store8(T *p, int n, const float (&v)[8]) {
   Eight<T> r;
   r.set(v);
-  r.store(p, n);
+  r.template store<EVEN>(p, n);
 }
 
 }  // namespace qoda
