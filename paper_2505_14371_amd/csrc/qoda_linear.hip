@@ -101,14 +101,19 @@ struct Operand {
       else offset[q] = (u32)(row * ld * (int)sizeof(T)) + (chunk * E < across ? chunk * 16 : 0);
     }
   }
-  // A whole step straight into shared memory: 16-byte aligned rows only.
+  // A whole step straight into shared memory: 16-byte aligned rows only.  The instruction is written out because the compiler, which cannot tell
+  // a step's place from the others', would wait for these loads before every read of shared memory; arrived() waits for them.  (It says that
+  // it does not keep m0 across: nothing else here uses it.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
   __device__ __forceinline__ void direct(int l, lds_ptr to) const {
     const char *p = reinterpret_cast<const char *>(base + (ROWS ? (long long)l : (long long)l * ld));
+    const u32 at = __builtin_amdgcn_readfirstlane((u32)(uintptr_t)to + (threadIdx.x & ~63u) * 16);
 #pragma unroll
     for (int q = 0; q < kMine; ++q)
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(p + offset[q]),
-                                       (__attribute__((address_space(3))) void *)(to + (q * WG + (int)(threadIdx.x & ~63u)) * 16), 16, 0, 0);
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(at + q * WG * 16), "v"(offset[q]), "s"(p) : "memory", "m0");
   }
+#pragma clang diagnostic pop
   // Any step by way of registers, entries beyond an edge 0.
   __device__ __forceinline__ void fetch(int l, v4u (&v)[kMine]) const {
 #pragma unroll
@@ -124,36 +129,57 @@ struct Operand {
 #pragma unroll
     for (int q = 0; q < kMine; ++q) *LDS(v4u, to + (q * WG + threadIdx.x) * 16) = v[q];
   }
-  // The lane's piece of 16 entries across (from `first` on; SIDE 1: every other four from first + 4 t on), half s of the step.
-  static __device__ __forceinline__ v4u piece(lds_ptr tile, int first, int t, int s) {
+  // The lane's piece of 16 entries across (from `first` on; SIDE 1: every other four from first + 4 t on), half s of the step, `first` counting from
+  // the wave's own first entry.  Where it lies is the lane's key, which lane_key() makes once, with `first`, t and s in bits that the key has
+  // no carry into: an exclusive or with a constant, or a constant offset.
+  static __device__ __forceinline__ u32 lane_key(int wave_first) {
     const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
-    const int a = first + (SIDE == 0 ? i : (i >> 2) * 8 + t * 4 + (i & 3));
     if constexpr (ROWS) {
-      return *LDS(v4u, tile + a * 128 + (((s * 4 + g) ^ row_swizzle<SIDE>(a)) * 16));
+      const int a = wave_first + (SIDE == 0 ? i : (i >> 2) * 8 + (i & 3));
+      return (u32)(a * 128 + ((g ^ row_swizzle<SIDE>(a)) * 16));
     } else if constexpr (sizeof(T) == 2) {
       // the lane names four adjacent entries of row 8 g + i / 4 (and of the row four further on), and receives one column's four
-      const int c4 = first + (SIDE == 0 ? (i & 3) * 4 : (i & 3) * 8 + t * 4);   // its four entries
+      const int l = g * 8 + (i >> 2);
+      const int chunk = (SIDE == 0 ? (i & 3) >> 1 : i & 3) ^ column_swizzle<T, SIDE, N>(l);
+      return (u32)((l * N * 2 + chunk * 16 + (SIDE == 0 ? (i & 1) * 8 : 0)) ^ (wave_first * 2));
+    } else {
+      const int l = g * 4;
+      const int chunk = (SIDE == 0 ? i >> 2 : (i >> 2) * 2) ^ column_swizzle<T, SIDE, N>(l);
+      return (u32)((l * N * 4 + chunk * 16 + (i & 3) * 4) ^ (wave_first * 4));
+    }
+  }
+  static __device__ __forceinline__ v4u piece(lds_ptr tile, u32 key, int first, int t, int s) {
+    if constexpr (ROWS) {
+      return *LDS(v4u, tile + (key ^ (s * 64)) + (first * 128 + t * 512));
+    } else if constexpr (sizeof(T) == 2) {
+      const lds_ptr p = tile + (key ^ (first * 2));
       v4u v;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const int l = s * 32 + g * 8 + h * 4 + (i >> 2);
-        const v4s r = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            LDS(v4s, tile + l * (N * 2) + (((c4 >> 3) ^ column_swizzle<T, SIDE, N>(l)) * 16) + (c4 & 4) * 2));
+        const v4s r = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS(v4s, p + ((s * 32 + h * 4) * N * 2 + t * 8)));
         const uint2 w = __builtin_bit_cast(uint2, r);
         v[2 * h] = w.x, v[2 * h + 1] = w.y;
       }
       return v;
     } else {
+      const lds_ptr p = tile + (key ^ (first * 4 + t * 16));
       v4u v;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int l = s * 16 + g * 4 + j;
-        v[j] = *LDS(u32, tile + l * (N * 4) + (((a >> 2) ^ column_swizzle<T, SIDE, N>(l)) * 16) + (a & 3) * 4);
-      }
+      for (int j = 0; j < 4; ++j) v[j] = *LDS(u32, p + (s * 16 + j) * N * 4);
       return v;
     }
   }
 };
+
+// A barrier of the workgroup behind which every wave's reads and writes of shared memory, direct loads among them, are done.
+__device__ __forceinline__ void arrived() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0);   // every counter
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
 
 template <class T>
 __device__ __forceinline__ v4f multiply(v4u b, v4u a, v4f c) {
@@ -276,69 +302,92 @@ __global__ void __launch_bounds__(64 * WM * WN) k_product(Product p, int tiles_m
   const bool with_sums = FORM == kProductColumns && p.sums && tn == 0 && wave % WN * FS < FM;
   float sum[FS] = {};
 
-  const auto compute = [&](lds_ptr ta, lds_ptr tb) {
+  typedef v4u PiecesA[FM];
+  typedef v4u PiecesB[2 * FN];
+  u32 key_a = A::lane_key(wm), key_b = B::lane_key(wn);
+  const auto read = [&](PiecesA &fa, PiecesB &fb, lds_ptr ta, lds_ptr tb, int s) {
+    // the pieces' places are made anew each time: kept, they would take the registers that pieces need
+    asm volatile("" : "+v"(key_a), "+v"(key_b));
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      v4u fa[FM], fb[2 * FN];
+    for (int y = 0; y < 2 * FN; ++y) fb[y] = B::piece(tb, key_b, y / 2 * 32, y & 1, s);
 #pragma unroll
-      for (int y = 0; y < 2 * FN; ++y) fb[y] = B::piece(tb, wn + y / 2 * 32, y & 1, s);
+    for (int x = 0; x < FM; ++x) fa[x] = A::piece(ta, key_a, x * 16, 0, s);
+  };
+  const u32 key_s = A::lane_key(wm + wave % WN * FS * 16);
+  const auto add_up = [&](lds_ptr ta) {
+    if constexpr (FORM == kProductColumns)
+      if (with_sums)
 #pragma unroll
-      for (int x = 0; x < FM; ++x) fa[x] = A::piece(ta, wm + x * 16, 0, s);
+        for (int s = 0; s < 2; ++s)
 #pragma unroll
-      for (int x = 0; x < FM; ++x)
+          for (int x = 0; x < FS; ++x) sum[x] = sum[x] + chunk_sum<T>(A::piece(ta, key_s, x * 16, 0, s));
+  };
+  const auto multiply_all = [&](const PiecesA &fa, const PiecesB &fb) {
 #pragma unroll
-        for (int y = 0; y < 2 * FN; ++y) c[x][y] = multiply<T>(fb[y], fa[x], c[x][y]);
-      if constexpr (FORM == kProductColumns)
-        if (with_sums)
+    for (int x = 0; x < FM; ++x)
 #pragma unroll
-          for (int x = 0; x < FS; ++x) sum[x] = sum[x] + chunk_sum<T>(A::piece(ta, wm + (wave % WN * FS + x) * 16, 0, s));
-    }
+      for (int y = 0; y < 2 * FN; ++y) c[x][y] = multiply<T>(fb[y], fa[x], c[x][y]);
   };
   const lds_ptr ta[2] = {(lds_ptr)a0, (lds_ptr)a1}, tb[2] = {(lds_ptr)b0, (lds_ptr)b1};
-  int rest = 0;   // the first step that direct loads cannot move: all, or a last one that ends inside
-  if constexpr (DIRECT) {
-    const int whole = k / kStep;
-    rest = whole;
-    if (whole > 0) {
-      a.direct(0, ta[0]);
-      b.direct(0, tb[0]);
+
+  // Steps that move by direct loads: all whole ones, or none.  While a step's first half is multiplied its second half is read from shared
+  // memory, and while that is multiplied the next step's first half: the matrix cores have work on both sides of the barrier.  It stands
+  // between the halves, when everybody has read the step, so that the step after the next may take its place.
+  v4u ra[A::kMine], rb[B::kMine];
+  const int whole = DIRECT ? k / kStep : steps;
+  const auto request = [&](int t, lds_ptr to_a, lds_ptr to_b) {
+    if constexpr (DIRECT) {
+      a.direct(t * kStep, to_a);
+      b.direct(t * kStep, to_b);
+    } else {   // by way of registers, which then take the step after it
+      A::store(ra, to_a);
+      B::store(rb, to_b);
+      if (t + 1 < whole) {
+        a.fetch((t + 1) * kStep, ra);
+        b.fetch((t + 1) * kStep, rb);
+      }
     }
+  };
+  if (whole > 0) {
+    if constexpr (!DIRECT) {
+      a.fetch(0, ra);
+      b.fetch(0, rb);
+    }
+    request(0, ta[0], tb[0]);
+    if (whole > 1) request(1, ta[1], tb[1]);
+    PiecesA fa0, fa1;
+    PiecesB fb0, fb1;
+    arrived();
+    read(fa0, fb0, ta[0], tb[0], 0);
     for (int t = 0; t < whole; t += 2) {
 #pragma unroll
       for (int h = 0; h < 2; ++h)
         if (t + h < whole) {
-          __syncthreads();   // step t + h is there, and nobody reads the other pair any more
-          if (t + h + 1 < whole) {
-            a.direct((t + h + 1) * kStep, ta[1 - h]);
-            b.direct((t + h + 1) * kStep, tb[1 - h]);
-          }
-          compute(ta[h], tb[h]);
+          read(fa1, fb1, ta[h], tb[h], 1);
+          multiply_all(fa0, fb0);
+          add_up(ta[h]);
+          arrived();   // the next step is there, and nobody reads this one any more
+          if (t + h + 2 < whole) request(t + h + 2, ta[h], tb[h]);
+          if (t + h + 1 < whole) read(fa0, fb0, ta[1 - h], tb[1 - h], 0);
+          multiply_all(fa1, fb1);
+          __builtin_amdgcn_sched_barrier(0);
         }
     }
   }
-  if (rest < steps) {
-    v4u ra[A::kMine], rb[B::kMine];
-    a.fetch(rest * kStep, ra);
-    b.fetch(rest * kStep, rb);
-    if (DIRECT) __syncthreads();   // nobody reads the first pair any more
-    A::store(ra, ta[0]);
+  if (whole < steps) {   // a last step that ends inside
+    a.fetch(whole * kStep, ra);
+    b.fetch(whole * kStep, rb);
+    A::store(ra, ta[0]);   // free: the last barrier was behind its last reader
     B::store(rb, tb[0]);
-    for (int t = rest; t < steps; t += 2) {
+    __syncthreads();
+    PiecesA fa;
+    PiecesB fb;
 #pragma unroll
-      for (int h = 0; h < (DIRECT ? 1 : 2); ++h)
-        if (t + h < steps) {
-          __syncthreads();
-          if (!DIRECT && t + h + 1 < steps) {
-            a.fetch((t + h + 1) * kStep, ra);
-            b.fetch((t + h + 1) * kStep, rb);
-          }
-          compute(ta[h], tb[h]);
-          if (!DIRECT && t + h + 1 < steps) {
-            A::store(ra, ta[1 - h]);
-            B::store(rb, tb[1 - h]);
-          }
-        }
+    for (int s = 0; s < 2; ++s) {
+      read(fa, fb, ta[0], tb[0], s);
+      multiply_all(fa, fb);
     }
+    add_up(ta[0]);
   }
 
   const int lane = threadIdx.x & 63, g = lane >> 4;
