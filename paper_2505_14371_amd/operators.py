@@ -24,7 +24,7 @@ from typing import Optional, Tuple
 
 import torch
 
-from . import qoda
+from . import build, qoda
 
 ACTIVATIONS = {"none": 0, "relu": 1, "leaky_relu": 2, "gelu": 3, "silu": 4}
 DTYPES = {torch.float32: 0, torch.bfloat16: 1}
@@ -38,10 +38,35 @@ _NORM = struct.Struct("@2i4q" + "Pqq" * 2 + "4Pd")
 _NORM_GRAD = struct.Struct("@2i4q" + "Pqq" * 4 + "6Pi0q")
 
 _lib = None
+_native = None          # the native look at the arguments, once the library is loaded
+
+
+def _find_native(L):
+    """csrc/qoda_torch.cpp's functions, if they are there and were built for this torch, given the library's calls."""
+    try:
+        from . import _qoda_torch as native
+    except ImportError:
+        return None
+    if getattr(native, "built_for", None) != build.built_for():
+        return None
+    names = []
+    for name in ("linear", "linear_input_grad", "linear_weight_grad"):
+        names += [name + "_workspace_bytes", name]
+    names += ["dropout", "dropout_grad"]
+    for name in ("group_norm", "group_norm_grad"):
+        names += [name + "_workspace_bytes", name]
+    native.use(tuple(C.cast(getattr(L, "qoda_" + n), C.c_void_p).value for n in names))
+    return native
+
+
+def _here():
+    """The current device and its current stream's handle."""
+    device = torch.cuda.current_device()
+    return device, torch._C._cuda_getCurrentRawStream(device)
 
 
 def _load():
-    global _lib
+    global _lib, _native
     if _lib is None:
         L = qoda.load()
         for name in ("linear", "linear_input_grad", "linear_weight_grad", "group_norm", "group_norm_grad"):
@@ -52,8 +77,26 @@ def _load():
         for call in (L.qoda_dropout, L.qoda_dropout_grad):
             call.argtypes, call.restype = [C.c_char_p, C.c_void_p], C.c_int
         L.qoda_operator_error.argtypes, L.qoda_operator_error.restype = [], C.c_char_p
+        if hasattr(torch._C, "_cuda_getCurrentRawStream"):     # not a public function of torch
+            _native = _find_native(L)
         _lib = L
     return _lib
+
+
+def _is_native() -> bool:
+    if _lib is None:
+        _load()
+    return _native is not None
+
+
+def _looked_at(call, *args):
+    """The native call's outputs; None where its arguments have to be looked at here."""
+    if not torch.cuda.is_initialized():
+        return None
+    out = call(*_here(), *args)
+    if type(out) is int:
+        _raise(out)
+    return out
 
 
 def operator_error() -> str:
@@ -149,6 +192,10 @@ def linear(x, weight, bias=None, residual=None, *, activation="none", p=0.0, see
     if stream is not None:
         with _on(stream):
             return linear(x, weight, bias, residual, activation=activation, p=p, seed=seed, offset=offset, keep_pre=keep_pre)
+    if _is_native():
+        out = _looked_at(_native.linear, x, weight, bias, residual, ACTIVATIONS.get(activation), p, seed, offset, keep_pre)
+        if out is not None:
+            return out
     dt, act = _first(x, "linear: x"), _activation(activation)
     if not isinstance(weight, torch.Tensor) or weight.dim() != 2:
         raise ValueError("linear: weight has to be a matrix")
@@ -167,6 +214,10 @@ def linear_input_grad(dz, weight, *, pre=None, activation="none", p=0.0, seed=0,
     if stream is not None:
         with _on(stream):
             return linear_input_grad(dz, weight, pre=pre, activation=activation, p=p, seed=seed, offset=offset, residual=residual)
+    if _is_native():
+        out = _looked_at(_native.linear_input_grad, dz, weight, pre, ACTIVATIONS.get(activation), p, seed, offset, residual)
+        if out is not None:
+            return out
     dt, act = _first(dz, "linear_input_grad: dz"), _activation(activation)
     if not isinstance(weight, torch.Tensor) or weight.dim() != 2:
         raise ValueError("linear_input_grad: weight has to be a matrix")
@@ -185,6 +236,9 @@ def linear_weight_grad(dz, x, dweight=None, dbias=None, *, bias=True, accumulate
     if stream is not None:
         with _on(stream):
             return linear_weight_grad(dz, x, dweight, dbias, bias=bias, accumulate=accumulate)
+    if _is_native() and (dbias is not None or not bias):
+        if _looked_at(_native.linear_weight_grad, dz, x, dweight, dbias, accumulate) is not None:
+            return dweight, dbias
     dt = _first(dz, "linear_weight_grad: dz")
     if not isinstance(x, torch.Tensor) or x.dim() == 0:
         raise ValueError("linear_weight_grad: x has to be a tensor with at least one dimension")
@@ -217,6 +271,10 @@ def dropout(x, p, seed, offset, *, activation="none", residual=None, stream=None
     if stream is not None:
         with _on(stream):
             return dropout(x, p, seed, offset, activation=activation, residual=residual)
+    if _is_native():
+        out = _looked_at(_native.entries, x, residual, ACTIVATIONS.get(activation), p, seed, offset, False)
+        if out is not None:
+            return out
     return _entries("dropout: x", _load().qoda_dropout, x, residual, "dropout: residual", activation, p, seed, offset)
 
 
@@ -225,6 +283,10 @@ def dropout_grad(dy, p, seed, offset, *, pre=None, activation="none", stream=Non
     if stream is not None:
         with _on(stream):
             return dropout_grad(dy, p, seed, offset, pre=pre, activation=activation)
+    if _is_native():
+        out = _looked_at(_native.entries, dy, pre, ACTIVATIONS.get(activation), p, seed, offset, True)
+        if out is not None:
+            return out
     return _entries("dropout_grad: dy", _load().qoda_dropout_grad, dy, pre, "dropout_grad: pre", activation, p, seed, offset)
 
 
@@ -263,6 +325,10 @@ def group_norm(x, groups, weight=None, bias=None, *, eps=1e-5, activation="none"
     if stream is not None:
         with _on(stream):
             return group_norm(x, groups, weight, bias, eps=eps, activation=activation)
+    if _is_native():
+        out = _looked_at(_native.group_norm, x, groups, weight, bias, eps, ACTIVATIONS.get(activation))
+        if out is not None:
+            return out
     dt, act = _first(x, "group_norm: x"), _activation(activation)
     n, s, c = _shape(x, "group_norm: x")
     y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
@@ -281,6 +347,10 @@ def group_norm_grad(dy, x, mean, rstd, groups, weight=None, bias=None, *, activa
         with _on(stream):
             return group_norm_grad(dy, x, mean, rstd, groups, weight, bias, activation=activation, residual=residual, dweight=dweight, dbias=dbias,
                                    accumulate=accumulate)
+    if _is_native() and (not accumulate or (dweight is not None and dbias is not None)):
+        out = _looked_at(_native.group_norm_grad, dy, x, mean, rstd, groups, weight, bias, ACTIVATIONS.get(activation), residual, dweight, dbias, accumulate)
+        if out is not None:
+            return out
     dt, act = _first(x, "group_norm_grad: x"), _activation(activation)
     n, s, c = _shape(x, "group_norm_grad: x")
     if accumulate and (dweight is None or dbias is None):

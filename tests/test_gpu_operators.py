@@ -399,7 +399,37 @@ def test_captured_calls_replay():
         torch.cuda.synchronize()
 
 
-def test_refusals():
+def every_call():
+    """Outputs of each operator on plain and on unusual arguments."""
+    g = torch.Generator(device="cuda").manual_seed(4)
+    r = lambda *shape: torch.randn(shape, device="cuda", generator=g)  # noqa: E731
+    x, w, b, z = r(2, 9, 24), r(40, 24), r(40), r(2, 9, 40)
+    out = []
+    for cast in (lambda t: t, lambda t: t.to(torch.bfloat16), lambda t: torch.nn.Parameter(t), lambda t: t[..., ::1].flip(0).flip(0)):
+        X, W, Z = cast(x), cast(w), cast(z)
+        out += [*ops.linear(X, W, b, Z, activation="gelu", p=0.2, seed=1, offset=2, keep_pre=True), ops.linear(X, W), ops.linear(X[0, 0], W)]
+        out += [ops.linear_input_grad(Z, W, pre=X, activation="silu", p=0.1, seed=3, offset=1, residual=X), ops.linear_input_grad(Z, W)]
+        out += [*ops.linear_weight_grad(Z, X), *ops.linear_weight_grad(Z, X, torch.ones(40, 24, device="cuda"), torch.ones(40, device="cuda"), accumulate=True)]
+        out += [ops.linear_weight_grad(Z, X, bias=False)[0], ops.dropout(X, 0.5, 1, 1, residual=X), ops.dropout_grad(X, 0.5, 1, 1), ops.dropout(X[0, 0], 0.5, 1, 1)]
+        y, mean, rstd = ops.group_norm(X, 4, b[:24], b[:24], activation="relu")
+        out += [y, mean, rstd, *ops.group_norm_grad(X, X, mean, rstd, 4, b[:24]), *ops.group_norm(X[0], 1)]
+        out += ops.group_norm_grad(X, X, mean, rstd, 4, residual=X, dweight=torch.ones(24, device="cuda"), dbias=torch.ones(24, device="cuda"), accumulate=True)
+    return out
+
+
+def test_arguments_looked_at_in_python_give_the_same(monkeypatch):
+    native = every_call()
+    monkeypatch.setattr(ops, "_native", None)
+    assert not ops._is_native()
+    for a, b in zip(native, every_call()):
+        assert a.dtype == b.dtype and a.shape == b.shape and torch.equal(a, b)
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_refusals(native, monkeypatch):
+    if not native:
+        monkeypatch.setattr(ops, "_native", None)
+        assert not ops._is_native()
     x, w = torch.randn((4, 8), device="cuda"), torch.randn((6, 8), device="cuda")
     bad = [
         lambda: ops.linear(x.cpu(), w), lambda: ops.linear(x, w.cpu()), lambda: ops.linear(x, w.half()), lambda: ops.linear(x.half(), w.half()),
