@@ -66,8 +66,9 @@ __device__ __forceinline__ v4u load_chunk(const T *p, int valid) {
   return v;
 }
 
-// One operand's tile: N entries across (rows of c for SIDE 0, columns for SIDE 1) by a step of l, moved by the WG threads.
-template <class T, bool ROWS, int SIDE, int N, int WG>
+// One operand's tile: N entries across (rows of c for SIDE 0, columns for SIDE 1) by a step of l, moved by the WG threads.  DIRECT: bytes that a
+// direct load into shared memory moves for a lane, 16 or 4, to which its rows have to be aligned; 0: by way of registers.
+template <class T, bool ROWS, int SIDE, int N, int WG, int DIRECT>
 struct Operand {
   static constexpr int E = 16 / (int)sizeof(T);                 // entries of a chunk
   static constexpr int kStep = kStepBytes / (int)sizeof(T);     // l of a step
@@ -79,11 +80,11 @@ struct Operand {
   const T *base;     // entry (first, 0)
   long long ld;
   int across, k;     // entries that exist across from the tile's first on, and along l
-  u32 offset[kMine]; // of the thread's chunks from the step's first entry, in bytes (direct loads)
+  static constexpr int kDirect = DIRECT ? kMine * 16 / DIRECT : 0;
+  u32 offset[DIRECT ? kDirect : 1]; // of what the thread's direct loads move, from the step's first entry, in bytes
 
-  // place q of the thread: row and (permuted) chunk in shared memory; the chunk it holds
-  static __device__ __forceinline__ void place(int q, int &row, int &chunk) {
-    const int at = q * WG + (int)threadIdx.x;
+  // place `at` in shared memory, in chunks: its row, and which chunk of it lies there
+  static __device__ __forceinline__ void place(int at, int &row, int &chunk) {
     row = at / kRowChunks;
     chunk = (at % kRowChunks) ^ (ROWS ? row_swizzle<SIDE>(row) : column_swizzle<T, SIDE, N>(row));
   }
@@ -92,26 +93,33 @@ struct Operand {
     across = end - first;
     k = k_;
     base = static_cast<const T *>(p) + (ROWS ? (long long)first * ld + k0 : (long long)k0 * ld + first);
+    if constexpr (DIRECT != 0)
 #pragma unroll
-    for (int q = 0; q < kMine; ++q) {
-      int row, chunk;
-      place(q, row, chunk);
-      // beyond the edge: what is loaded there is multiplied into sums that are not stored
-      if (ROWS) offset[q] = (u32)((row < across ? row : across - 1) * ld * (int)sizeof(T)) + chunk * 16;
-      else offset[q] = (u32)(row * ld * (int)sizeof(T)) + (chunk * E < across ? chunk * 16 : 0);
-    }
+      for (int q = 0; q < kDirect; ++q) {
+        const int at = q * WG + (int)threadIdx.x;   // in pieces of DIRECT bytes
+        int row, chunk;
+        place(at / (16 / DIRECT), row, chunk);
+        const int byte = chunk * 16 + at % (16 / DIRECT) * DIRECT;
+        // beyond the edge: what is loaded there is multiplied into sums that are not stored
+        if (ROWS) offset[q] = (u32)((row < across ? row : across - 1) * ld * (int)sizeof(T)) + byte;
+        else offset[q] = (u32)(row * ld * (int)sizeof(T)) + (byte / (int)sizeof(T) < across ? byte : 0);
+      }
   }
-  // A whole step straight into shared memory: 16-byte aligned rows only.  The instruction is written out because the compiler, which cannot tell
+  // A whole step straight into shared memory.  The instruction is written out because the compiler, which cannot tell
   // a step's place from the others', would wait for these loads before every read of shared memory; arrived() waits for them.  (It says that
   // it does not keep m0 across: nothing else here uses it.)
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
   __device__ __forceinline__ void direct(int l, lds_ptr to) const {
     const char *p = reinterpret_cast<const char *>(base + (ROWS ? (long long)l : (long long)l * ld));
-    const u32 at = __builtin_amdgcn_readfirstlane((u32)(uintptr_t)to + (threadIdx.x & ~63u) * 16);
+    const u32 at = __builtin_amdgcn_readfirstlane((u32)(uintptr_t)to + (threadIdx.x & ~63u) * DIRECT);
 #pragma unroll
-    for (int q = 0; q < kMine; ++q)
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(at + q * WG * 16), "v"(offset[q]), "s"(p) : "memory", "m0");
+    for (int q = 0; q < kDirect; ++q) {
+      if constexpr (DIRECT == 16)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(at + q * WG * 16), "v"(offset[q]), "s"(p) : "memory", "m0");
+      else
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(at + q * WG * 4), "v"(offset[q]), "s"(p) : "memory", "m0");
+    }
   }
 #pragma clang diagnostic pop
   // Any step by way of registers, entries beyond an edge 0.
@@ -119,7 +127,7 @@ struct Operand {
 #pragma unroll
     for (int q = 0; q < kMine; ++q) {
       int row, chunk;
-      place(q, row, chunk);
+      place(q * WG + (int)threadIdx.x, row, chunk);
       const int a = ROWS ? row : chunk * E, b = l + (ROWS ? chunk * E : row);
       const int valid = ROWS ? (a < across ? k - b : 0) : (b < k ? across - a : 0);
       v[q] = load_chunk<T>(base + (ROWS ? a * ld + b : b * ld + a), valid);
@@ -271,11 +279,11 @@ __device__ __forceinline__ void tile_of(int id, int tiles_m, int tiles_n, int &t
   tn = in / rows;
 }
 
-template <class T, int FORM, int BM, int BN, int WM, int WN, bool DIRECT>
+template <class T, int FORM, int BM, int BN, int WM, int WN, int DIRECT>
 __global__ void __launch_bounds__(64 * WM * WN) k_product(Product p, int tiles_m, int tiles_n, int steps_each) {
   constexpr int WG = 64 * WM * WN, FM = BM / WM / 16, FN = BN / WN / 32;
-  typedef Operand<T, FORM != kProductColumns, 0, BM, WG> A;
-  typedef Operand<T, FORM == kProductRows, 1, BN, WG> B;
+  typedef Operand<T, FORM != kProductColumns, 0, BM, WG, DIRECT> A;
+  typedef Operand<T, FORM == kProductRows, 1, BN, WG, DIRECT> B;
   constexpr int kStep = A::kStep;
   __shared__ __align__(16) char a0[BM * kStepBytes], b0[BN * kStepBytes], a1[BM * kStepBytes], b1[BN * kStepBytes];
 
@@ -330,64 +338,58 @@ __global__ void __launch_bounds__(64 * WM * WN) k_product(Product p, int tiles_m
   };
   const lds_ptr ta[2] = {(lds_ptr)a0, (lds_ptr)a1}, tb[2] = {(lds_ptr)b0, (lds_ptr)b1};
 
-  // Steps that move by direct loads: all whole ones, or none.  While a step's first half is multiplied its second half is read from shared
-  // memory, and while that is multiplied the next step's first half: the matrix cores have work on both sides of the barrier.  It stands
-  // between the halves, when everybody has read the step, so that the step after the next may take its place.
+  // While a step's first half is multiplied its second half is read from shared memory, and while that is multiplied the next step's first
+  // half: the matrix cores have work on both sides of the barrier.  It stands between the halves, when everybody has read the step, so
+  // that the step after the next may take its place.
+  // Direct loads move whole steps only.  A step that ends inside, which goes by way of registers, is the first to be taken: its loads
+  // and those of the whole step behind it are then on their way together.
   v4u ra[A::kMine], rb[B::kMine];
-  const int whole = DIRECT ? k / kStep : steps;
-  const auto request = [&](int t, lds_ptr to_a, lds_ptr to_b) {
-    if constexpr (DIRECT) {
-      a.direct(t * kStep, to_a);
-      b.direct(t * kStep, to_b);
+  const int ragged = DIRECT != 0 && k % kStep != 0 ? 1 : 0;
+  const auto request = [&](int t, lds_ptr to_a, lds_ptr to_b) {   // step t in the order in which they are taken
+    if constexpr (DIRECT != 0) {
+      a.direct((t - ragged) * kStep, to_a);
+      b.direct((t - ragged) * kStep, to_b);
     } else {   // by way of registers, which then take the step after it
       A::store(ra, to_a);
       B::store(rb, to_b);
-      if (t + 1 < whole) {
+      if (t + 1 < steps) {
         a.fetch((t + 1) * kStep, ra);
         b.fetch((t + 1) * kStep, rb);
       }
     }
   };
-  if (whole > 0) {
-    if constexpr (!DIRECT) {
-      a.fetch(0, ra);
-      b.fetch(0, rb);
+  if (steps > 0) {
+    if (DIRECT == 0 || ragged) {
+      const int first = ragged ? (steps - 1) * kStep : 0;
+      a.fetch(first, ra);
+      b.fetch(first, rb);
     }
-    request(0, ta[0], tb[0]);
-    if (whole > 1) request(1, ta[1], tb[1]);
+    if (ragged) {
+      if (steps > 1) request(1, ta[1], tb[1]);
+      A::store(ra, ta[0]);
+      B::store(rb, tb[0]);
+    } else {
+      request(0, ta[0], tb[0]);
+      if (steps > 1) request(1, ta[1], tb[1]);
+    }
     PiecesA fa0, fa1;
     PiecesB fb0, fb1;
     arrived();
     read(fa0, fb0, ta[0], tb[0], 0);
-    for (int t = 0; t < whole; t += 2) {
+    for (int t = 0; t < steps; t += 2) {
 #pragma unroll
       for (int h = 0; h < 2; ++h)
-        if (t + h < whole) {
+        if (t + h < steps) {
           read(fa1, fb1, ta[h], tb[h], 1);
           multiply_all(fa0, fb0);
           add_up(ta[h]);
           arrived();   // the next step is there, and nobody reads this one any more
-          if (t + h + 2 < whole) request(t + h + 2, ta[h], tb[h]);
-          if (t + h + 1 < whole) read(fa0, fb0, ta[1 - h], tb[1 - h], 0);
+          if (t + h + 2 < steps) request(t + h + 2, ta[h], tb[h]);
+          if (t + h + 1 < steps) read(fa0, fb0, ta[1 - h], tb[1 - h], 0);
           multiply_all(fa1, fb1);
           __builtin_amdgcn_sched_barrier(0);
         }
     }
-  }
-  if (whole < steps) {   // a last step that ends inside
-    a.fetch(whole * kStep, ra);
-    b.fetch(whole * kStep, rb);
-    A::store(ra, ta[0]);   // free: the last barrier was behind its last reader
-    B::store(rb, tb[0]);
-    __syncthreads();
-    PiecesA fa;
-    PiecesB fb;
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      read(fa, fb, ta[0], tb[0], s);
-      multiply_all(fa, fb);
-    }
-    add_up(ta[0]);
   }
 
   const int lane = threadIdx.x & 63, g = lane >> 4;
@@ -476,10 +478,20 @@ __global__ void __launch_bounds__(256) k_join(Product p, int splits) {
     for (long long q = first; q < total; q += stride) {
       const int i = (int)(q / blocks), j = (int)(q - i * blocks) * 8, n = p.n - j;
       float c[8] = {}, v[8];
-      for (int s = 0; s < splits; ++s) {
-        load8(p.partial + ((long long)s * p.m + i) * p.n + j, n, v);
+      const float *from = p.partial + (long long)i * p.n + j;
+      const long long each = (long long)p.m * p.n;
+      for (int s = 0; s < splits; s += 4) {   // four on their way
+        Eight<float> part[4];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) c[e] = c[e] + v[e];
+        for (int u = 0; u < 4; ++u)
+          if (s + u < splits) part[u].load(from + (s + u) * each, n);
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          if (s + u < splits) {
+            part[u].get(v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) c[e] = c[e] + v[e];
+          }
       }
       finish<T, FORM, decltype(a)::value>(p, i, j, n, c);
     }
@@ -497,11 +509,29 @@ __global__ void __launch_bounds__(256) k_join(Product p, int splits) {
 enum Tile { kFewRows, kTile32, kTile64, kTile128, kTile256 };
 struct Plan {
   Tile tile;
-  bool direct;
+  int direct;
   int tiles_m, tiles_n, splits, steps_each;
 };
 
 constexpr int kCus = 256;
+
+// What a cut would take, in us, from what was measured: the matrix cores' rate in a tile of each size, the time of a step that nothing but
+// its loads bounds, of a tile's start and end, and of the launch that joins splits.
+double time_of(const Product &p, int side, int a_cu, double rate, long long tiles, int steps, int splits) {
+  const int step = kStepBytes / (p.type == kF32 ? 4 : 2), steps_each = (steps + splits - 1) / splits;
+  const double flops = 2.0 * side * side * step, whole = rate / kCus;
+  long long left = tiles * splits;
+  double us = 0.0;
+  while (left > 0) {   // workgroups that share a CU share its matrix cores; the last ones are fewer
+    const long long now = left < (long long)a_cu * kCus ? left : (long long)a_cu * kCus;
+    const long long rounds = left / now;
+    const double sharing = (double)((now + kCus - 1) / kCus), one = sharing * flops / whole * 1e6;
+    us += (double)rounds * (2.0 + steps_each * (one > 0.5 ? one : 0.5));
+    left -= rounds * now;
+  }
+  if (splits > 1) us += 5.0 + (double)splits * p.m * p.n * 8.0 / 4e6;
+  return us;
+}
 
 Plan plan_of(const Product &p) {
   Plan q = {};
@@ -513,23 +543,37 @@ Plan plan_of(const Product &p) {
     q.tiles_m = 1, q.tiles_n = (p.n + 15) / 16;
     return q;
   }
-  // direct loads move aligned chunks of 16 bytes, by 32-bit offsets inside a tile
-  const auto fits = [&](const void *v, long long ld, bool rows) {
-    return reinterpret_cast<uintptr_t>(v) % 16 == 0 && ld * e % 16 == 0 && (rows ? 256 : step) * ld * e < (1ll << 31);
+  // direct loads: by 32-bit offsets inside a tile, 16 bytes a lane, or 4 where rows start at those (bf16: of even strides)
+  const auto fits = [&](const void *v, long long ld, bool rows, int bytes) {
+    return reinterpret_cast<uintptr_t>(v) % bytes == 0 && ld * e % bytes == 0 && (rows ? 256 : step) * ld * e < (1ll << 31);
   };
-  q.direct = p.n > 0 && fits(p.a, p.lda, p.form != kProductColumns) && fits(p.b, p.ldb, p.form == kProductRows);
+  for (const int bytes : {4, 16})
+    if (p.n > 0 && fits(p.a, p.lda, p.form != kProductColumns, bytes) && fits(p.b, p.ldb, p.form == kProductRows, bytes)) q.direct = bytes;
   const auto tiles = [&](int bm, int bn) { return (long long)((p.m + bm - 1) / bm) * (p.n > 0 ? (p.n + bn - 1) / bn : 1); };
   const int steps = p.k > 0 ? (p.k + step - 1) / step : 1;
-  int bm, bn, slots;
-  if (p.m <= 32) q.tile = kTile32, bm = 32, bn = 128, slots = 4 * kCus;
-  else if (q.direct && tiles(256, 256) >= kCus * 3 / 4) q.tile = kTile256, bm = bn = 256, slots = kCus;
-  else if (tiles(128, 128) * (steps < 16 ? 1 : steps / 8) >= kCus) q.tile = kTile128, bm = bn = 128, slots = 2 * kCus;
-  else q.tile = kTile64, bm = bn = 64, slots = 4 * kCus;
+  int bm, bn;
+  if (p.m <= 32) {
+    // few rows: the other operand is read once, by as many workgroups as fill the device, in parts of at least four steps
+    q.tile = kTile32, bm = 32, bn = 128;
+    const long long want = 4 * kCus / tiles(bm, bn), most = steps / 4;
+    q.splits = (int)(want < most ? want : most);
+    if (q.splits < 2) q.splits = 1;
+  } else {
+    // TFLOP/s of whole tiles, 16384 x 8192 x 2048 and 4096^2 x 2048: bf16 1250 (256), 1060 (128), 800 (64); fp32 140, 140, 132
+    const bool wide = p.type == kBf16;
+    const struct { Tile tile; int side, a_cu; double rate; } cuts[] = {
+        {kTile64, 64, 4, wide ? 800e12 : 132e12}, {kTile128, 128, 2, wide ? 1060e12 : 140e12}, {kTile256, 256, 1, wide ? 1250e12 : 140e12}};
+    double least = 0.0;
+    for (const auto &c : cuts) {
+      if (c.tile == kTile256 && q.direct != 16) continue;
+      const long long n = tiles(c.side, c.side);
+      for (int splits = 1; splits == 1 || (splits <= 16 && splits * 4 <= steps && n * splits <= c.a_cu * kCus && c.tile != kTile256); ++splits) {
+        const double us = time_of(p, c.side, c.a_cu, c.rate, n, steps, splits);
+        if (least == 0.0 || us < least) least = us, q.tile = c.tile, q.splits = splits, bm = bn = c.side;
+      }
+    }
+  }
   q.tiles_m = (p.m + bm - 1) / bm, q.tiles_n = p.n > 0 ? (p.n + bn - 1) / bn : 1;
-  // few tiles: the sum over l is split, into parts of at least four steps, until the device is full once
-  const long long want = slots / tiles(bm, bn), most = steps / 4;
-  q.splits = (int)(want < most ? want : most);
-  if (q.tile == kTile256 || q.splits < 2) q.splits = 1;
   q.steps_each = (steps + q.splits - 1) / q.splits;
   q.splits = (steps + q.steps_each - 1) / q.steps_each;
   return q;
@@ -538,8 +582,14 @@ Plan plan_of(const Product &p) {
 template <class T, int FORM, int BM, int BN, int WM, int WN>
 void launch(const Product &p, const Plan &q, hipStream_t s) {
   const dim3 grid((unsigned)(q.tiles_m * q.tiles_n), (unsigned)q.splits);
-  if (q.direct) k_product<T, FORM, BM, BN, WM, WN, true><<<grid, 64 * WM * WN, 0, s>>>(p, q.tiles_m, q.tiles_n, q.steps_each);
-  else if constexpr (BM < 256) k_product<T, FORM, BM, BN, WM, WN, false><<<grid, 64 * WM * WN, 0, s>>>(p, q.tiles_m, q.tiles_n, q.steps_each);
+  const auto run = [&](auto direct) {
+    k_product<T, FORM, BM, BN, WM, WN, decltype(direct)::value><<<grid, 64 * WM * WN, 0, s>>>(p, q.tiles_m, q.tiles_n, q.steps_each);
+  };
+  if (q.direct == 16) run(std::integral_constant<int, 16>());
+  else if constexpr (BM < 256) {
+    if (q.direct == 4) run(std::integral_constant<int, 4>());
+    else run(std::integral_constant<int, 0>());
+  }
 }
 
 template <class T, int FORM>
