@@ -525,7 +525,9 @@ double time_of(const Product &p, int side, int a_cu, double rate, long long tile
   while (left > 0) {   // workgroups that share a CU share its matrix cores; the last ones are fewer
     const long long now = left < (long long)a_cu * kCus ? left : (long long)a_cu * kCus;
     const long long rounds = left / now;
-    const double sharing = (double)((now + kCus - 1) / kCus), one = sharing * flops / whole * 1e6;
+    const int sharing = (int)((now + kCus - 1) / kCus);
+    const double alone = side == 256 || sharing > 2 ? 1.0 : sharing == 2 ? (a_cu > 2 ? 1.1 : 1.0) : 1.5;   // too few waves to fill a SIMD's gaps
+    const double one = alone * sharing * flops / whole * 1e6;
     us += (double)rounds * (2.0 + steps_each * (one > 0.5 ? one : 0.5));
     left -= rounds * now;
   }
