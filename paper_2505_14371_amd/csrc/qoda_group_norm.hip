@@ -721,11 +721,18 @@ __global__ void __launch_bounds__(NT) k_norm_maps_grad(GroupNorm g, Maps m) {
       if (threadIdx.x == 0) cb[0] = s1, cw[0] = s2;
     } else {
       for (int k = threadIdx.x; k < width; k += NT) {
+        const float *s = g.scratch + at.n * m.chunks * 2 * g.channels + from + k;
         float s1 = 0.0f, s2 = 0.0f;
-        for (int ch = 0; ch < m.chunks; ++ch) {
-          const float *s = g.scratch + ((at.n * m.chunks + ch) * 2) * g.channels + from + k;
-          s2 = s2 + s[0];
-          s1 = s1 + s[g.channels];
+        for (int ch = 0; ch < m.chunks; ch += 8) {   // eight on their way
+          float v1[8], v2[8];
+#pragma unroll
+          for (int u = 0; u < 8; ++u) {
+            const float *p = s + (long long)(ch + u < m.chunks ? ch + u : m.chunks - 1) * 2 * g.channels;
+            v2[u] = p[0], v1[u] = p[g.channels];
+          }
+#pragma unroll
+          for (int u = 0; u < 8; ++u)
+            if (ch + u < m.chunks) s2 = s2 + v2[u], s1 = s1 + v1[u];
         }
         cw[k] = s2, cb[k] = s1;
       }
@@ -772,8 +779,8 @@ __global__ void __launch_bounds__(NT) k_norm_maps_grad(GroupNorm g, Maps m) {
 // ------------------------------------------------------------------------------------------------ launches
 long long gcd(long long a, long long b) { return b == 0 ? a : gcd(b, a % b); }
 
-// A block: whole groups and whole vectors of eight, so that no thread's channels cross a block's edge more often than at the end; at least 64
-// channels (128 bytes of bf16 in a row), more where few positions would leave threads idle; at most 256 vectors.
+// A block: whole groups and whole vectors of eight, so that no thread's channels cross a block's edge more often than at the end; at least 128
+// bytes of a row, more where few positions would leave threads idle; at most 256 vectors.
 Maps maps_of(const GroupNorm &g, int threads, int each) {
   Maps m = {};
   m.per = (int)(g.channels / g.groups);
@@ -785,8 +792,9 @@ Maps maps_of(const GroupNorm &g, int threads, int each) {
   } else {
     long long unit = m.per / gcd(m.per, 8) * 8;
     if (unit > 512 || unit > g.channels) unit = m.per;
+    const long long least = g.type == kF32 ? 32 : 64;
     long long w = unit;
-    while (w < g.channels && w + unit <= kWidest && (w < 64 || (w + 7) / 8 * g.positions < kThreads)) w += unit;
+    while (w < g.channels && w + unit <= kWidest && (w < least || (w + 7) / 8 * g.positions < kThreads)) w += unit;
     if (w > g.channels) w = g.channels;
     m.width = (int)w;
     m.blocks = (int)((g.channels + w - 1) / w);

@@ -432,7 +432,7 @@ __global__ void __launch_bounds__(64 * WM * WN) k_product(Product p, int tiles_m
 // order along l is the same for both operands, and of no matter).  The waves' sums are joined in shared memory.
 template <class T, int NW>
 __global__ void __launch_bounds__(64 * NW) k_few_rows(Product p) {
-  constexpr int E = 16 / (int)sizeof(T), kRun = 8 * E, kAhead = 4;
+  constexpr int E = 16 / (int)sizeof(T), kRun = 8 * E, kAhead = NW > 4 ? 4 : 8;
   __shared__ v4f part[NW][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, i = lane & 15, g = lane >> 4;
   const int j0 = (int)blockIdx.x * 16;
