@@ -432,7 +432,7 @@ __global__ void __launch_bounds__(64 * WM * WN) k_product(Product p, int tiles_m
 // order along l is the same for both operands, and of no matter).  The waves' sums are joined in shared memory.
 template <class T, int NW>
 __global__ void __launch_bounds__(64 * NW) k_few_rows(Product p) {
-  constexpr int E = 16 / (int)sizeof(T), kRun = 8 * E, kAhead = NW > 4 ? 4 : 8;
+  constexpr int E = 16 / (int)sizeof(T), kRun = 8 * E, kAhead = NW > 4 ? (sizeof(T) == 4 ? 2 : 4) : 8;
   __shared__ v4f part[NW][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, i = lane & 15, g = lane >> 4;
   const int j0 = (int)blockIdx.x * 16;
@@ -561,13 +561,14 @@ Plan plan_of(const Product &p) {
     q.splits = (int)(want < most ? want : most);
     if (q.splits < 2) q.splits = 1;
   } else {
-    // TFLOP/s of whole tiles, 16384 x 8192 x 2048 and 4096^2 x 2048: bf16 1250 (256), 1060 (128), 800 (64); fp32 140, 140, 132
+    // TFLOP/s of whole tiles, 16384 x 8192 x 2048 and 4096 x 2048 x 2048: bf16 1250 (256), 1060 (128), 800 (64); fp32, whose matrix
+    // instructions take sixteen times as long for a piece, 140 (128), 132 (64)
     const bool wide = p.type == kBf16;
     const struct { Tile tile; int side, a_cu; double rate; } cuts[] = {
-        {kTile64, 64, 4, wide ? 800e12 : 132e12}, {kTile128, 128, 2, wide ? 1060e12 : 140e12}, {kTile256, 256, 1, wide ? 1250e12 : 140e12}};
+        {kTile64, 64, 4, wide ? 800e12 : 132e12}, {kTile128, 128, 2, wide ? 1060e12 : 140e12}, {kTile256, 256, 1, 1250e12}};
     double least = 0.0;
     for (const auto &c : cuts) {
-      if (c.tile == kTile256 && q.direct != 16) continue;
+      if (c.tile == kTile256 && (q.direct != 16 || !wide)) continue;
       const long long n = tiles(c.side, c.side);
       for (int splits = 1; splits == 1 || (splits <= 16 && splits * 4 <= steps && n * splits <= c.a_cu * kCus && c.tile != kTile256); ++splits) {
         const double us = time_of(p, c.side, c.a_cu, c.rate, n, steps, splits);
@@ -607,7 +608,9 @@ void launch(const Product &p, const Plan &q, hipStream_t s) {
     case kTile32: launch<T, FORM, 32, 128, 1, 4>(p, q, s); break;
     case kTile64: launch<T, FORM, 64, 64, 2, 2>(p, q, s); break;
     case kTile128: launch<T, FORM, 128, 128, 2, 2>(p, q, s); break;
-    case kTile256: launch<T, FORM, 256, 256, 2, 4>(p, q, s); break;
+    case kTile256:
+      if constexpr (sizeof(T) == 2) launch<T, FORM, 256, 256, 2, 4>(p, q, s);
+      break;
   }
   if (q.splits > 1) {
     const long long blocks = (long long)p.m * ((p.n + 7) / 8), groups = (blocks + 255) / 256;

@@ -25,18 +25,16 @@ template <> __device__ __forceinline__ bf16 from_float<bf16>(float v) { return b
 constexpr float kSlope = 0.2f;   // of leaky_relu
 constexpr float kLog2E = 1.4426950408889634f;
 
-// 1 - Phi(|z|) = erfc(|z| / sqrt 2) / 2 and exp(-z^2 / 2): formula 7.1.26 of Abramowitz and Stegun, erfc(x) = (a1 t + ... + a5 t^5) exp(-x^2)
-// with t = 1 / (1 + p x), whose error is at most 1.5e-7 -- that of 1 + erf in fp32.  The exponential is the density's too, so
-// the function and its derivative take one exponential and one reciprocal.
-__device__ __forceinline__ void normal_tail(float z, float &tail, float &e) {
-  const float x = fabsf(z) * 0.70710678118654752f;
-  const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3275911f, x, 1.0f));
+// The two factors of 1 - Phi(|z|) = erfc(|z| / sqrt 2) / 2 = q e with e = exp(-z^2 / 2): formula 7.1.26 of Abramowitz and Stegun, erfc(x) =
+// (a1 t + ... + a5 t^5) exp(-x^2) with t = 1 / (1 + p x), whose error is at most 1.5e-7 -- that of 1 + erf in fp32.  The exponential is the
+// density's too, so the function and its derivative take one exponential and one reciprocal.  (halves and roots of two are in the constants.)
+__device__ __forceinline__ void normal_tail(float z, float &q, float &e) {
+  const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3275911f * 0.70710678118654752f, fabsf(z), 1.0f));
   e = __builtin_amdgcn_exp2f(z * z * (-0.5f * kLog2E));
-  float q = __builtin_fmaf(1.061405429f, t, -1.453152027f);
-  q = __builtin_fmaf(q, t, 1.421413741f);
-  q = __builtin_fmaf(q, t, -0.284496736f);
-  q = __builtin_fmaf(q, t, 0.254829592f);
-  tail = 0.5f * q * t * e;
+  q = __builtin_fmaf(0.5f * 1.061405429f, t, 0.5f * -1.453152027f);
+  q = __builtin_fmaf(q, t, 0.5f * 1.421413741f);
+  q = __builtin_fmaf(q, t, 0.5f * -0.284496736f);
+  q = __builtin_fmaf(q, t, 0.5f * 0.254829592f) * t;
 }
 
 template <int ACT>
@@ -44,9 +42,9 @@ __device__ __forceinline__ float act(float z) {
   if constexpr (ACT == kActRelu) return z < 0.0f ? 0.0f : z;   // a NaN stays one
   if constexpr (ACT == kActLeakyRelu) return z > 0.0f ? z : kSlope * z;
   if constexpr (ACT == kActGelu) {
-    float tail, e;
-    normal_tail(z, tail, e);
-    return z * (z < 0.0f ? tail : 1.0f - tail);
+    float q, e;
+    normal_tail(z, q, e);
+    return z * (0.5f + copysignf(__builtin_fmaf(-q, e, 0.5f), z));   // Phi - 1/2 is odd
   }
   if constexpr (ACT == kActSilu) return z * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2E * z));
   return z;
@@ -57,35 +55,16 @@ __device__ __forceinline__ float act_slope(float z) {
   if constexpr (ACT == kActRelu) return z > 0.0f ? 1.0f : 0.0f;
   if constexpr (ACT == kActLeakyRelu) return z > 0.0f ? 1.0f : kSlope;
   if constexpr (ACT == kActGelu) {
-    float tail, e;
-    normal_tail(z, tail, e);
-    return __builtin_fmaf(z * 0.39894228040143268f, e, z < 0.0f ? tail : 1.0f - tail);
+    float q, e;
+    normal_tail(z, q, e);
+    // Phi - 1/2 + z phi is odd: 1/2 - q e + |z| e / sqrt(2 pi) on the right
+    return 0.5f + copysignf(__builtin_fmaf(e, __builtin_fmaf(fabsf(z), 0.39894228040143268f, -q), 0.5f), z);
   }
   if constexpr (ACT == kActSilu) {
     const float s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2E * z));
     return s * __builtin_fmaf(z, 1.0f - s, 1.0f);
   }
   return 1.0f;
-}
-
-// The same by an activation that is known at run time; the branch is one for the whole launch.
-__device__ __forceinline__ float act_of(int a, float z) {
-  switch (a) {
-    case kActRelu: return act<kActRelu>(z);
-    case kActLeakyRelu: return act<kActLeakyRelu>(z);
-    case kActGelu: return act<kActGelu>(z);
-    case kActSilu: return act<kActSilu>(z);
-    default: return z;
-  }
-}
-__device__ __forceinline__ float act_slope_of(int a, float z) {
-  switch (a) {
-    case kActRelu: return act_slope<kActRelu>(z);
-    case kActLeakyRelu: return act_slope<kActLeakyRelu>(z);
-    case kActGelu: return act_slope<kActGelu>(z);
-    case kActSilu: return act_slope<kActSilu>(z);
-    default: return 1.0f;
-  }
 }
 
 // Dropout of the eight entries 8 block .. 8 block + 7 of a row.  A lot is compared where it lies, in the upper half of a word: lot >= threshold

@@ -104,6 +104,94 @@ def test_linear_weight_grad(rows, cin, cout, dtype):
     assert torch.equal(ops.linear_weight_grad(dz, x)[1], db1)
 
 
+# what small products do not reach: the largest tiles with ragged ends on every side, sums split along l, rows at 4-byte and at odd addresses
+LARGER = [(8190, 536, 8184, 0, "bf16"), (8184, 8184, 600, 0, "bf16"), (3000, 410, 2100, 0, "bf16"), (1500, 411, 1001, 0, "bf16"), (616, 8184, 8184, 0, "bf16"), (200, 8200, 300, 0, "bf16"), (30, 4104, 520, 0, "bf16"),
+          (24, 5001, 333, 1, "bf16"), (3000, 410, 2100, 0, "f32"), (100, 6000, 130, 1, "f32"), (2050, 200, 2060, 0, "f32"), (20, 2000, 700, 0, "f32")]
+
+
+def near64(got, want, bound, dtype, what):
+    bound = bound + (want.abs() + bound) * (D.STORE[dtype] * 1.001) + 1e-38
+    bad = ~((got.double() - want).abs() <= bound)
+    if bad.any():
+        at = tuple(int(v) for v in bad.nonzero()[0])
+        pytest.fail(f"{what}: {int(bad.sum())} of {bad.numel()} off, first at {at}: {float(got[at])} for {float(want[at])}, bound {float(bound[at])}")
+
+
+@pytest.mark.parametrize("rows,cin,cout,pad,dtype", LARGER)
+def test_larger_products(rows, cin, cout, pad, dtype):
+    gen = torch.Generator(device="cuda").manual_seed(rows + cin)
+
+    def matrix(r, c, scale=1.0):
+        wide = torch.full((r, c + pad), float("nan"), device="cuda", dtype=TYPES[dtype])
+        wide[:, :c] = torch.randn((r, c), device="cuda", generator=gen) * scale
+        return wide[:, :c]
+
+    x, w, dz, r = matrix(rows, cin), matrix(cout, cin, cin ** -0.5), matrix(rows, cout), matrix(rows, cout)
+    X, W, Z, R = (t.double().contiguous() for t in (x, w, dz, r))
+    want, size = X @ W.t().contiguous(), X.abs() @ W.abs().t().contiguous()
+    y, pre = ops.linear(x, w, residual=r, activation="relu", keep_pre=True)
+    near64(pre, want, 2 * (cin + 4) * D.U32 * size, dtype, "pre")
+    near64(y, R + want.clamp(min=0), 2 * (cin + 4) * D.U32 * size + 4 * D.U32 * (R.abs() + want.abs()), dtype, "y")
+    want, size = Z @ W, Z.abs() @ W.abs()
+    near64(ops.linear_input_grad(dz, w), want, 2 * (cout + 4) * D.U32 * size, dtype, "dx")
+    want = torch.where(X > 0, want, torch.zeros_like(want)) + X
+    near64(ops.linear_input_grad(dz, w, pre=x, activation="relu", residual=x), want, 2 * (cout + 4) * D.U32 * size + 4 * D.U32 * (size + X.abs()), dtype, "dx through relu")
+    Zt = Z.t().contiguous()
+    want, size = Zt @ X, Zt.abs() @ X.abs()
+    dw, db = ops.linear_weight_grad(dz, x)
+    near64(dw, want, 2 * (rows + 4) * D.U32 * size, "f32", "dw")
+    near64(db, Z.sum(0), 2 * (rows + 4) * D.U32 * Z.abs().sum(0), "f32", "db")
+    again = ops.linear_weight_grad(dz, x, dw.clone(), db.clone(), accumulate=True)
+    near64(again[0], 2 * want, 4 * (rows + 4) * D.U32 * size, "f32", "dw added")
+    near64(again[1], 2 * Z.sum(0), 4 * (rows + 4) * D.U32 * Z.abs().sum(0), "f32", "db added")
+    assert torch.equal(ops.linear(x, w, residual=r, activation="relu"), y) and torch.equal(ops.linear_weight_grad(dz, x)[0], dw)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,cin,cout", [(7, 40, 33), (300, 200, 410), (20, 4000, 300), (130, 6000, 70)])
+def test_a_residual_may_be_the_outputs_memory(rows, cin, cout, dtype):
+    lib, dt = ops._load(), ops.DTYPES[TYPES[dtype]]
+    x, w, r = (torch.randn(s, device="cuda").to(TYPES[dtype]) for s in ((rows, cin), (cout, cin), (rows, cout)))
+    place = lambda t: (t.data_ptr(), t.shape[-1])  # noqa: E731
+
+    def call(name, pack, *args):
+        a = pack.pack(dt, *args)
+        need = getattr(lib, f"qoda_{name}_workspace_bytes")(a)
+        scratch = torch.empty(max(need, 16), dtype=torch.uint8, device="cuda")
+        assert getattr(lib, f"qoda_{name}")(a, scratch.data_ptr(), need, torch.cuda.current_stream().cuda_stream) == qoda.OK, ops.operator_error()
+
+    y = r.clone()
+    call("linear", ops._LINEAR, 3, rows, cin, cout, *place(x), *place(w), *place(y), *place(y), 0, 0, 0, 0.1, 1, 2)
+    assert torch.equal(y, ops.linear(x, w, residual=r, activation="gelu", p=0.1, seed=1, offset=2))
+    dx = x.clone()
+    call("linear_input_grad", ops._INPUT_GRAD, 0, rows, cin, cout, *place(r), *place(w), 0, 0, *place(dx), *place(dx), 0.1, 1, 2)
+    assert torch.equal(dx, ops.linear_input_grad(r, w, residual=x, p=0.1, seed=1, offset=2))
+    for both in (False, True):
+        y = r.clone()
+        a = ops._DROPOUT.pack(dt, 1, rows, cout, *place(y), *place(y if both else r), *place(y), 0.5, 3, 4)
+        assert lib.qoda_dropout(a, torch.cuda.current_stream().cuda_stream) == qoda.OK
+        assert torch.equal(y, ops.dropout(r, 0.5, 3, 4, activation="relu", residual=r))
+    n, mean, rstd = ops.group_norm(r, 1)
+    want = ops.group_norm_grad(n, r, mean, rstd, 1, residual=r)
+    dx, dw, db = r.clone(), torch.empty(cout, device="cuda"), torch.empty(cout, device="cuda")
+    three = lambda t: (t.data_ptr(), t.shape[-1], t.shape[-1])  # noqa: E731
+    call("group_norm_grad", ops._NORM_GRAD, 0, rows, 1, cout, 1, *three(n), *three(r), *three(dx), *three(dx), 0, 0, mean.data_ptr(), rstd.data_ptr(), dw.data_ptr(), db.data_ptr(), 0)
+    assert torch.equal(dx, want[0]) and torch.equal(dw, want[1]) and torch.equal(db, want[2])
+
+
+def test_a_workspace_that_is_too_small_is_refused():
+    x, w = torch.randn((20, 4000), device="cuda"), torch.randn((300, 4000), device="cuda")
+    y, lib = torch.zeros((20, 300), device="cuda"), ops._load()
+    a = ops._LINEAR.pack(0, 0, 20, 4000, 300, x.data_ptr(), 4000, w.data_ptr(), 4000, 0, 0, y.data_ptr(), 300, 0, 0, 0, 0.0, 0, 0)
+    need = lib.qoda_linear_workspace_bytes(a)
+    assert need > 0
+    scratch = torch.empty(need + 16, dtype=torch.uint8, device="cuda")
+    for p, n, said in ((None, 0, "workspace"), (scratch.data_ptr(), need - 1, "workspace"), (scratch.data_ptr() + 4, need, "16 bytes")):
+        assert lib.qoda_linear(a, p, n, None) == qoda.EINVAL and said in ops.operator_error()
+    torch.cuda.synchronize()
+    assert not y.any()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("activation", ACTS)
 @pytest.mark.parametrize("rows,cols,pad", [(0, 4, 0), (3, 0, 0), (1, 1, 0), (1, 4099, 0), (7, 8, 0), (5, 61, 0), (5, 61, 1), (33, 410, 6), (64, 256, 8), (300, 1031, 1)])
