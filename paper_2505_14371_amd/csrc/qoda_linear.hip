@@ -215,20 +215,33 @@ __device__ __forceinline__ float chunk_sum(v4u v) {
   }
 }
 
+// What the end of a product reads beside the sums, requested ahead of its use.
+template <class T, int FORM, int ACT>
+struct Beside {
+  Eight<T> pre, extra;
+  Eight<float> was;
+  __device__ __forceinline__ void load(const Product &p, int i, int j, int n) {
+    if constexpr (FORM == kProductColumns) {
+      if (p.accumulate) was.load(static_cast<const float *>(p.out) + (long long)i * p.ldo + j, n);
+    } else {
+      if constexpr (FORM == kProductMixed && ACT != kActNone) pre.load(static_cast<const T *>(p.pre) + (long long)i * p.ldp + j, n);
+      if (p.extra) extra.load(static_cast<const T *>(p.extra) + (long long)i * p.lde + j, n);
+    }
+  }
+};
+
 // c[i][j .. j + 7] (n of them exist; j a multiple of 8), after the sum over l, to where the call wants them.
 template <class T, int FORM, int ACT>
-__device__ __forceinline__ void finish(const Product &p, int i, int j, int n, float (&c)[8]) {
+__device__ __forceinline__ void finish(const Product &p, const Beside<T, FORM, ACT> &o, int i, int j, int n, float (&c)[8]) {
+  float other[8];
   if constexpr (FORM == kProductColumns) {
-    float *o = static_cast<float *>(p.out) + (long long)i * p.ldo + j;
     if (p.accumulate) {
-      float was[8];
-      load8(o, n, was);
+      o.was.get(other);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) c[e] = was[e] + c[e];
+      for (int e = 0; e < 8; ++e) c[e] = other[e] + c[e];
     }
-    store8(o, n, c);
+    store8(static_cast<float *>(p.out) + (long long)i * p.ldo + j, n, c);
   } else {
-    float other[8];
     if constexpr (FORM == kProductRows) {
       if (p.bias) {
         load8(p.bias + j, n, other);
@@ -239,13 +252,13 @@ __device__ __forceinline__ void finish(const Product &p, int i, int j, int n, fl
 #pragma unroll
       for (int e = 0; e < 8; ++e) c[e] = act<ACT>(c[e]);
     } else if constexpr (ACT != kActNone) {
-      load8(static_cast<const T *>(p.pre) + (long long)i * p.ldp + j, n, other);
+      o.pre.get(other);
 #pragma unroll
       for (int e = 0; e < 8; ++e) c[e] = c[e] * act_slope<ACT>(other[e]);
     }
     if (p.drop.threshold) drop8(p.drop, (u32)i, (u32)j >> 3, c);
     if (p.extra) {
-      load8(static_cast<const T *>(p.extra) + (long long)i * p.lde + j, n, other);
+      o.extra.get(other);
 #pragma unroll
       for (int e = 0; e < 8; ++e) c[e] = other[e] + c[e];
     }
@@ -406,25 +419,46 @@ __global__ void __launch_bounds__(64 * WM * WN) k_product(Product p, int tiles_m
           else p.sums[i] = p.accumulate ? p.sums[i] + v : v;
         }
       }
-  const auto each = [&](auto &&f) {
+  const auto row = [&](int x) { return i0 + wm + x * 16 + (lane & 15); };
+  const auto column = [&](int y) { return j0 + wn + y * 32 + g * 8; };
+  const auto sums = [&](int x, int y, float (&v)[8]) {
 #pragma unroll
-    for (int x = 0; x < FM; ++x) {
-      const int i = i0 + wm + x * 16 + (lane & 15);
-      if (i < p.m)
-#pragma unroll
-        for (int y = 0; y < FN; ++y) {
-          const int j = j0 + wn + y * 32 + g * 8;
-          if (j < p.n) {
-            float v[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = c[x][2 * y + e / 4][e & 3];
-            f(i, j, p.n - j, v);
-          }
-        }
-    }
+    for (int e = 0; e < 8; ++e) v[e] = c[x][2 * y + e / 4][e & 3];
   };
-  if (p.partial) each([&](int i, int j, int n, float (&v)[8]) { store8(p.partial + ((long long)blockIdx.y * p.m + i) * p.n + j, n, v); });
-  else by_activation<FORM>(p.activation, [&](auto a) { each([&](int i, int j, int n, float (&v)[8]) { finish<T, FORM, decltype(a)::value>(p, i, j, n, v); }); });
+  if (p.partial) {
+#pragma unroll
+    for (int x = 0; x < FM; ++x)
+#pragma unroll
+      for (int y = 0; y < FN; ++y)
+        if (row(x) < p.m && column(y) < p.n) {
+          float v[8];
+          sums(x, y, v);
+          store8(p.partial + ((long long)blockIdx.y * p.m + row(x)) * p.n + column(y), p.n - column(y), v);
+        }
+    return;
+  }
+  by_activation<FORM>(p.activation, [&](auto a) {
+    // in parts of at most four rows, whose reads are all on their way before the first is needed
+    constexpr int kPart = FM < 4 ? FM : 4;
+#pragma unroll
+    for (int x0 = 0; x0 < FM; x0 += kPart) {
+      Beside<T, FORM, decltype(a)::value> beside[kPart][FN];
+#pragma unroll
+      for (int x = 0; x < kPart; ++x)
+#pragma unroll
+        for (int y = 0; y < FN; ++y)
+          if (row(x0 + x) < p.m && column(y) < p.n) beside[x][y].load(p, row(x0 + x), column(y), p.n - column(y));
+#pragma unroll
+      for (int x = 0; x < kPart; ++x)
+#pragma unroll
+        for (int y = 0; y < FN; ++y)
+          if (row(x0 + x) < p.m && column(y) < p.n) {
+            float v[8];
+            sums(x0 + x, y, v);
+            finish(p, beside[x][y], row(x0 + x), column(y), p.n - column(y), v);
+          }
+    }
+  });
 }
 
 // x w^T for up to 16 rows of x: w is read once and that is the time.  A workgroup takes 16 rows of w, its NW waves the runs of 128 bytes along l in
@@ -466,7 +500,11 @@ __global__ void __launch_bounds__(64 * NW) k_few_rows(Product p) {
 #pragma unroll
       for (int w = 1; w < NW; ++w) v[e] = v[e] + part[w][(j + e) / 4 * 16 + row][e & 3];
     }
-    by_activation<kProductRows>(p.activation, [&](auto x) { finish<T, kProductRows, decltype(x)::value>(p, row, j0 + j, p.n - j0 - j, v); });
+    by_activation<kProductRows>(p.activation, [&](auto x) {
+      Beside<T, kProductRows, decltype(x)::value> beside;
+      beside.load(p, row, j0 + j, p.n - j0 - j);
+      finish(p, beside, row, j0 + j, p.n - j0 - j, v);
+    });
   }
 }
 
@@ -493,7 +531,9 @@ __global__ void __launch_bounds__(256) k_join(Product p, int splits) {
             for (int e = 0; e < 8; ++e) c[e] = c[e] + v[e];
           }
       }
-      finish<T, FORM, decltype(a)::value>(p, i, j, n, c);
+      Beside<T, FORM, decltype(a)::value> beside;
+      beside.load(p, i, j, n);
+      finish(p, beside, i, j, n, c);
     }
   });
   if constexpr (FORM == kProductColumns)
