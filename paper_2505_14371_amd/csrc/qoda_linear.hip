@@ -66,9 +66,9 @@ __device__ __forceinline__ v4u load_chunk(const T *p, int valid) {
   return v;
 }
 
-// One operand's tile: N entries across (rows of c for SIDE 0, columns for SIDE 1) by a step of l, moved by the WG threads.  DIRECT: bytes that a
-// direct load into shared memory moves for a lane, 16 or 4, to which its rows have to be aligned; 0: by way of registers.
-template <class T, bool ROWS, int SIDE, int N, int WG, int DIRECT>
+// One operand's tile: N entries across (rows of c for SIDE 0, columns for SIDE 1) by a step of l, moved by the WG threads.  DIRECT: by
+// loads straight into shared memory, 16 bytes a lane, which need addresses of whole words; otherwise by way of registers.
+template <class T, bool ROWS, int SIDE, int N, int WG, bool DIRECT>
 struct Operand {
   static constexpr int E = 16 / (int)sizeof(T);                 // entries of a chunk
   static constexpr int kStep = kStepBytes / (int)sizeof(T);     // l of a step
@@ -80,8 +80,7 @@ struct Operand {
   const T *base;     // entry (first, 0)
   long long ld;
   int across, k;     // entries that exist across from the tile's first on, and along l
-  static constexpr int kDirect = DIRECT ? kMine * 16 / DIRECT : 0;
-  u32 offset[DIRECT ? kDirect : 1]; // of what the thread's direct loads move, from the step's first entry, in bytes
+  u32 offset[DIRECT ? kMine : 1];   // of the chunks that the thread's direct loads move, from the step's first entry, in bytes
 
   // place `at` in shared memory, in chunks: its row, and which chunk of it lies there
   static __device__ __forceinline__ void place(int at, int &row, int &chunk) {
@@ -93,16 +92,14 @@ struct Operand {
     across = end - first;
     k = k_;
     base = static_cast<const T *>(p) + (ROWS ? (long long)first * ld + k0 : (long long)k0 * ld + first);
-    if constexpr (DIRECT != 0)
+    if constexpr (DIRECT)
 #pragma unroll
-      for (int q = 0; q < kDirect; ++q) {
-        const int at = q * WG + (int)threadIdx.x;   // in pieces of DIRECT bytes
+      for (int q = 0; q < kMine; ++q) {
         int row, chunk;
-        place(at / (16 / DIRECT), row, chunk);
-        const int byte = chunk * 16 + at % (16 / DIRECT) * DIRECT;
+        place(q * WG + (int)threadIdx.x, row, chunk);
         // beyond the edge: what is loaded there is multiplied into sums that are not stored
-        if (ROWS) offset[q] = (u32)((row < across ? row : across - 1) * ld * (int)sizeof(T)) + byte;
-        else offset[q] = (u32)(row * ld * (int)sizeof(T)) + (byte / (int)sizeof(T) < across ? byte : 0);
+        if (ROWS) offset[q] = (u32)((row < across ? row : across - 1) * ld * (int)sizeof(T)) + chunk * 16;
+        else offset[q] = (u32)(row * ld * (int)sizeof(T)) + (chunk * E < across ? chunk * 16 : 0);
       }
   }
   // A whole step straight into shared memory.  The instruction is written out because the compiler, which cannot tell
@@ -112,14 +109,10 @@ struct Operand {
 #pragma clang diagnostic ignored "-Winline-asm"
   __device__ __forceinline__ void direct(int l, lds_ptr to) const {
     const char *p = reinterpret_cast<const char *>(base + (ROWS ? (long long)l : (long long)l * ld));
-    const u32 at = __builtin_amdgcn_readfirstlane((u32)(uintptr_t)to + (threadIdx.x & ~63u) * DIRECT);
+    const u32 at = __builtin_amdgcn_readfirstlane((u32)(uintptr_t)to + (threadIdx.x & ~63u) * 16);
 #pragma unroll
-    for (int q = 0; q < kDirect; ++q) {
-      if constexpr (DIRECT == 16)
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(at + q * WG * 16), "v"(offset[q]), "s"(p) : "memory", "m0");
-      else
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(at + q * WG * 4), "v"(offset[q]), "s"(p) : "memory", "m0");
-    }
+    for (int q = 0; q < kMine; ++q)
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(at + q * WG * 16), "v"(offset[q]), "s"(p) : "memory", "m0");
   }
 #pragma clang diagnostic pop
   // Any step by way of registers, entries beyond an edge 0.
@@ -292,8 +285,8 @@ __device__ __forceinline__ void tile_of(int id, int tiles_m, int tiles_n, int &t
   tn = in / rows;
 }
 
-template <class T, int FORM, int BM, int BN, int WM, int WN, int DIRECT>
-__global__ void __launch_bounds__(64 * WM * WN) k_product(Product p, int tiles_m, int tiles_n, int steps_each) {
+template <class T, int FORM, int BM, int BN, int WM, int WN, bool DIRECT>
+__global__ void __launch_bounds__(64 * WM * WN) k_product(Product p, int tiles_m, int tiles_n, int steps_each, bool loose) {
   constexpr int WG = 64 * WM * WN, FM = BM / WM / 16, FN = BN / WN / 32;
   typedef Operand<T, FORM != kProductColumns, 0, BM, WG, DIRECT> A;
   typedef Operand<T, FORM == kProductRows, 1, BN, WG, DIRECT> B;
@@ -354,12 +347,13 @@ __global__ void __launch_bounds__(64 * WM * WN) k_product(Product p, int tiles_m
   // While a step's first half is multiplied its second half is read from shared memory, and while that is multiplied the next step's first
   // half: the matrix cores have work on both sides of the barrier.  It stands between the halves, when everybody has read the step, so
   // that the step after the next may take its place.
-  // Direct loads move whole steps only.  A step that ends inside, which goes by way of registers, is the first to be taken: its loads
-  // and those of the whole step behind it are then on their way together.
+  // Direct loads move whole steps only.  A last step that ends inside goes by way of registers and is the first to be taken: its loads
+  // and those of the whole step behind it are then on their way together.  So does the last step where rows are not aligned to chunks
+  // (loose): the chunk over a row's end, if any, then reads into the next row, which has to be there; an aligned one ends in the same 16 bytes.
   v4u ra[A::kMine], rb[B::kMine];
-  const int ragged = DIRECT != 0 && k % kStep != 0 ? 1 : 0;
+  const int ragged = DIRECT && (loose || k % kStep != 0) ? 1 : 0;
   const auto request = [&](int t, lds_ptr to_a, lds_ptr to_b) {   // step t in the order in which they are taken
-    if constexpr (DIRECT != 0) {
+    if constexpr (DIRECT) {
       a.direct((t - ragged) * kStep, to_a);
       b.direct((t - ragged) * kStep, to_b);
     } else {   // by way of registers, which then take the step after it
@@ -372,7 +366,7 @@ __global__ void __launch_bounds__(64 * WM * WN) k_product(Product p, int tiles_m
     }
   };
   if (steps > 0) {
-    if (DIRECT == 0 || ragged) {
+    if (!DIRECT || ragged) {
       const int first = ragged ? (steps - 1) * kStep : 0;
       a.fetch(first, ra);
       b.fetch(first, rb);
@@ -549,7 +543,7 @@ __global__ void __launch_bounds__(256) k_join(Product p, int splits) {
 enum Tile { kFewRows, kTile32, kTile64, kTile128, kTile256 };
 struct Plan {
   Tile tile;
-  int direct;
+  bool direct, loose;
   int tiles_m, tiles_n, splits, steps_each;
 };
 
@@ -585,12 +579,15 @@ Plan plan_of(const Product &p) {
     q.tiles_m = 1, q.tiles_n = (p.n + 15) / 16;
     return q;
   }
-  // direct loads: by 32-bit offsets inside a tile, 16 bytes a lane, or 4 where rows start at those (bf16: of even strides)
+  // direct loads: from whole words, by 32-bit offsets inside a tile
   const auto fits = [&](const void *v, long long ld, bool rows, int bytes) {
     return reinterpret_cast<uintptr_t>(v) % bytes == 0 && ld * e % bytes == 0 && (rows ? 256 : step) * ld * e < (1ll << 31);
   };
-  for (const int bytes : {4, 16})
-    if (p.n > 0 && fits(p.a, p.lda, p.form != kProductColumns, bytes) && fits(p.b, p.ldb, p.form == kProductRows, bytes)) q.direct = bytes;
+  const auto both = [&](int bytes) { return fits(p.a, p.lda, p.form != kProductColumns, bytes) && fits(p.b, p.ldb, p.form == kProductRows, bytes); };
+  q.loose = !both(16);
+  // (loose, across l: the next row, which a chunk over a row's end reads into, is at least a chunk)
+  const bool wide_rows = (p.form == kProductRows || p.n >= 8) && (p.form != kProductColumns || p.m >= 8);
+  q.direct = p.n > 0 && both(4) && (!q.loose || wide_rows);
   const auto tiles = [&](int bm, int bn) { return (long long)((p.m + bm - 1) / bm) * (p.n > 0 ? (p.n + bn - 1) / bn : 1); };
   const int steps = p.k > 0 ? (p.k + step - 1) / step : 1;
   int bm, bn;
@@ -608,7 +605,7 @@ Plan plan_of(const Product &p) {
         {kTile64, 64, 4, wide ? 800e12 : 132e12}, {kTile128, 128, 2, wide ? 1060e12 : 140e12}, {kTile256, 256, 1, 1250e12}};
     double least = 0.0;
     for (const auto &c : cuts) {
-      if (c.tile == kTile256 && (q.direct != 16 || !wide)) continue;
+      if (c.tile == kTile256 && !(q.direct && wide)) continue;
       const long long n = tiles(c.side, c.side);
       for (int splits = 1; splits == 1 || (splits <= 16 && splits * 4 <= steps && n * splits <= c.a_cu * kCus && c.tile != kTile256); ++splits) {
         const double us = time_of(p, c.side, c.a_cu, c.rate, n, steps, splits);
@@ -625,14 +622,8 @@ Plan plan_of(const Product &p) {
 template <class T, int FORM, int BM, int BN, int WM, int WN>
 void launch(const Product &p, const Plan &q, hipStream_t s) {
   const dim3 grid((unsigned)(q.tiles_m * q.tiles_n), (unsigned)q.splits);
-  const auto run = [&](auto direct) {
-    k_product<T, FORM, BM, BN, WM, WN, decltype(direct)::value><<<grid, 64 * WM * WN, 0, s>>>(p, q.tiles_m, q.tiles_n, q.steps_each);
-  };
-  if (q.direct == 16) run(std::integral_constant<int, 16>());
-  else if constexpr (BM < 256) {
-    if (q.direct == 4) run(std::integral_constant<int, 4>());
-    else run(std::integral_constant<int, 0>());
-  }
+  if (q.direct) k_product<T, FORM, BM, BN, WM, WN, true><<<grid, 64 * WM * WN, 0, s>>>(p, q.tiles_m, q.tiles_n, q.steps_each, q.loose);
+  else if constexpr (BM < 256) k_product<T, FORM, BM, BN, WM, WN, false><<<grid, 64 * WM * WN, 0, s>>>(p, q.tiles_m, q.tiles_n, q.steps_each, false);
 }
 
 template <class T, int FORM>
