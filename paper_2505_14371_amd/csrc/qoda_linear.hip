@@ -38,7 +38,7 @@ __device__ __forceinline__ int row_swizzle(int row) {
 // fp32: rows 4 g and 64 bytes, or every other 16 of 128.
 template <class T, int SIDE, int N>
 __device__ __forceinline__ int column_swizzle(int l) {
-  constexpr int kMask = N * (int)sizeof(T) / 16 - 1;   // of the row's chunks
+  constexpr int kChunks = N * (int)sizeof(T) / 16, kMask = (kChunks & -kChunks) - 1;   // inside the row, whose chunks may be 24
   if constexpr (sizeof(T) == 2) return (SIDE == 0 ? ((l & 3) << 1) | (l & 8) : (l & 3) << 2) & kMask;
   else return (SIDE == 0 ? l & 12 : ((l & 4) << 1) | ((l >> 3) & 1)) & kMask;
 }
@@ -75,7 +75,8 @@ struct Operand {
   static constexpr int kRowChunks = ROWS ? 8 : N / E;           // chunks of a row in shared memory
   static constexpr int kMine = N * 8 / WG;                      // chunks that a thread moves
   static_assert(N * 8 % WG == 0, "whole chunks a thread");
-  static_assert((N & (N - 1)) == 0, "chunks are permuted inside a row");
+  static constexpr bool kPower = (N & (N - 1)) == 0;
+  static_assert(kPower || (N % 64 == 0 && SIDE == 0 && sizeof(T) == 2), "what piece() knows");
 
   const T *base;     // entry (first, 0)
   long long ld;
@@ -141,6 +142,7 @@ struct Operand {
     } else if constexpr (sizeof(T) == 2) {
       // the lane names four adjacent entries of row 8 g + i / 4 (and of the row four further on), and receives one column's four
       const int l = g * 8 + (i >> 2);
+      if constexpr (!kPower) return (u32)(l * N * 2 + ((i & 3) >> 1) * 16 + (i & 1) * 8);
       const int chunk = (SIDE == 0 ? (i & 3) >> 1 : i & 3) ^ column_swizzle<T, SIDE, N>(l);
       return (u32)((l * N * 2 + chunk * 16 + (SIDE == 0 ? (i & 1) * 8 : 0)) ^ (wave_first * 2));
     } else {
@@ -149,11 +151,15 @@ struct Operand {
       return (u32)((l * N * 4 + chunk * 16 + (i & 3) * 4) ^ (wave_first * 4));
     }
   }
-  static __device__ __forceinline__ v4u piece(lds_ptr tile, u32 key, int first, int t, int s) {
+  static __device__ __forceinline__ v4u piece(lds_ptr tile, u32 key, int wave_first, int first, int t, int s) {
     if constexpr (ROWS) {
       return *LDS(v4u, tile + (key ^ (s * 64)) + (first * 128 + t * 512));
     } else if constexpr (sizeof(T) == 2) {
-      const lds_ptr p = tile + (key ^ (first * 2));
+      lds_ptr p = tile + (key ^ (first * 2));
+      if constexpr (!kPower) {   // rows are no power of two long: the chunks' permutation, of their lower three bits, apart from the rest
+        const u32 chunks = (u32)(wave_first + first) / 8, swizzle = (threadIdx.x & 12) << 3;
+        p = tile + (key + (chunks & ~7u) * 16 + (((chunks & 7u) * 16) ^ swizzle));
+      }
       v4u v;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -312,7 +318,7 @@ __global__ void __launch_bounds__(64 * WM * WN) k_product(Product p, int tiles_m
     for (int y = 0; y < 2 * FN; ++y) c[x][y] = v4f{0, 0, 0, 0};
 
   // the sums of a's columns: the waves of the first column of tiles share them, each for some of its rows of c
-  constexpr int FS = FM / WN > 0 ? FM / WN : 1;
+  constexpr int FS = (FM + WN - 1) / WN;
   const bool with_sums = FORM == kProductColumns && p.sums && tn == 0 && wave % WN * FS < FM;
   float sum[FS] = {};
 
@@ -323,9 +329,9 @@ __global__ void __launch_bounds__(64 * WM * WN) k_product(Product p, int tiles_m
     // the pieces' places are made anew each time: kept, they would take the registers that pieces need
     asm volatile("" : "+v"(key_a), "+v"(key_b));
 #pragma unroll
-    for (int y = 0; y < 2 * FN; ++y) fb[y] = B::piece(tb, key_b, y / 2 * 32, y & 1, s);
+    for (int y = 0; y < 2 * FN; ++y) fb[y] = B::piece(tb, key_b, wn, y / 2 * 32, y & 1, s);
 #pragma unroll
-    for (int x = 0; x < FM; ++x) fa[x] = A::piece(ta, key_a, x * 16, 0, s);
+    for (int x = 0; x < FM; ++x) fa[x] = A::piece(ta, key_a, wm, x * 16, 0, s);
   };
   const u32 key_s = A::lane_key(wm + wave % WN * FS * 16);
   const auto add_up = [&](lds_ptr ta) {
@@ -334,7 +340,7 @@ __global__ void __launch_bounds__(64 * WM * WN) k_product(Product p, int tiles_m
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
-          for (int x = 0; x < FS; ++x) sum[x] = sum[x] + chunk_sum<T>(A::piece(ta, key_s, x * 16, 0, s));
+          for (int x = 0; x < FS; ++x) sum[x] = sum[x] + chunk_sum<T>(A::piece(ta, key_s, wm + wave % WN * FS * 16, x * 16, 0, s));
   };
   const auto multiply_all = [&](const PiecesA &fa, const PiecesB &fb) {
 #pragma unroll
@@ -433,7 +439,7 @@ __global__ void __launch_bounds__(64 * WM * WN) k_product(Product p, int tiles_m
   }
   by_activation<FORM>(p.activation, [&](auto a) {
     // in parts of at most four rows, whose reads are all on their way before the first is needed
-    constexpr int kPart = FM < 4 ? FM : 4;
+    constexpr int kPart = FM % 4 == 0 ? 4 : FM % 3 == 0 ? 3 : FM;
 #pragma unroll
     for (int x0 = 0; x0 < FM; x0 += kPart) {
       Beside<T, FORM, decltype(a)::value> beside[kPart][FN];
@@ -540,7 +546,7 @@ __global__ void __launch_bounds__(256) k_join(Product p, int splits) {
 }
 
 // How a product is cut.
-enum Tile { kFewRows, kTile32, kTile64, kTile128, kTile256 };
+enum Tile { kFewRows, kTile32, kTile64, kTile128, kTile192, kTile256 };
 struct Plan {
   Tile tile;
   bool direct, loose;
@@ -551,16 +557,16 @@ constexpr int kCus = 256;
 
 // What a cut would take, in us, from what was measured: the matrix cores' rate in a tile of each size, the time of a step that nothing but
 // its loads bounds, of a tile's start and end, and of the launch that joins splits.
-double time_of(const Product &p, int side, int a_cu, double rate, long long tiles, int steps, int splits) {
+double time_of(const Product &p, int bm, int bn, int a_cu, double rate, long long tiles, int steps, int splits) {
   const int step = kStepBytes / (p.type == kF32 ? 4 : 2), steps_each = (steps + splits - 1) / splits;
-  const double flops = 2.0 * side * side * step, whole = rate / kCus;
+  const double flops = 2.0 * bm * bn * step, whole = rate / kCus;
   long long left = tiles * splits;
   double us = 0.0;
   while (left > 0) {   // workgroups that share a CU share its matrix cores; the last ones are fewer
     const long long now = left < (long long)a_cu * kCus ? left : (long long)a_cu * kCus;
     const long long rounds = left / now;
     const int sharing = (int)((now + kCus - 1) / kCus);
-    const double alone = side == 256 || sharing > 2 ? 1.0 : sharing == 2 ? (a_cu > 2 ? 1.1 : 1.0) : 1.5;   // too few waves to fill a SIMD's gaps
+    const double alone = bn == 256 || sharing > 2 ? 1.0 : sharing == 2 ? (a_cu > 2 ? 1.1 : 1.0) : 1.5;   // too few waves to fill a SIMD's gaps
     const double one = alone * sharing * flops / whole * 1e6;
     us += (double)rounds * (2.0 + steps_each * (one > 0.5 ? one : 0.5));
     left -= rounds * now;
@@ -598,18 +604,20 @@ Plan plan_of(const Product &p) {
     q.splits = (int)(want < most ? want : most);
     if (q.splits < 2) q.splits = 1;
   } else {
-    // TFLOP/s of whole tiles, 16384 x 8192 x 2048 and 4096 x 2048 x 2048: bf16 1250 (256), 1060 (128), 800 (64); fp32, whose matrix
+    // TFLOP/s of whole tiles, 16384 x 8192 x 2048 and 4096 x 2048 x 2048: bf16 1250 (256), 1200 (192 x 256), 1060 (128), 800 (64); fp32, whose matrix
     // instructions take sixteen times as long for a piece, 140 (128), 132 (64)
     const bool wide = p.type == kBf16;
-    const struct { Tile tile; int side, a_cu; double rate; } cuts[] = {
-        {kTile64, 64, 4, wide ? 800e12 : 132e12}, {kTile128, 128, 2, wide ? 1060e12 : 140e12}, {kTile256, 256, 1, 1250e12}};
+    const struct { Tile tile; int bm, bn, a_cu; double rate; } cuts[] = {{kTile64, 64, 64, 4, wide ? 800e12 : 132e12},
+                                                                         {kTile128, 128, 128, 2, wide ? 1060e12 : 140e12},
+                                                                         {kTile192, 192, 256, 1, 1200e12},
+                                                                         {kTile256, 256, 256, 1, 1250e12}};
     double least = 0.0;
     for (const auto &c : cuts) {
-      if (c.tile == kTile256 && !(q.direct && wide)) continue;
-      const long long n = tiles(c.side, c.side);
-      for (int splits = 1; splits == 1 || (splits <= 16 && splits * 4 <= steps && n * splits <= c.a_cu * kCus && c.tile != kTile256); ++splits) {
-        const double us = time_of(p, c.side, c.a_cu, c.rate, n, steps, splits);
-        if (least == 0.0 || us < least) least = us, q.tile = c.tile, q.splits = splits, bm = bn = c.side;
+      if (c.tile >= kTile192 && !(q.direct && wide)) continue;
+      const long long n = tiles(c.bm, c.bn);
+      for (int splits = 1; splits == 1 || (splits <= 16 && splits * 4 <= steps && n * splits <= c.a_cu * kCus && c.tile < kTile192); ++splits) {
+        const double us = time_of(p, c.bm, c.bn, c.a_cu, c.rate, n, steps, splits);
+        if (least == 0.0 || us < least) least = us, q.tile = c.tile, q.splits = splits, bm = c.bm, bn = c.bn;
       }
     }
   }
@@ -623,7 +631,7 @@ template <class T, int FORM, int BM, int BN, int WM, int WN>
 void launch(const Product &p, const Plan &q, hipStream_t s) {
   const dim3 grid((unsigned)(q.tiles_m * q.tiles_n), (unsigned)q.splits);
   if (q.direct) k_product<T, FORM, BM, BN, WM, WN, true><<<grid, 64 * WM * WN, 0, s>>>(p, q.tiles_m, q.tiles_n, q.steps_each, q.loose);
-  else if constexpr (BM < 256) k_product<T, FORM, BM, BN, WM, WN, false><<<grid, 64 * WM * WN, 0, s>>>(p, q.tiles_m, q.tiles_n, q.steps_each, false);
+  else if constexpr (BN < 256) k_product<T, FORM, BM, BN, WM, WN, false><<<grid, 64 * WM * WN, 0, s>>>(p, q.tiles_m, q.tiles_n, q.steps_each, false);
 }
 
 template <class T, int FORM>
@@ -639,6 +647,9 @@ void launch(const Product &p, const Plan &q, hipStream_t s) {
     case kTile32: launch<T, FORM, 32, 128, 1, 4>(p, q, s); break;
     case kTile64: launch<T, FORM, 64, 64, 2, 2>(p, q, s); break;
     case kTile128: launch<T, FORM, 128, 128, 2, 2>(p, q, s); break;
+    case kTile192:
+      if constexpr (sizeof(T) == 2) launch<T, FORM, 192, 256, 2, 4>(p, q, s);
+      break;
     case kTile256:
       if constexpr (sizeof(T) == 2) launch<T, FORM, 256, 256, 2, 4>(p, q, s);
       break;

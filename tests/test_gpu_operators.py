@@ -105,7 +105,7 @@ def test_linear_weight_grad(rows, cin, cout, dtype):
 
 
 # what small products do not reach: the largest tiles with ragged ends on every side, sums split along l, rows at 4-byte and at odd addresses
-LARGER = [(8190, 536, 8184, 0, "bf16"), (8184, 8184, 600, 0, "bf16"), (3000, 410, 2100, 0, "bf16"), (1500, 411, 1001, 0, "bf16"), (616, 8184, 8184, 0, "bf16"), (200, 8200, 300, 0, "bf16"), (30, 4104, 520, 0, "bf16"),
+LARGER = [(8190, 536, 8184, 0, "bf16"), (8184, 8184, 600, 0, "bf16"), (3000, 410, 2100, 0, "bf16"), (1500, 411, 1001, 0, "bf16"), (616, 8184, 8184, 0, "bf16"), (2000, 2040, 6136, 0, "bf16"), (6140, 2002, 2042, 2, "bf16"), (200, 8200, 300, 0, "bf16"), (30, 4104, 520, 0, "bf16"),
           (24, 5001, 333, 1, "bf16"), (3000, 410, 2100, 0, "f32"), (100, 6000, 130, 1, "f32"), (2050, 200, 2060, 0, "f32"), (20, 2000, 700, 0, "f32")]
 
 
