@@ -1,0 +1,73 @@
+"""Residual blocks on the operators: their gradients against torch's differentiation in 64 bits, and a training run."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+import operator_definitions as D  # noqa: E402
+from paper_2505_14371_amd.blocks import ResidualBlocks  # noqa: E402
+from paper_2505_14371_amd.harness import train_blocks  # noqa: E402
+
+
+@pytest.fixture(autouse=True)
+def gpu():
+    if not torch.cuda.is_available():
+        pytest.fail("a GPU test was selected but no GPU is visible")
+
+
+def reference(model, x, draw):
+    """The blocks in 64 bits on the CPU, differentiable, with the same masks."""
+    params = [q.detach().double().cpu().requires_grad_() for q in model.params]
+    x = x.double().cpu().requires_grad_()
+    h = x
+    factor = lambda rows, cols, i, site: torch.from_numpy(D.drop(np.ones((rows, cols)), model.p, model.seed, (draw * model.depth + i) * 2 + site))  # noqa: E731
+    act = {"gelu": torch.nn.functional.gelu, "silu": torch.nn.functional.silu, "relu": torch.relu}[model.activation]
+    for i in range(model.depth):
+        gamma, beta, w1, b1, w2, b2 = params[6 * i: 6 * i + 6]
+        n = torch.nn.functional.group_norm(h, model.groups, gamma, beta, 1e-5)
+        a = act(n @ w1.t() + b1) * factor(len(x), model.hidden, i, 0)
+        h = h + (a @ w2.t() + b2) * factor(len(x), model.width, i, 1)
+    return h, x, params
+
+
+@pytest.mark.parametrize("activation,groups,p", [("gelu", 1, 0.1), ("silu", 4, 0.5), ("relu", 1, 0.0)])
+def test_gradients_against_differentiation(activation, groups, p):
+    """fp32, three blocks: sums of at most 200 terms a product, six products deep, are good to 1e-5 of the largest entry."""
+    model = ResidualBlocks(60, 200, 3, groups=groups, activation=activation, p=p, dtype=torch.float32, seed=3)
+    for q in model.params:
+        q.add_(0.1 * torch.randn(q.shape, device="cuda", generator=torch.Generator(device="cuda").manual_seed(q.numel())))
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    x, dy = (torch.randn((70, 60), device="cuda", generator=gen) for _ in range(2))
+    weights, grads = model.weights(), model.gradients()
+    y, saved = model.forward(x, weights, draw=5)
+    dx = model.backward(dy, saved, weights, grads)
+    want, x64, params = reference(model, x, 5)
+    want.backward(dy.double().cpu())
+    for got, exact in [(y, want.detach()), (dx, x64.grad)] + [(g, q.grad) for g, q in zip(grads, params)]:
+        assert (got.double().cpu() - exact).abs().max() <= 1e-5 * (1 + exact.abs().max())
+    once = [g.clone() for g in grads]
+    model.backward(dy, saved, weights, grads, accumulate=True)
+    for g, o in zip(grads, once):
+        assert torch.allclose(g, 2 * o, rtol=1e-5, atol=1e-5 * float(o.abs().max()))
+
+
+def test_another_draw_drops_others_and_the_same_draw_the_same():
+    model = ResidualBlocks(64, 128, 2, p=0.3)
+    x, weights = torch.randn((50, 64), device="cuda").to(torch.bfloat16), model.weights()
+    a, b, c = (model.forward(x, weights, draw=d)[0] for d in (1, 1, 2))
+    assert torch.equal(a, b) and not torch.equal(a, c)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_training_lowers_the_loss(dtype):
+    losses, _, _ = train_blocks.train(width=64, hidden=128, depth=2, nodes=3, rows=256, rounds=40, dtype=dtype)
+    assert all(np.isfinite(losses)) and np.mean(losses[-5:]) < 0.9 * np.mean(losses[:3])
+
+
+def test_refusals():
+    with pytest.raises(ValueError):
+        ResidualBlocks(10, 20, 1, groups=3)
+    with pytest.raises(ValueError):
+        ResidualBlocks(10, 20, 1, dtype=torch.float16)
