@@ -663,28 +663,34 @@ __global__ void __launch_bounds__(NT) k_norm_maps_grad(GroupNorm g, Maps m) {
   groups8(m, at.vec * 8, q);
   const int per = m.blocks_a_group > 1 ? at.width : m.per, groups = at.width / per;
   const long long first = m.blocks_a_group > 1 ? at.block / m.blocks_a_group : at.c0 / m.per;
-  float mean[8], rstd[8], w[8], b[8];
+  // Per channel, few numbers, since the values take most of the registers: with r = rstd and a = r w, what goes through the activation is
+  // h w + b = x a + (b - mean a), the sum of d h is r times that of d (x - mean), and dx is d a - r m1 - (x - mean) r^2 m2.
+  float mean[8], rstd[8], wr[8], b[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    mean[j] = (EVEN ? at.own > 0 : j < at.own) ? g.mean[at.n * g.groups + first + q[j]] : 0.0f;
-    rstd[j] = (EVEN ? at.own > 0 : j < at.own) ? g.rstd[at.n * g.groups + first + q[j]] : 0.0f;
-    w[j] = b[j] = 0.0f;
+    const bool mine = EVEN ? at.own > 0 : j < at.own;
+    mean[j] = mine ? g.mean[at.n * g.groups + first + q[j]] : 0.0f;
+    rstd[j] = mine ? g.rstd[at.n * g.groups + first + q[j]] : 0.0f;
+    wr[j] = b[j] = 0.0f;
   }
   if (at.own > 0) {
-    vector8<EVEN>(g.weight ? g.weight + c : nullptr, 1.0f, at.own, w);
+    vector8<EVEN>(g.weight ? g.weight + c : nullptr, 1.0f, at.own, wr);
     vector8<EVEN>(g.bias ? g.bias + c : nullptr, 0.0f, at.own, b);
   }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) wr[j] = wr[j] * rstd[j], b[j] = __builtin_fmaf(-mean[j], wr[j], b[j]);
+  // h: x - mean; d: dy through the activation
   const auto back = [&](int u, float (&h)[8], float (&d)[8]) {
     rx[u].get(h);
     rd[u].get(d);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) h[j] = (h[j] - mean[j]) * rstd[j];
     if (g.activation != kActNone) {
       float z[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) z[j] = __builtin_fmaf(h[j], w[j], b[j]);
+      for (int j = 0; j < 8; ++j) z[j] = __builtin_fmaf(h[j], wr[j], b[j]);
       slope8(g.activation, z, d);
     }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) h[j] = h[j] - mean[j];
   };
   if constexpr (PASS != kJoined) {
     float vw[8] = {}, vb[8] = {};
@@ -696,6 +702,8 @@ __global__ void __launch_bounds__(NT) k_norm_maps_grad(GroupNorm g, Maps m) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) vw[j] = __builtin_fmaf(d[j], h[j], vw[j]), vb[j] = vb[j] + d[j];
       }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) vw[j] = vw[j] * rstd[j];
     channel_sums<NT>(m, at, vw, lanes, cw);
     channel_sums<NT>(m, at, vb, lanes, cb);
     float *o = g.scratch + ((at.n * m.chunks + at.chunk) * 2) * g.channels + at.c0;
@@ -758,7 +766,11 @@ __global__ void __launch_bounds__(NT) k_norm_maps_grad(GroupNorm g, Maps m) {
   if (at.own <= 0) return;
   float e1[8], e2[8];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) e1[j] = (EVEN ? at.own > 0 : j < at.own) ? m1[q[j]] : 0.0f, e2[j] = (EVEN ? at.own > 0 : j < at.own) ? m2[q[j]] : 0.0f;
+  for (int j = 0; j < 8; ++j) {
+    const bool mine = EVEN ? at.own > 0 : j < at.own;
+    e1[j] = mine ? rstd[j] * m1[q[j]] : 0.0f;
+    e2[j] = mine ? rstd[j] * rstd[j] * m2[q[j]] : 0.0f;
+  }
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const u32 p = at.p0 + at.row + u * m.rows;
@@ -768,7 +780,7 @@ __global__ void __launch_bounds__(NT) k_norm_maps_grad(GroupNorm g, Maps m) {
       back(u, h, d);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const float v = __builtin_fmaf(-h[j], e2[j], __builtin_fmaf(d[j], w[j], -e1[j])) * rstd[j];
+        const float v = __builtin_fmaf(-h[j], e2[j], __builtin_fmaf(d[j], wr[j], -e1[j]));
         d[j] = g.extra ? o[j] + v : v;
       }
       store8<EVEN>(static_cast<T *>(g.out) + at.n * g.out_sample + p * g.out_pos + c, at.own, d);
@@ -781,7 +793,7 @@ long long gcd(long long a, long long b) { return b == 0 ? a : gcd(b, a % b); }
 
 // A block: whole groups and whole vectors of eight, so that no thread's channels cross a block's edge more often than at the end; at least 128
 // bytes of a row, more where few positions would leave threads idle; at most 256 vectors.
-Maps maps_of(const GroupNorm &g, int threads, int each) {
+Maps maps_of(const GroupNorm &g, int threads, int each, int bytes = 128) {
   Maps m = {};
   m.per = (int)(g.channels / g.groups);
   m.blocks_a_group = 1;
@@ -792,7 +804,7 @@ Maps maps_of(const GroupNorm &g, int threads, int each) {
   } else {
     long long unit = m.per / gcd(m.per, 8) * 8;
     if (unit > 512 || unit > g.channels) unit = m.per;
-    const long long least = g.type == kF32 ? 32 : 64;
+    const long long least = bytes / (g.type == kF32 ? 4 : 2);
     long long w = unit;
     while (w < g.channels && w + unit <= kWidest && (w < least || (w + 7) / 8 * g.positions < kThreads)) w += unit;
     if (w > g.channels) w = g.channels;
@@ -838,8 +850,8 @@ template <class F>
 void by_even(const GroupNorm &g, F &&f) {
   bool even = g.channels / g.groups % 8 == 0;
   if (!even && g.positions > 1) {   // small groups side by side in blocks of whole eights
-    const Maps m = maps_of(g, kThreads, 1);
-    even = m.blocks_a_group == 1 && m.width % 8 == 0 && g.channels % 8 == 0;
+    const Maps m = maps_of(g, kThreads, 1), narrow = maps_of(g, kThreads, 1, 64);
+    even = m.blocks_a_group == 1 && m.width % 8 == 0 && narrow.width % 8 == 0 && g.channels % 8 == 0;
   }
   if (even) f(std::true_type());
   else f(std::false_type());
@@ -885,15 +897,19 @@ hipError_t norm(const GroupNorm &g, hipStream_t s) {
 // The gradient's cut of maps, and whether one launch does it.
 struct GradMaps {
   Maps m;
-  int each;
+  int threads, each;
   bool whole;
 };
 GradMaps grad_maps(const GroupNorm &g) {
-  GradMaps q = {maps_of(g, 256, 2), 2, true};
+  GradMaps q = {maps_of(g, 256, 2), 256, 2, true};
   if (whole(g, q.m)) return q;
-  q = {maps_of(g, 256, 4), 4, true};
-  if (!whole(g, q.m)) q.whole = false;
-  return q;
+  q = {maps_of(g, 256, 4), 256, 4, true};
+  if (whole(g, q.m)) return q;
+  if (g.type == kBf16) {   // two tensors of fp32 would not stay in the registers
+    q = {maps_of(g, 512, 8, 64), 512, 8, true};
+    if (whole(g, q.m)) return q;
+  }
+  return {maps_of(g, 256, 4), 256, 4, false};
 }
 
 template <class T>
@@ -934,6 +950,8 @@ hipError_t norm_grad(const GroupNorm &call, hipStream_t s) {
       if (!q.whole) {
         k_norm_maps_grad<T, 256, 4, kPieces, kEven><<<grid, 256, 0, s>>>(g, q.m);
         k_norm_maps_grad<T, 256, 4, kJoined, kEven><<<grid, 256, 0, s>>>(g, q.m);
+      } else if (q.threads == 512) {
+        if constexpr (sizeof(T) == 2) k_norm_maps_grad<T, 512, 8, kWhole, kEven><<<grid, 512, 0, s>>>(g, q.m);
       } else if (q.each == 2) {
         k_norm_maps_grad<T, 256, 2, kWhole, kEven><<<grid, 256, 0, s>>>(g, q.m);
       } else {
