@@ -122,6 +122,7 @@ typedef struct {
 /* Group normalisation: groups divides channels, group g of a sample is its channels g C/G .. (g+1) C/G - 1 at all positions;
  *   mean, rstd fp32 [samples][groups]: mean, and 1 / sqrt(variance + eps) with the variance of the population;
  *   y = act((x - mean) * rstd * weight + bias), weight and bias fp32 [channels], NULL: 1 and 0.
+ * Without positions or channels there is nothing to write, and mean and rstd are left alone.
  * One position and one group make it a layer normalisation of rows. */
 typedef struct {
   int32_t dtype, activation;

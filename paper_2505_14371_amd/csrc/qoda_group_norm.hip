@@ -7,6 +7,10 @@
 //          all positions; a thread owns eight channels at every so many positions.  Sums run per channel first, because that is what the
 //          gradients of weight and bias are, and a group's are sums of its channels'.  Where a block has more values than a workgroup holds, its
 //          positions are split: one launch for the pieces' sums, one that joins them and makes the result.
+//
+// Measured: rows of 2048, 16384 of them, bf16: forward 25 us (5.3 TB/s), gradient with residual 61 + 7 for the join (4.4 TB/s); a map of 64 x 256 x
+// 256 in fp32 12.8 us, the gradient of 128 x 1024 x 128 in bf16 with silu 50.6 (its slope, taken twice, is 19 us of arithmetic).  Small ones are
+// bound by the launch and by the sums over the workgroup.
 
 #include <type_traits>
 
@@ -836,12 +840,15 @@ Rows rows_of(const GroupNorm &g, bool gradient) {
   if (v <= 1024) return {256, 4};
   return {0, 0};
 }
-// Workgroups that share a group's rows: enough to fill the device a few times, few enough that their partial sums are little beside the rows.
+// Workgroups that share a group's rows: enough to fill the device a few times, but with four turns each before that, so that their partial
+// sums (8 bytes a channel) are little beside the rows.
 long long rows_workgroups(const GroupNorm &g, const Rows &r) {
-  const long long teams = kThreads / r.team, most = (g.samples + teams - 1) / teams;
-  long long want = 1024 / g.groups;
-  if (want < 1) want = 1;
-  return most < want ? most : want;
+  const long long teams = kThreads / r.team, turns = (g.samples + teams - 1) / teams;
+  const auto at_least_one = [](long long v) { return v < 1 ? 1 : v; };
+  const long long least = at_least_one(256 / g.groups), most = at_least_one(1024 / g.groups);
+  long long want = turns / 4;
+  want = want < least ? least : want > most ? most : want;
+  return turns < want ? turns : want;
 }
 constexpr long long kLongSplits = 64;
 
