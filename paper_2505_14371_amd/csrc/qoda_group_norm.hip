@@ -886,6 +886,7 @@ hipError_t norm(const GroupNorm &g, hipStream_t s) {
     Maps m;
     const auto grid = [&] { return dim3((unsigned)workgroups(g, m)); };
     if (m = maps_of(g, 256, 2), whole(g, m)) k_norm_maps<T, 256, 2, kWhole, kEven><<<grid(), 256, 0, s>>>(g, m);
+    else if (m = maps_of(g, 256, 4), whole(g, m)) k_norm_maps<T, 256, 4, kWhole, kEven><<<grid(), 256, 0, s>>>(g, m);
     else if (m = maps_of(g, 256, 8), whole(g, m)) k_norm_maps<T, 256, 8, kWhole, kEven><<<grid(), 256, 0, s>>>(g, m);
     else if (m = maps_of(g, 1024, 8), whole(g, m)) k_norm_maps<T, 1024, 8, kWhole, kEven><<<grid(), 1024, 0, s>>>(g, m);
     else {

@@ -39,6 +39,9 @@ _NORM_GRAD = struct.Struct("@2i4q" + "Pqq" * 4 + "6Pi0q")
 
 _lib = None
 _native = None          # the native look at the arguments, once the library is loaded
+_ready = False          # whether torch has been seen to have a device
+# the current device and its current stream's handle, without a Stream object; not public functions of torch
+_get_device, _get_stream = (getattr(torch._C, n, None) for n in ("_cuda_getDevice", "_cuda_getCurrentRawStream"))
 
 
 def _find_native(L):
@@ -59,12 +62,6 @@ def _find_native(L):
     return native
 
 
-def _here():
-    """The current device and its current stream's handle."""
-    device = torch.cuda.current_device()
-    return device, torch._C._cuda_getCurrentRawStream(device)
-
-
 def _load():
     global _lib, _native
     if _lib is None:
@@ -77,7 +74,7 @@ def _load():
         for call in (L.qoda_dropout, L.qoda_dropout_grad):
             call.argtypes, call.restype = [C.c_char_p, C.c_void_p], C.c_int
         L.qoda_operator_error.argtypes, L.qoda_operator_error.restype = [], C.c_char_p
-        if hasattr(torch._C, "_cuda_getCurrentRawStream"):     # not a public function of torch
+        if _get_device is not None and _get_stream is not None:
             _native = _find_native(L)
         _lib = L
     return _lib
@@ -91,9 +88,13 @@ def _is_native() -> bool:
 
 def _looked_at(call, *args):
     """The native call's outputs; None where its arguments have to be looked at here."""
-    if not torch.cuda.is_initialized():
-        return None
-    out = call(*_here(), *args)
+    global _ready
+    if not _ready:
+        if not torch.cuda.is_initialized():
+            return None
+        _ready = True
+    device = _get_device()
+    out = call(device, _get_stream(device), *args)
     if type(out) is int:
         _raise(out)
     return out
