@@ -396,22 +396,24 @@ __global__ void __launch_bounds__(kThreads) k_norm_long_channels(GroupNorm g) {
   store8(part + g.channels, n, sb);
 }
 
-// dweight and dbias from `count` rows of partial sums [2][channels]: 16 columns a workgroup, its 64 teams of 16 lanes take rows in turn.
-__global__ void __launch_bounds__(1024) k_norm_join(GroupNorm g, const float *part, long long count) {
+// dweight and dbias from `count` rows of partial sums [2][channels]: 16 columns a workgroup, its 64 teams of 16 lanes take rows in turn.  With `to`: the
+// sums of gridDim.y parts of the rows, a row each, which another launch joins.
+__global__ void __launch_bounds__(1024) k_norm_join(GroupNorm g, const float *part, long long count, float *to) {
   __shared__ float red[64][16 + 1];
   const int lane = threadIdx.x & 15, team = threadIdx.x / 16;
   const long long c = (long long)blockIdx.x * 16 + lane, total = 2 * g.channels;
+  const long long each = (count + gridDim.y - 1) / gridDim.y, first = blockIdx.y * each, end = first + each < count ? first + each : count;
   float s = 0.0f;
   if (c < total) {
-    long long r = team;
-    for (; r + 3 * 64 < count; r += 4 * 64) {   // four on their way
+    long long r = first + team;
+    for (; r + 3 * 64 < end; r += 4 * 64) {   // four on their way
       float v[4];
 #pragma unroll
       for (int q = 0; q < 4; ++q) v[q] = part[(r + q * 64) * total + c];
 #pragma unroll
       for (int q = 0; q < 4; ++q) s = s + v[q];
     }
-    for (; r < count; r += 64) s = s + part[r * total + c];
+    for (; r < end; r += 64) s = s + part[r * total + c];
   }
   red[team][lane] = s;
   __syncthreads();
@@ -419,9 +421,13 @@ __global__ void __launch_bounds__(1024) k_norm_join(GroupNorm g, const float *pa
   s = lanes_sum<64>(red[threadIdx.x & 63][column]);
   const long long o = (long long)blockIdx.x * 16 + column;
   if ((threadIdx.x & 63) == 0 && o < total) {
-    float *to = o < g.channels ? g.dweight : g.dbias;
+    if (to) {
+      to[blockIdx.y * total + o] = s;
+      return;
+    }
+    float *out = o < g.channels ? g.dweight : g.dbias;
     const long long at = o < g.channels ? o : o - g.channels;
-    if (to) to[at] = g.accumulate ? to[at] + s : s;
+    if (out) out[at] = g.accumulate ? out[at] + s : s;
   }
 }
 
@@ -852,6 +858,13 @@ long long rows_workgroups(const GroupNorm &g, const Rows &r) {
 }
 constexpr long long kLongSplits = 64;
 
+// Parts in which rows of partial sums are joined first: with many samples of few channels one workgroup would take them all (65536 samples of 4 positions
+// and 16 channels: 137 us in one part).
+long long join_parts(long long count) {
+  const long long parts = (count + 1023) / 1024;
+  return count <= 4096 ? 1 : parts < 256 ? parts : 256;
+}
+
 // Calls f with whether every eight entries exist together or not at all.
 template <class F>
 void by_even(const GroupNorm &g, F &&f) {
@@ -968,7 +981,16 @@ hipError_t norm_grad(const GroupNorm &call, hipStream_t s) {
     }
   });
   if (rc != hipSuccess) return rc;
-  if (sums) k_norm_join<<<dim3((unsigned)((2 * g.channels + 15) / 16)), 1024, 0, s>>>(g, g.scratch, count);
+  if (sums) {
+    const unsigned columns = (unsigned)((2 * g.channels + 15) / 16);
+    if (const long long parts = join_parts(count); parts > 1) {
+      float *to = g.scratch + count * 2 * g.channels;
+      k_norm_join<<<dim3(columns, (unsigned)parts), 1024, 0, s>>>(g, g.scratch, count, to);
+      k_norm_join<<<dim3(columns), 1024, 0, s>>>(g, to, parts, nullptr);
+    } else {
+      k_norm_join<<<dim3(columns), 1024, 0, s>>>(g, g.scratch, count, nullptr);
+    }
+  }
   return hipGetLastError();
 }
 
@@ -988,7 +1010,8 @@ size_t group_norm_scratch(const GroupNorm &g, bool gradient) {
   } else {
     count = g.samples * grad_maps(g).m.chunks;
   }
-  return (size_t)(count * 2 * g.channels) * sizeof(float);
+  const long long parts = join_parts(count);
+  return (size_t)((count + (parts > 1 ? parts : 0)) * 2 * g.channels) * sizeof(float);
 }
 
 hipError_t launch_group_norm(const GroupNorm &g, hipStream_t s) { return g.type == kF32 ? norm<float>(g, s) : norm<bf16>(g, s); }
