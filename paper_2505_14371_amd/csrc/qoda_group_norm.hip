@@ -531,7 +531,8 @@ __device__ __forceinline__ void group_sums(const Maps &m, const Place<NT> &at, c
   __syncthreads();
 }
 
-constexpr int kWidest = 2048;   // channels of a block
+// channels of a block, by the workgroup's threads: what its sums take of shared memory bounds how many workgroups a CU holds
+constexpr int widest(int threads) { return threads == 64 ? 512 : 2048; }
 
 // The group of each of a thread's channels, within the block.
 __device__ __forceinline__ void groups8(const Maps &m, int c, int (&q)[8]) {
@@ -546,8 +547,8 @@ enum MapsPass { kWhole = 0, kPieces = 1, kJoined = 2 };
 template <class T, int NT, int U, int PASS, bool EVEN>
 __global__ void __launch_bounds__(NT) k_norm_maps(GroupNorm g, Maps m) {
   __shared__ float lanes[PASS == kJoined ? 1 : NT * 8];
-  __shared__ float channels[PASS == kJoined ? 1 : kWidest];
-  __shared__ float means[kWidest], rstds[kWidest];   // per group of the block
+  __shared__ float channels[PASS == kJoined ? 1 : widest(NT)];
+  __shared__ float means[widest(NT)], rstds[widest(NT)];   // per group of the block
   const Place<NT> at(g, m);
   const T *x = static_cast<const T *>(g.x) + at.n * g.x_sample + at.c0 + at.vec * 8;
   Eight<T> raw[U];
@@ -657,7 +658,7 @@ __global__ void __launch_bounds__(NT) k_norm_maps(GroupNorm g, Maps m) {
 template <class T, int NT, int U, int PASS, bool EVEN>
 __global__ void __launch_bounds__(NT) k_norm_maps_grad(GroupNorm g, Maps m) {
   __shared__ float lanes[PASS == kJoined ? 1 : NT * 8];
-  __shared__ float cw[kWidest], cb[kWidest];   // per channel: the sums of d h and of d
+  __shared__ float cw[widest(NT)], cb[widest(NT)];   // per channel: the sums of d h and of d
   const Place<NT> at(g, m);
   const long long c = at.c0 + at.vec * 8;
   const T *x = static_cast<const T *>(g.x) + at.n * g.x_sample + c, *dy = static_cast<const T *>(g.dy) + at.n * g.dy_sample + c;
@@ -757,7 +758,7 @@ __global__ void __launch_bounds__(NT) k_norm_maps_grad(GroupNorm g, Maps m) {
     }
   }
   __syncthreads();
-  __shared__ float m1[kWidest], m2[kWidest];
+  __shared__ float m1[widest(NT)], m2[widest(NT)];
   const float total = (float)m.per * (float)g.positions;
   if (m.blocks_a_group > 1) {
     if (threadIdx.x == 0) m1[0] = cb[0] / total, m2[0] = cw[0] / total;
@@ -802,21 +803,22 @@ __global__ void __launch_bounds__(NT) k_norm_maps_grad(GroupNorm g, Maps m) {
 long long gcd(long long a, long long b) { return b == 0 ? a : gcd(b, a % b); }
 
 // A block: whole groups and whole vectors of eight, so that no thread's channels cross a block's edge more often than at the end; at least 128
-// bytes of a row, more where few positions would leave threads idle; at most 256 vectors.
+// bytes of a row, more where few positions would leave threads idle; at most as many channels as widest() says.
 Maps maps_of(const GroupNorm &g, int threads, int each, int bytes = 128) {
   Maps m = {};
   m.per = (int)(g.channels / g.groups);
   m.blocks_a_group = 1;
-  if (m.per > kWidest) {
-    m.blocks_a_group = (m.per + kWidest - 1) / kWidest;
-    m.width = kWidest;
+  const int most = widest(threads);
+  if (m.per > most) {
+    m.blocks_a_group = (m.per + most - 1) / most;
+    m.width = most;
     m.blocks = m.blocks_a_group * (int)g.groups;
   } else {
     long long unit = m.per / gcd(m.per, 8) * 8;
     if (unit > 512 || unit > g.channels) unit = m.per;
     const long long least = bytes / (g.type == kF32 ? 4 : 2);
     long long w = unit;
-    while (w < g.channels && w + unit <= kWidest && (w < least || (w + 7) / 8 * g.positions < kThreads)) w += unit;
+    while (w < g.channels && w + unit <= most && (w < least || (w + 7) / 8 * g.positions < (threads < kThreads ? threads : kThreads))) w += unit;
     if (w > g.channels) w = g.channels;
     m.width = (int)w;
     m.blocks = (int)((g.channels + w - 1) / w);
@@ -831,6 +833,10 @@ Maps maps_of(const GroupNorm &g, int threads, int each, int bytes = 128) {
 constexpr long long kMostWorkgroups = 0x7fffffff;
 long long workgroups(const GroupNorm &g, const Maps &m) { return (long long)m.blocks * m.chunks * g.samples; }
 bool whole(const GroupNorm &g, const Maps &m) { return m.chunks == 1 && m.blocks_a_group == 1 && workgroups(g, m) <= kMostWorkgroups; }
+
+// Small samples, many of them: a wave each, whose barriers are nothing (65536 samples of 4 positions and 16 channels: 93 us, in
+// workgroups of 256 410; 4096 of 16 and 64: 9.2, 26).
+bool wave_whole(const GroupNorm &g, const Maps &m) { return whole(g, m) && workgroups(g, m) >= 2048; }
 
 // The rows' cut: lanes of a team and eights a lane, or neither: longer.  The gradient keeps two sums for each of its entries: fewer a lane.
 struct Rows {
@@ -870,8 +876,9 @@ template <class F>
 void by_even(const GroupNorm &g, F &&f) {
   bool even = g.channels / g.groups % 8 == 0;
   if (!even && g.positions > 1) {   // small groups side by side in blocks of whole eights
-    const Maps m = maps_of(g, kThreads, 1), narrow = maps_of(g, kThreads, 1, 64);
-    even = m.blocks_a_group == 1 && m.width % 8 == 0 && narrow.width % 8 == 0 && g.channels % 8 == 0;
+    even = g.channels % 8 == 0;
+    for (const Maps &m : {maps_of(g, kThreads, 1), maps_of(g, kThreads, 1, 64), maps_of(g, 64, 1)})
+      even = even && (m.blocks_a_group == 1 ? m.width : m.per) % 8 == 0;
   }
   if (even) f(std::true_type());
   else f(std::false_type());
@@ -898,7 +905,9 @@ hipError_t norm(const GroupNorm &g, hipStream_t s) {
     }
     Maps m;
     const auto grid = [&] { return dim3((unsigned)workgroups(g, m)); };
-    if (m = maps_of(g, 256, 2), whole(g, m)) k_norm_maps<T, 256, 2, kWhole, kEven><<<grid(), 256, 0, s>>>(g, m);
+    if (m = maps_of(g, 64, 2), wave_whole(g, m)) k_norm_maps<T, 64, 2, kWhole, kEven><<<grid(), 64, 0, s>>>(g, m);
+    else if (m = maps_of(g, 64, 8), wave_whole(g, m)) k_norm_maps<T, 64, 8, kWhole, kEven><<<grid(), 64, 0, s>>>(g, m);
+    else if (m = maps_of(g, 256, 2), whole(g, m)) k_norm_maps<T, 256, 2, kWhole, kEven><<<grid(), 256, 0, s>>>(g, m);
     else if (m = maps_of(g, 256, 4), whole(g, m)) k_norm_maps<T, 256, 4, kWhole, kEven><<<grid(), 256, 0, s>>>(g, m);
     else if (m = maps_of(g, 256, 8), whole(g, m)) k_norm_maps<T, 256, 8, kWhole, kEven><<<grid(), 256, 0, s>>>(g, m);
     else if (m = maps_of(g, 1024, 8), whole(g, m)) k_norm_maps<T, 1024, 8, kWhole, kEven><<<grid(), 1024, 0, s>>>(g, m);
@@ -922,7 +931,11 @@ struct GradMaps {
   bool whole;
 };
 GradMaps grad_maps(const GroupNorm &g) {
-  GradMaps q = {maps_of(g, 256, 2), 256, 2, true};
+  GradMaps q = {maps_of(g, 64, 2), 64, 2, true};
+  if (wave_whole(g, q.m)) return q;
+  q = {maps_of(g, 64, 4), 64, 4, true};
+  if (wave_whole(g, q.m)) return q;
+  q = {maps_of(g, 256, 2), 256, 2, true};
   if (whole(g, q.m)) return q;
   q = {maps_of(g, 256, 4), 256, 4, true};
   if (whole(g, q.m)) return q;
@@ -971,6 +984,9 @@ hipError_t norm_grad(const GroupNorm &call, hipStream_t s) {
       if (!q.whole) {
         k_norm_maps_grad<T, 256, 4, kPieces, kEven><<<grid, 256, 0, s>>>(g, q.m);
         k_norm_maps_grad<T, 256, 4, kJoined, kEven><<<grid, 256, 0, s>>>(g, q.m);
+      } else if (q.threads == 64) {
+        if (q.each == 2) k_norm_maps_grad<T, 64, 2, kWhole, kEven><<<grid, 64, 0, s>>>(g, q.m);
+        else k_norm_maps_grad<T, 64, 4, kWhole, kEven><<<grid, 64, 0, s>>>(g, q.m);
       } else if (q.threads == 512) {
         if constexpr (sizeof(T) == 2) k_norm_maps_grad<T, 512, 8, kWhole, kEven><<<grid, 512, 0, s>>>(g, q.m);
       } else if (q.each == 2) {
@@ -999,7 +1015,7 @@ hipError_t norm_grad(const GroupNorm &call, hipStream_t s) {
 size_t group_norm_scratch(const GroupNorm &g, bool gradient) {
   if (g.samples == 0 || g.positions == 0 || g.channels == 0) return 0;
   if (!gradient) {
-    if (g.positions == 1 || whole(g, maps_of(g, 256, 2)) || whole(g, maps_of(g, 256, 8)) || whole(g, maps_of(g, 1024, 8))) return 0;
+    if (g.positions == 1 || wave_whole(g, maps_of(g, 64, 8)) || whole(g, maps_of(g, 256, 8)) || whole(g, maps_of(g, 1024, 8))) return 0;
     return (size_t)(g.samples * g.groups * maps_of(g, 256, 8).pieces_a_group) * 2 * sizeof(float);
   }
   long long count;

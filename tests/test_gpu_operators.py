@@ -251,7 +251,7 @@ def test_a_value_that_is_not_finite_stays_in_its_row_and_column():
 
 NORMS = [(1, 1, 1, 1), (3, 1, 2, 1), (5, 1, 410, 1), (4, 1, 2048, 1), (2, 1, 8192, 1), (3, 1, 16391, 1), (1000, 1, 16, 1), (2, 9, 6, 3), (3, 16, 32, 8), (2, 256, 64, 32),
          (1, 1023, 24, 2), (5, 33, 70, 1), (2, 4, 96, 96), (3, 100, 130, 13), (1, 5000, 8, 1), (7, 64, 512, 16), (2, 1, 64, 8), (2, 1024, 64, 16), (1, 5000, 64, 2),
-         (2, 3, 4100, 1), (1, 40, 5000, 2), (3, 1, 4100, 2), (2, 7, 264, 24), (1, 3000, 26, 2), (9000, 3, 8, 2), (0, 4, 8, 2), (3, 0, 8, 2), (2, 3, 0, 1)]
+         (2, 3, 4100, 1), (1, 40, 5000, 2), (3, 1, 4100, 2), (2, 7, 264, 24), (1, 3000, 26, 2), (9000, 3, 8, 2), (2100, 5, 20, 4), (2048, 9, 24, 3), (2500, 30, 40, 5), (2200, 2, 600, 2), (0, 4, 8, 2), (3, 0, 8, 2), (2, 3, 0, 1)]
 
 
 def norm_inputs(n, s, c, dtype, seed):
