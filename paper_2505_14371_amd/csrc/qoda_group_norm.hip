@@ -835,8 +835,8 @@ long long workgroups(const GroupNorm &g, const Maps &m) { return (long long)m.bl
 bool whole(const GroupNorm &g, const Maps &m) { return m.chunks == 1 && m.blocks_a_group == 1 && workgroups(g, m) <= kMostWorkgroups; }
 
 // Small samples, many of them: a wave each, whose barriers are nothing (65536 samples of 4 positions and 16 channels: 93 us, in
-// workgroups of 256 410; 4096 of 16 and 64: 9.2, 26).
-bool wave_whole(const GroupNorm &g, const Maps &m) { return whole(g, m) && workgroups(g, m) >= 2048; }
+// workgroups of 256 410; 1000 of 16 and 64 6.7, 8.9; 500 of 32 and 64 7.5 either way).
+bool wave_whole(const GroupNorm &g, const Maps &m) { return whole(g, m) && workgroups(g, m) >= 512; }
 
 // The rows' cut: lanes of a team and eights a lane, or neither: longer.  The gradient keeps two sums for each of its entries: fewer a lane.
 struct Rows {

@@ -237,8 +237,13 @@ def linear_weight_grad(dz, x, dweight=None, dbias=None, *, bias=True, accumulate
     if stream is not None:
         with _on(stream):
             return linear_weight_grad(dz, x, dweight, dbias, bias=bias, accumulate=accumulate)
-    if _is_native() and (dbias is not None or not bias):
-        if _looked_at(_native.linear_weight_grad, dz, x, dweight, dbias, accumulate) is not None:
+    if _is_native() and isinstance(dz, torch.Tensor) and isinstance(x, torch.Tensor) and dz.is_cuda and dz.dim() > 0 and x.dim() > 0:
+        if not accumulate:
+            if dweight is None:
+                dweight = torch.empty((dz.shape[-1], x.shape[-1]), dtype=torch.float32, device=dz.device)
+            if dbias is None and bias:
+                dbias = torch.empty(dz.shape[-1], dtype=torch.float32, device=dz.device)
+        if (dbias is not None or not bias) and _looked_at(_native.linear_weight_grad, dz, x, dweight, dbias, accumulate) is not None:
             return dweight, dbias
     dt = _first(dz, "linear_weight_grad: dz")
     if not isinstance(x, torch.Tensor) or x.dim() == 0:
