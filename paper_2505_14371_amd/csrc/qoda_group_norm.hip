@@ -9,7 +9,7 @@
 //          positions are split: one launch for the pieces' sums, one that joins them and makes the result.
 //
 // Measured: rows of 2048, 16384 of them, bf16: forward 25 us (5.3 TB/s), gradient with residual 61 + 7 for the join (4.4 TB/s); a map of 64 x 256 x
-// 256 in fp32 12.8 us, the gradient of 128 x 1024 x 128 in bf16 with silu 50.6 (its slope, taken twice, is 19 us of arithmetic).  Small ones are
+// 256 in fp32 12.5 us, the gradient of 128 x 1024 x 128 in bf16 with silu 50.7 (its slope, taken twice, is 19 us of arithmetic).  Small ones are
 // bound by the launch and by the sums over the workgroup.
 
 #include <type_traits>

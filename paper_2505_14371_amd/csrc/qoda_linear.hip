@@ -12,9 +12,9 @@
 // The matrix instruction's first operand is b's piece: a lane then holds four sums adjacent in a row of c, and b's entries are dealt
 // to the instructions so that those of two instructions are eight adjacent ones: 16 bytes of bf16 to store, and one block of lots.
 //
-// Measured, bf16: 16384 x 8192 x 2048 435 us (1263 TFLOP/s; the library's product 424), with dropout and residual 467; the input
-// gradient of 8192 x 8192 x 2048 through gelu 303, of which 215 to 226 the product, 45 the read of pre and 20 the slope; the weight gradient of
-// 6144 x 2048 over 8192 rows 199.  fp32: 4096 x 2048 x 2048 245 us (140 TFLOP/s).  The matrix cores bound the large ones; the ends of
+// Measured, bf16: 16384 x 8192 x 2048 435 us (1263 TFLOP/s; the library's product 424), with dropout and residual 462; the input
+// gradient of 8192 x 8192 x 2048 through gelu 299, of which 215 to 226 the product, 45 the read of pre and 20 the slope; the weight gradient of
+// 6144 x 2048 over 8192 rows 193.  fp32: 4096 x 2048 x 2048 245 us (140 TFLOP/s).  The matrix cores bound the large ones; the ends of
 // their tiles wait for memory, and a CU holds one such tile, so that nothing else runs meanwhile.  Short sums are bound by a tile's start and end:
 // 3300 x 410 x 2100 17 us for 7 steps.
 
