@@ -7,8 +7,8 @@
  * Conventions
  *   - No context: a call works on the device that is current and enqueues on `stream` (a hipStream_t as void*, NULL = the
  *     default stream) kernels only; it allocates nothing, waits for nothing and may be captured into a graph.  Scratch memory
- *     is the caller's: *_workspace_bytes() says how much a call needs (0 for many), on the call's stream until the call's work is done,
- *     aligned to 16 bytes.  Calls may be made from any number of host threads.
+ *     is the caller's: *_workspace_bytes() says how much a call with these arguments, addresses among them, needs (0 for many), on the
+ *     call's stream until the call's work is done, aligned to 16 bytes.  Calls may be made from any number of host threads.
  *   - Every call returns QODA_OK (0) or a negative error code, and then qoda_operator_error() describes it (the calling
  *     thread's last error).  Arguments are checked before anything is launched; nothing throws across this boundary.
  *   - A matrix is row-major: `data` points at entry (0, 0) in device memory, entries of a row are adjacent, rows are `stride`

@@ -563,7 +563,7 @@ struct Plan {
 constexpr int kCus = 256;
 
 // What a cut would take, in us, from what was measured (3300 x 410 x 832 16 us with splits by the number of tiles alone, 9 without; the fp32 weight gradient
-// of 2100 x 410 over 3300 rows 82 unsplit, 64 in three): the matrix cores' rate in a tile of each size, the time of a step that nothing but
+// of 2100 x 410 over 3300 rows 82 unsplit, 64 in three; 64 x 64 over 100000 rows 47 in 16 parts, 36 in those of the estimate): the matrix cores' rate in a tile of each size, the time of a step that nothing but
 // its loads bounds, of a tile's start and end, and of the launch that joins splits.
 double time_of(const Product &p, int bm, int bn, int a_cu, double rate, long long tiles, int steps, int splits) {
   const int step = kStepBytes / (p.type == kF32 ? 4 : 2), steps_each = (steps + splits - 1) / splits;
@@ -579,7 +579,7 @@ double time_of(const Product &p, int bm, int bn, int a_cu, double rate, long lon
     us += (double)rounds * (2.0 + steps_each * (one > 0.5 ? one : 0.5));
     left -= rounds * now;
   }
-  if (splits > 1) us += 5.0 + (double)splits * p.m * p.n * 8.0 / 4e6;
+  if (splits > 1) us += 5.0 + 0.4 * splits + (double)splits * p.m * p.n * 8.0 / 4e6;
   return us;
 }
 
@@ -606,9 +606,10 @@ Plan plan_of(const Product &p) {
   const int steps = p.k > 0 ? (p.k + step - 1) / step : 1;
   int bm, bn;
   if (p.m <= 32) {
-    // few rows: the other operand is read once, by as many workgroups as fill the device, in parts of at least four steps
+    // few rows: the other operand is read once, by as many workgroups as fill the device, in parts of at least four steps, and not so many that
+    // their join, which adds them one after the other, takes longer than they do
     q.tile = kTile32, bm = 32, bn = 128;
-    const long long want = 4 * kCus / tiles(bm, bn), most = steps / 4;
+    const long long want = 4 * kCus / tiles(bm, bn), most = steps / 4 < 64 ? steps / 4 : 64;
     q.splits = (int)(want < most ? want : most);
     if (q.splits < 2) q.splits = 1;
   } else {
@@ -623,7 +624,7 @@ Plan plan_of(const Product &p) {
     for (const auto &c : cuts) {
       if (c.tile >= kTile192 && !(q.direct && wide)) continue;
       const long long n = tiles(c.bm, c.bn);
-      for (int splits = 1; splits == 1 || (splits <= 16 && splits * 4 <= steps && n * splits <= c.a_cu * kCus && c.tile < kTile192); ++splits) {
+      for (int splits = 1; splits == 1 || (splits <= 64 && splits * 4 <= steps && n * splits <= c.a_cu * kCus && c.tile < kTile192); ++splits) {
         const double us = time_of(p, c.bm, c.bn, c.a_cu, c.rate, n, steps, splits);
         if (least == 0.0 || us < least) least = us, q.tile = c.tile, q.splits = splits, bm = c.bm, bn = c.bn;
       }
