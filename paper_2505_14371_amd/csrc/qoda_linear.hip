@@ -562,9 +562,10 @@ struct Plan {
 
 constexpr int kCus = 256;
 
-// What a cut would take, in us, from what was measured (3300 x 410 x 832 16 us with splits by the number of tiles alone, 9 without; the fp32 weight gradient
-// of 2100 x 410 over 3300 rows 82 unsplit, 64 in three; 64 x 64 over 100000 rows 47 in 16 parts, 36 in those of the estimate): the matrix cores' rate in a tile of each size, the time of a step that nothing but
-// its loads bounds, of a tile's start and end, and of the launch that joins splits.
+// What a cut would take, in us, from what was measured: the matrix cores' rate in a tile of each size, the time of a step that nothing but its
+// loads bounds, of a tile's start and end, and of the launch that joins splits.  (3300 x 410 x 832: 16 us with splits by the number of tiles
+// alone, 9 without; the fp32 weight gradient of 2100 x 410 over 3300 rows 82 unsplit, 64 in three parts; that of 64 x 64 over 100000 rows 47 in 16
+// parts, 36 in as many as this has it take.)
 double time_of(const Product &p, int bm, int bn, int a_cu, double rate, long long tiles, int steps, int splits) {
   const int step = kStepBytes / (p.type == kF32 ? 4 : 2), steps_each = (steps + splits - 1) / splits;
   const double flops = 2.0 * bm * bn * step, whole = rate / kCus;
