@@ -60,18 +60,18 @@ class ResidualBlocks:
     def forward(self, x: torch.Tensor, weights: Sequence[torch.Tensor], draw: int) -> Tuple[torch.Tensor, list]:
         """The blocks' output for rows x [..., width], and what backward() needs.  draw: numbers the call; another one drops others."""
         saved = [draw]
-        h = x
+        h = x.reshape(-1, x.shape[-1])       # rows: the norm would take dimensions in between as positions of one sample
         for i in range(self.depth):
             gamma, beta, _, b1, _, b2 = self.params[PER_BLOCK * i: PER_BLOCK * (i + 1)]
             n, mean, rstd = ops.group_norm(h, self.groups, gamma, beta)
             a, z = ops.linear(n, weights[2 * i], b1, activation=self.activation, keep_pre=True, **self._drop(draw, i, 0))
             saved.append((h, n, mean, rstd, z, a))
             h = ops.linear(a, weights[2 * i + 1], b2, residual=h, **self._drop(draw, i, 1))
-        return h, saved
+        return h.view(x.shape), saved
 
     def backward(self, dy: torch.Tensor, saved: list, weights: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], accumulate: bool = False) -> torch.Tensor:
         """The gradient of x, and those of the parameters into (accumulate: added to) ``grads``."""
-        draw, dh = saved[0], dy
+        draw, dh = saved[0], dy.reshape(-1, dy.shape[-1])
         for i in reversed(range(self.depth)):
             gamma, beta = self.params[PER_BLOCK * i: PER_BLOCK * i + 2]
             g_gamma, g_beta, g_w1, g_b1, g_w2, g_b2 = grads[PER_BLOCK * i: PER_BLOCK * (i + 1)]
@@ -82,4 +82,4 @@ class ResidualBlocks:
             ops.linear_weight_grad(d1, n, g_w1, g_b1, accumulate=accumulate)
             dn = ops.linear_input_grad(d1, weights[2 * i])
             dh, _, _ = ops.group_norm_grad(dn, h, mean, rstd, self.groups, gamma, beta, residual=dh, dweight=g_gamma, dbias=g_beta, accumulate=accumulate)
-        return dh
+        return dh.view(dy.shape)

@@ -71,3 +71,28 @@ def test_refusals():
         ResidualBlocks(10, 20, 1, groups=3)
     with pytest.raises(ValueError):
         ResidualBlocks(10, 20, 1, dtype=torch.float16)
+
+
+@pytest.mark.parametrize("groups", [1, 4])
+def test_dimensions_before_the_width_are_rows(groups):
+    """x of any number of dimensions gives what the same rows give as a matrix, forward and backward."""
+    model = ResidualBlocks(60, 200, 2, groups=groups, p=0.2, dtype=torch.float32, seed=3)
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    x, dy = (torch.randn((2, 5, 7, 60), device="cuda", generator=gen) for _ in range(2))
+    weights = model.weights()
+    for lead in ((2, 5, 7), (14, 5), (70, 1), (1, 70)):
+        grads, flat = model.gradients(), model.gradients()
+        y, saved = model.forward(x.view(*lead, 60), weights, draw=5)
+        dx = model.backward(dy.view(*lead, 60), saved, weights, grads)
+        y2, saved = model.forward(x.view(70, 60), weights, draw=5)
+        dx2 = model.backward(dy.view(70, 60), saved, weights, flat)
+        assert y.shape == dx.shape == (*lead, 60)
+        assert torch.equal(y.view(70, 60), y2) and torch.equal(dx.view(70, 60), dx2)
+        assert all(torch.equal(a, b) for a, b in zip(grads, flat))
+    y, saved = model.forward(x[0, 0, 0], weights, draw=5)
+    dx = model.backward(dy[0, 0, 0], saved, weights, grads)
+    y2, saved = model.forward(x[0, 0, :1], weights, draw=5)
+    assert y.shape == dx.shape == (60,) and torch.equal(y, y2[0])
+    assert torch.equal(dx, model.backward(dy[0, 0, :1], saved, weights, flat)[0])
+    with pytest.raises(ValueError):                       # rows of another width, also where their entries would make up whole rows
+        model.forward(x.view(-1, 30), weights, draw=5)
