@@ -255,7 +255,7 @@ PyObject *group_norm(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
   return answered(args, nargs, 8, [&](int64_t device, void *stream) {
     const First x(args[2], device, 2);
     const int64_t n = x.t.size(0), groups = number<int64_t>(args[3]);
-    if (groups < 1 || n == 0) throw Unknown();
+    if (groups < 1 || x.t.numel() == 0) throw Unknown();
     const int64_t positions = x.rows / n;
     const at::Tensor y = rows_of(x, x.cols), mean = output(x, {n, groups}, at::kFloat), rstd = output(x, {n, groups}, at::kFloat);
     const qoda_group_norm_args a = {x.dtype, (int32_t)number<int64_t>(args[7]), n, positions, x.cols, groups, values(args[2], x), {y.data_ptr(), positions * x.cols, x.cols},

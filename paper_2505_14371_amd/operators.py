@@ -327,7 +327,7 @@ def _shape(x: torch.Tensor, name: str) -> Tuple[int, int, int]:
 
 def group_norm(x, groups, weight=None, bias=None, *, eps=1e-5, activation="none", stream=None):
     """(act(normalised x * weight + bias), mean, rstd) of x [samples, ..., channels]; mean and rstd [samples, groups], fp32, are what the
-    gradient needs.  groups=1 and no position dimensions: the layer normalisation of rows."""
+    gradient needs (NaN where there is no position or channel).  groups=1 and no position dimensions: the layer normalisation of rows."""
     if stream is not None:
         with _on(stream):
             return group_norm(x, groups, weight, bias, eps=eps, activation=activation)
@@ -340,6 +340,9 @@ def group_norm(x, groups, weight=None, bias=None, *, eps=1e-5, activation="none"
     y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
     mean = torch.empty((n, max(groups, 0)), dtype=torch.float32, device=x.device)
     rstd = torch.empty_like(mean)
+    if s * c == 0:          # the library leaves them alone
+        mean.fill_(float("nan"))
+        rstd.fill_(float("nan"))
     _run("group_norm", _NORM.pack(dt, act, n, s, c, groups, *_values(x, x, "group_norm: x"), y.data_ptr(), s * c, c,
                                   _vector(weight, x, "group_norm: weight", c), _vector(bias, x, "group_norm: bias", c),
                                   mean.data_ptr(), rstd.data_ptr(), eps), x.device)
