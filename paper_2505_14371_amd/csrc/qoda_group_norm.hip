@@ -674,34 +674,32 @@ __global__ void __launch_bounds__(NT) k_norm_maps_grad(GroupNorm g, Maps m) {
   groups8(m, at.vec * 8, q);
   const int per = m.blocks_a_group > 1 ? at.width : m.per, groups = at.width / per;
   const long long first = m.blocks_a_group > 1 ? at.block / m.blocks_a_group : at.c0 / m.per;
-  // Per channel, few numbers, since the values take most of the registers: with r = rstd and a = r w, what goes through the activation is
-  // h w + b = x a + (b - mean a), the sum of d h is r times that of d (x - mean), and dx is d a - r m1 - (x - mean) r^2 m2.
-  float mean[8], rstd[8], wr[8], b[8];
+  // What goes through the activation is computed as in the forward pass, operation by operation: an entry is on the same side of a kink in both, and
+  // a mean far from 0 costs nothing (as x (rstd w) + (b - mean rstd w) it would be a difference of large numbers).
+  float mean[8], rstd[8], w[8], b[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     const bool mine = EVEN ? at.own > 0 : j < at.own;
     mean[j] = mine ? g.mean[at.n * g.groups + first + q[j]] : 0.0f;
     rstd[j] = mine ? g.rstd[at.n * g.groups + first + q[j]] : 0.0f;
-    wr[j] = b[j] = 0.0f;
+    w[j] = b[j] = 0.0f;
   }
   if (at.own > 0) {
-    vector8<EVEN>(g.weight ? g.weight + c : nullptr, 1.0f, at.own, wr);
+    vector8<EVEN>(g.weight ? g.weight + c : nullptr, 1.0f, at.own, w);
     vector8<EVEN>(g.bias ? g.bias + c : nullptr, 0.0f, at.own, b);
   }
-#pragma unroll
-  for (int j = 0; j < 8; ++j) wr[j] = wr[j] * rstd[j], b[j] = __builtin_fmaf(-mean[j], wr[j], b[j]);
-  // h: x - mean; d: dy through the activation
+  // h: the normalised values; d: dy through the activation
   const auto back = [&](int u, float (&h)[8], float (&d)[8]) {
     rx[u].get(h);
     rd[u].get(d);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) h[j] = (h[j] - mean[j]) * rstd[j];
     if (g.activation != kActNone) {
       float z[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) z[j] = __builtin_fmaf(h[j], wr[j], b[j]);
+      for (int j = 0; j < 8; ++j) z[j] = __builtin_fmaf(h[j], w[j], b[j]);
       slope8(g.activation, z, d);
     }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) h[j] = h[j] - mean[j];
   };
   if constexpr (PASS != kJoined) {
     float vw[8] = {}, vb[8] = {};
@@ -713,8 +711,6 @@ __global__ void __launch_bounds__(NT) k_norm_maps_grad(GroupNorm g, Maps m) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) vw[j] = __builtin_fmaf(d[j], h[j], vw[j]), vb[j] = vb[j] + d[j];
       }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) vw[j] = vw[j] * rstd[j];
     channel_sums<NT>(m, at, vw, lanes, cw);
     channel_sums<NT>(m, at, vb, lanes, cb);
     float *o = g.scratch + ((at.n * m.chunks + at.chunk) * 2) * g.channels + at.c0;
@@ -779,8 +775,8 @@ __global__ void __launch_bounds__(NT) k_norm_maps_grad(GroupNorm g, Maps m) {
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     const bool mine = EVEN ? at.own > 0 : j < at.own;
-    e1[j] = mine ? rstd[j] * m1[q[j]] : 0.0f;
-    e2[j] = mine ? rstd[j] * rstd[j] * m2[q[j]] : 0.0f;
+    e1[j] = mine ? m1[q[j]] : 0.0f;
+    e2[j] = mine ? m2[q[j]] : 0.0f;
   }
 #pragma unroll
   for (int u = 0; u < U; ++u) {
@@ -791,7 +787,7 @@ __global__ void __launch_bounds__(NT) k_norm_maps_grad(GroupNorm g, Maps m) {
       back(u, h, d);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const float v = __builtin_fmaf(-h[j], e2[j], __builtin_fmaf(d[j], wr[j], -e1[j]));
+        const float v = __builtin_fmaf(-h[j], e2[j], __builtin_fmaf(d[j], w[j], -e1[j])) * rstd[j];
         d[j] = g.extra ? o[j] + v : v;
       }
       store8<EVEN>(static_cast<T *>(g.out) + at.n * g.out_sample + p * g.out_pos + c, at.own, d);
