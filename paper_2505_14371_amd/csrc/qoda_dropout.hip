@@ -58,7 +58,7 @@ __global__ void __launch_bounds__(256) k_entries(Entries e, Divisor blocks) {
       mine[u].get(v);
       if (EXTRA) other[u].get(o);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = !GRAD ? act<ACT>(v[j]) : EXTRA ? v[j] * act_slope<ACT>(o[j]) : v[j];
+      for (int j = 0; j < 8; ++j) v[j] = !GRAD ? act<T, ACT>(v[j]) : EXTRA ? v[j] * act_slope<T, ACT>(o[j]) : v[j];
       if (DROP) drop8(e.drop, (u32)row[u], block[u], v);
       if (!GRAD && EXTRA)
 #pragma unroll

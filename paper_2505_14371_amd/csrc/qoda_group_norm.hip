@@ -81,10 +81,11 @@ __device__ __forceinline__ void vector8(const float *p, float otherwise, int n, 
   }
 }
 
+template <class T>
 __device__ __forceinline__ void act8(int a, float (&v)[8]) {
   const auto all = [&](auto c) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = act<decltype(c)::value>(v[j]);
+    for (int j = 0; j < 8; ++j) v[j] = act<T, decltype(c)::value>(v[j]);
   };
   switch (a) {
     case kActRelu: return all(std::integral_constant<int, kActRelu>());
@@ -95,10 +96,11 @@ __device__ __forceinline__ void act8(int a, float (&v)[8]) {
   }
 }
 // v times the slope at z
+template <class T>
 __device__ __forceinline__ void slope8(int a, const float (&z)[8], float (&v)[8]) {
   const auto all = [&](auto c) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = v[j] * act_slope<decltype(c)::value>(z[j]);
+    for (int j = 0; j < 8; ++j) v[j] = v[j] * act_slope<T, decltype(c)::value>(z[j]);
   };
   switch (a) {
     case kActRelu: return all(std::integral_constant<int, kActRelu>());
@@ -110,18 +112,18 @@ __device__ __forceinline__ void slope8(int a, const float (&z)[8], float (&v)[8]
 }
 
 // Eight normalised values times weight plus bias, through the activation.
-template <bool EVEN = false>
+template <class T, bool EVEN = false>
 __device__ __forceinline__ void normalised8(const GroupNorm &g, long long c, int n, float mean, float rstd, float (&v)[8]) {
   float w[8], b[8];
   vector8<EVEN>(g.weight ? g.weight + c : nullptr, 1.0f, n, w);
   vector8<EVEN>(g.bias ? g.bias + c : nullptr, 0.0f, n, b);
 #pragma unroll
   for (int j = 0; j < 8; ++j) v[j] = __builtin_fmaf((v[j] - mean) * rstd, w[j], b[j]);
-  act8(g.activation, v);
+  act8<T>(g.activation, v);
 }
 
 // h: the normalised values of x; d: dy through the activation; w: the weights.
-template <bool EVEN = false>
+template <class T, bool EVEN = false>
 __device__ __forceinline__ void back8(const GroupNorm &g, long long c, int n, float mean, float rstd, float (&h)[8], float (&d)[8], float (&w)[8]) {
 #pragma unroll
   for (int j = 0; j < 8; ++j) h[j] = (h[j] - mean) * rstd;
@@ -131,7 +133,7 @@ __device__ __forceinline__ void back8(const GroupNorm &g, long long c, int n, fl
     vector8<EVEN>(g.bias ? g.bias + c : nullptr, 0.0f, n, z);
 #pragma unroll
     for (int j = 0; j < 8; ++j) z[j] = __builtin_fmaf(h[j], w[j], z[j]);
-    slope8(g.activation, z, d);
+    slope8<T>(g.activation, z, d);
   }
 }
 
@@ -190,7 +192,7 @@ __global__ void __launch_bounds__(kThreads) k_norm_rows(GroupNorm g) {
     if (n > 0) {
       float e[8];
       raw[v].get(e);
-      normalised8<EVEN>(g, row.c0 + at, n, mean, rstd, e);
+      normalised8<T, EVEN>(g, row.c0 + at, n, mean, rstd, e);
       store8<EVEN>(y + at, n, e);
     }
   }
@@ -226,7 +228,7 @@ __global__ void __launch_bounds__(1024) k_norm_long_rows(GroupNorm g) {
   for (long long at = threadIdx.x * 8; at < len; at += 8192) {
     const int n = clip(len - at);
     load8(x + at, n, e);
-    normalised8(g, row.c0 + at, n, mean, rstd, e);
+    normalised8<T>(g, row.c0 + at, n, mean, rstd, e);
     store8(y + at, n, e);
   }
 }
@@ -265,7 +267,7 @@ __global__ void __launch_bounds__(kThreads) k_norm_rows_grad(GroupNorm g) {
         float h[8], d[8], w[8];
         rx[v].get(h);
         rd[v].get(d);   // 0 beyond the row
-        back8<EVEN>(g, c0 + at, len - at, mean, rstd, h, d, w);
+        back8<T, EVEN>(g, c0 + at, len - at, mean, rstd, h, d, w);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           if (!EVEN && len - at <= j) d[j] = 0.0f, h[j] = 0.0f;
@@ -287,7 +289,7 @@ __global__ void __launch_bounds__(kThreads) k_norm_rows_grad(GroupNorm g) {
           float h[8], d[8], w[8], o[8];
           rx[v].get(h);
           rd[v].get(d);
-          back8<EVEN>(g, c0 + at, len - at, mean, rstd, h, d, w);
+          back8<T, EVEN>(g, c0 + at, len - at, mean, rstd, h, d, w);
           if (g.extra) re[v].get(o);
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
@@ -350,7 +352,7 @@ __global__ void __launch_bounds__(1024) k_norm_long_rows_grad(GroupNorm g) {
     const int n = clip(len - at);
     load8(x + at, n, h);
     load8(dy + at, n, d);
-    back8(g, row.c0 + at, n, mean, rstd, h, d, w);
+    back8<T>(g, row.c0 + at, n, mean, rstd, h, d, w);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const float u = j < n ? d[j] * w[j] : 0.0f;
@@ -363,7 +365,7 @@ __global__ void __launch_bounds__(1024) k_norm_long_rows_grad(GroupNorm g) {
     const int n = clip(len - at);
     load8(x + at, n, h);
     load8(dy + at, n, d);
-    back8(g, row.c0 + at, n, mean, rstd, h, d, w);
+    back8<T>(g, row.c0 + at, n, mean, rstd, h, d, w);
     float o[8] = {};
     if (g.extra) load8(static_cast<const T *>(g.extra) + row.n * g.extra_sample + row.c0 + at, n, o);
 #pragma unroll
@@ -387,7 +389,7 @@ __global__ void __launch_bounds__(kThreads) k_norm_long_channels(GroupNorm g) {
     float h[8], d[8], w[8];
     load8(static_cast<const T *>(g.x) + s * g.x_sample + c, n, h);
     load8(static_cast<const T *>(g.dy) + s * g.dy_sample + c, n, d);
-    back8(g, c, n, g.mean[s * g.groups + gr], g.rstd[s * g.groups + gr], h, d, w);
+    back8<T>(g, c, n, g.mean[s * g.groups + gr], g.rstd[s * g.groups + gr], h, d, w);
 #pragma unroll
     for (int j = 0; j < 8; ++j) sw[j] = __builtin_fmaf(d[j], h[j], sw[j]), sb[j] = sb[j] + d[j];
   }
@@ -647,7 +649,7 @@ __global__ void __launch_bounds__(NT) k_norm_maps(GroupNorm g, Maps m) {
       raw[u].get(e);
 #pragma unroll
       for (int j = 0; j < 8; ++j) e[j] = __builtin_fmaf((e[j] - mean[j]) * rstd[j], w[j], b[j]);
-      act8(g.activation, e);
+      act8<T>(g.activation, e);
       store8<EVEN>(y + (long long)p * g.out_pos, at.own, e);
     }
   }
@@ -698,7 +700,7 @@ __global__ void __launch_bounds__(NT) k_norm_maps_grad(GroupNorm g, Maps m) {
       float z[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) z[j] = __builtin_fmaf(h[j], w[j], b[j]);
-      slope8(g.activation, z, d);
+      slope8<T>(g.activation, z, d);
     }
   };
   if constexpr (PASS != kJoined) {

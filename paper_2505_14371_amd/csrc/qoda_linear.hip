@@ -255,11 +255,11 @@ __device__ __forceinline__ void finish(const Product &p, const Beside<T, FORM, A
       }
       if (p.pre) store8(static_cast<T *>(p.pre) + (long long)i * p.ldp + j, n, c);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) c[e] = act<ACT>(c[e]);
+      for (int e = 0; e < 8; ++e) c[e] = act<T, ACT>(c[e]);
     } else if constexpr (ACT != kActNone) {
       o.pre.get(other);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) c[e] = c[e] * act_slope<ACT>(other[e]);
+      for (int e = 0; e < 8; ++e) c[e] = c[e] * act_slope<T, ACT>(other[e]);
     }
     if (p.drop.threshold) drop8(p.drop, (u32)i, (u32)j >> 3, c);
     if (p.extra) {

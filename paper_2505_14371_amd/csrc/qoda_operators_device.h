@@ -25,40 +25,62 @@ template <> __device__ __forceinline__ bf16 from_float<bf16>(float v) { return b
 constexpr float kSlope = 0.2f;   // of leaky_relu
 constexpr float kLog2E = 1.4426950408889634f;
 
-// The two factors of 1 - Phi(|z|) = erfc(|z| / sqrt 2) / 2 = q e with e = exp(-z^2 / 2): formula 7.1.26 of Abramowitz and Stegun, erfc(x) =
-// (a1 t + ... + a5 t^5) exp(-x^2) with t = 1 / (1 + p x), whose error is at most 1.5e-7 -- that of 1 + erf in fp32.  The exponential is the
-// density's too, so the function and its derivative take one exponential and one reciprocal.  (halves and roots of two are in the constants.)
+// The two factors of 1 - Phi(|z|) = erfc(|z| / sqrt 2) / 2 = q e with e = exp(-z^2 / 2), which is the density's factor too, so that gelu and its slope take
+// one exponential and one reciprocal.  q is a polynomial in t = 1 / (1 + c |z|), fitted here (linear programming over 0 <= |z| <= 14.5), without its constant.
+//   fp32: nine terms, off by 2e-8 of q at most, and corrected to first order for the rounding of t: dq/d|z| = |z| q - 1 / sqrt(2 pi).  gelu and its slope
+//         of normal values are off by 3.5e-8 and 4.0e-8 in the square mean, which is what fp32's erf and exp give.
+//   bf16: seven terms, off by 3e-8 at most and by 4e-5 of q e at most: nothing beside the store's rounding, nor in fp32 sums of many entries.
+template <class T>
 __device__ __forceinline__ void normal_tail(float z, float &q, float &e) {
-  const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3275911f * 0.70710678118654752f, fabsf(z), 1.0f));
   e = __builtin_amdgcn_exp2f(z * z * (-0.5f * kLog2E));
-  q = __builtin_fmaf(0.5f * 1.061405429f, t, 0.5f * -1.453152027f);
-  q = __builtin_fmaf(q, t, 0.5f * 1.421413741f);
-  q = __builtin_fmaf(q, t, 0.5f * -0.284496736f);
-  q = __builtin_fmaf(q, t, 0.5f * 0.254829592f) * t;
+  if constexpr (sizeof(T) == 4) {
+    constexpr float kC = 0.27f;
+    const float a = fminf(fabsf(z), 16.0f), d = __builtin_fmaf(kC, a, 1.0f), t = __builtin_amdgcn_rcpf(d);   // e is 0 from 14.5 on
+    q = __builtin_fmaf(0.028961099684238434f, t, -0.12648585438728333f);
+    q = __builtin_fmaf(q, t, 0.16978614032268524f);
+    q = __builtin_fmaf(q, t, -0.0692107304930687f);
+    q = __builtin_fmaf(q, t, 0.10782559961080551f);
+    q = __builtin_fmaf(q, t, 0.07204962521791458f);
+    q = __builtin_fmaf(q, t, 0.10181060433387756f);
+    q = __builtin_fmaf(q, t, 0.10754287242889404f);
+    q = __builtin_fmaf(q, t, 0.10772065818309784f) * t;
+    const float off = __builtin_fmaf(-d, t, 1.0f) - __builtin_fmaf(kC, a, 1.0f - d) * t;   // by how much of itself t is too small
+    q = __builtin_fmaf(__builtin_fmaf(-a, q, 0.39894228040143268f) * off, d * (1.0f / kC), q);
+  } else {
+    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.34f, fabsf(z), 1.0f));
+    q = __builtin_fmaf(0.04579341039061546f, t, -0.20435094833374023f);
+    q = __builtin_fmaf(q, t, 0.270133376121521f);
+    q = __builtin_fmaf(q, t, -0.03557766228914261f);
+    q = __builtin_fmaf(q, t, 0.15860435366630554f);
+    q = __builtin_fmaf(q, t, 0.12934985756874084f);
+    q = __builtin_fmaf(q, t, 0.13604764640331268f) * t;
+  }
 }
 
-template <int ACT>
+// Of a call whose entries are of type T.
+template <class T, int ACT>
 __device__ __forceinline__ float act(float z) {
   if constexpr (ACT == kActRelu) return z < 0.0f ? 0.0f : z;   // a NaN stays one
   if constexpr (ACT == kActLeakyRelu) return z > 0.0f ? z : kSlope * z;
   if constexpr (ACT == kActGelu) {
     float q, e;
-    normal_tail(z, q, e);
-    return z * (0.5f + copysignf(__builtin_fmaf(-q, e, 0.5f), z));   // Phi - 1/2 is odd
+    normal_tail<T>(z, q, e);
+    return z * (z < 0.0f ? q * e : __builtin_fmaf(-q, e, 1.0f));
   }
   if constexpr (ACT == kActSilu) return z * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2E * z));
   return z;
 }
 
-template <int ACT>
+template <class T, int ACT>
 __device__ __forceinline__ float act_slope(float z) {
   if constexpr (ACT == kActRelu) return z > 0.0f ? 1.0f : 0.0f;
   if constexpr (ACT == kActLeakyRelu) return z > 0.0f ? 1.0f : kSlope;
   if constexpr (ACT == kActGelu) {
     float q, e;
-    normal_tail(z, q, e);
-    // Phi - 1/2 + z phi is odd: 1/2 - q e + |z| e / sqrt(2 pi) on the right
-    return 0.5f + copysignf(__builtin_fmaf(e, __builtin_fmaf(fabsf(z), 0.39894228040143268f, -q), 0.5f), z);
+    normal_tail<T>(z, q, e);
+    // Phi + z phi: on the left q e - |z| e / sqrt(2 pi), on the right one less what it is at -z
+    const float w = __builtin_fmaf(-0.39894228040143268f, fabsf(z), q);
+    return z < 0.0f ? w * e : __builtin_fmaf(-w, e, 1.0f);
   }
   if constexpr (ACT == kActSilu) {
     const float s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2E * z));
