@@ -2,6 +2,7 @@
 // small model that was most of the host's time (four lists of 17 tensors: 20 us in Python, under 2 here).  The operators' arguments: a call
 // on small tensors took the host 9 to 13 us in Python, and the device 5.  A module of the interpreter, not part of libqoda's C ABI.
 #include <ATen/ops/empty.h>
+#include <c10/core/GradMode.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "../../include/qoda_operators.h"
@@ -87,6 +88,16 @@ const at::Tensor &tensor(PyObject *o) {
   const at::Tensor *t = plain_tensor(o);
   if (!t || !t->defined()) throw Unknown();
   return *t;
+}
+
+// Tensors that torch is to differentiate by: for the caller's own code, which answers with what says that nothing is recorded.
+void not_followed(std::initializer_list<PyObject *> inputs) {
+  const bool recording = c10::GradMode::is_enabled();
+  for (PyObject *o : inputs) {
+    if (o == Py_None) continue;
+    const at::Tensor &t = tensor(o);
+    if ((recording && t.requires_grad()) || t._fw_grad(0).defined()) throw Unknown();
+  }
 }
 
 // A call's first tensor: its rows and columns, type and device are the call's.
@@ -192,6 +203,7 @@ PyObject *outcome(int rc, std::initializer_list<at::Tensor> outputs) {
 // (device, stream, x, weight, bias, residual, activation, p, seed, offset, keep_pre)
 PyObject *linear(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
   return answered(args, nargs, 11, [&](int64_t device, void *stream) {
+    not_followed({args[2], args[3], args[4], args[5]});
     const First x(args[2], device, 1);
     const at::Tensor &w = tensor(args[3]);
     if (w.dim() != 2) throw Unknown();
@@ -241,6 +253,7 @@ PyObject *linear_weight_grad(PyObject *, PyObject *const *args, Py_ssize_t nargs
 // (device, stream, x, extra, activation, p, seed, offset, gradient)
 PyObject *entries(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
   return answered(args, nargs, 9, [&](int64_t device, void *stream) {
+    if (!truth(args[8])) not_followed({args[2], args[3]});
     const First x(args[2], device, 1);
     qoda_dropout_args a = {x.dtype, (int32_t)number<int64_t>(args[4]), x.rows, x.cols, matrix(args[2], x, x.rows, x.cols), matrix(args[3], x, x.rows, x.cols), {},
                            number<double>(args[5]), number<uint64_t>(args[6]), number<uint64_t>(args[7])};
@@ -253,6 +266,7 @@ PyObject *entries(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
 // (device, stream, x, groups, weight, bias, eps, activation)
 PyObject *group_norm(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
   return answered(args, nargs, 8, [&](int64_t device, void *stream) {
+    not_followed({args[2], args[4], args[5]});
     const First x(args[2], device, 2);
     const int64_t n = x.t.size(0), groups = number<int64_t>(args[3]);
     if (groups < 1 || x.t.numel() == 0) throw Unknown();

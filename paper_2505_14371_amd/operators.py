@@ -15,6 +15,10 @@ Matrices are tensors of fp32 or bfloat16 whose last dimension is adjacent; the d
 statistics and gradients of parameters are fp32.  ``activation``: "none", "relu", "leaky_relu" (slope 0.2), "gelu" or "silu".
 Dropout keeps entry (r, c) by a draw that (seed, offset, r, c) fixes, so that a gradient call with the same p, seed and offset
 has the forward call's mask; two calls whose masks are to differ have different offsets.
+
+Each operator has its gradient as a call of its own, and nothing is recorded for torch's differentiation.  Outputs of ``linear``, ``dropout``
+and ``group_norm`` on tensors that require a gradient, outside ``torch.no_grad()``, require one too, and raise where it is asked for; tangents
+are refused.  What the gradient calls return is plain.
 """
 from __future__ import annotations
 
@@ -187,6 +191,31 @@ def _word(v: int, name: str) -> int:
     return v
 
 
+class _NotRecorded(torch.autograd.Function):
+    """A call's outputs, which raise where torch would differentiate them."""
+
+    @staticmethod
+    def forward(ctx, said, call, *inputs):
+        ctx.said = said
+        return call()
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise RuntimeError(ctx.said)
+
+
+def _unless_followed(name: str, gradient: str, inputs, call):
+    """The outputs of ``call`` if torch is to differentiate by one of its inputs, otherwise None."""
+    inputs = [t for t in inputs if isinstance(t, torch.Tensor)]
+    said = f"{name} records nothing for torch's differentiation: its gradient is {gradient}"
+    level = torch.autograd.forward_ad
+    if level._current_level >= 0 and any(level.unpack_dual(t).tangent is not None for t in inputs):
+        raise RuntimeError(said)
+    if torch.is_grad_enabled() and any(t.requires_grad for t in inputs):
+        return _NotRecorded.apply(said, call, *inputs)
+    return None
+
+
 def linear(x, weight, bias=None, residual=None, *, activation="none", p=0.0, seed=0, offset=0, keep_pre=False, stream=None):
     """residual + drop(act(x weight^T + bias)); with keep_pre also x weight^T + bias, for the gradient of an activation.
     x [..., in], weight [out, in], bias fp32 [out], residual [..., out]."""
@@ -197,6 +226,10 @@ def linear(x, weight, bias=None, residual=None, *, activation="none", p=0.0, see
         out = _looked_at(_native.linear, x, weight, bias, residual, ACTIVATIONS.get(activation), p, seed, offset, keep_pre)
         if out is not None:
             return out
+    out = _unless_followed("linear", "linear_input_grad and linear_weight_grad", (x, weight, bias, residual), lambda: linear(
+        x, weight, bias, residual, activation=activation, p=p, seed=seed, offset=offset, keep_pre=keep_pre))
+    if out is not None:
+        return out
     dt, act = _first(x, "linear: x"), _activation(activation)
     if not isinstance(weight, torch.Tensor) or weight.dim() != 2:
         raise ValueError("linear: weight has to be a matrix")
@@ -281,6 +314,9 @@ def dropout(x, p, seed, offset, *, activation="none", residual=None, stream=None
         out = _looked_at(_native.entries, x, residual, ACTIVATIONS.get(activation), p, seed, offset, False)
         if out is not None:
             return out
+    out = _unless_followed("dropout", "dropout_grad", (x, residual), lambda: dropout(x, p, seed, offset, activation=activation, residual=residual))
+    if out is not None:
+        return out
     return _entries("dropout: x", _load().qoda_dropout, x, residual, "dropout: residual", activation, p, seed, offset)
 
 
@@ -335,6 +371,9 @@ def group_norm(x, groups, weight=None, bias=None, *, eps=1e-5, activation="none"
         out = _looked_at(_native.group_norm, x, groups, weight, bias, eps, ACTIVATIONS.get(activation))
         if out is not None:
             return out
+    out = _unless_followed("group_norm", "group_norm_grad", (x, weight, bias), lambda: group_norm(x, groups, weight, bias, eps=eps, activation=activation))
+    if out is not None:
+        return out
     dt, act = _first(x, "group_norm: x"), _activation(activation)
     n, s, c = _shape(x, "group_norm: x")
     y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
