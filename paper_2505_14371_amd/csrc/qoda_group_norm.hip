@@ -399,12 +399,14 @@ __global__ void __launch_bounds__(kThreads) k_norm_long_channels(GroupNorm g) {
 }
 
 // dweight and dbias from `count` rows of partial sums [2][channels]: 16 columns a workgroup, its 64 teams of 16 lanes take rows in turn.  With `to`: the
-// sums of gridDim.y parts of the rows, a row each, which another launch joins.
-__global__ void __launch_bounds__(1024) k_norm_join(GroupNorm g, const float *part, long long count, float *to) {
+// sums of parts of `each` rows, a row a part.  A part's workgroups are adjacent.
+__global__ void __launch_bounds__(1024) k_norm_join(GroupNorm g, const float *part, long long count, long long each, float *to) {
   __shared__ float red[64][16 + 1];
   const int lane = threadIdx.x & 15, team = threadIdx.x / 16;
-  const long long c = (long long)blockIdx.x * 16 + lane, total = 2 * g.channels;
-  const long long each = (count + gridDim.y - 1) / gridDim.y, first = blockIdx.y * each, end = first + each < count ? first + each : count;
+  const long long total = 2 * g.channels;
+  const u32 columns = (u32)((total + 15) / 16), y = blockIdx.x / columns, x = blockIdx.x - y * columns;
+  const long long c = (long long)x * 16 + lane;
+  const long long first = y * each, end = first + each < count ? first + each : count;
   float s = 0.0f;
   if (c < total) {
     long long r = first + team;
@@ -421,10 +423,10 @@ __global__ void __launch_bounds__(1024) k_norm_join(GroupNorm g, const float *pa
   __syncthreads();
   const int column = threadIdx.x / 64;   // a wave adds up a column's
   s = lanes_sum<64>(red[threadIdx.x & 63][column]);
-  const long long o = (long long)blockIdx.x * 16 + column;
+  const long long o = (long long)x * 16 + column;
   if ((threadIdx.x & 63) == 0 && o < total) {
     if (to) {
-      to[blockIdx.y * total + o] = s;
+      to[y * total + o] = s;
       return;
     }
     float *out = o < g.channels ? g.dweight : g.dbias;
@@ -444,6 +446,7 @@ struct Maps {
   int rows;              // positions at a time
   int chunk, chunks;     // positions of a piece, pieces
   int pieces_a_group;    // chunks, times blocks_a_group
+  bool apart;            // the pieces' sums are joined by a launch of their own, not by each workgroup that needs them
 };
 
 // What a workgroup works on, and its thread's channels.
@@ -544,8 +547,44 @@ __device__ __forceinline__ void groups8(const Maps &m, int c, int (&q)[8]) {
 
 enum MapsPass { kWhole = 0, kPieces = 1, kJoined = 2 };
 
+// Up to so many pieces of a sample (gradient) or of a group (forward) are joined by each workgroup that needs them, which saves a launch; more are joined
+// once, so that a map's time grows with its size and not with its square.  Gradient of bf16, joined by each and once: 32 pieces (2 x 4096 x 64) 16.3 and
+// 18.4 us, 64 (57 x 4096 x 128 in one group) 86 and 69, 512 (8 x 65536 x 128) 416 and 152.  Forward, 256 pieces (8 x 65536 x 128): 104 and 79 us.
+constexpr int kTogether = 32, kTogetherForward = 128;
+
+// The values of a piece: `per` channels, or a block's share of them, at `chunk` positions, or what is left.
+__device__ __forceinline__ float piece_values(const GroupNorm &g, const Maps &m, int piece) {
+  const int in = m.blocks_a_group > 1 ? piece % m.blocks_a_group : 0, ch = m.blocks_a_group > 1 ? piece / m.blocks_a_group : piece;
+  const int w = m.blocks_a_group > 1 ? (m.per - in * m.width < m.width ? m.per - in * m.width : m.width) : m.per;
+  const int p = g.positions - (long long)ch * m.chunk < m.chunk ? (int)(g.positions - (long long)ch * m.chunk) : m.chunk;
+  return (float)w * (float)p;
+}
+// Mean and 1 / sqrt(variance + eps) of a group from its pieces' means and squares (Chan et al.: squares about the common mean), by a team of lanes, the
+// same in each.
+template <int TEAM>
+__device__ __forceinline__ void join_pieces(const GroupNorm &g, const Maps &m, const float *s, float &mean, float &rstd) {
+  __shared__ float red[2][TEAM > 64 ? TEAM / 64 : 1];
+  const float total = (float)m.per * (float)g.positions;
+  const int lane = threadIdx.x % TEAM;
+  mean = 0.0f;
+  for (int i = lane; i < m.pieces_a_group; i += TEAM) mean = __builtin_fmaf(s[2ll * i], piece_values(g, m, i) / total, mean);
+  mean = team_sum<TEAM>(mean, red[0]);
+  float sq = 0.0f;
+  for (int i = lane; i < m.pieces_a_group; i += TEAM) {
+    const float d = s[2ll * i] - mean;
+    sq = sq + __builtin_fmaf(d * d, piece_values(g, m, i), s[2ll * i + 1]);
+  }
+  rstd = 1.0f / sqrtf(team_sum<TEAM>(sq, red[1]) / total + g.eps);
+}
+// A workgroup a group: its pieces are read once, where each workgroup that makes a piece's result would read all of them.
+__global__ void __launch_bounds__(1024) k_norm_maps_join(GroupNorm g, Maps m) {
+  float mean, rstd;
+  join_pieces<1024>(g, m, g.scratch + (long long)blockIdx.x * m.pieces_a_group * 2, mean, rstd);
+  if (threadIdx.x == 0) g.mean[blockIdx.x] = mean, g.rstd[blockIdx.x] = rstd;
+}
+
 // kWhole: a block's values are in registers from the mean to the result.  kPieces: mean and squares of a piece, per group, to
-// scratch[n][group][piece][2].  kJoined: those of the group's pieces joined (Chan et al.: squares about the common mean), and the result.
+// scratch[n][group][piece][2].  kJoined: those of the group's pieces joined, where k_norm_maps_join has not done that, and the result.
 template <class T, int NT, int U, int PASS, bool EVEN>
 __global__ void __launch_bounds__(NT) k_norm_maps(GroupNorm g, Maps m) {
   __shared__ float lanes[PASS == kJoined ? 1 : NT * 8];
@@ -605,30 +644,16 @@ __global__ void __launch_bounds__(NT) k_norm_maps(GroupNorm g, Maps m) {
     }
     for (int k = threadIdx.x; k < groups; k += NT) rstds[k] = 1.0f / sqrtf(rstds[k] / count + g.eps);
   } else {
-    // the pieces' values: `per` channels, or a block's share of them, at `chunk` positions, or what is left
-    const auto values = [&](int piece) {
-      const int in = m.blocks_a_group > 1 ? piece % m.blocks_a_group : 0, ch = m.blocks_a_group > 1 ? piece / m.blocks_a_group : piece;
-      const int w = m.blocks_a_group > 1 ? (m.per - in * m.width < m.width ? m.per - in * m.width : m.width) : m.per;
-      const int p = g.positions - ch * m.chunk < m.chunk ? (int)(g.positions - ch * m.chunk) : m.chunk;
-      return (float)w * (float)p;
-    };
-    const float total = (float)m.per * (float)g.positions;
     for (int k = threadIdx.x / 64; k < groups; k += NT / 64) {   // a wave a group
-      const float *s = g.scratch + (at.n * g.groups + first + k) * m.pieces_a_group * 2;
-      float mean = 0.0f;
-      for (int i = threadIdx.x & 63; i < m.pieces_a_group; i += 64) mean = __builtin_fmaf(s[2 * i], values(i) / total, mean);
-      mean = lanes_sum<64>(mean);
-      float sq = 0.0f;
-      for (int i = threadIdx.x & 63; i < m.pieces_a_group; i += 64) {
-        const float d = s[2 * i] - mean;
-        sq = sq + __builtin_fmaf(d * d, values(i), s[2 * i + 1]);
-      }
-      sq = lanes_sum<64>(sq);
-      if ((threadIdx.x & 63) == 0) means[k] = mean, rstds[k] = 1.0f / sqrtf(sq / total + g.eps);
+      const long long r = at.n * g.groups + first + k;
+      float mean, rstd;
+      if (m.apart) mean = g.mean[r], rstd = g.rstd[r];
+      else join_pieces<64>(g, m, g.scratch + r * m.pieces_a_group * 2, mean, rstd);
+      if ((threadIdx.x & 63) == 0) means[k] = mean, rstds[k] = rstd;
     }
   }
   __syncthreads();
-  if (at.chunk == 0 && (m.blocks_a_group == 1 || at.block % m.blocks_a_group == 0))
+  if (!(PASS == kJoined && m.apart) && at.chunk == 0 && (m.blocks_a_group == 1 || at.block % m.blocks_a_group == 0))
     for (int k = threadIdx.x; k < groups; k += NT) {
       g.mean[at.n * g.groups + first + k] = means[k];
       g.rstd[at.n * g.groups + first + k] = rstds[k];
@@ -655,10 +680,27 @@ __global__ void __launch_bounds__(NT) k_norm_maps(GroupNorm g, Maps m) {
   }
 }
 
+// What dx needs of groups wider than a block: the sums of a sample's channels, [n][2][channels], weighted and summed over each of its groups, to
+// out[n][group][2].  A workgroup a group.
+__global__ void __launch_bounds__(1024) k_norm_group_sums(GroupNorm g, const float *sums, float2 *out) {
+  __shared__ float2 red[16];
+  const long long n = blockIdx.x / (u32)g.groups, c0 = (blockIdx.x - n * g.groups) * (g.channels / g.groups), end = c0 + g.channels / g.groups;
+  const float *s = sums + n * 2 * g.channels;
+  float s1 = 0.0f, s2 = 0.0f;
+  for (long long c = c0 + threadIdx.x; c < end; c += 1024) {
+    const float w = g.weight ? g.weight[c] : 1.0f;
+    s2 = __builtin_fmaf(s[c], w, s2);
+    s1 = __builtin_fmaf(s[g.channels + c], w, s1);
+  }
+  team_sums<1024>(s1, s2, red);
+  if (threadIdx.x == 0) out[blockIdx.x] = {s1, s2};
+}
+
 // The gradient.  Per channel of a piece: the sums of d (dy through the activation) and of d h, to scratch[n][chunk][2][channels];
-// from them come dweight and dbias, and, weighted and summed over a group, what dx needs.
+// from them come dweight and dbias, and, weighted and summed over a group, what dx needs.  kJoined: they come from `sums`, [n][2][channels] where
+// the chunks have been joined (m.apart) and as kPieces left them otherwise, or, for groups wider than a block, from `of_groups`.
 template <class T, int NT, int U, int PASS, bool EVEN>
-__global__ void __launch_bounds__(NT) k_norm_maps_grad(GroupNorm g, Maps m) {
+__global__ void __launch_bounds__(NT) k_norm_maps_grad(GroupNorm g, Maps m, const float *sums, const float2 *of_groups) {
   __shared__ float lanes[PASS == kJoined ? 1 : NT * 8];
   __shared__ float cw[widest(NT)], cb[widest(NT)];   // per channel: the sums of d h and of d
   const Place<NT> at(g, m);
@@ -719,37 +761,26 @@ __global__ void __launch_bounds__(NT) k_norm_maps_grad(GroupNorm g, Maps m) {
     for (int k = threadIdx.x; k < at.width; k += NT) o[k] = cw[k], o[g.channels + k] = cb[k];
     if constexpr (PASS == kPieces) return;
   } else {
-    // over all of the group, which may be wider than the block
-    const long long from = m.blocks_a_group > 1 ? first * m.per : at.c0;
-    const int width = m.blocks_a_group > 1 ? m.per : at.width;
-    if (m.blocks_a_group > 1) {   // one group: sums over its channels, kept in one place
-      float s1 = 0.0f, s2 = 0.0f;
-      for (int k = threadIdx.x; k < width; k += NT) {
-        const float wk = g.weight ? g.weight[from + k] : 1.0f;
-        for (int ch = 0; ch < m.chunks; ++ch) {
-          const float *s = g.scratch + ((at.n * m.chunks + ch) * 2) * g.channels + from + k;
-          s2 = __builtin_fmaf(s[0], wk, s2);
-          s1 = __builtin_fmaf(s[g.channels], wk, s1);
-        }
+    if (m.blocks_a_group > 1) {
+      if (threadIdx.x == 0) {
+        const float2 of = of_groups[at.n * g.groups + first];
+        cb[0] = of.x, cw[0] = of.y;
       }
-      __shared__ float red[2][NT / 64];
-      s1 = team_sum<NT>(s1, red[0]);
-      s2 = team_sum<NT>(s2, red[1]);
-      if (threadIdx.x == 0) cb[0] = s1, cw[0] = s2;
     } else {
-      for (int k = threadIdx.x; k < width; k += NT) {
-        const float *s = g.scratch + at.n * m.chunks * 2 * g.channels + from + k;
+      const int parts = m.apart ? 1 : m.chunks;
+      for (int k = threadIdx.x; k < at.width; k += NT) {
+        const float *s = sums + at.n * parts * 2 * g.channels + at.c0 + k;
         float s1 = 0.0f, s2 = 0.0f;
-        for (int ch = 0; ch < m.chunks; ch += 8) {   // eight on their way
+        for (int ch = 0; ch < parts; ch += 8) {   // eight on their way
           float v1[8], v2[8];
 #pragma unroll
           for (int u = 0; u < 8; ++u) {
-            const float *p = s + (long long)(ch + u < m.chunks ? ch + u : m.chunks - 1) * 2 * g.channels;
+            const float *p = s + (long long)(ch + u < parts ? ch + u : parts - 1) * 2 * g.channels;
             v2[u] = p[0], v1[u] = p[g.channels];
           }
 #pragma unroll
           for (int u = 0; u < 8; ++u)
-            if (ch + u < m.chunks) s2 = s2 + v2[u], s1 = s1 + v1[u];
+            if (ch + u < parts) s2 = s2 + v2[u], s1 = s1 + v1[u];
         }
         cw[k] = s2, cb[k] = s1;
       }
@@ -915,7 +946,9 @@ hipError_t norm(const GroupNorm &g, hipStream_t s) {
         rc = hipErrorInvalidValue;
         return;
       }
+      m.apart = m.pieces_a_group > kTogetherForward;
       k_norm_maps<T, 256, 8, kPieces, kEven><<<grid(), 256, 0, s>>>(g, m);
+      if (m.apart) k_norm_maps_join<<<dim3((unsigned)(g.samples * g.groups)), 1024, 0, s>>>(g, m);
       k_norm_maps<T, 256, 8, kJoined, kEven><<<grid(), 256, 0, s>>>(g, m);
     }
   });
@@ -941,14 +974,24 @@ GradMaps grad_maps(const GroupNorm &g) {
     q = {maps_of(g, 512, 8, 64), 512, 8, true};
     if (whole(g, q.m)) return q;
   }
-  return {maps_of(g, 256, 4), 256, 4, false};
+  q = {maps_of(g, 256, 4), 256, 4, false};
+  q.m.apart = q.m.chunks > kTogether || q.m.blocks_a_group > 1;
+  return q;
+}
+// Rows of partial sums that dweight and dbias are made of.
+long long rows_of_sums(const GroupNorm &g, const Maps &m) { return g.samples * (m.apart ? 1 : m.chunks); }
+// ... and floats in front of them: those of the pieces that they are joined from, and the groups' sums.
+long long before_sums(const GroupNorm &g, const Maps &m) {
+  return !m.apart ? 0 : g.samples * 2 * (m.chunks * g.channels + (m.blocks_a_group > 1 ? g.groups : 0));
 }
 
 template <class T>
 hipError_t norm_grad(const GroupNorm &call, hipStream_t s) {
   GroupNorm g = call;
   const bool sums = g.dweight || g.dbias;
-  long long count = 0;   // rows of partial sums
+  long long count = 0;   // rows of partial sums, from part on
+  float *part = g.scratch;
+  const unsigned columns = (unsigned)((2 * g.channels + 15) / 16);
   hipError_t rc = hipSuccess;
   by_even(g, [&](auto even) {
     constexpr bool kEven = decltype(even)::value;
@@ -978,31 +1021,39 @@ hipError_t norm_grad(const GroupNorm &call, hipStream_t s) {
         return;
       }
       const dim3 grid((unsigned)workgroups(g, q.m));
-      count = g.samples * q.m.chunks;
+      count = rows_of_sums(g, q.m);
+      part = g.scratch + before_sums(g, q.m);
       if (!q.whole) {
-        k_norm_maps_grad<T, 256, 4, kPieces, kEven><<<grid, 256, 0, s>>>(g, q.m);
-        k_norm_maps_grad<T, 256, 4, kJoined, kEven><<<grid, 256, 0, s>>>(g, q.m);
+        k_norm_maps_grad<T, 256, 4, kPieces, kEven><<<grid, 256, 0, s>>>(g, q.m, nullptr, nullptr);
+        float2 *of_groups = nullptr;
+        if (q.m.apart) {
+          k_norm_join<<<dim3(columns * (unsigned)g.samples), 1024, 0, s>>>(g, g.scratch, g.samples * q.m.chunks, q.m.chunks, part);
+          if (q.m.blocks_a_group > 1) {
+            of_groups = reinterpret_cast<float2 *>(g.scratch + g.samples * 2 * q.m.chunks * g.channels);
+            k_norm_group_sums<<<dim3((unsigned)(g.samples * g.groups)), 1024, 0, s>>>(g, part, of_groups);
+          }
+        }
+        k_norm_maps_grad<T, 256, 4, kJoined, kEven><<<grid, 256, 0, s>>>(g, q.m, part, of_groups);
       } else if (q.threads == 64) {
-        if (q.each == 2) k_norm_maps_grad<T, 64, 2, kWhole, kEven><<<grid, 64, 0, s>>>(g, q.m);
-        else k_norm_maps_grad<T, 64, 4, kWhole, kEven><<<grid, 64, 0, s>>>(g, q.m);
+        if (q.each == 2) k_norm_maps_grad<T, 64, 2, kWhole, kEven><<<grid, 64, 0, s>>>(g, q.m, nullptr, nullptr);
+        else k_norm_maps_grad<T, 64, 4, kWhole, kEven><<<grid, 64, 0, s>>>(g, q.m, nullptr, nullptr);
       } else if (q.threads == 512) {
-        if constexpr (sizeof(T) == 2) k_norm_maps_grad<T, 512, 8, kWhole, kEven><<<grid, 512, 0, s>>>(g, q.m);
+        if constexpr (sizeof(T) == 2) k_norm_maps_grad<T, 512, 8, kWhole, kEven><<<grid, 512, 0, s>>>(g, q.m, nullptr, nullptr);
       } else if (q.each == 2) {
-        k_norm_maps_grad<T, 256, 2, kWhole, kEven><<<grid, 256, 0, s>>>(g, q.m);
+        k_norm_maps_grad<T, 256, 2, kWhole, kEven><<<grid, 256, 0, s>>>(g, q.m, nullptr, nullptr);
       } else {
-        k_norm_maps_grad<T, 256, 4, kWhole, kEven><<<grid, 256, 0, s>>>(g, q.m);
+        k_norm_maps_grad<T, 256, 4, kWhole, kEven><<<grid, 256, 0, s>>>(g, q.m, nullptr, nullptr);
       }
     }
   });
   if (rc != hipSuccess) return rc;
   if (sums) {
-    const unsigned columns = (unsigned)((2 * g.channels + 15) / 16);
     if (const long long parts = join_parts(count); parts > 1) {
-      float *to = g.scratch + count * 2 * g.channels;
-      k_norm_join<<<dim3(columns, (unsigned)parts), 1024, 0, s>>>(g, g.scratch, count, to);
-      k_norm_join<<<dim3(columns), 1024, 0, s>>>(g, to, parts, nullptr);
+      float *to = part + count * 2 * g.channels;
+      k_norm_join<<<dim3(columns * (unsigned)parts), 1024, 0, s>>>(g, part, count, (count + parts - 1) / parts, to);
+      k_norm_join<<<dim3(columns), 1024, 0, s>>>(g, to, parts, parts, nullptr);
     } else {
-      k_norm_join<<<dim3(columns), 1024, 0, s>>>(g, g.scratch, count, nullptr);
+      k_norm_join<<<dim3(columns), 1024, 0, s>>>(g, part, count, count, nullptr);
     }
   }
   return hipGetLastError();
@@ -1016,16 +1067,17 @@ size_t group_norm_scratch(const GroupNorm &g, bool gradient) {
     if (g.positions == 1 || wave_whole(g, maps_of(g, 64, 8)) || whole(g, maps_of(g, 256, 8)) || whole(g, maps_of(g, 1024, 8))) return 0;
     return (size_t)(g.samples * g.groups * maps_of(g, 256, 8).pieces_a_group) * 2 * sizeof(float);
   }
-  long long count;
+  long long count, before = 0;
   if (g.positions == 1) {
     if (!g.dweight && !g.dbias) return 0;
     const Rows r = rows_of(g, true);
     count = r.team == 0 ? (g.samples < kLongSplits ? g.samples : kLongSplits) : rows_workgroups(g, r);
   } else {
-    count = g.samples * grad_maps(g).m.chunks;
+    const Maps m = grad_maps(g).m;
+    count = rows_of_sums(g, m), before = before_sums(g, m);
   }
   const long long parts = join_parts(count);
-  return (size_t)((count + (parts > 1 ? parts : 0)) * 2 * g.channels) * sizeof(float);
+  return (size_t)(before + (count + (parts > 1 ? parts : 0)) * 2 * g.channels) * sizeof(float);
 }
 
 hipError_t launch_group_norm(const GroupNorm &g, hipStream_t s) { return g.type == kF32 ? norm<float>(g, s) : norm<bf16>(g, s); }
