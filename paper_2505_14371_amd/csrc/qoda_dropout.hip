@@ -32,7 +32,7 @@ constexpr int kEach = 4;   // blocks of eight entries a thread: so many loads on
 template <class T, int ACT, bool GRAD, bool EXTRA, bool DROP, bool EVEN>
 __global__ void __launch_bounds__(256) k_entries(Entries e, Divisor blocks) {
   // the workgroup's first block by a 64-bit division, the others from it in 32 bits
-  const long long total = e.rows * blocks.d, q0 = (long long)blockIdx.x * (256 * kEach);
+  const long long total = e.rows * blocks.d, q0 = (e.first + blockIdx.x) * (256 * kEach);
   const long long row0 = q0 / blocks.d;
   const u32 col0 = (u32)(q0 - row0 * blocks.d);
   const T *x = static_cast<const T *>(e.x), *extra = static_cast<const T *>(e.extra);
@@ -100,9 +100,10 @@ void launch(const Entries &e, unsigned grid, const Divisor &d, hipStream_t s) {
 hipError_t launch_entries(const Entries &e, hipStream_t s) {
   const u32 blocks = (u32)((e.cols + 7) / 8);
   const long long groups = (e.rows * blocks + 256 * kEach - 1) / (256 * kEach);
-  if (groups > 0x7fffffffll) return hipErrorInvalidValue;
-  if (e.type == kF32) launch<float>(e, (unsigned)groups, divisor(blocks), s);
-  else launch<bf16>(e, (unsigned)groups, divisor(blocks), s);
+  in_launches(e, groups, 256, [&](const Entries &part, unsigned grid) {
+    if (e.type == kF32) launch<float>(part, grid, divisor(blocks), s);
+    else launch<bf16>(part, grid, divisor(blocks), s);
+  });
   return hipGetLastError();
 }
 

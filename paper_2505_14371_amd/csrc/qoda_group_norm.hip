@@ -154,7 +154,7 @@ __global__ void __launch_bounds__(kThreads) k_norm_rows(GroupNorm g) {
   const int lane = threadIdx.x % TEAM;
   const int len = (int)(g.channels / g.groups);
   const long long rows = g.samples * g.groups;
-  long long r = (long long)blockIdx.x * (kThreads / TEAM) + threadIdx.x / TEAM;
+  long long r = (g.first + blockIdx.x) * (kThreads / TEAM) + threadIdx.x / TEAM;
   const bool real = r < rows;
   if (!real) r = rows - 1;   // a team without a row goes along with the last one's, and stores nothing
   const Row row(g, r, len);
@@ -202,7 +202,7 @@ __global__ void __launch_bounds__(kThreads) k_norm_rows(GroupNorm g) {
 template <class T>
 __global__ void __launch_bounds__(1024) k_norm_long_rows(GroupNorm g) {
   __shared__ float red[2][16];
-  const long long r = blockIdx.x, len = g.channels / g.groups;
+  const long long r = g.first + blockIdx.x, len = g.channels / g.groups;
   const Row row(g, r, len);
   const T *x = static_cast<const T *>(g.x) + row.n * g.x_sample + row.c0;
   T *y = static_cast<T *>(g.out) + row.n * g.out_sample + row.c0;
@@ -242,7 +242,7 @@ __global__ void __launch_bounds__(kThreads) k_norm_rows_grad(GroupNorm g) {
   __shared__ float join[kTeams > 1 ? TEAM * V * 8 : 1];
   const int lane = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
   const int len = (int)(g.channels / g.groups);
-  const long long c0 = (long long)blockIdx.x * len;
+  const long long gr = g.first + blockIdx.x, c0 = gr * len;
   float sw[V][8] = {}, sb[V][8] = {};
   const float inv = 1.0f / (float)len;
   int turn = 0;
@@ -258,7 +258,7 @@ __global__ void __launch_bounds__(kThreads) k_norm_rows_grad(GroupNorm g) {
       rd[v].template load<EVEN>(dy + at, len - at);
       if (g.extra) re[v].template load<EVEN>(static_cast<const T *>(g.extra) + n * g.extra_sample + c0 + at, len - at);
     }
-    const float mean = g.mean[n * g.groups + blockIdx.x], rstd = g.rstd[n * g.groups + blockIdx.x];
+    const float mean = g.mean[n * g.groups + gr], rstd = g.rstd[n * g.groups + gr];
     float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
@@ -342,7 +342,7 @@ __global__ void __launch_bounds__(kThreads) k_norm_rows_grad(GroupNorm g) {
 template <class T>
 __global__ void __launch_bounds__(1024) k_norm_long_rows_grad(GroupNorm g) {
   __shared__ float red[2][16];
-  const long long r = blockIdx.x, len = g.channels / g.groups;
+  const long long r = g.first + blockIdx.x, len = g.channels / g.groups;
   const Row row(g, r, len);
   const float mean = g.mean[r], rstd = g.rstd[r];
   const T *x = static_cast<const T *>(g.x) + row.n * g.x_sample + row.c0, *dy = static_cast<const T *>(g.dy) + row.n * g.dy_sample + row.c0;
@@ -404,8 +404,7 @@ __global__ void __launch_bounds__(1024) k_norm_join(GroupNorm g, const float *pa
   __shared__ float red[64][16 + 1];
   const int lane = threadIdx.x & 15, team = threadIdx.x / 16;
   const long long total = 2 * g.channels;
-  const u32 columns = (u32)((total + 15) / 16), y = blockIdx.x / columns, x = blockIdx.x - y * columns;
-  const long long c = (long long)x * 16 + lane;
+  const long long columns = (total + 15) / 16, id = g.first + blockIdx.x, y = to ? id / columns : 0, x = id - y * columns, c = x * 16 + lane;
   const long long first = y * each, end = first + each < count ? first + each : count;
   float s = 0.0f;
   if (c < total) {
@@ -423,7 +422,7 @@ __global__ void __launch_bounds__(1024) k_norm_join(GroupNorm g, const float *pa
   __syncthreads();
   const int column = threadIdx.x / 64;   // a wave adds up a column's
   s = lanes_sum<64>(red[threadIdx.x & 63][column]);
-  const long long o = (long long)x * 16 + column;
+  const long long o = x * 16 + column;
   if ((threadIdx.x & 63) == 0 && o < total) {
     if (to) {
       to[y * total + o] = s;
@@ -460,8 +459,9 @@ struct Place {
   int vec, row;       // the thread's
   int own;            // channels that it owns (<= 0: none), from c0 + 8 vec on
   __device__ __forceinline__ Place(const GroupNorm &g, const Maps &m) {
-    n = blockIdx.x / (u32)(m.blocks * m.chunks);
-    const int piece = (int)(blockIdx.x - (u32)n * (u32)(m.blocks * m.chunks));
+    const u32 id = (u32)g.first + blockIdx.x, each = (u32)(m.blocks * m.chunks);
+    n = id / each;
+    const int piece = (int)(id - (u32)n * each);
     chunk = piece / m.blocks;
     block = piece - chunk * m.blocks;
     if (m.blocks_a_group > 1) {
@@ -579,8 +579,9 @@ __device__ __forceinline__ void join_pieces(const GroupNorm &g, const Maps &m, c
 // A workgroup a group: its pieces are read once, where each workgroup that makes a piece's result would read all of them.
 __global__ void __launch_bounds__(1024) k_norm_maps_join(GroupNorm g, Maps m) {
   float mean, rstd;
-  join_pieces<1024>(g, m, g.scratch + (long long)blockIdx.x * m.pieces_a_group * 2, mean, rstd);
-  if (threadIdx.x == 0) g.mean[blockIdx.x] = mean, g.rstd[blockIdx.x] = rstd;
+  const long long r = g.first + blockIdx.x;
+  join_pieces<1024>(g, m, g.scratch + r * m.pieces_a_group * 2, mean, rstd);
+  if (threadIdx.x == 0) g.mean[r] = mean, g.rstd[r] = rstd;
 }
 
 // kWhole: a block's values are in registers from the mean to the result.  kPieces: mean and squares of a piece, per group, to
@@ -684,7 +685,8 @@ __global__ void __launch_bounds__(NT) k_norm_maps(GroupNorm g, Maps m) {
 // out[n][group][2].  A workgroup a group.
 __global__ void __launch_bounds__(1024) k_norm_group_sums(GroupNorm g, const float *sums, float2 *out) {
   __shared__ float2 red[16];
-  const long long n = blockIdx.x / (u32)g.groups, c0 = (blockIdx.x - n * g.groups) * (g.channels / g.groups), end = c0 + g.channels / g.groups;
+  const u32 r = (u32)g.first + blockIdx.x, gr = r % (u32)g.groups;
+  const long long n = r / (u32)g.groups, c0 = gr * (g.channels / g.groups), end = c0 + g.channels / g.groups;
   const float *s = sums + n * 2 * g.channels;
   float s1 = 0.0f, s2 = 0.0f;
   for (long long c = c0 + threadIdx.x; c < end; c += 1024) {
@@ -693,7 +695,7 @@ __global__ void __launch_bounds__(1024) k_norm_group_sums(GroupNorm g, const flo
     s1 = __builtin_fmaf(s[g.channels + c], w, s1);
   }
   team_sums<1024>(s1, s2, red);
-  if (threadIdx.x == 0) out[blockIdx.x] = {s1, s2};
+  if (threadIdx.x == 0) out[r] = {s1, s2};
 }
 
 // The gradient.  Per channel of a piece: the sums of d (dy through the activation) and of d h, to scratch[n][chunk][2][channels];
@@ -859,7 +861,7 @@ Maps maps_of(const GroupNorm &g, int threads, int each, int bytes = 128) {
   m.pieces_a_group = m.chunks * m.blocks_a_group;
   return m;
 }
-constexpr long long kMostWorkgroups = 0x7fffffff;
+constexpr long long kMostWorkgroups = 0x7fffffff;   // 32-bit numbers in the kernels
 long long workgroups(const GroupNorm &g, const Maps &m) { return (long long)m.blocks * m.chunks * g.samples; }
 bool whole(const GroupNorm &g, const Maps &m) { return m.chunks == 1 && m.blocks_a_group == 1 && workgroups(g, m) <= kMostWorkgroups; }
 
@@ -900,6 +902,9 @@ long long join_parts(long long count) {
   return count <= 4096 ? 1 : parts < 256 ? parts : 256;
 }
 
+template <int N>
+using number = std::integral_constant<int, N>;
+
 // Calls f with whether every eight entries exist together or not at all.
 template <class F>
 void by_even(const GroupNorm &g, F &&f) {
@@ -922,24 +927,30 @@ hipError_t norm(const GroupNorm &g, hipStream_t s) {
       const long long rows = g.samples * g.groups;
       const Rows r = rows_of(g, false);
       if (r.team == 0) {
-        k_norm_long_rows<T><<<dim3((unsigned)rows), 1024, 0, s>>>(g);
+        in_launches(g, rows, 1024, [&](const GroupNorm &some, unsigned grid) { k_norm_long_rows<T><<<dim3(grid), 1024, 0, s>>>(some); });
         return;
       }
-      const unsigned grid = (unsigned)((rows + kThreads / r.team - 1) / (kThreads / r.team));
-      if (r.team == 16) k_norm_rows<T, 16, 1, kEven><<<dim3(grid), kThreads, 0, s>>>(g);
-      else if (r.team == 64 && r.each == 1) k_norm_rows<T, 64, 1, kEven><<<dim3(grid), kThreads, 0, s>>>(g);
-      else if (r.team == 64) k_norm_rows<T, 64, 4, kEven><<<dim3(grid), kThreads, 0, s>>>(g);
-      else k_norm_rows<T, 256, 4, kEven><<<dim3(grid), kThreads, 0, s>>>(g);
+      in_launches(g, (rows + kThreads / r.team - 1) / (kThreads / r.team), kThreads, [&](const GroupNorm &some, unsigned grid) {
+        if (r.team == 16) k_norm_rows<T, 16, 1, kEven><<<dim3(grid), kThreads, 0, s>>>(some);
+        else if (r.team == 64 && r.each == 1) k_norm_rows<T, 64, 1, kEven><<<dim3(grid), kThreads, 0, s>>>(some);
+        else if (r.team == 64) k_norm_rows<T, 64, 4, kEven><<<dim3(grid), kThreads, 0, s>>>(some);
+        else k_norm_rows<T, 256, 4, kEven><<<dim3(grid), kThreads, 0, s>>>(some);
+      });
       return;
     }
     Maps m;
-    const auto grid = [&] { return dim3((unsigned)workgroups(g, m)); };
-    if (m = maps_of(g, 64, 2), wave_whole(g, m)) k_norm_maps<T, 64, 2, kWhole, kEven><<<grid(), 64, 0, s>>>(g, m);
-    else if (m = maps_of(g, 64, 8), wave_whole(g, m)) k_norm_maps<T, 64, 8, kWhole, kEven><<<grid(), 64, 0, s>>>(g, m);
-    else if (m = maps_of(g, 256, 2), whole(g, m)) k_norm_maps<T, 256, 2, kWhole, kEven><<<grid(), 256, 0, s>>>(g, m);
-    else if (m = maps_of(g, 256, 4), whole(g, m)) k_norm_maps<T, 256, 4, kWhole, kEven><<<grid(), 256, 0, s>>>(g, m);
-    else if (m = maps_of(g, 256, 8), whole(g, m)) k_norm_maps<T, 256, 8, kWhole, kEven><<<grid(), 256, 0, s>>>(g, m);
-    else if (m = maps_of(g, 1024, 8), whole(g, m)) k_norm_maps<T, 1024, 8, kWhole, kEven><<<grid(), 1024, 0, s>>>(g, m);
+    const auto run = [&](auto threads, auto each, auto pass) {
+      constexpr int kNt = decltype(threads)::value;
+      in_launches(g, workgroups(g, m), kNt, [&](const GroupNorm &some, unsigned grid) {
+        k_norm_maps<T, kNt, decltype(each)::value, decltype(pass)::value, kEven><<<dim3(grid), kNt, 0, s>>>(some, m);
+      });
+    };
+    if (m = maps_of(g, 64, 2), wave_whole(g, m)) run(number<64>(), number<2>(), number<kWhole>());
+    else if (m = maps_of(g, 64, 8), wave_whole(g, m)) run(number<64>(), number<8>(), number<kWhole>());
+    else if (m = maps_of(g, 256, 2), whole(g, m)) run(number<256>(), number<2>(), number<kWhole>());
+    else if (m = maps_of(g, 256, 4), whole(g, m)) run(number<256>(), number<4>(), number<kWhole>());
+    else if (m = maps_of(g, 256, 8), whole(g, m)) run(number<256>(), number<8>(), number<kWhole>());
+    else if (m = maps_of(g, 1024, 8), whole(g, m)) run(number<1024>(), number<8>(), number<kWhole>());
     else {
       m = maps_of(g, 256, 8);
       if (workgroups(g, m) > kMostWorkgroups) {
@@ -947,9 +958,10 @@ hipError_t norm(const GroupNorm &g, hipStream_t s) {
         return;
       }
       m.apart = m.pieces_a_group > kTogetherForward;
-      k_norm_maps<T, 256, 8, kPieces, kEven><<<grid(), 256, 0, s>>>(g, m);
-      if (m.apart) k_norm_maps_join<<<dim3((unsigned)(g.samples * g.groups)), 1024, 0, s>>>(g, m);
-      k_norm_maps<T, 256, 8, kJoined, kEven><<<grid(), 256, 0, s>>>(g, m);
+      run(number<256>(), number<8>(), number<kPieces>());
+      if (m.apart)
+        in_launches(g, g.samples * g.groups, 1024, [&](const GroupNorm &some, unsigned grid) { k_norm_maps_join<<<dim3(grid), 1024, 0, s>>>(some, m); });
+      run(number<256>(), number<8>(), number<kJoined>());
     }
   });
   return rc != hipSuccess ? rc : hipGetLastError();
@@ -991,7 +1003,11 @@ hipError_t norm_grad(const GroupNorm &call, hipStream_t s) {
   const bool sums = g.dweight || g.dbias;
   long long count = 0;   // rows of partial sums, from part on
   float *part = g.scratch;
-  const unsigned columns = (unsigned)((2 * g.channels + 15) / 16);
+  // `rows` rows of partial sums, in parts of `each`
+  const auto join = [&](const float *from, long long rows, long long each, float *to) {
+    const long long columns = (2 * g.channels + 15) / 16, parts = to ? (rows + each - 1) / each : 1;
+    in_launches(g, columns * parts, 1024, [&](const GroupNorm &some, unsigned grid) { k_norm_join<<<dim3(grid), 1024, 0, s>>>(some, from, rows, each, to); });
+  };
   hipError_t rc = hipSuccess;
   by_even(g, [&](auto even) {
     constexpr bool kEven = decltype(even)::value;
@@ -1004,45 +1020,52 @@ hipError_t norm_grad(const GroupNorm &call, hipStream_t s) {
           const long long eights = ((g.channels / g.groups + 7) / 8) * g.groups;
           k_norm_long_channels<T><<<dim3((unsigned)((eights + kThreads - 1) / kThreads), (unsigned)count), kThreads, 0, s>>>(g);
         }
-        k_norm_long_rows_grad<T><<<dim3((unsigned)(g.samples * g.groups)), 1024, 0, s>>>(g);
+        in_launches(g, g.samples * g.groups, 1024, [&](const GroupNorm &some, unsigned grid) { k_norm_long_rows_grad<T><<<dim3(grid), 1024, 0, s>>>(some); });
         return;
       }
       count = rows_workgroups(g, r);
-      const dim3 grid((unsigned)g.groups, (unsigned)count);
-      if (r.team == 16) k_norm_rows_grad<T, 16, 1, kEven><<<grid, kThreads, 0, s>>>(g);
-      else if (r.team == 64 && r.each == 1) k_norm_rows_grad<T, 64, 1, kEven><<<grid, kThreads, 0, s>>>(g);
-      else if (r.team == 64) k_norm_rows_grad<T, 64, 2, kEven><<<grid, kThreads, 0, s>>>(g);
-      else if (r.each == 1) k_norm_rows_grad<T, 256, 1, kEven><<<grid, kThreads, 0, s>>>(g);
-      else k_norm_rows_grad<T, 256, 4, kEven><<<grid, kThreads, 0, s>>>(g);
+      in_launches(g, g.groups, kThreads, [&](const GroupNorm &some, unsigned x) {
+        const dim3 grid(x, (unsigned)count);
+        if (r.team == 16) k_norm_rows_grad<T, 16, 1, kEven><<<grid, kThreads, 0, s>>>(some);
+        else if (r.team == 64 && r.each == 1) k_norm_rows_grad<T, 64, 1, kEven><<<grid, kThreads, 0, s>>>(some);
+        else if (r.team == 64) k_norm_rows_grad<T, 64, 2, kEven><<<grid, kThreads, 0, s>>>(some);
+        else if (r.each == 1) k_norm_rows_grad<T, 256, 1, kEven><<<grid, kThreads, 0, s>>>(some);
+        else k_norm_rows_grad<T, 256, 4, kEven><<<grid, kThreads, 0, s>>>(some);
+      });
     } else if (g.samples > 0 && g.positions > 0) {
       const GradMaps q = grad_maps(g);
       if (workgroups(g, q.m) > kMostWorkgroups) {
         rc = hipErrorInvalidValue;
         return;
       }
-      const dim3 grid((unsigned)workgroups(g, q.m));
       count = rows_of_sums(g, q.m);
       part = g.scratch + before_sums(g, q.m);
+      float2 *of_groups = nullptr;
+      const auto run = [&](auto threads, auto each, auto pass) {
+        constexpr int kNt = decltype(threads)::value;
+        in_launches(g, workgroups(g, q.m), kNt, [&](const GroupNorm &some, unsigned grid) {
+          k_norm_maps_grad<T, kNt, decltype(each)::value, decltype(pass)::value, kEven><<<dim3(grid), kNt, 0, s>>>(some, q.m, part, of_groups);
+        });
+      };
       if (!q.whole) {
-        k_norm_maps_grad<T, 256, 4, kPieces, kEven><<<grid, 256, 0, s>>>(g, q.m, nullptr, nullptr);
-        float2 *of_groups = nullptr;
+        run(number<256>(), number<4>(), number<kPieces>());
         if (q.m.apart) {
-          k_norm_join<<<dim3(columns * (unsigned)g.samples), 1024, 0, s>>>(g, g.scratch, g.samples * q.m.chunks, q.m.chunks, part);
+          join(g.scratch, g.samples * q.m.chunks, q.m.chunks, part);
           if (q.m.blocks_a_group > 1) {
             of_groups = reinterpret_cast<float2 *>(g.scratch + g.samples * 2 * q.m.chunks * g.channels);
-            k_norm_group_sums<<<dim3((unsigned)(g.samples * g.groups)), 1024, 0, s>>>(g, part, of_groups);
+            in_launches(g, g.samples * g.groups, 1024, [&](const GroupNorm &some, unsigned grid) { k_norm_group_sums<<<dim3(grid), 1024, 0, s>>>(some, part, of_groups); });
           }
         }
-        k_norm_maps_grad<T, 256, 4, kJoined, kEven><<<grid, 256, 0, s>>>(g, q.m, part, of_groups);
+        run(number<256>(), number<4>(), number<kJoined>());
       } else if (q.threads == 64) {
-        if (q.each == 2) k_norm_maps_grad<T, 64, 2, kWhole, kEven><<<grid, 64, 0, s>>>(g, q.m, nullptr, nullptr);
-        else k_norm_maps_grad<T, 64, 4, kWhole, kEven><<<grid, 64, 0, s>>>(g, q.m, nullptr, nullptr);
+        if (q.each == 2) run(number<64>(), number<2>(), number<kWhole>());
+        else run(number<64>(), number<4>(), number<kWhole>());
       } else if (q.threads == 512) {
-        if constexpr (sizeof(T) == 2) k_norm_maps_grad<T, 512, 8, kWhole, kEven><<<grid, 512, 0, s>>>(g, q.m, nullptr, nullptr);
+        if constexpr (sizeof(T) == 2) run(number<512>(), number<8>(), number<kWhole>());
       } else if (q.each == 2) {
-        k_norm_maps_grad<T, 256, 2, kWhole, kEven><<<grid, 256, 0, s>>>(g, q.m, nullptr, nullptr);
+        run(number<256>(), number<2>(), number<kWhole>());
       } else {
-        k_norm_maps_grad<T, 256, 4, kWhole, kEven><<<grid, 256, 0, s>>>(g, q.m, nullptr, nullptr);
+        run(number<256>(), number<4>(), number<kWhole>());
       }
     }
   });
@@ -1050,10 +1073,11 @@ hipError_t norm_grad(const GroupNorm &call, hipStream_t s) {
   if (sums) {
     if (const long long parts = join_parts(count); parts > 1) {
       float *to = part + count * 2 * g.channels;
-      k_norm_join<<<dim3(columns * (unsigned)parts), 1024, 0, s>>>(g, part, count, (count + parts - 1) / parts, to);
-      k_norm_join<<<dim3(columns), 1024, 0, s>>>(g, to, parts, parts, nullptr);
+      const long long each = (count + parts - 1) / parts;
+      join(part, count, each, to);
+      join(to, (count + each - 1) / each, parts, nullptr);
     } else {
-      k_norm_join<<<dim3(columns), 1024, 0, s>>>(g, part, count, count, nullptr);
+      join(part, count, count, nullptr);
     }
   }
   return hipGetLastError();

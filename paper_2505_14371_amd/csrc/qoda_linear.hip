@@ -306,7 +306,7 @@ __global__ void __launch_bounds__(64 * WM * WN) k_product(Product p, int tiles_m
   __shared__ __align__(16) char a0[BM * kStepBytes], b0[BN * kStepBytes], a1[BM * kStepBytes], b1[BN * kStepBytes];
 
   int tm, tn;
-  tile_of((int)blockIdx.x, tiles_m, tiles_n, tm, tn);
+  tile_of((int)(p.first + blockIdx.x), tiles_m, tiles_n, tm, tn);
   const int i0 = tm * BM, j0 = tn * BN;
   const int k0 = (int)blockIdx.y * steps_each * kStep;
   const int k = (long long)p.k - k0 < (long long)steps_each * kStep ? p.k - k0 : steps_each * kStep;   // of this split
@@ -476,7 +476,7 @@ __global__ void __launch_bounds__(64 * NW) k_few_rows(Product p) {
   constexpr int E = 16 / (int)sizeof(T), kRun = 8 * E, kAhead = NW > 4 ? (sizeof(T) == 4 ? 2 : 4) : 8;
   __shared__ v4f part[NW][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, i = lane & 15, g = lane >> 4;
-  const int j0 = (int)blockIdx.x * 16;
+  const int j0 = (int)(p.first + blockIdx.x) * 16;
   const T *b = static_cast<const T *>(p.b) + (long long)(j0 + i < p.n ? j0 + i : p.n - 1) * p.ldb;
   const T *a = static_cast<const T *>(p.a) + (long long)(i < p.m ? i : 0) * p.lda;
   v4f c = {0, 0, 0, 0};
@@ -639,9 +639,12 @@ Plan plan_of(const Product &p) {
 
 template <class T, int FORM, int BM, int BN, int WM, int WN>
 void launch(const Product &p, const Plan &q, hipStream_t s) {
-  const dim3 grid((unsigned)(q.tiles_m * q.tiles_n), (unsigned)q.splits);
-  if (q.direct) k_product<T, FORM, BM, BN, WM, WN, true><<<grid, 64 * WM * WN, 0, s>>>(p, q.tiles_m, q.tiles_n, q.steps_each, q.loose);
-  else if constexpr (BN < 256) k_product<T, FORM, BM, BN, WM, WN, false><<<grid, 64 * WM * WN, 0, s>>>(p, q.tiles_m, q.tiles_n, q.steps_each, false);
+  constexpr int WG = 64 * WM * WN;
+  in_launches(p, (long long)q.tiles_m * q.tiles_n, WG, [&](const Product &part, unsigned x) {
+    const dim3 grid(x, (unsigned)q.splits);
+    if (q.direct) k_product<T, FORM, BM, BN, WM, WN, true><<<grid, WG, 0, s>>>(part, q.tiles_m, q.tiles_n, q.steps_each, q.loose);
+    else if constexpr (BN < 256) k_product<T, FORM, BM, BN, WM, WN, false><<<grid, WG, 0, s>>>(part, q.tiles_m, q.tiles_n, q.steps_each, false);
+  });
 }
 
 template <class T, int FORM>
@@ -650,7 +653,7 @@ void launch(const Product &p, const Plan &q, hipStream_t s) {
     case kFewRows:
       if constexpr (FORM == kProductRows) {
         // with few workgroups more waves each
-        if (q.tiles_n >= kCus) k_few_rows<T, 4><<<dim3((unsigned)q.tiles_n), 256, 0, s>>>(p);
+        if (q.tiles_n >= kCus) in_launches(p, q.tiles_n, 256, [&](const Product &part, unsigned grid) { k_few_rows<T, 4><<<dim3(grid), 256, 0, s>>>(part); });
         else k_few_rows<T, 16><<<dim3((unsigned)q.tiles_n), 1024, 0, s>>>(p);
       }
       return;

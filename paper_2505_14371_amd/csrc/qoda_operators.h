@@ -39,6 +39,7 @@ struct Product {
   int activation, accumulate;
   Drop drop;
   float *partial;   // products split over l: [splits][m][n]
+  long long first;  // of in_launches()
 };
 
 struct Entries {   // y = extra + drop(act(x)), or gradient: y = drop(x * act'(extra))
@@ -48,6 +49,7 @@ struct Entries {   // y = extra + drop(act(x)), or gradient: y = drop(x * act'(e
   void *y;
   long long ldx, lde, ldy;
   Drop drop;
+  long long first;
 };
 
 struct GroupNorm {
@@ -61,7 +63,17 @@ struct GroupNorm {
   float *dweight, *dbias;
   float eps;
   float *scratch;
+  long long first;
 };
+
+// HIP launches fewer than 2^32 work-items along a dimension of the grid.  Calls launch(args, grid.x) for `workgroups` of `threads` each, in as many
+// launches as that takes; a kernel's workgroup is number args.first + blockIdx.x.
+template <class Args, class F>
+void in_launches(const Args &args, long long workgroups, int threads, F &&launch) {
+  const long long most = ((1ll << 32) - 1) / threads;
+  Args a = args;
+  for (a.first = 0; a.first < workgroups; a.first += most) launch(a, (unsigned)(workgroups - a.first < most ? workgroups - a.first : most));
+}
 
 size_t product_scratch(const Product &p);        // bytes of p.partial
 hipError_t launch_product(const Product &p, hipStream_t s);
