@@ -136,6 +136,11 @@ def _activation(name: str) -> int:
         raise ValueError(f"activation {name!r}: one of {', '.join(ACTIVATIONS)}") from None
 
 
+def _number(activation) -> Optional[int]:
+    """For the native look, which takes None for an activation that it does not know."""
+    return ACTIVATIONS.get(activation) if isinstance(activation, str) else None
+
+
 def _first(t: torch.Tensor, name: str) -> int:
     """The type of a call's first tensor."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
@@ -223,7 +228,7 @@ def linear(x, weight, bias=None, residual=None, *, activation="none", p=0.0, see
         with _on(stream):
             return linear(x, weight, bias, residual, activation=activation, p=p, seed=seed, offset=offset, keep_pre=keep_pre)
     if _is_native():
-        out = _looked_at(_native.linear, x, weight, bias, residual, ACTIVATIONS.get(activation), p, seed, offset, keep_pre)
+        out = _looked_at(_native.linear, x, weight, bias, residual, _number(activation), p, seed, offset, keep_pre)
         if out is not None:
             return out
     out = _unless_followed("linear", "linear_input_grad and linear_weight_grad", (x, weight, bias, residual), lambda: linear(
@@ -249,7 +254,7 @@ def linear_input_grad(dz, weight, *, pre=None, activation="none", p=0.0, seed=0,
         with _on(stream):
             return linear_input_grad(dz, weight, pre=pre, activation=activation, p=p, seed=seed, offset=offset, residual=residual)
     if _is_native():
-        out = _looked_at(_native.linear_input_grad, dz, weight, pre, ACTIVATIONS.get(activation), p, seed, offset, residual)
+        out = _looked_at(_native.linear_input_grad, dz, weight, pre, _number(activation), p, seed, offset, residual)
         if out is not None:
             return out
     dt, act = _first(dz, "linear_input_grad: dz"), _activation(activation)
@@ -311,7 +316,7 @@ def dropout(x, p, seed, offset, *, activation="none", residual=None, stream=None
         with _on(stream):
             return dropout(x, p, seed, offset, activation=activation, residual=residual)
     if _is_native():
-        out = _looked_at(_native.entries, x, residual, ACTIVATIONS.get(activation), p, seed, offset, False)
+        out = _looked_at(_native.entries, x, residual, _number(activation), p, seed, offset, False)
         if out is not None:
             return out
     out = _unless_followed("dropout", "dropout_grad", (x, residual), lambda: dropout(x, p, seed, offset, activation=activation, residual=residual))
@@ -326,7 +331,7 @@ def dropout_grad(dy, p, seed, offset, *, pre=None, activation="none", stream=Non
         with _on(stream):
             return dropout_grad(dy, p, seed, offset, pre=pre, activation=activation)
     if _is_native():
-        out = _looked_at(_native.entries, dy, pre, ACTIVATIONS.get(activation), p, seed, offset, True)
+        out = _looked_at(_native.entries, dy, pre, _number(activation), p, seed, offset, True)
         if out is not None:
             return out
     return _entries("dropout_grad: dy", _load().qoda_dropout_grad, dy, pre, "dropout_grad: pre", activation, p, seed, offset)
@@ -368,7 +373,7 @@ def group_norm(x, groups, weight=None, bias=None, *, eps=1e-5, activation="none"
         with _on(stream):
             return group_norm(x, groups, weight, bias, eps=eps, activation=activation)
     if _is_native():
-        out = _looked_at(_native.group_norm, x, groups, weight, bias, eps, ACTIVATIONS.get(activation))
+        out = _looked_at(_native.group_norm, x, groups, weight, bias, eps, _number(activation))
         if out is not None:
             return out
     out = _unless_followed("group_norm", "group_norm_grad", (x, weight, bias), lambda: group_norm(x, groups, weight, bias, eps=eps, activation=activation))
@@ -396,7 +401,7 @@ def group_norm_grad(dy, x, mean, rstd, groups, weight=None, bias=None, *, activa
             return group_norm_grad(dy, x, mean, rstd, groups, weight, bias, activation=activation, residual=residual, dweight=dweight, dbias=dbias,
                                    accumulate=accumulate)
     if _is_native() and (not accumulate or (dweight is not None and dbias is not None)):
-        out = _looked_at(_native.group_norm_grad, dy, x, mean, rstd, groups, weight, bias, ACTIVATIONS.get(activation), residual, dweight, dbias, accumulate)
+        out = _looked_at(_native.group_norm_grad, dy, x, mean, rstd, groups, weight, bias, _number(activation), residual, dweight, dbias, accumulate)
         if out is not None:
             return out
     dt, act = _first(x, "group_norm_grad: x"), _activation(activation)

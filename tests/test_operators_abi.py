@@ -120,3 +120,14 @@ def test_share_of_kept_entries():
         share = (D.lots(64, n // 64, 7, 3) >= D.threshold(p)).mean()
         assert abs(share - (1 - p)) < 5 * np.sqrt(p * (1 - p) / n)
     assert (D.lots(64, 64, 7, 3) != D.lots(64, 64, 7, 4)).mean() > 0.99
+
+
+@pytest.mark.parametrize("activation", [["gelu"], {}, None, 3])
+def test_an_activation_of_another_type_is_refused_as_a_value(lib, activation):
+    x = pytest.importorskip("torch").zeros((2, 2))
+    s = x[:, 0]
+    for call in (lambda: ops.linear(x, x, activation=activation), lambda: ops.linear_input_grad(x, x, pre=x, activation=activation),
+                 lambda: ops.dropout(x, 0.5, 1, 1, activation=activation), lambda: ops.dropout_grad(x, 0.5, 1, 1, pre=x, activation=activation),
+                 lambda: ops.group_norm(x, 1, activation=activation), lambda: ops.group_norm_grad(x, x, s, s, 1, activation=activation)):
+        with pytest.raises(ValueError):
+            call()
