@@ -2,8 +2,8 @@
 
     python -m paper_2505_14371_amd.harness.train_blocks [--width 512] [--hidden 2048] [--depth 4] [--nodes 4] [--rows 2048] [--rounds 60]
 
-The task is synthetic: the rows of a fixed random two-layer map, to be matched in the mean square.  Prints the loss and the time
-of a round, and what part of it the model and the optimiser take.
+The task is synthetic: the rows of a fixed random two-layer map, to be matched.  The loss is a row's sum of squares, in the mean over the
+rows and the nodes.  Prints the loss and the time of a round, and what part of it the model and the optimiser take.
 """
 from __future__ import annotations
 
@@ -25,6 +25,12 @@ def batch(width: int, rows: int, nodes: int, seed: int, dtype):
     return [v.to(dtype) for v in x], [v + torch.tanh(v @ a) @ b for v in x]
 
 
+def loss_of(y: torch.Tensor, target: torch.Tensor):
+    """(a node's loss, its gradient by y in y's type)"""
+    off, rows = y.float() - target, target.numel() // target.shape[-1]
+    return off.square().sum() / rows, (off * (2.0 / rows)).to(y.dtype)
+
+
 def train(width=512, hidden=2048, depth=4, nodes=4, rows=2048, rounds=60, points=16, p=0.1, dtype=torch.bfloat16, seed=0):
     """(losses of the rounds, seconds of a round, seconds of its model part): medians over the rounds behind the first three."""
     model = ResidualBlocks(width, hidden, depth, p=p, dtype=dtype, seed=seed)
@@ -39,9 +45,9 @@ def train(width=512, hidden=2048, depth=4, nodes=4, rows=2048, rounds=60, points
         loss = torch.zeros((), device="cuda")
         for k in range(nodes):
             y, saved = model.forward(x[k], weights, draw=t * nodes + k)
-            off = y.float() - target[k]
-            loss += off.square().mean() / nodes
-            model.backward((off * (2.0 / off.numel() * width)).to(dtype), saved, weights, grads[k])
+            one, dy = loss_of(y, target[k])
+            loss += one / nodes
+            model.backward(dy, saved, weights, grads[k])
         torch.cuda.synchronize()
         part.append(time.perf_counter() - start)
         opt.step(grads)
