@@ -297,8 +297,9 @@ __device__ __forceinline__ void tile_of(int id, int tiles_m, int tiles_n, int &t
   tn = in / rows;
 }
 
+// (Tiles of 128 are held to the registers of two waves a SIMD, which plan_of() counts on; without that the fp32 input gradient's took 272.)
 template <class T, int FORM, int BM, int BN, int WM, int WN, bool DIRECT>
-__global__ void __launch_bounds__(64 * WM * WN) k_product(Product p, int tiles_m, int tiles_n, int steps_each, bool loose) {
+__global__ void __launch_bounds__(64 * WM * WN, BN == 128 && BM == 128 ? 2 : 1) k_product(Product p, int tiles_m, int tiles_n, int steps_each, bool loose) {
   constexpr int WG = 64 * WM * WN, FM = BM / WM / 16, FN = BN / WN / 32;
   typedef Operand<T, FORM != kProductColumns, 0, BM, WG, DIRECT> A;
   typedef Operand<T, FORM == kProductRows, 1, BN, WG, DIRECT> B;
