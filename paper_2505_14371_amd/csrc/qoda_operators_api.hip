@@ -194,15 +194,15 @@ struct Values { long long sample, position; };
 
 int check_values(const char *call, const char *name, const qoda_channels_last &v, int64_t samples, int64_t positions, int64_t channels,
                  size_t bytes, bool optional, Values *out) {
-  // a stride that no entry is reached by stands for the dense one
+  // a stride that no entry is reached by is not looked at
   out->position = positions > 1 ? v.position : channels;
-  out->sample = samples > 1 ? v.sample : out->position * positions;
+  out->sample = samples > 1 ? v.sample : 0;
   if (samples == 0 || positions == 0 || channels == 0) return QODA_OK;
   if (!v.data) return optional ? QODA_OK : fail(QODA_EINVAL, "%s: %s is null", call, name);
   if (!aligned(v.data, bytes)) return fail(QODA_EINVAL, "%s: %s is not aligned to its entries", call, name);
   // positions apart by at least the channels, samples by at least what the positions span: no two entries share an address
-  if (out->position < channels || out->position >= kMostStride || out->sample < (positions - 1) * out->position + channels ||
-      out->sample >= kMostStride * 1024)
+  if (out->position < channels || out->position >= kMostStride ||
+      (samples > 1 && (out->sample < (__int128)(positions - 1) * out->position + channels || out->sample >= kMostStride * 1024)))
     return fail(QODA_EINVAL, "%s: the strides of %s do not fit its %lld channels and %lld positions", call, name, (long long)channels, (long long)positions);
   return QODA_OK;
 }

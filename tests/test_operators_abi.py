@@ -131,3 +131,12 @@ def test_an_activation_of_another_type_is_refused_as_a_value(lib, activation):
                  lambda: ops.group_norm(x, 1, activation=activation), lambda: ops.group_norm_grad(x, x, s, s, 1, activation=activation)):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.parametrize("positions,position,sample", [(1 << 30, 1 << 34, 24), ((1 << 31) - 65536, 1 << 33, 8), (1 << 30, 1 << 39, 1 << 49)])
+def test_strides_whose_product_passes_64_bits_are_refused(lib, positions, position, sample):
+    """Samples that would lie inside one another: what a sample spans is more than its stride, also where it is no 64-bit number."""
+    dense = (8192, positions * 8, 8)
+    for x, y in (((4096, sample, position), dense), (dense, (4096, sample, position))):
+        a = ops._NORM.pack(0, 0, 2, positions, 8, 2, *x, *y, 0, 0, 4096, 4096, 1e-5)
+        assert lib.qoda_group_norm_workspace_bytes(a) == qoda.EINVAL and b"strides" in lib.qoda_operator_error()
