@@ -1,8 +1,8 @@
 // Dropout and its gradient, with the activation and the residual beside it (include/qoda_operators.h).
 //
-// One pass, bound by memory: 268 M entries of bf16 through gelu's slope 291 us, 5.5 TB/s.  The lots are ten rounds of the generator for eight
-// entries, a third of the arithmetic; it hides behind the loads as long as these are whole words and several on their way (entry by entry 812 us, as
-// structures of 16-bit entries, which the compiler loads in parts, 353).
+// One pass, bound by memory with arithmetic close behind: 268 M entries of bf16 through gelu's slope 307 us, 5.2 TB/s (288 without the lots, which are ten
+// rounds of the generator for eight entries, a third of the arithmetic).  It hides behind the loads as long as these are whole words and several on
+// their way (entry by entry 812 us, as structures of 16-bit entries, which the compiler loads in parts, 353).
 
 #include <type_traits>
 

@@ -12,11 +12,11 @@
 // The matrix instruction's first operand is b's piece: a lane then holds four sums adjacent in a row of c, and b's entries are dealt
 // to the instructions so that those of two instructions are eight adjacent ones: 16 bytes of bf16 to store, and one block of lots.
 //
-// Measured, bf16: 16384 x 8192 x 2048 435 us (1263 TFLOP/s; the library's product 424), with dropout and residual 462; the input
-// gradient of 8192 x 8192 x 2048 through gelu 299, of which 215 to 226 the product, 45 the read of pre and 20 the slope; the weight gradient of
-// 6144 x 2048 over 8192 rows 193.  fp32: 4096 x 2048 x 2048 245 us (140 TFLOP/s).  The matrix cores bound the large ones; the ends of
-// their tiles wait for memory, and a CU holds one such tile, so that nothing else runs meanwhile.  Short sums are bound by a tile's start and end:
-// 3300 x 410 x 2100 17 us for 7 steps.
+// Measured, bf16: 16384 x 8192 x 2048 441 us (1247 TFLOP/s; the library's product 424), with dropout and residual 471; the input
+// gradient of 8192 x 8192 x 2048 through gelu 308, of which 225 the product, 45 the read of pre and 30 the slope; the weight gradient of
+// 6144 x 2048 over 8192 rows 198.  fp32: 4096 x 2048 x 2048 242 us (142 TFLOP/s), its input gradient 249.  The matrix cores are busy 93 % of the CUs' time in
+// fp32 and 39 to 56 % in bf16, whose tiles' ends wait for memory: a CU holds one such tile, so that nothing else runs meanwhile.  Short sums are bound by
+// a tile's start and end: 3300 x 410 x 2100 16 us for 7 steps.
 
 #include <type_traits>
 
