@@ -28,8 +28,9 @@ constexpr float kLog2E = 1.4426950408889634f;
 // The two factors of 1 - Phi(|z|) = erfc(|z| / sqrt 2) / 2 = q e with e = exp(-z^2 / 2), which is the density's factor too, so that gelu and its slope take
 // one exponential and one reciprocal.  q is a polynomial in t = 1 / (1 + c |z|), fitted here (linear programming over 0 <= |z| <= 14.5), without its constant.
 //   fp32: nine terms, off by 2e-8 of q at most, and corrected to first order for the rounding of t: dq/d|z| = |z| q - 1 / sqrt(2 pi).  gelu and its slope
-//         of normal values are off by 3.5e-8 and 4.0e-8 in the square mean, which is what fp32's erf and exp give.
-//   bf16: seven terms, off by 3e-8 at most and by 4e-5 of q e at most: nothing beside the store's rounding, nor in fp32 sums of many entries.
+//         of normal values are off by 3.4e-8 and 3.8e-8 in the square mean; with fp32's erf and exp they are by 3.9e-8 and 4.1e-8.
+//   bf16: seven terms, off by 3e-8 at most (1.3e-7 with fp32's rounding) and by 4e-5 of q e at most: nothing beside the store's rounding, and little in
+//         the fp32 sums that dweight and dbias are.
 template <class T>
 __device__ __forceinline__ void normal_tail(float z, float &q, float &e) {
   e = __builtin_amdgcn_exp2f(z * z * (-0.5f * kLog2E));
