@@ -1,0 +1,42 @@
+// What the host side of the operators of include/qoda_matrices.h hands to their kernels.
+#pragma once
+
+#include "qoda_operators.h"
+
+namespace qoda {
+
+typedef unsigned char u8;
+
+// A microscaled matrix: rows of 128 bytes a step of 256 entries, and scales of 256 bytes for 64 rows and four blocks.
+constexpr int kMxStep = 256;
+inline long long mx_steps(long long cols) { return (cols + kMxStep - 1) / kMxStep; }
+inline long long mx_groups(long long rows) { return (rows + 63) / 64; }
+
+struct MxRounding {   // x is read, q written; values: the other way round
+  int type, transposed, stochastic;
+  long long rows, cols;       // of x
+  void *x;
+  long long ldx;
+  u8 *codes, *scales;
+  unsigned int k0, k1, o0, o1;   // the lots' key and the upper half of their counter
+  long long first;               // of in_launches()
+};
+
+// p: sizes, outputs and epilogue as in a product of entries; its operands are these.
+struct MxProduct {
+  Product p;
+  const u8 *a, *a_scales, *b, *b_scales;   // a: null where the rows are plain (x)
+  const void *x;
+  long long ldx;
+  int steps;                               // of 256 entries along the sum
+  long long first;
+};
+
+hipError_t launch_mx_quantize(const MxRounding &q, hipStream_t s);
+hipError_t launch_mx_values(const MxRounding &q, hipStream_t s);
+hipError_t launch_mx_row_sums(const u8 *codes, const u8 *scales, long long rows, long long cols, float *sums, bool accumulate, hipStream_t s);
+bool mx_takes_plain_rows(const Product &p);   // whether the product rounds plain rows itself
+size_t mx_product_scratch(const MxProduct &p);
+hipError_t launch_mx_product(const MxProduct &p, hipStream_t s);
+
+}  // namespace qoda

@@ -1,0 +1,224 @@
+// Host side of the operators declared in include/qoda_matrices.h: checks of arguments, and the kernels' arguments from the caller's.
+
+#include "../../include/qoda_matrices.h"
+#include "qoda_matrices.h"
+#include "qoda_operators_checks.h"
+
+using namespace qoda;
+
+namespace {
+
+size_t code_bytes(int64_t rows, int64_t cols) { return (size_t)rows * (size_t)mx_steps(cols) * 128; }
+size_t scale_bytes(int64_t rows, int64_t cols) { return (size_t)mx_groups(rows) * (size_t)mx_steps(cols) * 512; }
+
+int check_mx(const char *call, const char *name, const qoda_mx &q, int64_t rows, int64_t cols) {
+  if (rows == 0 || cols == 0) return QODA_OK;
+  if (!q.codes || !q.scales) return fail(QODA_EINVAL, "%s: %s is null", call, name);
+  if (!aligned(q.codes, 16) || !aligned(q.scales, 16)) return fail(QODA_EINVAL, "%s: codes or scales of %s are not aligned to 16 bytes", call, name);
+  return QODA_OK;
+}
+
+int check_sum(const char *call, int64_t k) {
+  if (k > QODA_MX_MAX_SUM) return fail(QODA_EINVAL, "%s: sums over %lld entries; %d at most", call, (long long)k, QODA_MX_MAX_SUM);
+  return QODA_OK;
+}
+
+int check_type(const char *call, int32_t dtype) { return check_common(call, dtype, kActNone); }
+
+int rounding_of(const qoda_mx_quantize_args *a, MxRounding *q) {
+  const char *call = "qoda_mx_quantize";
+  if (!a) return fail(QODA_EINVAL, "%s: null arguments", call);
+  TRY(check_type(call, a->dtype));
+  TRY(check_sides(call, a->rows, a->cols, 0));
+  TRY(check_matrix(call, "x", a->x, a->rows, a->cols, entry_bytes(a->dtype), false));
+  TRY(check_mx(call, "q", a->q, a->rows, a->cols));
+  const uint64_t key = a->seed ^ QODA_MX_KEY;
+  *q = {};
+  q->type = a->dtype, q->transposed = a->transposed != 0, q->stochastic = a->stochastic != 0;
+  q->rows = a->rows, q->cols = a->cols;
+  q->x = a->x.data, q->ldx = stride_of(a->x, a->rows, a->cols);
+  q->codes = static_cast<u8 *>(a->q.codes), q->scales = static_cast<u8 *>(a->q.scales);
+  q->k0 = (unsigned)key, q->k1 = (unsigned)(key >> 32), q->o0 = (unsigned)a->offset, q->o1 = (unsigned)(a->offset >> 32);
+  return QODA_OK;
+}
+
+void operands(MxProduct *m, const qoda_mx &a, const qoda_mx &b, int64_t k) {
+  m->a = static_cast<const u8 *>(a.codes), m->a_scales = static_cast<const u8 *>(a.scales);
+  m->b = static_cast<const u8 *>(b.codes), m->b_scales = static_cast<const u8 *>(b.scales);
+  m->steps = (int)mx_steps(k);
+  m->p.k = (int)k;
+}
+
+int linear_of(const qoda_mx_linear_args *a, MxProduct *m) {
+  const char *call = "qoda_mx_linear";
+  if (!a) return fail(QODA_EINVAL, "%s: null arguments", call);
+  TRY(check_common(call, a->dtype, a->activation));
+  TRY(check_sides(call, a->rows, a->in, a->out));
+  TRY(check_sum(call, a->in));
+  *m = {};
+  Product *p = &m->p;
+  TRY(make_drop(call, a->p, a->seed, a->offset, &p->drop));
+  const size_t e = entry_bytes(a->dtype);
+  if (a->out > 0) {
+    if (a->x.data) TRY(check_matrix(call, "x", a->x, a->rows, a->in, e, false));
+    else TRY(check_mx(call, "x", a->xq, a->rows, a->in));
+  }
+  if (a->rows > 0) TRY(check_mx(call, "w", a->w, a->out, a->in));
+  TRY(check_matrix(call, "residual", a->residual, a->rows, a->out, e, true));
+  TRY(check_matrix(call, "y", a->y, a->rows, a->out, e, false));
+  TRY(check_matrix(call, "pre", a->pre, a->rows, a->out, e, true));
+  if (!aligned(a->bias, 4)) return fail(QODA_EINVAL, "%s: bias is not aligned to its entries", call);
+  p->form = kProductRows, p->type = a->dtype;
+  p->m = (int)a->rows, p->n = (int)a->out;
+  p->out = a->y.data, p->ldo = stride_of(a->y, a->rows, a->out);
+  p->pre = a->pre.data, p->ldp = stride_of(a->pre, a->rows, a->out);
+  p->extra = a->residual.data, p->lde = stride_of(a->residual, a->rows, a->out);
+  p->bias = a->bias, p->activation = a->activation;
+  operands(m, a->xq, a->w, a->in);
+  m->x = a->x.data, m->ldx = stride_of(a->x, a->rows, a->in);
+  return QODA_OK;
+}
+
+int input_grad_of(const qoda_mx_linear_input_grad_args *a, MxProduct *m) {
+  const char *call = "qoda_mx_linear_input_grad";
+  if (!a) return fail(QODA_EINVAL, "%s: null arguments", call);
+  TRY(check_common(call, a->dtype, a->activation));
+  TRY(check_sides(call, a->rows, a->in, a->out));
+  TRY(check_sum(call, a->out));
+  *m = {};
+  Product *p = &m->p;
+  TRY(make_drop(call, a->p, a->seed, a->offset, &p->drop));
+  const size_t e = entry_bytes(a->dtype);
+  if (a->in > 0) {
+    if (a->dz.data) TRY(check_matrix(call, "dz", a->dz, a->rows, a->out, e, false));
+    else TRY(check_mx(call, "dz", a->dzq, a->rows, a->out));
+  }
+  if (a->rows > 0) TRY(check_mx(call, "wt", a->wt, a->in, a->out));
+  TRY(check_matrix(call, "pre", a->pre, a->rows, a->in, e, a->activation == kActNone));
+  TRY(check_matrix(call, "residual", a->residual, a->rows, a->in, e, true));
+  TRY(check_matrix(call, "dx", a->dx, a->rows, a->in, e, false));
+  p->form = kProductMixed, p->type = a->dtype;
+  p->m = (int)a->rows, p->n = (int)a->in;
+  p->out = a->dx.data, p->ldo = stride_of(a->dx, a->rows, a->in);
+  p->pre = a->activation == kActNone ? nullptr : a->pre.data, p->ldp = stride_of(a->pre, a->rows, a->in);
+  p->extra = a->residual.data, p->lde = stride_of(a->residual, a->rows, a->in);
+  p->activation = a->activation;
+  operands(m, a->dzq, a->wt, a->out);
+  m->x = a->dz.data, m->ldx = stride_of(a->dz, a->rows, a->out);
+  return QODA_OK;
+}
+
+int weight_grad_of(const qoda_mx_linear_weight_grad_args *a, MxProduct *m) {
+  const char *call = "qoda_mx_linear_weight_grad";
+  if (!a) return fail(QODA_EINVAL, "%s: null arguments", call);
+  TRY(check_sides(call, a->rows, a->in, a->out));
+  TRY(check_sum(call, a->rows));
+  *m = {};
+  Product *p = &m->p;
+  TRY(check_mx(call, "dzt", a->dzt, a->out, a->rows));
+  if (a->out > 0) TRY(check_mx(call, "xt", a->xt, a->in, a->rows));
+  TRY(check_matrix(call, "dw", a->dw, a->out, a->in, 4, false));
+  if (!aligned(a->dbias, 4)) return fail(QODA_EINVAL, "%s: dbias is not aligned to its entries", call);
+  p->form = kProductColumns, p->type = kF32;
+  p->m = (int)a->out, p->n = (int)a->in;
+  p->out = a->dw.data, p->ldo = stride_of(a->dw, a->out, a->in);
+  p->accumulate = a->accumulate != 0;
+  operands(m, a->dzt, a->xt, a->rows);
+  m->x = nullptr;
+  return QODA_OK;
+}
+
+// The rows that the product does not round itself are rounded into the workspace, before the split sums.
+size_t rounded_bytes(const MxProduct &m) {
+  if (!m.x || m.p.m == 0 || m.p.n == 0 || m.p.k == 0 || mx_takes_plain_rows(m.p)) return 0;
+  return code_bytes(m.p.m, m.p.k) + scale_bytes(m.p.m, m.p.k);
+}
+
+template <class Args>
+int64_t scratch_of(const Args *a, int (*make)(const Args *, MxProduct *)) {
+  MxProduct m;
+  const int rc = make(a, &m);
+  return rc != QODA_OK ? rc : (int64_t)(rounded_bytes(m) + mx_product_scratch(m));
+}
+
+int run(const char *call, MxProduct *m, void *workspace, size_t bytes, void *stream) {
+  if (m->p.m == 0 || m->p.n == 0) return QODA_OK;
+  const size_t rounded = rounded_bytes(*m);
+  TRY(check_workspace(call, workspace, bytes, rounded + mx_product_scratch(*m)));
+  u8 *w = static_cast<u8 *>(workspace);
+  if (m->x && m->p.k > 0 && mx_takes_plain_rows(m->p)) {
+    m->a = nullptr;
+  } else if (m->x) {
+    MxRounding q = {};
+    q.type = m->p.type, q.rows = m->p.m, q.cols = m->p.k;
+    q.x = const_cast<void *>(m->x), q.ldx = m->ldx;
+    q.codes = w, q.scales = w + code_bytes(m->p.m, m->p.k);
+    m->a = q.codes, m->a_scales = q.scales;
+    if (m->p.k > 0) TRY(done(call, launch_mx_quantize(q, static_cast<hipStream_t>(stream))));
+  }
+  m->p.partial = reinterpret_cast<float *>(w + rounded);
+  return done(call, launch_mx_product(*m, static_cast<hipStream_t>(stream)));
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t qoda_mx_code_bytes(int64_t rows, int64_t cols) {
+  const int rc = check_sides("qoda_mx_code_bytes", rows, cols, 0);
+  return rc != QODA_OK ? rc : (int64_t)code_bytes(rows, cols);
+}
+
+int64_t qoda_mx_scale_bytes(int64_t rows, int64_t cols) {
+  const int rc = check_sides("qoda_mx_scale_bytes", rows, cols, 0);
+  return rc != QODA_OK ? rc : (int64_t)scale_bytes(rows, cols);
+}
+
+int qoda_mx_quantize(const qoda_mx_quantize_args *a, void *stream) {
+  MxRounding q;
+  TRY(rounding_of(a, &q));
+  if (q.rows == 0 || q.cols == 0) return QODA_OK;
+  return done("qoda_mx_quantize", launch_mx_quantize(q, static_cast<hipStream_t>(stream)));
+}
+
+int qoda_mx_values(const qoda_mx_values_args *a, void *stream) {
+  const char *call = "qoda_mx_values";
+  if (!a) return fail(QODA_EINVAL, "%s: null arguments", call);
+  TRY(check_type(call, a->dtype));
+  TRY(check_sides(call, a->rows, a->cols, 0));
+  TRY(check_mx(call, "q", a->q, a->rows, a->cols));
+  TRY(check_matrix(call, "y", a->y, a->rows, a->cols, entry_bytes(a->dtype), false));
+  if (a->rows == 0 || a->cols == 0) return QODA_OK;
+  MxRounding q = {};
+  q.type = a->dtype, q.rows = a->rows, q.cols = a->cols;
+  q.x = a->y.data, q.ldx = stride_of(a->y, a->rows, a->cols);
+  q.codes = static_cast<u8 *>(a->q.codes), q.scales = static_cast<u8 *>(a->q.scales);
+  return done(call, launch_mx_values(q, static_cast<hipStream_t>(stream)));
+}
+
+int64_t qoda_mx_linear_workspace_bytes(const qoda_mx_linear_args *a) { return scratch_of(a, linear_of); }
+int64_t qoda_mx_linear_input_grad_workspace_bytes(const qoda_mx_linear_input_grad_args *a) { return scratch_of(a, input_grad_of); }
+int64_t qoda_mx_linear_weight_grad_workspace_bytes(const qoda_mx_linear_weight_grad_args *a) { return scratch_of(a, weight_grad_of); }
+
+int qoda_mx_linear(const qoda_mx_linear_args *a, void *workspace, size_t workspace_bytes, void *stream) {
+  MxProduct m;
+  TRY(linear_of(a, &m));
+  return run("qoda_mx_linear", &m, workspace, workspace_bytes, stream);
+}
+
+int qoda_mx_linear_input_grad(const qoda_mx_linear_input_grad_args *a, void *workspace, size_t workspace_bytes, void *stream) {
+  MxProduct m;
+  TRY(input_grad_of(a, &m));
+  return run("qoda_mx_linear_input_grad", &m, workspace, workspace_bytes, stream);
+}
+
+int qoda_mx_linear_weight_grad(const qoda_mx_linear_weight_grad_args *a, void *workspace, size_t workspace_bytes, void *stream) {
+  const char *call = "qoda_mx_linear_weight_grad";
+  MxProduct m;
+  TRY(weight_grad_of(a, &m));
+  TRY(run(call, &m, workspace, workspace_bytes, stream));
+  if (!a->dbias || a->out == 0) return QODA_OK;
+  return done(call, launch_mx_row_sums(m.a, m.a_scales, a->out, a->rows, a->dbias, a->accumulate != 0, static_cast<hipStream_t>(stream)));
+}
+
+}  // extern "C"

@@ -1,0 +1,390 @@
+// Products between microscaled matrices, of include/qoda_matrices.h: c[i][j] = sum over l of a(i, l) b(j, l), with the epilogues of qoda_linear.hip.
+//
+// The matrix instruction sums 128 products an entry, in four blocks of 32 with a scale each: a lane's 16 bytes are one block of one row, and the
+// scale is a byte of another register.  One dword of scales holds those of a lane's four pieces (64 rows), which is the order they lie in.  A workgroup computes
+// BM x BN sums in steps of 256 entries (128 bytes) along l; a step's codes and scales go straight into shared memory, twice, and while one step is
+// multiplied the next is on its way, as in qoda_linear.hip.  Rows are filled up to whole steps, so that there are no ragged ones.
+//
+// Both operands' pieces take every other four of eight rows: a lane then holds eight sums adjacent in a row of c.
+
+#include <utility>
+
+#include "qoda_mx_device.h"
+#include "qoda_product_device.h"
+
+namespace qoda {
+
+namespace {
+
+typedef int v8i __attribute__((ext_vector_type(8)));
+
+template <class F, int... I>
+__device__ __forceinline__ void each_of(F &&f, std::integer_sequence<int, I...>) { (f(std::integral_constant<int, I>()), ...); }
+template <int N, class F>
+__device__ __forceinline__ void each(F &&f) { each_of(f, std::make_integer_sequence<int, N>()); }
+
+// FB, FA: the bytes of the scales' registers.
+template <int FB, int FA>
+__device__ __forceinline__ v4f multiply_blocks(v4u b, v4u a, v4f c, u32 sb, u32 sa) {
+  const v8i x = {(int)b[0], (int)b[1], (int)b[2], (int)b[3], 0, 0, 0, 0}, y = {(int)a[0], (int)a[1], (int)a[2], (int)a[3], 0, 0, 0, 0};
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, c, 4, 4, FB, (int)sb, FA, (int)sa);   // 4: codes of four bits
+}
+
+// A side's scales, as they lie: 256 bytes for 64 rows and half a step.
+template <int N>
+struct Scales {
+  static constexpr int kHalf = N * 4;      // bytes of half a step
+  const u8 *base;
+  long long groups;
+  int first, last;                         // groups of 64 rows
+  __device__ __forceinline__ void start(const u8 *p, long long rows, int row) {
+    base = p, groups = (rows + 63) / 64, first = row / 64, last = (int)groups - 1;
+  }
+  // Half s of a step, by a wave: 16 bytes a lane.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+  __device__ __forceinline__ void direct(long long step, int s, lds_ptr to) const {
+    const int lane = threadIdx.x & 63;
+    if (lane >= kHalf / 16) return;
+    const int group = first + lane / 16;   // beyond the last rows: scales of sums that are not stored
+    const u8 *p = base + (2 * step + s) * groups * 256;
+    const u32 offset = (u32)(group < last ? group : last) * 256u + (lane & 15) * 16;
+    const u32 at = __builtin_amdgcn_readfirstlane((u32)(uintptr_t)to + s * kHalf);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(at), "v"(offset), "s"(p) : "memory", "m0");
+  }
+#pragma clang diagnostic pop
+  // The scales of a wave's pieces 4 q .. 4 q + 3, from its row `row` of the tile on; HALF: of the wave's only two pieces, 32 rows.
+  template <bool HALF>
+  static __device__ __forceinline__ u32 piece(lds_ptr tile, int row, int q, int s) {
+    const u32 w = *LDS(u32, tile + s * kHalf + (row / 64 + q) * 256 + (threadIdx.x & 63) * 4);
+    return HALF && row & 32 ? w >> 16 : w;
+  }
+};
+
+template <class T, int FORM, int BM, int BN, int WM, int WN>
+__global__ void __launch_bounds__(64 * WM * WN, BM == 128 ? 2 : 1) k_mx_product(MxProduct m, int tiles_m, int tiles_n, int steps_each) {
+  constexpr int WG = 64 * WM * WN, FM = BM / WM / 16, FN = BN / WN / 16, QM = (FM + 3) / 4, QN = (FN + 3) / 4;
+  static_assert(FM % 2 == 0 && FN % 2 == 0 && (FM == 2 || FM % 4 == 0) && (FN == 2 || FN % 4 == 0) && WG >= 256, "what the scales' order knows");
+  typedef Operand<bf16, true, 1, BM, WG, true> A;   // in words of 16 bits: four codes
+  typedef Operand<bf16, true, 1, BN, WG, true> B;
+  typedef Scales<BM> SA;
+  typedef Scales<BN> SB;
+  __shared__ __align__(16) char a0[BM * kStepBytes], b0[BN * kStepBytes], a1[BM * kStepBytes], b1[BN * kStepBytes];
+  __shared__ __align__(16) char s0[(BM + BN) * 8], s1[(BM + BN) * 8];
+
+  const Product &p = m.p;
+  int tm, tn;
+  tile_of((int)(m.first + blockIdx.x), tiles_m, tiles_n, tm, tn);
+  const int i0 = __builtin_amdgcn_readfirstlane(tm) * BM, j0 = __builtin_amdgcn_readfirstlane(tn) * BN;
+  const int step0 = (int)blockIdx.y * steps_each, steps = m.steps - step0 < steps_each ? m.steps - step0 : steps_each;
+  A a;
+  B b;
+  a.start(m.a, (long long)m.steps * 64, i0, p.m, step0 * 64, steps * 64);
+  b.start(m.b, (long long)m.steps * 64, j0, p.n, step0 * 64, steps * 64);
+  SA sa;
+  SB sb;
+  sa.start(m.a_scales, p.m, i0);
+  sb.start(m.b_scales, p.n, j0);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
+
+  v4f c[FM][FN];
+#pragma unroll
+  for (int x = 0; x < FM; ++x)
+#pragma unroll
+    for (int y = 0; y < FN; ++y) c[x][y] = v4f{0, 0, 0, 0};
+
+  struct Pieces {
+    v4u a[FM], b[FN];
+    u32 sa[QM], sb[QN];
+  };
+  u32 key_a = A::lane_key(wm), key_b = B::lane_key(wn);
+  const auto read = [&](Pieces &f, lds_ptr ta, lds_ptr tb, lds_ptr ts, int s) {
+    asm volatile("" : "+v"(key_a), "+v"(key_b));   // made anew each time, as in k_product
+#pragma unroll
+    for (int q = 0; q < QN; ++q) f.sb[q] = SB::template piece<FN == 2>(ts + BM * 8, wn, q, s);
+#pragma unroll
+    for (int q = 0; q < QM; ++q) f.sa[q] = SA::template piece<FM == 2>(ts, wm, q, s);
+#pragma unroll
+    for (int y = 0; y < FN; ++y) f.b[y] = B::piece(tb, key_b, wn, y / 2 * 32, y & 1, s);
+#pragma unroll
+    for (int x = 0; x < FM; ++x) f.a[x] = A::piece(ta, key_a, wm, x / 2 * 32, x & 1, s);
+  };
+  const auto multiply_all = [&](const Pieces &f) {
+    each<FM>([&](auto x) {
+      each<FN>([&](auto y) { c[x][y] = multiply_blocks<y % 4, x % 4>(f.b[y], f.a[x], c[x][y], f.sb[y / 4], f.sa[x / 4]); });
+    });
+  };
+  const lds_ptr ta[2] = {(lds_ptr)a0, (lds_ptr)a1}, tb[2] = {(lds_ptr)b0, (lds_ptr)b1}, ts[2] = {(lds_ptr)s0, (lds_ptr)s1};
+  const auto request = [&](int t, int h) {
+    a.direct(t * 64, ta[h]);
+    b.direct(t * 64, tb[h]);
+    if (wave < 2) sa.direct(step0 + t, wave, ts[h]);
+    else if (wave < 4) sb.direct(step0 + t, wave - 2, ts[h] + BM * 8);
+  };
+  if (steps > 0) {
+    request(0, 0);
+    if (steps > 1) request(1, 1);
+    Pieces f0, f1;
+    arrived();
+    read(f0, ta[0], tb[0], ts[0], 0);
+    for (int t = 0; t < steps; t += 2) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        if (t + h < steps) {
+          read(f1, ta[h], tb[h], ts[h], 1);
+          multiply_all(f0);
+          arrived();   // the next step is there, and nobody reads this one any more
+          if (t + h + 2 < steps) request(t + h + 2, h);
+          if (t + h + 1 < steps) read(f0, ta[1 - h], tb[1 - h], ts[1 - h], 0);
+          multiply_all(f1);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+  }
+
+  const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+  const auto row = [&](int x) { return i0 + wm + x / 2 * 32 + (i >> 2) * 8 + (x & 1) * 4 + (i & 3); };
+  const auto column = [&](int y) { return j0 + wn + y * 32 + g * 8; };
+  const auto sums = [&](int x, int y, float (&v)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = c[x][2 * y + e / 4][e & 3];
+  };
+  if (p.partial) {
+#pragma unroll
+    for (int x = 0; x < FM; ++x)
+#pragma unroll
+      for (int y = 0; y < FN / 2; ++y)
+        if (row(x) < p.m && column(y) < p.n) {
+          float v[8];
+          sums(x, y, v);
+          store8(p.partial + ((long long)blockIdx.y * p.m + row(x)) * p.n + column(y), p.n - column(y), v);
+        }
+    return;
+  }
+  by_activation<FORM>(p.activation, [&](auto act) {
+    constexpr int kPart = FM < 4 ? FM : 4;   // rows whose reads are all on their way before the first is needed
+#pragma unroll
+    for (int x0 = 0; x0 < FM; x0 += kPart) {
+      Beside<T, FORM, decltype(act)::value> beside[kPart][FN / 2];
+#pragma unroll
+      for (int x = 0; x < kPart; ++x)
+#pragma unroll
+        for (int y = 0; y < FN / 2; ++y)
+          if (row(x0 + x) < p.m && column(y) < p.n) beside[x][y].load(p, row(x0 + x), column(y), p.n - column(y));
+#pragma unroll
+      for (int x = 0; x < kPart; ++x)
+#pragma unroll
+        for (int y = 0; y < FN / 2; ++y)
+          if (row(x0 + x) < p.m && column(y) < p.n) {
+            float v[8];
+            sums(x0 + x, y, v);
+            finish(p, beside[x][y], row(x0 + x), column(y), p.n - column(y), v);
+          }
+    }
+  });
+}
+
+// Up to 16 rows of x, plain ones rounded here: b is read once, and that is the time.  A workgroup takes 32 rows of b, its NW waves the steps in turn; a
+// lane's block of x is 32 adjacent entries, so that its scale needs no other lane.
+template <class T, int FORM, int NW, bool PLAIN>
+__global__ void __launch_bounds__(64 * NW) k_mx_few_rows(MxProduct m) {
+  constexpr int kAhead = 2;
+  __shared__ v4f part[NW][2][64];
+  const Product &p = m.p;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, i = lane & 15, g = lane >> 4;
+  const int j0 = (int)(m.first + blockIdx.x) * 32;
+  const long long groups = ((long long)p.n + 63) / 64, row_bytes = (long long)m.steps * 128;
+  const u8 *b[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int j = j0 + (i >> 2) * 8 + h * 4 + (i & 3);
+    b[h] = m.b + (long long)(j < p.n ? j : p.n - 1) * row_bytes + g * 16;
+  }
+  const u8 *sb = m.b_scales + (long long)(j0 / 64) * 256 + lane * 4 + (j0 & 32 ? 2 : 0);
+  const u8 *a = PLAIN ? nullptr : m.a + (long long)(i < p.m ? i : 0) * row_bytes + g * 16;
+  const u8 *sa = PLAIN ? nullptr : m.a_scales + scale_place(i, g);
+  const T *x = static_cast<const T *>(m.x) + (long long)(i < p.m ? i : 0) * m.ldx;
+  v4f c[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+  for (int t0 = wave; t0 < m.steps; t0 += NW * kAhead) {
+    v4u fb[kAhead][2][2], fa[kAhead][2];
+    u32 qb[kAhead][2], qa[kAhead][2];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int t = t0 + u * NW;
+      if (t < m.steps)
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) __builtin_memcpy(&fb[u][s][h], b[h] + (long long)t * 128 + s * 64, 16);
+          unsigned short w;
+          __builtin_memcpy(&w, sb + (2ll * t + s) * groups * 256, 2);
+          qb[u][s] = w;
+          if constexpr (!PLAIN) {
+            __builtin_memcpy(&fa[u][s], a + (long long)t * 128 + s * 64, 16);
+            qa[u][s] = sa[(2ll * t + s) * 256];   // up to 16 rows: one group
+          }
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int t = t0 + u * NW;
+      if (t >= m.steps) break;
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        if constexpr (PLAIN) {
+          const long long l = (long long)t * kMxStep + s * 128 + g * 32;
+          Eight<T> e[4];
+          u32 most = 0;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const long long left = p.k - l - 8 * k;
+            e[k].load(x + l + 8 * k, i < p.m ? (left < 8 ? (int)left : 8) : 0);
+          }
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const u32 one = most_of(e[k]);
+            most = most > one ? most : one;
+          }
+          qa[u][s] = scale_byte(most, false);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) fa[u][s][k] = qa[u][s] == 255u ? 0u : codes_nearest(e[k], scale_of(qa[u][s]));
+        } else if (i >= p.m) {
+          fa[u][s] = v4u{0, 0, 0, 0};
+        }
+        c[0] = multiply_blocks<0, 0>(fb[u][s][0], fa[u][s], c[0], qb[u][s], qa[u][s]);
+        c[1] = multiply_blocks<1, 0>(fb[u][s][1], fa[u][s], c[1], qb[u][s], qa[u][s]);
+      }
+    }
+  }
+  part[wave][0][lane] = c[0];
+  part[wave][1][lane] = c[1];
+  __syncthreads();
+  // the sum of row i and column 8 g + 4 h + r of the 32 lies in lane 16 g + i of half h, place r
+  const int row = (int)threadIdx.x / 4, q = threadIdx.x & 3, j = j0 + q * 8;
+  if (row < p.m && row < 16 && j < p.n) {
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      v[e] = part[0][e / 4][q * 16 + row][e & 3];
+#pragma unroll
+      for (int w = 1; w < NW; ++w) v[e] = v[e] + part[w][e / 4][q * 16 + row][e & 3];
+    }
+    by_activation<FORM>(p.activation, [&](auto act) {
+      Beside<T, FORM, decltype(act)::value> beside;
+      beside.load(p, row, j, p.n - j);
+      finish(p, beside, row, j, p.n - j, v);
+    });
+  }
+}
+
+enum Tile { kFewRows, kTile64, kTile128 };
+struct Plan {
+  Tile tile;
+  int tiles_m, tiles_n, splits, steps_each;
+};
+
+constexpr int kCus = 256;
+
+// What a cut would take, in us: the matrix cores' rate in whole tiles, a step's least time, a tile's start and end, the join of splits.
+double time_of(const Product &p, int bm, int bn, int a_cu, double rate, long long tiles, int steps, int splits) {
+  const int steps_each = (steps + splits - 1) / splits;
+  const double one = 2.0 * bm * bn * kMxStep / (rate / kCus) * 1e6;
+  long long left = tiles * splits;
+  double us = 0.0;
+  while (left > 0) {
+    const long long now = left < (long long)a_cu * kCus ? left : (long long)a_cu * kCus, rounds = left / now;
+    const int sharing = (int)((now + kCus - 1) / kCus);
+    const double step = sharing * one;
+    us += (double)rounds * (2.0 + steps_each * (step > 0.4 ? step : 0.4));
+    left -= rounds * now;
+  }
+  if (splits > 1) us += 5.0 + 0.4 * splits + (double)splits * p.m * p.n * 8.0 / 4e6;
+  return us;
+}
+
+Plan plan_of(const MxProduct &m) {
+  const Product &p = m.p;
+  Plan q = {};
+  q.splits = 1;
+  if (p.m == 0 || p.n == 0) return q;
+  if (mx_takes_plain_rows(p)) {
+    q.tile = kFewRows, q.tiles_m = 1, q.tiles_n = (p.n + 31) / 32;
+    return q;
+  }
+  const struct { Tile tile; int side, a_cu; double rate; } cuts[] = {{kTile64, 64, 2, 1500e12}, {kTile128, 128, 2, 2500e12}};
+  const int steps = m.steps > 0 ? m.steps : 1;
+  double least = 0.0;
+  int side = 0;
+  for (const auto &c : cuts) {
+    const long long n = ((p.m + c.side - 1ll) / c.side) * ((p.n + c.side - 1ll) / c.side);
+    for (int splits = 1; splits == 1 || (splits <= 64 && splits * 2 <= steps && n * splits <= c.a_cu * kCus); ++splits) {
+      const double us = time_of(p, c.side, c.side, c.a_cu, c.rate, n, steps, splits);
+      if (least == 0.0 || us < least) least = us, q.tile = c.tile, q.splits = splits, side = c.side;
+    }
+  }
+  q.tiles_m = (int)((p.m + side - 1ll) / side), q.tiles_n = (int)((p.n + side - 1ll) / side);
+  q.steps_each = (steps + q.splits - 1) / q.splits;
+  q.splits = (steps + q.steps_each - 1) / q.steps_each;
+  return q;
+}
+
+template <class T, int FORM, int BM, int BN, int WM, int WN>
+void launch_tiles(const MxProduct &m, const Plan &q, hipStream_t s) {
+  constexpr int WG = 64 * WM * WN;
+  in_launches(m, (long long)q.tiles_m * q.tiles_n, WG, [&](const MxProduct &part, unsigned x) {
+    k_mx_product<T, FORM, BM, BN, WM, WN><<<dim3(x, (unsigned)q.splits), WG, 0, s>>>(part, q.tiles_m, q.tiles_n, q.steps_each);
+  });
+}
+
+template <class T, int FORM>
+void launch(const MxProduct &m, const Plan &q, hipStream_t s) {
+  switch (q.tile) {
+    case kFewRows:
+      if constexpr (FORM != kProductColumns) {
+        // with few workgroups more waves each
+        const bool many = q.tiles_n >= 4 * kCus;
+        const auto go = [&](auto plain) {
+          constexpr bool kPlain = decltype(plain)::value;
+          if (many) in_launches(m, q.tiles_n, 256, [&](const MxProduct &part, unsigned grid) { k_mx_few_rows<T, FORM, 4, kPlain><<<dim3(grid), 256, 0, s>>>(part); });
+          else k_mx_few_rows<T, FORM, 16, kPlain><<<dim3((unsigned)q.tiles_n), 1024, 0, s>>>(m);
+        };
+        if (m.a) go(std::false_type());
+        else go(std::true_type());
+      }
+      return;
+    case kTile64: launch_tiles<T, FORM, 64, 64, 2, 2>(m, q, s); break;
+    case kTile128: launch_tiles<T, FORM, 128, 128, 2, 2>(m, q, s); break;
+  }
+  if (q.splits > 1) {
+    const long long blocks = (long long)m.p.m * ((m.p.n + 7) / 8), groups = (blocks + 255) / 256;
+    k_join<T, FORM><<<dim3((unsigned)(groups < 4 * kCus ? groups : 4 * kCus)), 256, 0, s>>>(m.p, q.splits);
+  }
+}
+
+template <class T>
+void launch(const MxProduct &m, const Plan &q, hipStream_t s) {
+  if (m.p.form == kProductRows) launch<T, kProductRows>(m, q, s);
+  else launch<T, kProductMixed>(m, q, s);
+}
+
+}  // namespace
+
+bool mx_takes_plain_rows(const Product &p) { return p.form != kProductColumns && p.m <= 16; }
+
+size_t mx_product_scratch(const MxProduct &m) {
+  const Plan q = plan_of(m);
+  return q.splits < 2 ? 0 : sizeof(float) * (size_t)q.splits * (size_t)m.p.m * m.p.n;
+}
+
+hipError_t launch_mx_product(const MxProduct &call, hipStream_t s) {
+  MxProduct m = call;
+  const Plan q = plan_of(m);
+  if ((long long)q.tiles_m * q.tiles_n > 0x7fffffffll) return hipErrorInvalidValue;
+  if (q.splits < 2) m.p.partial = nullptr;
+  if (m.p.form == kProductColumns) launch<float, kProductColumns>(m, q, s);
+  else if (m.p.type == kF32) launch<float>(m, q, s);
+  else launch<bf16>(m, q, s);
+  return hipGetLastError();
+}
+
+}  // namespace qoda

@@ -209,12 +209,22 @@ class _NotRecorded(torch.autograd.Function):
         raise RuntimeError(ctx.said)
 
 
+def _tangents(inputs) -> bool:
+    level = torch.autograd.forward_ad
+    return level._current_level >= 0 and any(level.unpack_dual(t).tangent is not None for t in inputs)
+
+
+def _followed(inputs) -> bool:
+    """Whether torch is to differentiate by one of a call's inputs."""
+    inputs = [t for t in inputs if isinstance(t, torch.Tensor)]
+    return _tangents(inputs) or (torch.is_grad_enabled() and any(t.requires_grad for t in inputs))
+
+
 def _unless_followed(name: str, gradient: str, inputs, call):
     """The outputs of ``call`` if torch is to differentiate by one of its inputs, otherwise None."""
     inputs = [t for t in inputs if isinstance(t, torch.Tensor)]
     said = f"{name} records nothing for torch's differentiation: its gradient is {gradient}"
-    level = torch.autograd.forward_ad
-    if level._current_level >= 0 and any(level.unpack_dual(t).tangent is not None for t in inputs):
+    if _tangents(inputs):
         raise RuntimeError(said)
     if torch.is_grad_enabled() and any(t.requires_grad for t in inputs):
         return _NotRecorded.apply(said, call, *inputs)
