@@ -1,7 +1,7 @@
 /*
  * qoda_matrices.h -- C ABI of what is done with a model's matrices in a round, on MI355X (gfx950): rounding to four bits with a shared
- * scale for every 32 entries (microscaled floating point), and products between such matrices with the epilogues of qoda_operators.h and
- * both gradients.  Exported by libqoda beside the calls of qoda.h
+ * scale for every 32 entries (microscaled floating point), products between such matrices with the epilogues of qoda_operators.h and
+ * both gradients, and the orthogonalisation of an update by Newton-Schulz products.  Exported by libqoda beside the calls of qoda.h
  * and qoda_operators.h; the conventions of qoda_operators.h hold (no context, nothing allocated, only kernels enqueued, errors by code and
  * qoda_operator_error(), sizes of zero, strides, any number of host threads, capture into graphs).
  *
@@ -96,6 +96,26 @@ int64_t qoda_mx_linear_weight_grad_workspace_bytes(const qoda_mx_linear_weight_g
 int qoda_mx_linear(const qoda_mx_linear_args *a, void *workspace, size_t workspace_bytes, void *stream);
 int qoda_mx_linear_input_grad(const qoda_mx_linear_input_grad_args *a, void *workspace, size_t workspace_bytes, void *stream);
 int qoda_mx_linear_weight_grad(const qoda_mx_linear_weight_grad_args *a, void *workspace, size_t workspace_bytes, void *stream);
+
+/* x = the orthogonalised g, matrix by matrix of a batch: entry (n, i, j) is data[n * batch_stride + i * row_stride + j].
+ *   X_0 = g / (|g| + eps), |g| the root of the sum of squares;  A = X X^T,  X <- a X + (b A + c A A) X, steps times;
+ * where g has more rows than columns X^T takes X's place, with the same result.  Accurate as fp32 products are: entries that the matrix cores take are
+ * pairs of fp16 numbers, of 22 bits.  a, b, c are finite, and the singular values stay below 2^40 for every g (a bound from a, b and c; otherwise
+ * QODA_EINVAL).  The smaller side is at most 2^17, the larger at most 2^22.  x may be g itself.  A matrix with an infinity or a NaN becomes NaN throughout, if steps > 0. */
+typedef struct {
+  void *data;
+  int64_t matrix, row; /* entries from one matrix, and from one row, to the next */
+} qoda_matrices;
+
+typedef struct {
+  int32_t dtype, steps;
+  int64_t matrices, rows, cols;
+  qoda_matrices g, x;
+  double a, b, c, eps;
+} qoda_orthogonalize_args;
+
+int64_t qoda_orthogonalize_workspace_bytes(const qoda_orthogonalize_args *a);
+int qoda_orthogonalize(const qoda_orthogonalize_args *a, void *workspace, size_t workspace_bytes, void *stream);
 
 #ifdef __cplusplus
 }

@@ -10,7 +10,7 @@ import warnings
 _HERE = os.path.dirname(os.path.abspath(__file__))
 SOURCES = [os.path.join(_HERE, "csrc", f) for f in ("qoda_kernels.hip", "qoda_api.hip", "qoda_linear.hip", "qoda_dropout.hip",
                                                      "qoda_group_norm.hip", "qoda_operators_api.hip", "qoda_mx_quantize.hip", "qoda_mx_product.hip",
-                                                     "qoda_matrices_api.hip")]
+                                                     "qoda_orthogonal.hip", "qoda_matrices_api.hip")]
 LIB = os.path.join(_HERE, "libqoda.so")
 PROBE_SRC = os.path.join(_HERE, "harness", "qoda_probe.hip")
 TORCH_SRC = os.path.join(_HERE, "csrc", "qoda_torch.cpp")

@@ -32,6 +32,38 @@ struct MxProduct {
   long long first;
 };
 
+// Matrices g [rows][cols]; X [m][n] is g or its transpose, m <= n, both sides filled up to multiples of 32.
+struct Orthogonal {
+  int type, steps, transposed, parts;
+  long long matrices, rows, cols, m, n;
+  const void *g;
+  void *x;
+  long long g_matrix, g_row, x_matrix, x_row;
+  double a, b, c, eps;
+  double *squares;   // [matrices][parts]
+  void *xs, *xt;     // X and its transpose in pairs of fp16
+  float scale;
+  long long first;
+};
+
+// out = a b^T factor + e extra of matrices of pairs, a [m][k], b [n][k], e and out [m][n], out_t [n][m] the transpose of out; x: where the result goes
+// instead, in the caller's type.  symmetric: m = n and out = out_t, of which the tiles above the diagonal are computed.
+struct PairProduct {
+  int symmetric, type, x_transposed;
+  long long matrices, m, n, k;
+  const void *a, *b, *e;
+  void *out, *out_t, *x;
+  long long x_matrix, x_row, x_rows, x_cols;
+  float factor, extra;
+  float *partial;   // of split sums: [splits][matrices][m][n]
+  long long first;
+};
+
+bool orthogonal_bounded(double a, double b, double c, int steps);
+void orthogonal_sides(Orthogonal *o);
+size_t orthogonal_scratch(const Orthogonal &o);
+hipError_t launch_orthogonalize(const Orthogonal &o, void *workspace, hipStream_t s);
+
 hipError_t launch_mx_quantize(const MxRounding &q, hipStream_t s);
 hipError_t launch_mx_values(const MxRounding &q, hipStream_t s);
 hipError_t launch_mx_row_sums(const u8 *codes, const u8 *scales, long long rows, long long cols, float *sums, bool accumulate, hipStream_t s);

@@ -160,6 +160,45 @@ int run(const char *call, MxProduct *m, void *workspace, size_t bytes, void *str
   return done(call, launch_mx_product(*m, static_cast<hipStream_t>(stream)));
 }
 
+constexpr int64_t kMostLeast = 1 << 17, kMostSideOfUpdate = 1 << 22;   // 32-bit offsets inside a tile, and numbers of tiles
+
+int check_matrices(const char *call, const char *name, const qoda_matrices &v, int64_t n, int64_t rows, int64_t cols, size_t bytes, long long *row, long long *matrix) {
+  *row = rows > 1 ? v.row : cols;   // a stride that no entry is reached by is not looked at
+  *matrix = n > 1 ? v.matrix : 0;
+  if (!v.data) return fail(QODA_EINVAL, "%s: %s is null", call, name);
+  if (!aligned(v.data, bytes)) return fail(QODA_EINVAL, "%s: %s is not aligned to its entries", call, name);
+  if (*row < cols || *row >= kMostStride || (n > 1 && (*matrix < (__int128)(rows - 1) * *row + cols || *matrix >= kMostStride * 1024)))
+    return fail(QODA_EINVAL, "%s: the strides of %s do not fit matrices of %lld rows and %lld columns", call, name, (long long)rows, (long long)cols);
+  return QODA_OK;
+}
+
+int orthogonal_of(const qoda_orthogonalize_args *a, Orthogonal *o) {
+  const char *call = "qoda_orthogonalize";
+  if (!a) return fail(QODA_EINVAL, "%s: null arguments", call);
+  TRY(check_type(call, a->dtype));
+  TRY(check_sides(call, a->matrices, a->rows, a->cols));
+  if (a->steps < 0) return fail(QODA_EINVAL, "%s: %d steps", call, a->steps);
+  if (!(a->eps >= 0.0) || !std::isfinite(a->eps)) return fail(QODA_EINVAL, "%s: eps = %g", call, a->eps);
+  if (!std::isfinite(a->a) || !std::isfinite(a->b) || !std::isfinite(a->c) || !orthogonal_bounded(a->a, a->b, a->c, a->steps))
+    return fail(QODA_EINVAL, "%s: %d steps with the coefficients %g, %g, %g may leave 2^40", call, a->steps, a->a, a->b, a->c);
+  *o = {};
+  o->type = a->dtype, o->steps = a->steps;
+  o->matrices = a->matrices, o->rows = a->rows, o->cols = a->cols;
+  if (a->matrices == 0 || a->rows == 0 || a->cols == 0) return QODA_OK;
+  const int64_t least = a->rows < a->cols ? a->rows : a->cols, most = a->rows < a->cols ? a->cols : a->rows;
+  if (least > kMostLeast || most > kMostSideOfUpdate)
+    return fail(QODA_EINVAL, "%s: sides of %lld and %lld; %lld and %lld at most", call, (long long)least, (long long)most, (long long)kMostLeast, (long long)kMostSideOfUpdate);
+  const size_t e = entry_bytes(a->dtype);
+  TRY(check_matrices(call, "g", a->g, a->matrices, a->rows, a->cols, e, &o->g_row, &o->g_matrix));
+  TRY(check_matrices(call, "x", a->x, a->matrices, a->rows, a->cols, e, &o->x_row, &o->x_matrix));
+  o->g = a->g.data, o->x = a->x.data;
+  o->a = a->a, o->b = a->b, o->c = a->c, o->eps = a->eps;
+  orthogonal_sides(o);
+  return QODA_OK;
+}
+
+bool nothing(const Orthogonal &o) { return o.matrices == 0 || o.rows == 0 || o.cols == 0; }
+
 }  // namespace
 
 extern "C" {
@@ -219,6 +258,20 @@ int qoda_mx_linear_weight_grad(const qoda_mx_linear_weight_grad_args *a, void *w
   TRY(run(call, &m, workspace, workspace_bytes, stream));
   if (!a->dbias || a->out == 0) return QODA_OK;
   return done(call, launch_mx_row_sums(m.a, m.a_scales, a->out, a->rows, a->dbias, a->accumulate != 0, static_cast<hipStream_t>(stream)));
+}
+
+int64_t qoda_orthogonalize_workspace_bytes(const qoda_orthogonalize_args *a) {
+  Orthogonal o;
+  const int rc = orthogonal_of(a, &o);
+  return rc != QODA_OK ? rc : nothing(o) ? 0 : (int64_t)orthogonal_scratch(o);
+}
+
+int qoda_orthogonalize(const qoda_orthogonalize_args *a, void *workspace, size_t workspace_bytes, void *stream) {
+  Orthogonal o;
+  TRY(orthogonal_of(a, &o));
+  if (nothing(o)) return QODA_OK;
+  TRY(check_workspace("qoda_orthogonalize", workspace, workspace_bytes, orthogonal_scratch(o)));
+  return done("qoda_orthogonalize", launch_orthogonalize(o, workspace, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -1,0 +1,565 @@
+// Orthogonalisation of updates by Newton-Schulz products, of include/qoda_matrices.h: X <- a X + (b A + c A A) X with A = X X^T.
+//
+// Small singular values grow by a in every step, and so do the errors of what they came from: sums of fp16 or bf16 products would leave them wrong in the
+// second digit.  A number is therefore a pair of fp16 numbers, high + low, of 22 bits, and a product three matrix instructions: high high, high low and
+// low high, summed in fp32.  Matrices are scaled by powers of two that the polynomial's bound on the singular values allows, so that the low parts are
+// no subnormal numbers where they matter.
+//
+// The work is done on X [m][n] with m <= n (g, or its transpose).  Every product is of rows with rows: X is kept beside its transpose, and A and
+// B = b A + c A A are symmetric, so that half of their tiles are computed and stored twice.  In memory 32 high parts of a row are followed by their low
+// parts, 128 bytes, which is a step along l in shared memory, as in qoda_linear.hip.  Sides are filled up to multiples of 32 with zeros.
+
+#include <cmath>
+
+#include "qoda_matrices.h"
+#include "qoda_product_device.h"
+
+namespace qoda {
+
+namespace {
+
+typedef _Float16 v8h __attribute__((ext_vector_type(8)));
+
+constexpr int kWg = 256;
+typedef unsigned short half_bits;
+
+__host__ __device__ inline long long up32(long long v) { return (v + 31) & ~31ll; }
+
+// Eight adjacent entries of a row of pairs, from column j (a multiple of 8) on; ld: entries of a row.
+__device__ __forceinline__ char *pair_place(void *base, long long ld, long long i, int j) {
+  return static_cast<char *>(base) + i * ld * 4 + (j >> 5) * 128 + (j & 31) * 2;
+}
+__device__ __forceinline__ void store_pairs(char *p, const float (&v)[8]) {
+  v8h hi, lo;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    hi[e] = (_Float16)v[e];
+    lo[e] = (_Float16)(v[e] - (float)hi[e]);
+  }
+  __builtin_memcpy(p, &hi, 16);
+  __builtin_memcpy(p + 64, &lo, 16);
+}
+__device__ __forceinline__ void load_pairs(const char *p, float (&v)[8]) {
+  v8h hi, lo;
+  __builtin_memcpy(&hi, p, 16);
+  __builtin_memcpy(&lo, p + 64, 16);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = (float)hi[e] + (float)lo[e];
+}
+
+// The sums of squares of a matrix in parts, each by a workgroup, in 64 bits.
+template <class T>
+__global__ void __launch_bounds__(kWg) k_squares(Orthogonal o) {
+  __shared__ double part[kWg / 64];
+  const long long id = o.first + blockIdx.x, matrix = id / o.parts;
+  const int p = (int)(id - matrix * o.parts);
+  const T *g = static_cast<const T *>(o.g) + matrix * o.g_matrix;
+  const long long eights = (o.cols + 7) / 8, total = o.rows * eights;
+  double sum = 0.0;
+  for (long long q = (long long)p * kWg + threadIdx.x; q < total; q += (long long)o.parts * kWg) {
+    const long long r = q / eights, c = (q - r * eights) * 8;
+    float v[8];
+    load8(g + r * o.g_row + c, o.cols - c < 8 ? (int)(o.cols - c) : 8, v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum = sum + (double)v[e] * (double)v[e];
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) sum = sum + __shfl_xor(sum, d);
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) o.squares[id] = (part[0] + part[1]) + (part[2] + part[3]);
+}
+
+// 1 / (|g| + eps) of a matrix, from the parts' sums in their order.
+__device__ __forceinline__ double inverse_norm(const Orthogonal &o, long long matrix) {
+  double sum = 0.0;
+  for (int p = (int)(threadIdx.x & 63); p < o.parts; p += 64) sum = sum + o.squares[matrix * o.parts + p];
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) sum = sum + __shfl_xor(sum, d);
+  return 1.0 / (sqrt(sum) + o.eps);
+}
+
+// X_0, scaled, and its transpose from g: 64 x 64 entries a workgroup, by way of shared memory.  STEPS false: nothing else is to be done, and x receives X_0.
+template <class T, bool STEPS>
+__global__ void __launch_bounds__(kWg) k_start(Orthogonal o, long long tiles_r, long long tiles_c) {
+  __shared__ float tile[64][65];
+  const long long id = o.first + blockIdx.x, each = tiles_r * tiles_c, matrix = id / each, in = id - matrix * each;
+  const long long r0 = in / tiles_c * 64, c0 = (in - in / tiles_c * tiles_c) * 64;
+  const double inverse = inverse_norm(o, matrix) * (STEPS ? (double)o.scale : 1.0);
+  const T *g = static_cast<const T *>(o.g) + matrix * o.g_matrix;
+  const int t = threadIdx.x, chunk = (t & 7) * 8;
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int row = u * 32 + (t >> 3);
+    const long long r = r0 + row, c = c0 + chunk;
+    float v[8];
+    load8(g + r * o.g_row + c, r < o.rows ? (o.cols - c < 8 ? (int)(o.cols - c) : 8) : 0, v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = (float)((double)v[e] * inverse);
+    if constexpr (STEPS) {
+      if (r >= o.rows || c + 7 >= o.cols)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (r >= o.rows || c + e >= o.cols) v[e] = 0.0f;   // filled up, also where the inverse is no number
+      const long long pad_r = up32(o.rows), pad_c = up32(o.cols);
+      char *rows_of = static_cast<char *>(o.transposed ? o.xt : o.xs) + matrix * o.m * o.n * 4;
+      if (r < pad_r && c < pad_c) store_pairs(pair_place(rows_of, pad_c, r, (int)c), v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) tile[row][chunk + e] = v[e];
+    } else if (r < o.rows && c < o.cols) {
+      store8(static_cast<T *>(o.x) + matrix * o.x_matrix + r * o.x_row + c, o.cols - c < 8 ? (int)(o.cols - c) : 8, v);
+    }
+  }
+  if constexpr (STEPS) {
+    __syncthreads();
+    char *columns_of = static_cast<char *>(o.transposed ? o.xs : o.xt) + matrix * o.m * o.n * 4;
+    const long long pad_r = up32(o.rows), pad_c = up32(o.cols);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int row = u * 32 + (t >> 3);
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = tile[chunk + e][row];
+      if (c0 + row < pad_c && r0 + chunk < pad_r) store_pairs(pair_place(columns_of, pad_r, c0 + row, (int)(r0 + chunk)), v);
+    }
+  }
+}
+
+// What becomes of eight sums adjacent in a row: v = sums * factor + what E has there * extra, which is then stored as T's or as pairs.
+struct Place {
+  const PairProduct &p;
+  long long matrix;
+  __device__ __forceinline__ void finish(int i, int j, float (&v)[8]) const {
+    if (p.e) {
+      float was[8];
+      load_pairs(pair_place(const_cast<char *>(static_cast<const char *>(p.e) + matrix * p.m * p.n * 4), p.n, i, j), was);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = __builtin_fmaf(was[e], p.extra, v[e] * p.factor);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = v[e] * p.factor;
+    }
+  }
+  template <class T>
+  __device__ __forceinline__ void plain(long long i, long long j, const float (&v)[8]) const {
+    if (i < p.x_rows && j < p.x_cols) store8(static_cast<T *>(p.x) + matrix * p.x_matrix + i * p.x_row + j, p.x_cols - j < 8 ? (int)(p.x_cols - j) : 8, v);
+  }
+  // row i of the result from column j on
+  __device__ __forceinline__ void row(int i, int j, const float (&v)[8]) const {
+    if (p.x) {
+      if (!p.x_transposed) p.type == kF32 ? plain<float>(i, j, v) : plain<bf16>(i, j, v);
+    } else {
+      store_pairs(pair_place(static_cast<char *>(p.out) + matrix * p.m * p.n * 4, p.n, i, j), v);
+    }
+  }
+  // row j of its transpose, from column i on
+  __device__ __forceinline__ void column(int i, int j, const float (&v)[8]) const {
+    if (p.x) {
+      if (p.x_transposed) p.type == kF32 ? plain<float>(j, i, v) : plain<bf16>(j, i, v);
+    } else {
+      store_pairs(pair_place(static_cast<char *>(p.out_t) + matrix * p.m * p.n * 4, p.m, j, i), v);
+    }
+  }
+  __device__ __forceinline__ bool columns_wanted() const { return p.x ? p.x_transposed != 0 : p.out_t != nullptr; }
+};
+
+// Tile `at` of a symmetric product: those with tm <= tn, column by column.
+__device__ __forceinline__ void upper_tile(int at, int &tm, int &tn) {
+  int n = (int)((sqrtf(8.0f * (float)at + 1.0f) - 1.0f) * 0.5f);
+  while ((long long)n * (n + 1) / 2 > at) --n;
+  while ((long long)(n + 1) * (n + 2) / 2 <= at) ++n;
+  tn = n, tm = at - (int)((long long)n * (n + 1) / 2);
+}
+
+__device__ __forceinline__ v4f multiply_halves(v4u b, v4u a, v4f c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, b), __builtin_bit_cast(v8h, a), c, 0, 0, 0);
+}
+
+// c = a b^T of matrices of pairs, [m][k] and [n][k].
+template <int BM, int BN, int WM, int WN>
+__global__ void __launch_bounds__(64 * WM * WN, BM == 128 ? 2 : 1) k_pair_product(PairProduct p, int tiles_m, int tiles_n, int steps_each) {
+  constexpr int WG = 64 * WM * WN, FM = BM / WM / 16, FN = BN / WN / 32, kSide = BM / WM < 64 ? BM / WM : 64, kRow = kSide + 4;
+  typedef Operand<bf16, true, 0, BM, WG, true> A;   // entries of 16 bits: 32 high parts and their 32 low parts are a step
+  typedef Operand<bf16, true, 1, BN, WG, true> B;
+  constexpr int kTiles = 2 * (BM + BN) * kStepBytes;
+  static_assert(WM * WN * 32 * kRow * 4 <= kTiles, "the transposing end fits");
+  __shared__ __align__(16) char shared[kTiles];
+
+  const int each = p.symmetric ? tiles_m * (tiles_m + 1) / 2 : tiles_m * tiles_n;
+  const long long id = p.first + blockIdx.x;
+  const int matrix = __builtin_amdgcn_readfirstlane((int)(id / each)), in = (int)(id - (long long)matrix * each);
+  int tm, tn;
+  if (p.symmetric) upper_tile(in, tm, tn);
+  else tile_of(in, tiles_m, tiles_n, tm, tn);
+  tm = __builtin_amdgcn_readfirstlane(tm), tn = __builtin_amdgcn_readfirstlane(tn);
+  const int i0 = tm * BM, j0 = tn * BN;
+  const int all = (int)(p.k / 32), step0 = (int)blockIdx.y * steps_each, steps = all - step0 < steps_each ? all - step0 : steps_each;
+  A a;
+  B b;
+  a.start(static_cast<const char *>(p.a) + (long long)matrix * p.m * p.k * 4, p.k * 2, i0, (int)p.m, step0 * 64, steps * 64);
+  b.start(static_cast<const char *>(p.b) + (long long)matrix * p.n * p.k * 4, p.k * 2, j0, (int)p.n, step0 * 64, steps * 64);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
+
+  v4f c[FM][2 * FN];
+#pragma unroll
+  for (int x = 0; x < FM; ++x)
+#pragma unroll
+    for (int y = 0; y < 2 * FN; ++y) c[x][y] = v4f{0, 0, 0, 0};
+
+  const lds_ptr base = (lds_ptr)shared;
+  const lds_ptr ta[2] = {base, base + BM * kStepBytes}, tb[2] = {base + 2 * BM * kStepBytes, base + (2 * BM + BN) * kStepBytes};
+  typedef v4u PiecesA[FM];
+  typedef v4u PiecesB[2 * FN];
+  u32 key_a = A::lane_key(wm), key_b = B::lane_key(wn);
+  const auto read_a = [&](PiecesA &f, int h, int s) {
+    asm volatile("" : "+v"(key_a));   // made anew each time, as in k_product
+#pragma unroll
+    for (int x = 0; x < FM; ++x) f[x] = A::piece(ta[h], key_a, wm, x * 16, 0, s);
+  };
+  const auto read_b = [&](PiecesB &f, int h, int s) {
+    asm volatile("" : "+v"(key_b));
+#pragma unroll
+    for (int y = 0; y < 2 * FN; ++y) f[y] = B::piece(tb[h], key_b, wn, y / 2 * 32, y & 1, s);
+  };
+  const auto multiply_all = [&](const PiecesA &fa, const PiecesB &fb) {
+#pragma unroll
+    for (int x = 0; x < FM; ++x)
+#pragma unroll
+      for (int y = 0; y < 2 * FN; ++y) c[x][y] = multiply_halves(fb[y], fa[x], c[x][y]);
+  };
+  const auto request = [&](int t, int h) {
+    a.direct(t * 64, ta[h]);
+    b.direct(t * 64, tb[h]);
+  };
+  PiecesA a_hi, a_lo;
+  PiecesB b_hi, b_lo;
+  request(0, 0);
+  if (steps > 1) request(1, 1);
+  arrived();
+  read_a(a_hi, 0, 0);
+  read_b(b_hi, 0, 0);
+  for (int t = 0; t < steps; t += 2) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      if (t + h < steps) {
+        read_b(b_lo, h, 1);
+        read_a(a_lo, h, 1);
+        multiply_all(a_hi, b_hi);
+        arrived();   // the next step is there, and nobody reads this one any more
+        if (t + h + 2 < steps) request(t + h + 2, h);
+        multiply_all(a_hi, b_lo);
+        if (t + h + 1 < steps) read_a(a_hi, 1 - h, 0);
+        multiply_all(a_lo, b_hi);
+        if (t + h + 1 < steps) read_b(b_hi, 1 - h, 0);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+  }
+
+  const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+  const auto row = [&](int x) { return i0 + wm + x * 16 + i; };
+  const auto column = [&](int y) { return j0 + wn + y * 32 + g * 8; };
+  const auto sums = [&](int x, int y, float (&v)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = c[x][2 * y + e / 4][e & 3];
+  };
+  if (p.partial) {
+    float *to = p.partial + ((long long)blockIdx.y * p.matrices + matrix) * p.m * p.n;
+#pragma unroll
+    for (int x = 0; x < FM; ++x)
+#pragma unroll
+      for (int y = 0; y < FN; ++y)
+        if (row(x) < p.m && column(y) < p.n) {
+          float v[8];
+          sums(x, y, v);
+          store8<true>(to + (long long)row(x) * p.n + column(y), 8, v);
+        }
+    return;
+  }
+  const Place place{p, matrix};
+  const bool columns = place.columns_wanted() && !(p.symmetric && tm == tn);
+  const lds_ptr mine = base + wave * 32 * kRow * 4;
+  __syncthreads();   // the tiles' memory is taken for the transposed result, a wave's own part of it
+#pragma unroll
+  for (int y = 0; y < FN; ++y)
+#pragma unroll
+    for (int x0 = 0; x0 < FM; x0 += kSide / 16) {
+#pragma unroll
+      for (int x = 0; x < kSide / 16; ++x) {
+        float v[8];
+        sums(x0 + x, y, v);
+        if (row(x0 + x) < p.m && column(y) < p.n) {
+          place.finish(row(x0 + x), column(y), v);
+          place.row(row(x0 + x), column(y), v);
+        }
+        if (columns)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) *LDS(float, mine + ((g * 8 + e) * kRow + x * 16 + i) * 4) = v[e];
+      }
+      if (columns) {
+        __builtin_amdgcn_wave_barrier();
+        constexpr int kChunks = kSide / 8;
+#pragma unroll
+        for (int u = 0; u < 32 * kChunks / 64; ++u) {
+          const int at = u * 64 + lane, jj = at / kChunks, ii = at % kChunks * 8;
+          float v[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = *LDS(float, mine + (jj * kRow + ii + e) * 4);
+          const int ci = i0 + wm + x0 * 16 + ii, cj = j0 + wn + y * 32 + jj;
+          if (ci < p.m && cj < p.n) place.column(ci, cj, v);
+        }
+        __builtin_amdgcn_wave_barrier();
+      }
+    }
+}
+
+// The splits' sums added up in their order, and finished: 64 x 64 entries a workgroup.
+__global__ void __launch_bounds__(kWg) k_pair_join(PairProduct p, int splits) {
+  __shared__ float tile[64][65];
+  const long long tiles_m = (p.m + 63) / 64, tiles_n = (p.n + 63) / 64, each = p.symmetric ? tiles_m * (tiles_m + 1) / 2 : tiles_m * tiles_n;
+  const long long id = p.first + blockIdx.x, matrix = id / each;
+  const int in = (int)(id - matrix * each);
+  int tm, tn;
+  if (p.symmetric) upper_tile(in, tm, tn);
+  else tm = (int)(in / tiles_n), tn = (int)(in - tm * tiles_n);
+  const Place place{p, matrix};
+  const bool columns = place.columns_wanted() && !(p.symmetric && tm == tn);
+  const int t = threadIdx.x, chunk = (t & 7) * 8;
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int row = u * 32 + (t >> 3), i = tm * 64 + row, j = tn * 64 + chunk;
+    float c[8] = {};
+    if (i < p.m && j < p.n) {
+      const float *from = p.partial + matrix * p.m * p.n + (long long)i * p.n + j;
+      const long long far = p.matrices * p.m * p.n;
+      for (int s = 0; s < splits; s += 4) {   // four on their way
+        Eight<float> part[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          if (s + q < splits) part[q].load<true>(from + (s + q) * far, 8);
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          if (s + q < splits) {
+            float v[8];
+            part[q].get(v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) c[e] = c[e] + v[e];
+          }
+      }
+      place.finish(i, j, c);
+      place.row(i, j, c);
+    }
+    if (columns)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) tile[row][chunk + e] = c[e];
+  }
+  if (!columns) return;
+  __syncthreads();
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int row = u * 32 + (t >> 3);
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = tile[chunk + e][row];
+    const int i = tm * 64 + chunk, j = tn * 64 + row;
+    if (i < p.m && j < p.n) place.column(i, j, v);
+  }
+}
+
+constexpr int kCus = 256;
+
+enum Tile { kTile64, kTile128, kTile256 };
+struct Cut {
+  Tile tile;
+  int side, splits, steps_each;
+};
+
+long long tiles_of(const PairProduct &p, int side) {
+  const long long a = (p.m + side - 1) / side, b = (p.n + side - 1) / side;
+  return (p.symmetric ? a * (a + 1) / 2 : a * b) * p.matrices;
+}
+
+// The cut with the least estimated time: a tile's rate, its start and end, the join of splits.
+Cut cut_of(const PairProduct &p) {
+  const int steps = (int)(p.k / 32);
+  const struct { Tile tile; int side, a_cu; double rate; } cuts[] = {{kTile64, 64, 4, 300e12}, {kTile128, 128, 2, 380e12}, {kTile256, 256, 1, 420e12}};
+  Cut best = {};
+  double least = 0.0;
+  for (const auto &c : cuts) {
+    const long long tiles = tiles_of(p, c.side);
+    for (int splits = 1; splits == 1 || (splits <= 16 && splits * 4 <= steps && tiles * splits <= (long long)c.a_cu * kCus); ++splits) {
+      const int each = (steps + splits - 1) / splits;
+      const double one = 2.0 * c.side * c.side * 32.0 / (c.rate / kCus) * 1e6;
+      long long left = tiles * splits;
+      double us = 0.0;
+      while (left > 0) {
+        const long long now = left < (long long)c.a_cu * kCus ? left : (long long)c.a_cu * kCus, rounds = left / now;
+        const double step = (double)((now + kCus - 1) / kCus) * one;
+        us += (double)rounds * (3.0 + each * (step > 0.3 ? step : 0.3));
+        left -= rounds * now;
+      }
+      if (splits > 1) us += 5.0 + (double)splits * p.matrices * p.m * p.n * (p.symmetric ? 4.0 : 8.0) / 4e6;
+      if (least == 0.0 || us < least) least = us, best = {c.tile, c.side, splits, each};
+    }
+  }
+  best.splits = (steps + best.steps_each - 1) / best.steps_each;
+  return best;
+}
+
+template <int SIDE, int WM, int WN>
+void launch_tiles(const PairProduct &p, const Cut &c, hipStream_t s) {
+  const int tm = (int)((p.m + SIDE - 1) / SIDE), tn = (int)((p.n + SIDE - 1) / SIDE);
+  in_launches(p, tiles_of(p, SIDE), 64 * WM * WN, [&](const PairProduct &part, unsigned x) {
+    k_pair_product<SIDE, SIDE, WM, WN><<<dim3(x, (unsigned)c.splits), 64 * WM * WN, 0, s>>>(part, tm, tn, c.steps_each);
+  });
+}
+
+void launch_pairs(PairProduct p, float *partial, hipStream_t s) {
+  const Cut c = cut_of(p);
+  p.partial = c.splits > 1 ? partial : nullptr;
+  switch (c.tile) {
+    case kTile64: launch_tiles<64, 2, 2>(p, c, s); break;
+    case kTile128: launch_tiles<128, 2, 2>(p, c, s); break;
+    case kTile256: launch_tiles<256, 2, 4>(p, c, s); break;
+  }
+  if (c.splits > 1)
+    in_launches(p, tiles_of(p, 64), kWg, [&](const PairProduct &part, unsigned x) { k_pair_join<<<dim3(x), kWg, 0, s>>>(part, c.splits); });
+}
+
+// The three products of a step, without their operands' places.
+PairProduct shape_of(const Orthogonal &o, int which) {
+  PairProduct p = {};
+  p.matrices = o.matrices;
+  p.m = o.m, p.n = which == 2 ? o.n : o.m, p.k = which == 0 ? o.n : o.m;
+  p.symmetric = which != 2;
+  return p;
+}
+
+struct Layout {   // of the workspace, in bytes
+  size_t squares, xs, xt[2], a, b, partial, all;
+};
+Layout layout_of(const Orthogonal &o) {
+  Layout l = {};
+  size_t at = 0;
+  const auto take = [&](size_t bytes) {
+    const size_t here = at;
+    at += (bytes + 255) & ~(size_t)255;
+    return here;
+  };
+  l.squares = take(sizeof(double) * (size_t)o.matrices * o.parts);
+  if (o.steps > 0) {
+    const size_t wide = (size_t)o.matrices * o.m * o.n * 4, square = (size_t)o.matrices * o.m * o.m * 4;
+    l.xs = take(wide), l.xt[0] = take(wide), l.xt[1] = take(wide);
+    l.a = take(square), l.b = take(square);
+    size_t most = 0;
+    for (int w = 0; w < 3; ++w) {
+      const PairProduct p = shape_of(o, w);
+      const Cut c = cut_of(p);
+      const size_t bytes = c.splits > 1 ? (size_t)c.splits * p.matrices * p.m * p.n * 4 : 0;
+      most = bytes > most ? bytes : most;
+    }
+    l.partial = take(most);
+  }
+  l.all = at;
+  return l;
+}
+
+// The largest |a s + b s^3 + c s^5| for s in [0, most].
+double largest(double a, double b, double c, double most) {
+  const auto at = [&](double s) { return std::fabs(s * (a + s * s * (b + s * s * c))); };
+  double v = at(most);
+  const double d = 9.0 * b * b - 20.0 * a * c;   // of the slope a + 3 b u + 5 c u^2, u = s^2
+  double roots[2];
+  int n = 0;
+  if (c != 0.0) {
+    if (d >= 0.0) roots[n++] = (-3.0 * b + std::sqrt(d)) / (10.0 * c), roots[n++] = (-3.0 * b - std::sqrt(d)) / (10.0 * c);
+  } else if (b != 0.0) {
+    roots[n++] = -a / (3.0 * b);
+  }
+  for (int i = 0; i < n; ++i)
+    if (roots[i] > 0.0 && roots[i] < most * most) v = std::fmax(v, at(std::sqrt(roots[i])));
+  return v;
+}
+// ... and |b u + c u^2| for u in [0, most].
+double largest_inner(double b, double c, double most) {
+  const auto at = [&](double u) { return std::fabs(u * (b + c * u)); };
+  double v = at(most);
+  if (c != 0.0 && -b / (2.0 * c) > 0.0 && -b / (2.0 * c) < most) v = std::fmax(v, at(-b / (2.0 * c)));
+  return v;
+}
+
+constexpr double kLeast = 1.0 / (1ll << 40), kMost = (double)(1ll << 40);
+
+// The largest power of two whose product with numbers of this size fp16 holds, with room for their rounding.
+int exponent_for(double size) { return (int)std::floor(std::log2(60000.0 / std::fmax(size, kLeast))); }
+
+}  // namespace
+
+bool orthogonal_bounded(double a, double b, double c, int steps) {
+  double s = 1.0;
+  for (int k = 0; k < steps; ++k) {
+    if (largest_inner(b, c, s * s) > kMost) return false;
+    s = largest(a, b, c, s);
+    if (!(s <= kMost)) return false;
+    if (k > 200) return true;   // the bound does not grow any more, or has long been left
+  }
+  return true;
+}
+
+void orthogonal_sides(Orthogonal *o) {
+  o->transposed = o->rows > o->cols;
+  o->m = up32(o->transposed ? o->cols : o->rows), o->n = up32(o->transposed ? o->rows : o->cols);
+  const long long eights = o->rows * ((o->cols + 7) / 8), parts = (eights + kWg * 8 - 1) / (kWg * 8);
+  o->parts = (int)(parts < 1 ? 1 : parts > 256 ? 256 : parts);
+}
+
+size_t orthogonal_scratch(const Orthogonal &o) { return layout_of(o).all; }
+
+hipError_t launch_orthogonalize(const Orthogonal &call, void *workspace, hipStream_t s) {
+  Orthogonal o = call;
+  const Layout l = layout_of(o);
+  char *w = static_cast<char *>(workspace);
+  o.squares = reinterpret_cast<double *>(w + l.squares);
+  o.xs = w + l.xs, o.xt = w + l.xt[0];
+  double size = 1.0;
+  int ex = exponent_for(size);
+  o.scale = std::ldexp(1.0f, ex);
+  in_launches(o, o.matrices * o.parts, kWg, [&](const Orthogonal &part, unsigned x) {
+    if (o.type == kF32) k_squares<float><<<dim3(x), kWg, 0, s>>>(part);
+    else k_squares<bf16><<<dim3(x), kWg, 0, s>>>(part);
+  });
+  const long long tr = (o.rows + 63) / 64, tc = (o.cols + 63) / 64;
+  in_launches(o, o.matrices * tr * tc, kWg, [&](const Orthogonal &part, unsigned x) {
+    if (o.steps == 0) {
+      if (o.type == kF32) k_start<float, false><<<dim3(x), kWg, 0, s>>>(part, tr, tc);
+      else k_start<bf16, false><<<dim3(x), kWg, 0, s>>>(part, tr, tc);
+    } else {
+      if (o.type == kF32) k_start<float, true><<<dim3(x), kWg, 0, s>>>(part, tr, tc);
+      else k_start<bf16, true><<<dim3(x), kWg, 0, s>>>(part, tr, tc);
+    }
+  });
+  float *partial = reinterpret_cast<float *>(w + l.partial);
+  for (int k = 0; k < o.steps; ++k) {
+    const double next = largest(o.a, o.b, o.c, size);
+    const int ea = exponent_for(size * size), eb = exponent_for(largest_inner(o.b, o.c, size * size)), en = exponent_for(next);
+    const bool last = k + 1 == o.steps;
+    char *xt = w + l.xt[k & 1];
+    PairProduct p = shape_of(o, 0);   // A
+    p.a = p.b = o.xs, p.out = p.out_t = w + l.a;
+    p.factor = std::ldexp(1.0f, ea - 2 * ex);
+    launch_pairs(p, partial, s);
+    p = shape_of(o, 1);               // B = b A + c A A
+    p.a = p.b = p.e = w + l.a, p.out = p.out_t = w + l.b;
+    p.factor = (float)std::ldexp(o.c, eb - 2 * ea), p.extra = (float)std::ldexp(o.b, eb - ea);
+    launch_pairs(p, partial, s);
+    p = shape_of(o, 2);               // a X + B X
+    const int to = last ? 0 : en;
+    p.a = w + l.b, p.b = xt, p.e = o.xs, p.out = o.xs, p.out_t = w + l.xt[1 - (k & 1)];
+    p.factor = std::ldexp(1.0f, to - eb - ex), p.extra = (float)std::ldexp(o.a, to - ex);
+    if (last) p.x = o.x, p.x_matrix = o.x_matrix, p.x_row = o.x_row, p.x_rows = o.rows, p.x_cols = o.cols, p.x_transposed = o.transposed, p.type = o.type;
+    launch_pairs(p, partial, s);
+    size = next, ex = en;
+  }
+  return hipGetLastError();
+}
+
+}  // namespace qoda

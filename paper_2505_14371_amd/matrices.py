@@ -1,5 +1,5 @@
 """Thin binding over the operators of include/qoda_matrices.h on torch tensors: matrices in four bits (microscaled: a scale for every 32
-entries), and products between them and their gradients.
+entries), products between them and their gradients, and the orthogonalisation of an update by Newton-Schulz products.
 
 Argument marshalling only, as in ``operators``: every operator runs in the library's HIP kernels, and there is no CPU fallback.  Outputs and
 scratch memory come from torch's allocator, on the stream that the call runs on (``stream``: a torch stream or a handle; None: the current one).
@@ -10,6 +10,7 @@ scratch memory come from torch's allocator, on the stream that the call runs on 
     dx = mx_linear_input_grad(dz, wt)
     dzt = microscale(dy, transposed=True, rounding="stochastic", seed=s, offset=o + 1)
     mx_linear_weight_grad(dzt, microscale(x, transposed=True), dweight=g_w, dbias=g_b)    # fp32, into the vector that is quantized
+    orthogonalize(g_w, out=g_w)                                                           # ... or its orthogonalised form
 
 An operand of a product has its blocks along what the product sums over, so that a matrix that is summed over both ways is rounded twice.  Plain
 rows in a product's first place are rounded to nearest inside the call; up to 16 of them take one launch.  ``activation``, ``p``, ``seed``, ``offset``, ``residual``, biases and gradients of parameters are as in ``operators``, and
@@ -26,6 +27,7 @@ from . import operators as ops
 from . import qoda
 
 ROUNDINGS = {"nearest": 0, "stochastic": 1}
+QUINTIC = (3.4445, -4.7750, 2.0315)       # singular values from 0.002 |g| on come to 0.68 to 1.21 in five steps
 
 # the argument structures of the header, packed as C lays them out
 _QUANTIZE = struct.Struct("@3i2q" + "PqPP" + "QQ")
@@ -33,6 +35,7 @@ _VALUES = struct.Struct("@i2q" + "PP" + "Pq")
 _LINEAR = struct.Struct("@2i3q" + "Pq" + "PP" * 2 + "Pq" * 3 + "PdQQ")
 _INPUT_GRAD = struct.Struct("@2i3q" + "Pq" + "PP" * 2 + "Pq" * 3 + "dQQ")
 _WEIGHT_GRAD = struct.Struct("@i3q" + "PP" * 2 + "Pq" + "P")
+_ORTHOGONALIZE = struct.Struct("@2i3q" + "Pqq" * 2 + "4d")
 
 _lib = None
 
@@ -41,7 +44,7 @@ def _load():
     global _lib
     if _lib is None:
         L = ops._load()
-        for name in ("mx_linear", "mx_linear_input_grad", "mx_linear_weight_grad"):
+        for name in ("mx_linear", "mx_linear_input_grad", "mx_linear_weight_grad", "orthogonalize"):
             size, call = getattr(L, f"qoda_{name}_workspace_bytes"), getattr(L, f"qoda_{name}")
             size.argtypes, size.restype = [C.c_char_p], C.c_int64
             call.argtypes, call.restype = [C.c_char_p, C.c_void_p, C.c_size_t, C.c_void_p], C.c_int
@@ -242,3 +245,39 @@ def mx_linear_weight_grad(dz_t, x_t, dweight=None, dbias=None, *, bias=True, acc
         bool(accumulate), rows, cin, cout, *_mx(dz_t), *_mx(x_t), *ops._matrix(dweight, dz_t.codes, "mx_linear_weight_grad: dweight", cout, cin, torch.float32),
         ops._vector(dbias, dz_t.codes, "mx_linear_weight_grad: dbias", cout)), dz_t.device)
     return dweight, dbias
+
+def _matrices(t: torch.Tensor, like: torch.Tensor, name: str):
+    """Address, strides of matrices and rows, of [..., rows, columns]."""
+    if not isinstance(t, torch.Tensor) or t.device != like.device or t.dtype != like.dtype or t.shape != like.shape:
+        raise ValueError(f"{name}: a {like.dtype} tensor of shape {tuple(like.shape)} on {like.device} is wanted")
+    n = 1
+    for d in t.shape[:-2]:
+        n *= d
+    try:
+        t = t.view(n, *t.shape[-2:])
+    except RuntimeError:
+        raise ValueError(f"{name}: the matrices of strides {t.stride()} are not evenly spaced") from None
+    if t.shape[2] > 1 and t.stride(2) != 1:
+        raise ValueError(f"{name}: entries of a row have to be adjacent")
+    return t.data_ptr(), t.stride(0), t.stride(1)
+
+
+def orthogonalize(g, *, steps=5, coefficients=QUINTIC, eps=1e-7, out=None, stream=None):
+    """The matrices g [..., rows, columns] with their singular values brought towards 1: X = g / (|g| + eps), then ``steps`` times
+    X <- a X + (b A + c A A) X with A = X X^T and (a, b, c) = coefficients.  Written to out, if given, which may be g; of g's type."""
+    if stream is not None:
+        with _on(stream):
+            return orthogonalize(g, steps=steps, coefficients=coefficients, eps=eps, out=out)
+    if ops._followed((g, out)):
+        raise RuntimeError("orthogonalize records nothing for torch's differentiation; g.detach() is orthogonalised")
+    dt = ops._first(g, "orthogonalize: g")
+    if g.dim() < 2:
+        raise ValueError("orthogonalize: g: [..., rows, columns] is wanted")
+    a, b, c = coefficients
+    n, (rows, cols) = 1, g.shape[-2:]
+    for d in g.shape[:-2]:
+        n *= d
+    x = torch.empty(g.shape, dtype=g.dtype, device=g.device) if out is None else out
+    _run("orthogonalize", _ORTHOGONALIZE.pack(dt, steps, n, rows, cols, *_matrices(g, g, "orthogonalize: g"), *_matrices(x, g, "orthogonalize: out"),
+                                              a, b, c, eps), g.device)
+    return x

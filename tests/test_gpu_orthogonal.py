@@ -1,0 +1,171 @@
+"""Orthogonalisation of include/qoda_matrices.h against its formula in 64 bits.
+
+How far off fp32 accuracy leaves it: X_0 and every product are off by about u = 2^-22 of the norm of what they are made of (pairs of fp16 hold 22 bits,
+sums of k terms in fp32 add root k units of 2^-24 in the mean and k at most); a step multiplies what is there by at most the largest slope of its
+polynomial.  The Frobenius norm of the error is therefore at most the sum over the steps of (error of a step) (the slopes behind it)."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+import matrix_definitions as M  # noqa: E402
+import operator_definitions as D  # noqa: E402
+from paper_2505_14371_amd import matrices as mats  # noqa: E402
+from paper_2505_14371_amd import qoda  # noqa: E402
+
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+Q = mats.QUINTIC
+
+
+@pytest.fixture(autouse=True)
+def gpu():
+    if not torch.cuda.is_available():
+        pytest.fail("a GPU test was selected but no GPU is visible")
+
+
+def bound(x0, steps, coefficients, k):
+    """Of the Frobenius norm of the error, for one matrix of norm at most 1 that sums of k terms are taken of."""
+    a, b, c = coefficients
+    s = np.linspace(0, 1, 4001)
+    unit = 2.0**-22 + np.sqrt(k) * 2.0**-24
+    off, top = 2.0**-23, 1.0                       # the rounding of X_0
+    norm = np.linalg.norm(x0)
+    for _ in range(steps):
+        s = np.linspace(0, top, 4001)
+        slope = np.abs(a + 3 * b * s**2 + 5 * c * s**4).max()
+        gain = abs(a) + abs(b) * top**2 + abs(c) * top**4          # of the step's terms, each with its own rounding
+        off = off * slope + 4 * unit * gain * norm
+        sv = np.linalg.svd(x0, compute_uv=False)
+        sv = np.abs(a * sv + b * sv**3 + c * sv**5)
+        x0 = np.diag(sv)
+        norm, top = np.linalg.norm(sv), max(top, np.abs(a * s + b * s**3 + c * s**5).max())
+    return off
+
+
+def matrices(rng, *shape):
+    m, n = shape[-2:]
+    r = max(1, min(m, n) // 16)
+    return (rng.standard_normal(shape[:-1] + (r,)) @ rng.standard_normal(shape[:-2] + (r, n)) / np.sqrt(r) + 0.3 * rng.standard_normal(shape)) * 1e-3
+
+
+def put(a, dtype, pad=0):
+    t = torch.from_numpy(np.asarray(a, dtype=np.float32)).to(TYPES[dtype])
+    wide = torch.full(t.shape[:-1] + (t.shape[-1] + pad,), float("nan"), dtype=TYPES[dtype])
+    wide[..., : t.shape[-1]] = t
+    return wide.cuda()[..., : t.shape[-1]], t.double().numpy()
+
+
+def check(got, g, steps, coefficients, eps, dtype):
+    want = M.orthogonalize(g, steps, coefficients, eps)
+    got = got.double().cpu().numpy()
+    assert got.shape == want.shape
+    m, n = g.shape[-2:]
+    for q, w, x in zip(got.reshape(-1, m, n), want.reshape(-1, m, n), g.reshape(-1, m, n)):
+        b = bound(x / (np.linalg.norm(x) + eps), steps, coefficients, max(m, n))
+        off = q - w
+        store = D.STORE[dtype] * np.linalg.norm(w) * 1.01
+        assert np.linalg.norm(off) <= b + store, (np.linalg.norm(off), b, store)
+        assert np.abs(off).max() <= b + D.STORE[dtype] * 1.01 * np.abs(w).max()
+
+
+SHAPES = [(1, 1), (1, 7), (9, 1), (2, 3), (16, 16), (31, 33), (32, 32), (37, 61), (61, 37), (64, 64), (65, 64), (100, 300), (410, 129), (128, 640), (257, 255)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("m,n", SHAPES)
+def test_orthogonalize(m, n, dtype):
+    rng = np.random.default_rng([m, n])
+    i = SHAPES.index((m, n))
+    steps, pad, batch = (5, 1, 3, 6, 0)[i % 5], (0, 1, 8)[i % 3], ((), (3,), (2, 2))[(i // 2) % 3]
+    g, gd = put(matrices(rng, *batch, m, n), dtype, pad)
+    x = mats.orthogonalize(g, steps=steps)
+    assert x.dtype == TYPES[dtype] and x.shape == g.shape and x.is_contiguous()
+    check(x, gd, steps, Q, 1e-7, dtype)
+    assert torch.equal(mats.orthogonalize(g, steps=steps), x)
+    if steps:
+        assert mats.orthogonalize(g, steps=steps, out=g) is g and torch.equal(g, x)
+
+
+@pytest.mark.parametrize("coefficients,steps", [((1.5, -0.5, 0.0), 8), ((2.0, -1.5, 0.5), 6), ((1.0, 0.0, 0.0), 4), ((0.0, 0.0, 0.0), 2), ((3.0, 1.0, 0.0), 3), ((0.0, 0.0, 1.0), 2),
+                                                ((-2.0, 1.5, -0.5), 5), ((1e-3, 1e-4, 1e-4), 3), ((100.0, -20.0, 3.0), 2)])
+def test_other_polynomials(coefficients, steps):
+    g, gd = put(matrices(np.random.default_rng(2), 70, 90), "f32")
+    check(mats.orthogonalize(g, steps=steps, coefficients=coefficients), gd, steps, coefficients, 1e-7, "f32")
+
+
+@pytest.mark.parametrize("scale", [1e-30, 1e-7, 1.0, 1e18, 1e30])
+def test_any_magnitude(scale):
+    """The sum of squares leaves fp32's range on both sides; eps counts only where g is as small."""
+    g, gd = put(matrices(np.random.default_rng(4), 40, 50) * scale, "f32")
+    eps = 1e-7 if scale >= 1e-7 else 0.0
+    check(mats.orthogonalize(g, eps=eps), gd, 5, Q, eps, "f32")
+
+
+def test_nothing_and_zeros():
+    for shape in ((0, 4, 5), (3, 0, 5), (3, 5, 0)):
+        assert mats.orthogonalize(torch.zeros(shape, device="cuda")).shape == shape
+    z = torch.zeros(2, 33, 40, device="cuda")
+    z[1] = torch.randn(33, 40, device="cuda")
+    x = mats.orthogonalize(z)
+    assert torch.equal(x[0], torch.zeros_like(x[0])) and torch.isfinite(x[1]).all()
+    assert torch.isnan(mats.orthogonalize(z, eps=0.0)[0]).all()
+
+
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+@pytest.mark.parametrize("shape", [(33, 70), (70, 33), (140, 200)])
+def test_infinities_and_nan_stay_in_their_matrix(shape, bad):
+    g = torch.randn(3, *shape, device="cuda")
+    want = mats.orthogonalize(g)
+    g[1, 3, 5] = bad
+    got = mats.orthogonalize(g)
+    assert torch.isnan(got[1]).all() and torch.equal(got[0], want[0]) and torch.equal(got[2], want[2])
+
+
+def test_what_lies_between_rows_and_matrices_is_left_alone():
+    store = torch.full((3, 50, 80), 7.0, device="cuda")
+    g = torch.randn(3, 45, 70, device="cuda")
+    out = store[:, :45, :70]
+    assert torch.equal(mats.orthogonalize(g, out=out), mats.orthogonalize(g))
+    store[:, :45, :70] = 7.0
+    assert (store == 7.0).all()
+
+
+# tiles of every size, sums split along l, both ways round; against 64 bits on the GPU
+LARGER = [(1, 700, 1500), (1, 1600, 600), (2, 1000, 1000), (16, 410, 2100), (1, 2048, 2048), (1, 100, 20000), (40, 200, 180)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("batch,m,n", LARGER)
+def test_larger(batch, m, n, dtype):
+    gen = torch.Generator("cuda").manual_seed(m)
+    g = (torch.randn(batch, m, n, device="cuda", generator=gen) * 1e-3).to(TYPES[dtype])
+    got = mats.orthogonalize(g).double()
+    x = g.double()
+    x = x / (x.square().sum((1, 2), keepdim=True).sqrt() + 1e-7)
+    for _ in range(5):
+        s = torch.matmul(x, x.transpose(1, 2).contiguous()) if m <= n else torch.matmul(x.transpose(1, 2).contiguous(), x)
+        p = Q[1] * s + Q[2] * torch.matmul(s, s)
+        x = Q[0] * x + (torch.matmul(p, x) if m <= n else torch.matmul(x, p))
+    # singular values of random entries: the smallest are 1 / root(n) of the norm times 1 - root(m / n), and grow by less than 3.4445^5 = 485
+    norm = x.flatten(1).norm(dim=1)
+    off = (got - x).flatten(1).norm(dim=1)
+    store = D.STORE[dtype] * 1.01
+    assert (off <= (485 * 16 * (2.0**-22 + max(m, n) ** 0.5 * 2.0**-24) / norm + store) * norm).all(), (off / norm)
+
+
+def test_refusals():
+    g = torch.randn(4, 5, device="cuda")
+    for bad in (lambda: mats.orthogonalize(g[0]), lambda: mats.orthogonalize(g.half()), lambda: mats.orthogonalize(g.cpu()), lambda: mats.orthogonalize(g.t()),
+                lambda: mats.orthogonalize(g, out=torch.empty(5, 4, device="cuda")), lambda: mats.orthogonalize(g, out=g.bfloat16()),
+                lambda: mats.orthogonalize(torch.zeros(3, 2, 4, 5, device="cuda").transpose(0, 1))):
+        with pytest.raises(ValueError):
+            bad()
+    with pytest.raises(qoda.QodaError, match="strides"):        # a matrix inside another's rows
+        mats.orthogonalize(torch.zeros(4, 3, 5, device="cuda").transpose(0, 1))
+    for bad in (dict(steps=-1), dict(eps=-1.0), dict(eps=float("nan")), dict(coefficients=(float("inf"), 0, 0)), dict(coefficients=(50.0, 0, 0), steps=30)):
+        with pytest.raises(qoda.QodaError):
+            mats.orthogonalize(g, **bad)
+    with pytest.raises(RuntimeError, match="differentiation"):
+        mats.orthogonalize(g.clone().requires_grad_())

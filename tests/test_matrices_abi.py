@@ -15,7 +15,8 @@ torch = pytest.importorskip("torch")
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 HEADER = os.path.join(ROOT, "include", "qoda_matrices.h")
 STRUCTS = {"qoda_mx_quantize_args": ("_QUANTIZE", "offset"), "qoda_mx_values_args": ("_VALUES", "y"), "qoda_mx_linear_args": ("_LINEAR", "offset"),
-           "qoda_mx_linear_input_grad_args": ("_INPUT_GRAD", "offset"), "qoda_mx_linear_weight_grad_args": ("_WEIGHT_GRAD", "dbias")}
+           "qoda_mx_linear_input_grad_args": ("_INPUT_GRAD", "offset"), "qoda_mx_linear_weight_grad_args": ("_WEIGHT_GRAD", "dbias"),
+           "qoda_orthogonalize_args": ("_ORTHOGONALIZE", "eps")}
 
 
 @pytest.fixture(scope="module")
@@ -84,7 +85,11 @@ def weight_grad(rows=4, cin=8, cout=6, dc=A, dsc=A, xc=A, xsc=A, dw=A, dws=8, db
     return "mx_linear_weight_grad", mats._WEIGHT_GRAD.pack(0, rows, cin, cout, dc, dsc, xc, xsc, dw, dws, db)
 
 
-BIG = (1 << 24) + 1
+def orthogonalize(dtype=0, steps=5, n=2, rows=4, cols=6, g=A, gm=24, gr=6, x=A, xm=24, xr=6, a=3.4445, b=-4.7750, c=2.0315, eps=1e-7):
+    return "orthogonalize", mats._ORTHOGONALIZE.pack(dtype, steps, n, rows, cols, g, gm, gr, x, xm, xr, a, b, c, eps)
+
+
+BIG, INF, NAN = (1 << 24) + 1, float("inf"), float("nan")
 REFUSED = [
     (quantize(dtype=2), "dtype 2"), (quantize(rows=-1), "size of -1"), (quantize(cols=1 << 31), "size of"), (quantize(x=0), "x is null"), (quantize(x=A + 2), "x is not aligned"),
     (quantize(xs=7), "stride of 7"), (quantize(codes=0), "q is null"), (quantize(scales=0), "q is null"), (quantize(codes=A + 8), "16 bytes"), (quantize(scales=A + 4), "16 bytes"),
@@ -97,6 +102,11 @@ REFUSED = [
     (input_grad(wc=0), "wt is null"), (input_grad(dx=0), "dx is null"), (input_grad(dxs=1), "dx has a stride"), (input_grad(r=A, rs=2), "residual has a stride"), (input_grad(p=-0.1), "p = "),
     (weight_grad(rows=BIG), "sums over"), (weight_grad(rows=-1), "size"), (weight_grad(dc=0), "dzt is null"), (weight_grad(xsc=0), "xt is null"), (weight_grad(xc=A + 8), "16 bytes"),
     (weight_grad(dw=0), "dw is null"), (weight_grad(dw=A + 2), "dw is not aligned"), (weight_grad(dws=7), "stride of 7"), (weight_grad(db=A + 1), "dbias is not aligned"),
+    (orthogonalize(dtype=7), "dtype 7"), (orthogonalize(steps=-1), "-1 steps"), (orthogonalize(n=-1), "size"), (orthogonalize(eps=-1e-9), "eps"), (orthogonalize(eps=NAN), "eps"), (orthogonalize(eps=INF), "eps"),
+    (orthogonalize(a=NAN), "coefficients"), (orthogonalize(b=INF), "coefficients"), (orthogonalize(a=1e13), "2^40"), (orthogonalize(a=10.0, b=0.0, c=0.0, steps=13), "2^40"),
+    (orthogonalize(b=1e30, c=-1e30), "2^40"), (orthogonalize(g=0), "g is null"), (orthogonalize(x=0), "x is null"), (orthogonalize(g=A + 2), "g is not aligned"), (orthogonalize(xr=5), "strides of x"),
+    (orthogonalize(gm=23), "strides of g"), (orthogonalize(gm=-24), "strides of g"), (orthogonalize(rows=(1 << 17) + 1, cols=(1 << 17) + 1, gr=1 << 18, gm=1 << 36, xr=1 << 18, xm=1 << 36), "sides"),
+    (orthogonalize(rows=1, cols=(1 << 22) + 1), "sides"),
 ]
 
 
@@ -117,12 +127,13 @@ def test_refusals(lib, at):
 
 
 def test_null_arguments(lib):
-    for name in ("mx_quantize", "mx_values", "mx_linear", "mx_linear_input_grad", "mx_linear_weight_grad"):
+    for name in ("mx_quantize", "mx_values", "mx_linear", "mx_linear_input_grad", "mx_linear_weight_grad", "orthogonalize"):
         assert call(lib, name, None) == qoda.EINVAL and "null" in lib.qoda_operator_error().decode()
 
 
 @pytest.mark.parametrize("args", [quantize(rows=0, x=0, codes=0), quantize(cols=0, x=0, scales=0), values(rows=0, codes=0, y=0), linear(rows=0, x=0, y=0, wc=0), linear(cout=0, y=0, wc=0),
-                                  input_grad(rows=0, dz=0, dx=0), input_grad(cin=0, dx=0), weight_grad(cout=0, dw=0, dc=0), weight_grad(cin=0, xc=0, dw=0)])
+                                  input_grad(rows=0, dz=0, dx=0), input_grad(cin=0, dx=0), weight_grad(cout=0, dw=0, dc=0), weight_grad(cin=0, xc=0, dw=0),
+                                  orthogonalize(n=0, g=0), orthogonalize(rows=0, x=0), orthogonalize(cols=0, g=0, x=0)])
 def test_empty_outputs_need_nothing(lib, args):
     assert call(lib, *args) == qoda.OK, lib.qoda_operator_error()
 
@@ -152,3 +163,12 @@ def test_arguments_that_python_refuses(lib):
             bad()
     with pytest.raises(RuntimeError, match="no derivative"):
         mats.microscale(torch.zeros(3, 4, requires_grad=True))
+
+
+def test_bounded_polynomials_are_taken_for_any_number_of_steps(lib):
+    for steps in (0, 1, 1000, 2**31 - 1):
+        assert lib.qoda_orthogonalize_workspace_bytes(orthogonalize(steps=steps)[1]) > 0
+    assert lib.qoda_orthogonalize_workspace_bytes(orthogonalize(a=10.0, b=0.0, c=0.0, steps=12)[1]) > 0
+    name, args = orthogonalize()
+    need = lib.qoda_orthogonalize_workspace_bytes(args)
+    assert call(lib, name, args, A, need - 1) == qoda.EINVAL and "workspace" in lib.qoda_operator_error().decode()
