@@ -69,8 +69,8 @@ __global__ void __launch_bounds__(64 * WM * WN, BM == 128 ? 2 : 1) k_mx_product(
   typedef Operand<bf16, true, 1, BN, WG, true> B;
   typedef Scales<BM> SA;
   typedef Scales<BN> SB;
-  __shared__ __align__(16) char a0[BM * kStepBytes], b0[BN * kStepBytes], a1[BM * kStepBytes], b1[BN * kStepBytes];
-  __shared__ __align__(16) char s0[(BM + BN) * 8], s1[(BM + BN) * 8];
+  constexpr u32 kBuffer = (BM + BN) * (kStepBytes + 8);   // both sides' codes and scales of a step
+  __shared__ __align__(16) char shared[2 * kBuffer];
 
   const Product &p = m.p;
   int tm, tn;
@@ -97,9 +97,12 @@ __global__ void __launch_bounds__(64 * WM * WN, BM == 128 ? 2 : 1) k_mx_product(
     v4u a[FM], b[FN];
     u32 sa[QM], sb[QN];
   };
+  const lds_ptr base = (lds_ptr)shared;
+  u32 now = 0;   // the buffer of the step that is multiplied
   u32 key_a = A::lane_key(wm), key_b = B::lane_key(wn);
-  const auto read = [&](Pieces &f, lds_ptr ta, lds_ptr tb, lds_ptr ts, int s) {
+  const auto read = [&](Pieces &f, u32 from, int s) {
     asm volatile("" : "+v"(key_a), "+v"(key_b));   // made anew each time, as in k_product
+    const lds_ptr ta = base + from, tb = ta + BM * kStepBytes, ts = tb + BN * kStepBytes;
 #pragma unroll
     for (int q = 0; q < QN; ++q) f.sb[q] = SB::template piece<FN == 2>(ts + BM * 8, wn, q, s);
 #pragma unroll
@@ -114,31 +117,37 @@ __global__ void __launch_bounds__(64 * WM * WN, BM == 128 ? 2 : 1) k_mx_product(
       each<FN>([&](auto y) { c[x][y] = multiply_blocks<y % 4, x % 4>(f.b[y], f.a[x], c[x][y], f.sb[y / 4], f.sa[x / 4]); });
     });
   };
-  const lds_ptr ta[2] = {(lds_ptr)a0, (lds_ptr)a1}, tb[2] = {(lds_ptr)b0, (lds_ptr)b1}, ts[2] = {(lds_ptr)s0, (lds_ptr)s1};
-  const auto request = [&](int t, int h) {
-    a.direct(t * 64, ta[h]);
-    b.direct(t * 64, tb[h]);
-    if (wave < 2) sa.direct(step0 + t, wave, ts[h]);
-    else if (wave < 4) sb.direct(step0 + t, wave - 2, ts[h] + BM * 8);
+  const auto here = [&] {   // the sums so far are wanted here: otherwise the compiler takes their instructions behind the barrier and the branch after it
+#pragma unroll
+    for (int x = 0; x < FM; ++x)
+#pragma unroll
+      for (int y = 0; y < FN; ++y) asm volatile("" : "+v"(c[x][y]));
   };
+  const auto request = [&](int t, u32 to) {
+    const lds_ptr ta = base + to, tb = ta + BM * kStepBytes, ts = tb + BN * kStepBytes;
+    a.direct(t * 64, ta);
+    b.direct(t * 64, tb);
+    if (wave < 2) sa.direct(step0 + t, wave, ts);
+    else if (wave < 4) sb.direct(step0 + t, wave - 2, ts + BM * 8);
+  };
+  // One block without branches around what is read and multiplied: behind the last step the next one's pieces are read all the same, from what the buffer
+  // holds, and not used.  (With branches the compiler kept copies of the sums.)
   if (steps > 0) {
     request(0, 0);
-    if (steps > 1) request(1, 1);
+    if (steps > 1) request(1, kBuffer);
     Pieces f0, f1;
     arrived();
-    read(f0, ta[0], tb[0], ts[0], 0);
-    for (int t = 0; t < steps; t += 2) {
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-        if (t + h < steps) {
-          read(f1, ta[h], tb[h], ts[h], 1);
-          multiply_all(f0);
-          arrived();   // the next step is there, and nobody reads this one any more
-          if (t + h + 2 < steps) request(t + h + 2, h);
-          if (t + h + 1 < steps) read(f0, ta[1 - h], tb[1 - h], ts[1 - h], 0);
-          multiply_all(f1);
-          __builtin_amdgcn_sched_barrier(0);
-        }
+    read(f0, 0, 0);
+    for (int t = 0; t < steps; ++t) {
+      read(f1, now, 1);
+      multiply_all(f0);
+      here();
+      arrived();   // the next step is there, and nobody reads this one any more
+      if (t + 2 < steps) request(t + 2, now);
+      now = kBuffer - now;
+      read(f0, now, 0);
+      multiply_all(f1);
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
 
@@ -162,7 +171,7 @@ __global__ void __launch_bounds__(64 * WM * WN, BM == 128 ? 2 : 1) k_mx_product(
     return;
   }
   by_activation<FORM>(p.activation, [&](auto act) {
-    constexpr int kPart = FM < 4 ? FM : 4;   // rows whose reads are all on their way before the first is needed
+    constexpr int kPart = FM < 4 || sizeof(T) == 4 ? 2 : 4;   // rows whose reads are all on their way before the first is needed
 #pragma unroll
     for (int x0 = 0; x0 < FM; x0 += kPart) {
       Beside<T, FORM, decltype(act)::value> beside[kPart][FN / 2];
@@ -277,7 +286,7 @@ __global__ void __launch_bounds__(64 * NW) k_mx_few_rows(MxProduct m) {
   }
 }
 
-enum Tile { kFewRows, kTile64, kTile128 };
+enum Tile { kFewRows, kTile64, kTile128, kTile256 };
 struct Plan {
   Tile tile;
   int tiles_m, tiles_n, splits, steps_each;
@@ -311,7 +320,7 @@ Plan plan_of(const MxProduct &m) {
     q.tile = kFewRows, q.tiles_m = 1, q.tiles_n = (p.n + 31) / 32;
     return q;
   }
-  const struct { Tile tile; int side, a_cu; double rate; } cuts[] = {{kTile64, 64, 2, 1500e12}, {kTile128, 128, 2, 2500e12}};
+  const struct { Tile tile; int side, a_cu; double rate; } cuts[] = {{kTile64, 64, 2, 1500e12}, {kTile128, 128, 2, 2500e12}, {kTile256, 256, 1, 3500e12}};
   const int steps = m.steps > 0 ? m.steps : 1;
   double least = 0.0;
   int side = 0;
@@ -354,6 +363,7 @@ void launch(const MxProduct &m, const Plan &q, hipStream_t s) {
       return;
     case kTile64: launch_tiles<T, FORM, 64, 64, 2, 2>(m, q, s); break;
     case kTile128: launch_tiles<T, FORM, 128, 128, 2, 2>(m, q, s); break;
+    case kTile256: launch_tiles<T, FORM, 256, 256, 2, 4>(m, q, s); break;
   }
   if (q.splits > 1) {
     const long long blocks = (long long)m.p.m * ((m.p.n + 7) / 8), groups = (blocks + 255) / 256;

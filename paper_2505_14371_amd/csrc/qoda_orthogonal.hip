@@ -207,19 +207,20 @@ __global__ void __launch_bounds__(64 * WM * WN, BM == 128 ? 2 : 1) k_pair_produc
     for (int y = 0; y < 2 * FN; ++y) c[x][y] = v4f{0, 0, 0, 0};
 
   const lds_ptr base = (lds_ptr)shared;
-  const lds_ptr ta[2] = {base, base + BM * kStepBytes}, tb[2] = {base + 2 * BM * kStepBytes, base + (2 * BM + BN) * kStepBytes};
+  constexpr u32 kBuffer = (BM + BN) * kStepBytes;
+  u32 now = 0;   // the buffer of the step that is multiplied
   typedef v4u PiecesA[FM];
   typedef v4u PiecesB[2 * FN];
   u32 key_a = A::lane_key(wm), key_b = B::lane_key(wn);
-  const auto read_a = [&](PiecesA &f, int h, int s) {
+  const auto read_a = [&](PiecesA &f, u32 from, int s) {
     asm volatile("" : "+v"(key_a));   // made anew each time, as in k_product
 #pragma unroll
-    for (int x = 0; x < FM; ++x) f[x] = A::piece(ta[h], key_a, wm, x * 16, 0, s);
+    for (int x = 0; x < FM; ++x) f[x] = A::piece(base + from, key_a, wm, x * 16, 0, s);
   };
-  const auto read_b = [&](PiecesB &f, int h, int s) {
+  const auto read_b = [&](PiecesB &f, u32 from, int s) {
     asm volatile("" : "+v"(key_b));
 #pragma unroll
-    for (int y = 0; y < 2 * FN; ++y) f[y] = B::piece(tb[h], key_b, wn, y / 2 * 32, y & 1, s);
+    for (int y = 0; y < 2 * FN; ++y) f[y] = B::piece(base + from + BM * kStepBytes, key_b, wn, y / 2 * 32, y & 1, s);
   };
   const auto multiply_all = [&](const PiecesA &fa, const PiecesB &fb) {
 #pragma unroll
@@ -227,32 +228,31 @@ __global__ void __launch_bounds__(64 * WM * WN, BM == 128 ? 2 : 1) k_pair_produc
 #pragma unroll
       for (int y = 0; y < 2 * FN; ++y) c[x][y] = multiply_halves(fb[y], fa[x], c[x][y]);
   };
-  const auto request = [&](int t, int h) {
-    a.direct(t * 64, ta[h]);
-    b.direct(t * 64, tb[h]);
+  const auto request = [&](int t, u32 to) {
+    a.direct(t * 64, base + to);
+    b.direct(t * 64, base + to + BM * kStepBytes);
   };
+  // One block without branches around what is read and multiplied: behind the last step the next one's pieces are read all the same, from what the buffer
+  // holds, and not used.  (With branches the compiler kept copies of the sums.)
   PiecesA a_hi, a_lo;
   PiecesB b_hi, b_lo;
   request(0, 0);
-  if (steps > 1) request(1, 1);
+  if (steps > 1) request(1, kBuffer);
   arrived();
   read_a(a_hi, 0, 0);
   read_b(b_hi, 0, 0);
-  for (int t = 0; t < steps; t += 2) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-      if (t + h < steps) {
-        read_b(b_lo, h, 1);
-        read_a(a_lo, h, 1);
-        multiply_all(a_hi, b_hi);
-        arrived();   // the next step is there, and nobody reads this one any more
-        if (t + h + 2 < steps) request(t + h + 2, h);
-        multiply_all(a_hi, b_lo);
-        if (t + h + 1 < steps) read_a(a_hi, 1 - h, 0);
-        multiply_all(a_lo, b_hi);
-        if (t + h + 1 < steps) read_b(b_hi, 1 - h, 0);
-        __builtin_amdgcn_sched_barrier(0);
-      }
+  for (int t = 0; t < steps; ++t) {
+    read_b(b_lo, now, 1);
+    read_a(a_lo, now, 1);
+    multiply_all(a_hi, b_hi);
+    arrived();   // the next step is there, and nobody reads this one any more
+    if (t + 2 < steps) request(t + 2, now);
+    now = kBuffer - now;
+    multiply_all(a_hi, b_lo);
+    read_a(a_hi, now, 0);
+    multiply_all(a_lo, b_hi);
+    read_b(b_hi, now, 0);
+    __builtin_amdgcn_sched_barrier(0);
   }
 
   const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
