@@ -5,7 +5,7 @@
 #include <c10/core/GradMode.h>
 #include <torch/csrc/autograd/python_variable.h>
 
-#include "../../include/qoda_operators.h"
+#include "../../include/qoda_matrices.h"
 
 #include <cstdint>
 #include <cstring>
@@ -66,21 +66,23 @@ struct Calls {   // of the library that the caller has loaded
   decltype(&qoda_group_norm_grad) norm_grad;
 } calls;
 
-// use(addresses): the calls above, in their order.
-PyObject *use(PyObject *, PyObject *addresses) {
-  constexpr Py_ssize_t n = sizeof calls / sizeof(void *);
+PyObject *used(PyObject *addresses, void *to, size_t bytes, const char *said) {
+  void *p[32];
+  const Py_ssize_t n = (Py_ssize_t)(bytes / sizeof(void *));
   if (!PyTuple_CheckExact(addresses) || PyTuple_GET_SIZE(addresses) != n) {
-    PyErr_SetString(PyExc_TypeError, "use(addresses)");
+    PyErr_SetString(PyExc_TypeError, said);
     return nullptr;
   }
-  void *p[n];
   for (Py_ssize_t i = 0; i < n; ++i) {
     p[i] = PyLong_AsVoidPtr(PyTuple_GET_ITEM(addresses, i));
     if (PyErr_Occurred()) return nullptr;
   }
-  memcpy(&calls, p, sizeof p);
+  memcpy(to, p, bytes);
   Py_RETURN_NONE;
 }
+
+// use(addresses): the calls above, in their order.
+PyObject *use(PyObject *, PyObject *addresses) { return used(addresses, &calls, sizeof calls, "use(addresses)"); }
 
 struct Unknown {};   // thrown inside a function whose arguments are not plain
 
@@ -296,6 +298,200 @@ PyObject *group_norm_grad(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
   });
 }
 
+// ---- include/qoda_matrices.h
+
+struct MatrixCalls {
+  decltype(&qoda_mx_quantize) quantize;
+  decltype(&qoda_mx_values) values;
+  decltype(&qoda_mx_linear_workspace_bytes) linear_bytes;
+  decltype(&qoda_mx_linear) linear;
+  decltype(&qoda_mx_linear_input_grad_workspace_bytes) input_grad_bytes;
+  decltype(&qoda_mx_linear_input_grad) input_grad;
+  decltype(&qoda_mx_linear_weight_grad_workspace_bytes) weight_grad_bytes;
+  decltype(&qoda_mx_linear_weight_grad) weight_grad;
+  decltype(&qoda_orthogonalize_workspace_bytes) orthogonalize_bytes;
+  decltype(&qoda_orthogonalize) orthogonalize;
+} matrix_calls;
+
+// use_matrices(addresses): the calls above, in their order.
+PyObject *use_matrices(PyObject *, PyObject *addresses) { return used(addresses, &matrix_calls, sizeof matrix_calls, "use_matrices(addresses)"); }
+
+// A microscaled matrix, as (codes, scales, rows, columns): the caller's class has looked at their shapes.
+struct Mx {
+  const at::Tensor &codes, &scales;
+  int64_t rows, cols;
+  Mx(PyObject *o, int64_t device) : codes(tensor(part(o, 0))), scales(tensor(part(o, 1))), rows(number<int64_t>(part(o, 2))), cols(number<int64_t>(part(o, 3))) {
+    if (!codes.is_cuda() || codes.get_device() != device || !scales.is_cuda() || scales.get_device() != device) throw Unknown();
+  }
+  static PyObject *part(PyObject *o, Py_ssize_t i) {
+    if (!PyTuple_CheckExact(o) || PyTuple_GET_SIZE(o) != 4) throw Unknown();
+    return PyTuple_GET_ITEM(o, i);
+  }
+  qoda_mx as_is() const { return {codes.data_ptr(), scales.data_ptr()}; }
+};
+
+at::Tensor bytes_of(const at::Tensor &like, at::IntArrayRef sizes) { return at::empty(sizes, like.options().dtype(at::kByte)); }
+
+// (device, stream, x, transposed, stochastic, seed, offset): (codes, scales)
+PyObject *microscale(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
+  return answered(args, nargs, 7, [&](int64_t device, void *stream) {
+    if (!matrix_calls.quantize) throw Unknown();
+    not_followed({args[2]});
+    const First x(args[2], device, 1);
+    const bool transposed = truth(args[3]);
+    const int64_t rows = transposed ? x.cols : x.rows, cols = transposed ? x.rows : x.cols, steps = (cols + 255) / 256;
+    if (rows > QODA_MAX_SIDE || cols > QODA_MAX_SIDE) throw Unknown();
+    const at::Tensor codes = bytes_of(x.t, {rows, 128 * steps}), scales = bytes_of(x.t, {2 * steps, (rows + 63) / 64, 256});
+    const qoda_mx_quantize_args a = {x.dtype, transposed, truth(args[4]), x.rows, x.cols, matrix(args[2], x, x.rows, x.cols), {codes.data_ptr(), scales.data_ptr()},
+                                     number<uint64_t>(args[5]), number<uint64_t>(args[6])};
+    return outcome(matrix_calls.quantize(&a, stream), {codes, scales});
+  });
+}
+
+// The rows of a product's first operand: plain, or microscaled with a type for what goes with them.
+struct Rows {
+  const at::Tensor *t;      // whose device and, plain, type the others have
+  at::ScalarType type;
+  int32_t dtype;
+  int64_t rows, cols;
+  qoda_matrix plain = {nullptr, 0};
+  qoda_mx mx = {nullptr, nullptr};
+  c10::SmallVector<int64_t, 6> front;
+  Rows(PyObject *o, PyObject *bf16, int64_t device) {
+    if (PyTuple_CheckExact(o)) {
+      const Mx q(o, device);
+      t = &q.codes, rows = q.rows, cols = q.cols, mx = q.as_is();
+      dtype = truth(bf16) ? QODA_BF16 : QODA_F32;
+      type = dtype == QODA_BF16 ? at::kBFloat16 : at::kFloat;
+      front = {rows};
+    } else {
+      if (bf16 != Py_None) throw Unknown();
+      const First x(o, device, 1);
+      t = &x.t, rows = x.rows, cols = x.cols, dtype = x.dtype, type = x.t.scalar_type();
+      plain = matrix(o, x, rows, cols);
+      front.assign(x.t.sizes().begin(), x.t.sizes().end() - 1);
+    }
+  }
+  at::Tensor output(int64_t columns) const {
+    c10::SmallVector<int64_t, 6> sizes = front;
+    sizes.push_back(columns);
+    return at::empty(sizes, t->options().dtype(type));
+  }
+  qoda_matrix beside(PyObject *o, const First &like, int64_t columns) const { return matrix(o, like, rows, columns); }
+};
+
+// First of a tensor that this code has made: its type and device are what other arguments are compared with.
+First made(const at::Tensor &t, PyObject *&holder, int64_t device) {
+  holder = THPVariable_Wrap(t);
+  return First(holder, device, 1);
+}
+struct Held {   // a reference that goes with the scope
+  PyObject *o = nullptr;
+  ~Held() { Py_XDECREF(o); }
+};
+
+// The call with its workspace on the device of `like`: 0, or the library's error code.
+template <class Args, class Bytes, class Call>
+int with_scratch(const at::Tensor &like, const Args &a, Bytes bytes, Call call, void *stream) {
+  const int64_t need = bytes(&a);
+  if (need < 0) return (int)need;
+  at::Tensor scratch;
+  if (need > 0) scratch = bytes_of(like, {need});
+  return call(&a, need > 0 ? scratch.data_ptr() : nullptr, (size_t)need, stream);
+}
+
+// (device, stream, x, weight, bias, residual, activation, p, seed, offset, keep_pre, bf16); bf16: of the outputs, None where x is plain
+PyObject *mx_linear(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
+  return answered(args, nargs, 12, [&](int64_t device, void *stream) {
+    if (!matrix_calls.linear) throw Unknown();
+    if (!PyTuple_CheckExact(args[2])) not_followed({args[2]});
+    not_followed({args[4], args[5]});
+    const Rows x(args[2], args[11], device);
+    const Mx w(args[3], device);
+    if (w.cols != x.cols) throw Unknown();
+    const at::Tensor y = x.output(w.rows);
+    Held held;
+    const First like = made(y, held.o, device);
+    qoda_mx_linear_args a = {x.dtype, (int32_t)number<int64_t>(args[6]), x.rows, x.cols, w.rows, x.plain, x.mx, w.as_is(), x.beside(args[5], like, w.rows),
+                             {y.data_ptr(), w.rows}, {}, vector(args[4], like, w.rows), number<double>(args[7]), number<uint64_t>(args[8]), number<uint64_t>(args[9])};
+    if (!truth(args[10])) return outcome(with_scratch(y, a, matrix_calls.linear_bytes, matrix_calls.linear, stream), {y});
+    const at::Tensor pre = x.output(w.rows);
+    a.pre = {pre.data_ptr(), w.rows};
+    return outcome(with_scratch(y, a, matrix_calls.linear_bytes, matrix_calls.linear, stream), {y, pre});
+  });
+}
+
+// (device, stream, dz, weight_t, pre, activation, p, seed, offset, residual, bf16)
+PyObject *mx_linear_input_grad(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
+  return answered(args, nargs, 11, [&](int64_t device, void *stream) {
+    if (!matrix_calls.input_grad) throw Unknown();
+    const Rows dz(args[2], args[10], device);
+    const Mx wt(args[3], device);
+    if (wt.cols != dz.cols) throw Unknown();
+    const at::Tensor dx = dz.output(wt.rows);
+    Held held;
+    const First like = made(dx, held.o, device);
+    const qoda_mx_linear_input_grad_args a = {dz.dtype, (int32_t)number<int64_t>(args[5]), dz.rows, wt.rows, dz.cols, dz.plain, dz.mx, wt.as_is(), dz.beside(args[4], like, wt.rows),
+                                              dz.beside(args[9], like, wt.rows), {dx.data_ptr(), wt.rows}, number<double>(args[6]), number<uint64_t>(args[7]),
+                                              number<uint64_t>(args[8])};
+    return outcome(with_scratch(dx, a, matrix_calls.input_grad_bytes, matrix_calls.input_grad, stream), {dx});
+  });
+}
+
+// (device, stream, dz_t, x_t, dweight, dbias, accumulate), with both outputs given (dbias may be None); answers with True
+PyObject *mx_linear_weight_grad(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
+  return answered(args, nargs, 7, [&](int64_t device, void *stream) -> PyObject * {
+    if (!matrix_calls.weight_grad) throw Unknown();
+    const Mx dzt(args[2], device), xt(args[3], device);
+    if (dzt.cols != xt.cols || args[4] == Py_None) throw Unknown();
+    const First dw(args[4], device, 2);
+    if (dw.dtype != QODA_F32) throw Unknown();
+    const qoda_mx_linear_weight_grad_args a = {truth(args[6]), dzt.cols, xt.rows, dzt.rows, dzt.as_is(), xt.as_is(), matrix(args[4], dw, dzt.rows, xt.rows), vector(args[5], dw, dzt.rows)};
+    const int rc = with_scratch(dzt.codes, a, matrix_calls.weight_grad_bytes, matrix_calls.weight_grad, stream);
+    if (rc != QODA_OK) return PyLong_FromLong(rc);
+    Py_RETURN_TRUE;
+  });
+}
+
+// (device, stream, q, bf16)
+PyObject *mx_values(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
+  return answered(args, nargs, 4, [&](int64_t device, void *stream) {
+    if (!matrix_calls.values) throw Unknown();
+    const Mx q(args[2], device);
+    const bool wide = !truth(args[3]);
+    const at::Tensor y = at::empty({q.rows, q.cols}, q.codes.options().dtype(wide ? at::kFloat : at::kBFloat16));
+    const qoda_mx_values_args a = {wide ? QODA_F32 : QODA_BF16, q.rows, q.cols, q.as_is(), {y.data_ptr(), q.cols}};
+    return outcome(matrix_calls.values(&a, stream), {y});
+  });
+}
+
+// (device, stream, g, steps, a, b, c, eps, out); out: None makes it
+PyObject *orthogonalize(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
+  return answered(args, nargs, 9, [&](int64_t device, void *stream) {
+    if (!matrix_calls.orthogonalize) throw Unknown();
+    not_followed({args[2], args[8]});
+    const First g(args[2], device, 2);
+    const int64_t rows = g.t.size(g.t.dim() - 2), n = rows > 0 ? g.rows / rows : 0;
+    const auto places = [&](const at::Tensor &t) -> qoda_matrices {
+      if (t.is_contiguous()) return {t.data_ptr(), rows * g.cols, g.cols};
+      if (t.dim() > 3 || (g.cols > 1 && t.stride(t.dim() - 1) != 1)) throw Unknown();
+      return {t.data_ptr(), t.dim() == 3 ? t.stride(0) : 0, t.stride(t.dim() - 2)};
+    };
+    const at::Tensor x = args[8] == Py_None ? rows_of(g, g.cols) : tensor(args[8]);
+    if (rows == 0 || !x.is_cuda() || x.get_device() != device || x.scalar_type() != g.t.scalar_type() || x.sizes() != g.t.sizes()) throw Unknown();
+    const int64_t steps = number<int64_t>(args[3]);
+    if (steps > INT32_MAX || steps < INT32_MIN) throw Unknown();
+    const qoda_orthogonalize_args a = {g.dtype, (int32_t)steps, n, rows, g.cols, places(g.t), places(x), number<double>(args[4]), number<double>(args[5]), number<double>(args[6]),
+                                       number<double>(args[7])};
+    const int rc = with_scratch(g.t, a, matrix_calls.orthogonalize_bytes, matrix_calls.orthogonalize, stream);
+    if (rc == QODA_OK && args[8] != Py_None) {
+      Py_INCREF(args[8]);
+      return args[8];
+    }
+    return outcome(rc, {x});
+  });
+}
+
 PyCFunction fast(PyObject *(*f)(PyObject *, PyObject *const *, Py_ssize_t)) { return reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)); }
 
 PyMethodDef methods[] = {{"gather", fast(gather), METH_FASTCALL, nullptr},
@@ -306,6 +502,13 @@ PyMethodDef methods[] = {{"gather", fast(gather), METH_FASTCALL, nullptr},
                          {"entries", fast(entries), METH_FASTCALL, nullptr},
                          {"group_norm", fast(group_norm), METH_FASTCALL, nullptr},
                          {"group_norm_grad", fast(group_norm_grad), METH_FASTCALL, nullptr},
+                         {"use_matrices", use_matrices, METH_O, nullptr},
+                         {"microscale", fast(microscale), METH_FASTCALL, nullptr},
+                         {"mx_values", fast(mx_values), METH_FASTCALL, nullptr},
+                         {"mx_linear", fast(mx_linear), METH_FASTCALL, nullptr},
+                         {"mx_linear_input_grad", fast(mx_linear_input_grad), METH_FASTCALL, nullptr},
+                         {"mx_linear_weight_grad", fast(mx_linear_weight_grad), METH_FASTCALL, nullptr},
+                         {"orthogonalize", fast(orthogonalize), METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_qoda_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

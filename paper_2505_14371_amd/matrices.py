@@ -38,10 +38,11 @@ _WEIGHT_GRAD = struct.Struct("@i3q" + "PP" * 2 + "Pq" + "P")
 _ORTHOGONALIZE = struct.Struct("@2i3q" + "Pqq" * 2 + "4d")
 
 _lib = None
+_native = None          # the native look at the arguments, once the library is loaded
 
 
 def _load():
-    global _lib
+    global _lib, _native
     if _lib is None:
         L = ops._load()
         for name in ("mx_linear", "mx_linear_input_grad", "mx_linear_weight_grad", "orthogonalize"):
@@ -52,8 +53,20 @@ def _load():
             call.argtypes, call.restype = [C.c_char_p, C.c_void_p], C.c_int
         for size in (L.qoda_mx_code_bytes, L.qoda_mx_scale_bytes):
             size.argtypes, size.restype = [C.c_int64, C.c_int64], C.c_int64
+        if ops._native is not None:
+            names = ["mx_quantize", "mx_values"]
+            for name in ("mx_linear", "mx_linear_input_grad", "mx_linear_weight_grad", "orthogonalize"):
+                names += [name + "_workspace_bytes", name]
+            ops._native.use_matrices(tuple(C.cast(getattr(L, "qoda_" + n), C.c_void_p).value for n in names))
+            _native = ops._native
         _lib = L
     return _lib
+
+
+def _is_native() -> bool:
+    if _lib is None:
+        _load()
+    return _native is not None
 
 
 def _on(stream):
@@ -70,7 +83,7 @@ class Microscaled:
     """A matrix of rows x cols in four bits, rounded by ``microscale`` or laid out by the caller as include/qoda_matrices.h says: ``codes`` and ``scales``
     are contiguous uint8 tensors on one device, [rows, 128 s] and [2 s, rows / 64 rounded up, 256], s = cols / 256 rounded up."""
 
-    __slots__ = ("codes", "scales", "rows", "cols")
+    __slots__ = ("_parts",)
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, rows: int, cols: int):
         for t, shape, name in zip((codes, scales), _shapes(rows, cols), ("codes", "scales")):
@@ -78,21 +91,24 @@ class Microscaled:
                 raise ValueError(f"Microscaled: {name} of {rows} rows and {cols} columns are a contiguous uint8 tensor of shape {shape}")
         if codes.device != scales.device:
             raise ValueError("Microscaled: codes and scales are on different devices")
-        self.codes, self.scales, self.rows, self.cols = codes, scales, rows, cols
+        self._parts = (codes, scales, rows, cols)
 
-    @property
-    def shape(self):
-        return torch.Size((self.rows, self.cols))
-
-    @property
-    def device(self):
-        return self.codes.device
+    codes = property(lambda self: self._parts[0])
+    scales = property(lambda self: self._parts[1])
+    rows = property(lambda self: self._parts[2])
+    cols = property(lambda self: self._parts[3])
+    shape = property(lambda self: torch.Size(self._parts[2:]))
+    device = property(lambda self: self._parts[0].device)
 
     def values(self, dtype=torch.float32, *, stream=None) -> torch.Tensor:
         """What the codes stand for, a matrix of float32 or bfloat16."""
         if stream is not None:
             with _on(stream):
                 return self.values(dtype)
+        if _is_native():
+            out = ops._looked_at(_native.mx_values, self._parts, _bf16(dtype))
+            if out is not None:
+                return out
         dt = _type(dtype, "values")
         _current(self, "values")
         y = torch.empty((self.rows, self.cols), dtype=dtype, device=self.device)
@@ -101,6 +117,22 @@ class Microscaled:
 
     def __repr__(self) -> str:
         return f"Microscaled({self.rows} x {self.cols}, {self.device})"
+
+
+def _bf16(dtype):
+    """For the native look, which takes None for a type that it does not know."""
+    return True if dtype is torch.bfloat16 else False if dtype is torch.float32 else None
+
+
+def _plain_or_parts(x, dtype):
+    """A product's first operand and its type, for the native look."""
+    if type(x) is Microscaled:
+        return x._parts, True if dtype is None else _bf16(dtype)
+    return x, None if dtype is None or (isinstance(x, torch.Tensor) and dtype is x.dtype) else False
+
+
+def _parts(q):
+    return q._parts if type(q) is Microscaled else None
 
 
 def _mx(q):
@@ -151,6 +183,13 @@ def microscale(x, *, transposed=False, rounding="nearest", seed=0, offset=0, str
             return microscale(x, transposed=transposed, rounding=rounding, seed=seed, offset=offset)
     if not isinstance(rounding, str) or rounding not in ROUNDINGS:
         raise ValueError(f"rounding {rounding!r}: one of {', '.join(ROUNDINGS)}")
+    if _is_native():
+        out = ops._looked_at(_native.microscale, x, transposed, rounding == "stochastic", seed, offset)
+        if out is not None:
+            rows, cols = x.numel() // x.shape[-1] if x.shape[-1] else ops._rows(x), x.shape[-1]
+            q = Microscaled.__new__(Microscaled)
+            q._parts = (*out, cols, rows) if transposed else (*out, rows, cols)
+            return q
     if ops._followed((x,)):
         raise RuntimeError("microscale: rounding has no derivative, and nothing is recorded for torch's differentiation; x.detach() is rounded")
     dt = ops._first(x, "microscale: x")
@@ -185,6 +224,11 @@ def mx_linear(x, weight, bias=None, residual=None, *, activation="none", p=0.0, 
     if stream is not None:
         with _on(stream):
             return mx_linear(x, weight, bias, residual, activation=activation, p=p, seed=seed, offset=offset, keep_pre=keep_pre, dtype=dtype)
+    if _is_native():
+        first, bf16 = _plain_or_parts(x, dtype)
+        out = ops._looked_at(_native.mx_linear, first, _parts(weight), bias, residual, ops._number(activation), p, seed, offset, keep_pre, bf16)
+        if out is not None:
+            return out
     out = ops._unless_followed("mx_linear", "mx_linear_input_grad and mx_linear_weight_grad", (x, bias, residual), lambda: mx_linear(
         x, weight, bias, residual, activation=activation, p=p, seed=seed, offset=offset, keep_pre=keep_pre, dtype=dtype))
     if out is not None:
@@ -209,6 +253,11 @@ def mx_linear_input_grad(dz, weight_t, *, pre=None, activation="none", p=0.0, se
     if stream is not None:
         with _on(stream):
             return mx_linear_input_grad(dz, weight_t, pre=pre, activation=activation, p=p, seed=seed, offset=offset, residual=residual, dtype=dtype)
+    if _is_native():
+        first, bf16 = _plain_or_parts(dz, dtype)
+        out = ops._looked_at(_native.mx_linear_input_grad, first, _parts(weight_t), pre, ops._number(activation), p, seed, offset, residual, bf16)
+        if out is not None:
+            return out
     dt, dtype, rows, cout, front, plain, dzq = _first(dz, "mx_linear_input_grad: dz", dtype)
     act = ops._activation(activation)
     if not isinstance(weight_t, Microscaled):
@@ -229,6 +278,13 @@ def mx_linear_weight_grad(dz_t, x_t, dweight=None, dbias=None, *, bias=True, acc
     if stream is not None:
         with _on(stream):
             return mx_linear_weight_grad(dz_t, x_t, dweight, dbias, bias=bias, accumulate=accumulate)
+    if _is_native() and type(dz_t) is Microscaled and type(x_t) is Microscaled and dz_t.codes.is_cuda and not (accumulate and (dweight is None or (bias and dbias is None))):
+        if dweight is None:
+            dweight = torch.empty((dz_t.rows, x_t.rows), dtype=torch.float32, device=dz_t.device)
+        if dbias is None and bias:
+            dbias = torch.empty(dz_t.rows, dtype=torch.float32, device=dz_t.device)
+        if ops._looked_at(_native.mx_linear_weight_grad, dz_t._parts, x_t._parts, dweight, dbias, accumulate) is not None:
+            return dweight, dbias
     for q, name in ((dz_t, "dz_t"), (x_t, "x_t")):
         if not isinstance(q, Microscaled):
             raise ValueError(f"mx_linear_weight_grad: {name}: a Microscaled matrix is wanted")
@@ -268,12 +324,16 @@ def orthogonalize(g, *, steps=5, coefficients=QUINTIC, eps=1e-7, out=None, strea
     if stream is not None:
         with _on(stream):
             return orthogonalize(g, steps=steps, coefficients=coefficients, eps=eps, out=out)
+    a, b, c = coefficients
+    if _is_native():
+        x = ops._looked_at(_native.orthogonalize, g, steps, a, b, c, eps, out)
+        if x is not None:
+            return x
     if ops._followed((g, out)):
         raise RuntimeError("orthogonalize records nothing for torch's differentiation; g.detach() is orthogonalised")
     dt = ops._first(g, "orthogonalize: g")
     if g.dim() < 2:
         raise ValueError("orthogonalize: g: [..., rows, columns] is wanted")
-    a, b, c = coefficients
     n, (rows, cols) = 1, g.shape[-2:]
     for d in g.shape[:-2]:
         n *= d

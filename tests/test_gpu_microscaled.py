@@ -241,3 +241,62 @@ def test_larger(rows, cin, cout):
         want, bound = torch.matmul(a, b), D.sum_bound(k, 1.0) * torch.matmul(a.abs(), b.abs())
         bad = ~((got.double() - want).abs() <= bound + want.abs() * 2.0**-24 + 1e-38)
         assert not bad.any(), (int(bad.sum()), bad.nonzero()[0])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_the_look_at_the_arguments_in_python_gives_the_same(monkeypatch, dtype):
+    rng = np.random.default_rng(8)
+    x, dz, r = (put(rng.standard_normal(s), dtype, 3)[0] for s in ((40, 300), (40, 70), (40, 70)))
+    w, b, g = put(rng.standard_normal((70, 300)))[0], put(rng.standard_normal(70))[0], put(rng.standard_normal((2, 30, 50)), dtype, 2)[0]
+
+    def everything():
+        wq, wt, xq = mats.microscale(w), mats.microscale(w, transposed=True), mats.microscale(x, rounding="stochastic", seed=1, offset=2)
+        dzt, xt = mats.microscale(dz, transposed=True), mats.microscale(x, transposed=True)
+        out = [wq.codes, wq.scales, wt.codes, wt.scales, xq.values(), xq.values(torch.bfloat16)]
+        out += mats.mx_linear(x, wq, b, r, activation="gelu", p=0.3, seed=4, offset=5, keep_pre=True)
+        out += [mats.mx_linear(x.view(4, 10, 300) if x.is_contiguous() else x, wq), mats.mx_linear(xq, wq, dtype=torch.float32), mats.mx_linear(xq, wq), mats.mx_linear(x[7], wq)]
+        out += [mats.mx_linear_input_grad(dz, wt, pre=x, activation="silu", p=0.2, seed=3, residual=x), mats.mx_linear_input_grad(mats.microscale(dz), wt, dtype=torch.bfloat16)]
+        out += mats.mx_linear_weight_grad(dzt, xt)
+        dw, db = torch.ones(70, 300, device="cuda"), torch.ones(70, device="cuda")
+        out += mats.mx_linear_weight_grad(dzt, xt, dw, db, accumulate=True)
+        out += [mats.mx_linear_weight_grad(dzt, xt, bias=False)[0], mats.orthogonalize(g), mats.orthogonalize(g, steps=2, out=torch.empty_like(g))]
+        return out
+
+    native = everything()
+    assert mats._native is not None
+    monkeypatch.setattr(mats, "_native", None)
+    for a, c in zip(native, everything()):
+        assert a.dtype == c.dtype and torch.equal(a, c)
+
+
+@pytest.mark.parametrize("look", ["native", "python"])
+def test_refusals(monkeypatch, look):
+    mats._load()
+    if look == "python":
+        monkeypatch.setattr(mats, "_native", None)
+    x, w = torch.randn(20, 64, device="cuda"), mats.microscale(torch.randn(32, 64, device="cuda"))
+    q, r = mats.microscale(x), torch.randn(20, 32, device="cuda")
+    for bad in (lambda: mats.microscale(x.half()), lambda: mats.microscale(x.t()), lambda: mats.microscale(x.cpu()), lambda: mats.microscale(x, rounding="down"),
+                lambda: mats.microscale(x, seed=-1), lambda: mats.microscale(x, offset=1 << 64), lambda: mats.microscale(torch.tensor(1.0, device="cuda")), lambda: mats.microscale(3),
+                lambda: mats.mx_linear(x[:, :40], w), lambda: mats.mx_linear(x, x), lambda: mats.mx_linear(q, w, residual=r), lambda: mats.mx_linear(x, w, dtype=torch.bfloat16),
+                lambda: mats.mx_linear(q, w, dtype=torch.float16), lambda: mats.mx_linear(x, w, r), lambda: mats.mx_linear(x, w, activation="tanh"), lambda: mats.mx_linear(x, w, residual=r[:10]),
+                lambda: mats.mx_linear(x, w, seed=-1), lambda: mats.mx_linear_input_grad(x, w, pre=r.bfloat16()), lambda: mats.mx_linear_input_grad(q, q.values()),
+                lambda: mats.mx_linear_weight_grad(q, mats.microscale(x[:, :40])), lambda: mats.mx_linear_weight_grad(q, q, accumulate=True), lambda: mats.mx_linear_weight_grad(q, q, dweight=torch.empty(20, 64, device="cuda")),
+                lambda: mats.mx_linear_weight_grad(q, q, dweight=torch.empty(20, 20)), lambda: mats.mx_linear_weight_grad(q, q, dbias=torch.empty(21, device="cuda")),
+                lambda: q.values(torch.float64), lambda: mats.mx_linear(mats.Microscaled(q.codes.cpu(), q.scales.cpu(), 20, 64), w)):
+        with pytest.raises(ValueError):
+            bad()
+    from paper_2505_14371_amd import qoda
+
+    for bad in (lambda: mats.mx_linear(x, w, p=1.5), lambda: mats.mx_linear_input_grad(x, w, activation="relu")):
+        with pytest.raises(qoda.QodaError):
+            bad()
+    x.requires_grad_()
+    with pytest.raises(RuntimeError, match="no derivative"):
+        mats.microscale(x)
+    y = mats.mx_linear(x, w)
+    assert y.requires_grad
+    with pytest.raises(RuntimeError, match="records nothing"):
+        y.sum().backward()
+    with torch.no_grad():
+        assert not mats.mx_linear(x, w).requires_grad and mats.microscale(x).shape == (20, 64)
