@@ -46,6 +46,17 @@ struct Orthogonal {
   long long first;
 };
 
+// What the sums of a step's three products, and what is added to the second and third, are multiplied with.
+struct StepFactors {
+  float a, b, b_extra, x, x_extra;
+};
+constexpr int kMostSmallSteps = 16;
+struct SmallOrthogonal {
+  Orthogonal o;
+  StepFactors f[kMostSmallSteps];
+  long long first;
+};
+
 // out = a b^T factor + e extra of matrices of pairs, a [m][k], b [n][k], e and out [m][n], out_t [n][m] the transpose of out; x: where the result goes
 // instead, in the caller's type.  symmetric: m = n and out = out_t, of which the tiles above the diagonal are computed.
 struct PairProduct {

@@ -23,22 +23,23 @@ __device__ __forceinline__ void store_scales(const MxRounding &a, const u8 *s, l
   }
 }
 
-template <class T, bool STOCHASTIC>
-__global__ void __launch_bounds__(kWg) k_mx_rows(MxRounding a, long long groups, long long steps) {
+// U: rows that a lane takes one after the other, of 64 / U that the workgroup has at a time.
+template <class T, bool STOCHASTIC, int U>
+__global__ void __launch_bounds__(2048 / U) k_mx_rows(MxRounding a, long long groups, long long steps) {
   __shared__ __align__(16) u8 scales[512];
   const long long id = a.first + blockIdx.x, group = id / steps, step = id - group * steps;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, eight = lane & 31;
   const long long c0 = step * kMxStep + eight * 8;
   const int n = a.cols - c0 < 8 ? (int)(a.cols - c0) : 8;
-  const int row0 = wave * 16 + (lane >> 5);
-  Eight<T> v[8];
+  const int row0 = wave * 2 * U + (lane >> 5);
+  Eight<T> v[U];
 #pragma unroll
-  for (int u = 0; u < 8; ++u) {
+  for (int u = 0; u < U; ++u) {
     const long long r = group * 64 + row0 + 2 * u;
     v[u].load(static_cast<const T *>(a.x) + r * a.ldx + c0, r < a.rows ? n : 0);
   }
 #pragma unroll
-  for (int u = 0; u < 8; ++u) {
+  for (int u = 0; u < U; ++u) {
     const int row = row0 + 2 * u;
     const long long r = group * 64 + row;
     u32 most = most_of(v[u]), other = __shfl_xor(most, 1);
@@ -147,19 +148,29 @@ __global__ void __launch_bounds__(kWg) k_mx_columns(MxRounding a, long long grou
   store_scales(a, scales, group, groups, step);
 }
 
+// Eight entries a lane, 64 rows by 256 entries a workgroup, as they were rounded.
 template <class T>
 __global__ void __launch_bounds__(kWg) k_mx_values(MxRounding a, long long groups, long long steps) {
-  const long long eights = (a.cols + 7) / 8, at = (a.first + blockIdx.x) * kWg + threadIdx.x;
-  if (at >= a.rows * eights) return;
-  const long long r = at / eights, e = at - r * eights;
-  u32 codes;
-  __builtin_memcpy(&codes, a.codes + r * steps * 128 + e * 4, 4);
-  const long long block = e >> 2;
-  const u32 byte = a.scales[((block >> 2) * groups + (r >> 6)) * 256 + scale_place((int)(r & 63), (int)(block & 3))];
-  float v[8];
-  values_of(codes, byte, v);
-  const long long left = a.cols - 8 * e;
-  store8(static_cast<T *>(a.x) + r * a.ldx + 8 * e, left < 8 ? (int)left : 8, v);
+  const long long id = a.first + blockIdx.x, group = id / steps, step = id - group * steps;
+  const int eight = threadIdx.x & 31, row0 = threadIdx.x >> 5;
+  const long long c0 = step * kMxStep + eight * 8;
+  const int n = a.cols - c0 < 8 ? (int)(a.cols - c0) : 8, last = a.rows - group * 64 < 64 ? (int)(a.rows - group * 64) - 1 : 63;
+  const u8 *codes = a.codes + (group * 64 * steps + step) * 128 + eight * 4, *scales = a.scales + ((2 * step + (eight >> 4)) * groups + group) * 256;
+  u32 w[8], byte[8];
+#pragma unroll
+  for (int u = 0; u < 8; ++u) {   // rows behind the last one: that one's again
+    const int row = row0 + 8 * u < last ? row0 + 8 * u : last;
+    __builtin_memcpy(&w[u], codes + row * steps * 128, 4);
+    byte[u] = scales[scale_place(row, eight >> 2 & 3)];
+  }
+  T *y = static_cast<T *>(a.x) + group * 64 * a.ldx + c0;
+#pragma unroll
+  for (int u = 0; u < 8; ++u)
+    if (row0 + 8 * u <= last) {
+      float v[8];
+      values_of(w[u], byte[u], v);
+      store8(y + (row0 + 8 * u) * a.ldx, n, v);
+    }
 }
 
 // The sums of the rows of a microscaled matrix, a wave a row, in fp32.
@@ -191,10 +202,14 @@ template <class T, bool STOCHASTIC>
 void launch_rounding(const MxRounding &q, hipStream_t s) {
   const long long rows = q.transposed ? q.cols : q.rows, along = q.transposed ? q.rows : q.cols;
   const long long groups = mx_groups(rows), steps = mx_steps(along);
-  in_launches(q, groups * steps, kWg, [&](const MxRounding &part, unsigned grid) {
-    if (q.transposed) k_mx_columns<T, STOCHASTIC><<<dim3(grid), kWg, 0, s>>>(part, groups, steps);
-    else k_mx_rows<T, STOCHASTIC><<<dim3(grid), kWg, 0, s>>>(part, groups, steps);
-  });
+  if (q.transposed) {
+    in_launches(q, groups * steps, kWg, [&](const MxRounding &part, unsigned grid) { k_mx_columns<T, STOCHASTIC><<<dim3(grid), kWg, 0, s>>>(part, groups, steps); });
+  } else if (groups * steps < 512) {
+    // fewer workgroups than the device holds: more waves each
+    k_mx_rows<T, STOCHASTIC, 2><<<dim3((unsigned)(groups * steps)), 1024, 0, s>>>(q, groups, steps);
+  } else {
+    in_launches(q, groups * steps, kWg, [&](const MxRounding &part, unsigned grid) { k_mx_rows<T, STOCHASTIC, 8><<<dim3(grid), kWg, 0, s>>>(part, groups, steps); });
+  }
 }
 
 }  // namespace
@@ -206,8 +221,8 @@ hipError_t launch_mx_quantize(const MxRounding &q, hipStream_t s) {
 }
 
 hipError_t launch_mx_values(const MxRounding &q, hipStream_t s) {
-  const long long groups = mx_groups(q.rows), steps = mx_steps(q.cols), eights = q.rows * ((q.cols + 7) / 8);
-  in_launches(q, (eights + kWg - 1) / kWg, kWg, [&](const MxRounding &part, unsigned grid) {
+  const long long groups = mx_groups(q.rows), steps = mx_steps(q.cols);
+  in_launches(q, groups * steps, kWg, [&](const MxRounding &part, unsigned grid) {
     if (q.type == kF32) k_mx_values<float><<<dim3(grid), kWg, 0, s>>>(part, groups, steps);
     else k_mx_values<bf16><<<dim3(grid), kWg, 0, s>>>(part, groups, steps);
   });

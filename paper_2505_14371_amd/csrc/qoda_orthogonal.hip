@@ -365,6 +365,190 @@ __global__ void __launch_bounds__(kWg) k_pair_join(PairProduct p, int splits) {
   }
 }
 
+// Matrices that fit into a workgroup's shared memory with their transpose, A and B: all steps in one launch, a workgroup a matrix.  Rows of pairs as above,
+// 16 bytes further apart than they are long, so that the 16 rows of a read lie in different banks.  A wave takes every eighth pair of a product's pieces of 16 x 16,
+// adjacent ones, which share an operand: what bounds a step is reads of shared memory, the time from one to the sum, and the barriers.  Pieces of X are
+// computed both ways round, from the same operands, which costs less than turning them.
+constexpr int kSmallWaves = 8, kSmallWg = 64 * kSmallWaves;
+
+struct SmallPlaces {   // bytes
+  int x_row, a_row, xt, a, b, all;   // rows of X, and of the others
+  __host__ __device__ SmallPlaces(int m, int n) {
+    x_row = n * 4 + 16, a_row = m * 4 + 16;
+    xt = m * x_row, a = xt + n * a_row, b = a + m * a_row, all = b + m * a_row;
+  }
+};
+
+typedef _Float16 v4h __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ lds_ptr small_place(lds_ptr m, int row_bytes, int i, int j) { return m + i * row_bytes + (j >> 5) * 128 + (j & 31) * 2; }
+__device__ __forceinline__ void small_store(lds_ptr p, v4f v) {
+  v4h hi, lo;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    hi[e] = (_Float16)v[e];
+    lo[e] = (_Float16)(v[e] - (float)hi[e]);
+  }
+  *LDS(v4h, p) = hi;
+  *LDS(v4h, p + 64) = lo;
+}
+__device__ __forceinline__ v4f small_load(lds_ptr p) {
+  const v4h hi = *LDS(v4h, p), lo = *LDS(v4h, p + 64);
+  v4f v;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] = (float)hi[e] + (float)lo[e];
+  return v;
+}
+
+// A wave's pairs of pieces of a product of rows with rows, `across` pieces (an even number) in a row of the result.
+template <int P>
+struct SmallPairs {
+  int mine, ia[P], ib[P];
+  __device__ __forceinline__ SmallPairs(int wave, int pairs, int across) {
+    mine = (pairs - wave + kSmallWaves - 1) / kSmallWaves;
+#pragma unroll
+    for (int u = 0; u < P; ++u) {
+      const int q = 2 * (u * kSmallWaves + wave), row = q / across;
+      ia[u] = __builtin_amdgcn_readfirstlane(row * 16), ib[u] = __builtin_amdgcn_readfirstlane((q - row * across) * 16);
+    }
+  }
+};
+// Pieces (ia, ib) and (ia, ib + 16).  c: lane 16 g + i has the sums of a's row i with b's rows 4 g .. 4 g + 3; d, TURNED: of b's row i with a's.
+template <bool TURNED>
+__device__ __forceinline__ void small_sums(lds_ptr a, int ia, lds_ptr b, int ib, int row_bytes, int steps, v4f (&c)[2], v4f (&d)[2]) {
+  const int lane = threadIdx.x & 63, key = (lane & 15) * row_bytes + (lane >> 4) * 16;
+  lds_ptr pa = a + (ia * row_bytes + key), pb = b + (ib * row_bytes + key);
+#pragma unroll
+  for (int h = 0; h < 2; ++h) c[h] = d[h] = v4f{0, 0, 0, 0};
+#pragma unroll 1
+  for (int k = 0; k < steps; ++k, pa += 128, pb += 128) {
+    const v4u ah = *LDS(v4u, pa), al = *LDS(v4u, pa + 64);
+    v4u bh[2], bl[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) bh[h] = *LDS(v4u, pb + h * 16 * row_bytes), bl[h] = *LDS(v4u, pb + h * 16 * row_bytes + 64);
+#pragma unroll
+    for (int part = 0; part < 3; ++part)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const v4u fa = part == 2 ? al : ah, fb = part == 1 ? bl[h] : bh[h];
+        c[h] = multiply_halves(fb, fa, c[h]);
+        if constexpr (TURNED) d[h] = multiply_halves(fa, fb, d[h]);
+      }
+  }
+}
+
+// P: pairs of pieces of X that a wave has.
+template <class T, int P, int BYTES>
+__global__ void __launch_bounds__(kSmallWg) k_small(SmallOrthogonal s) {
+  __shared__ __align__(16) char shared[BYTES];
+  __shared__ double part[kSmallWaves];
+  const Orthogonal &o = s.o;
+  const long long matrix = s.first + blockIdx.x;
+  const int m = (int)o.m, n = (int)o.n, rows = (int)o.rows, cols = (int)o.cols, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+  const SmallPlaces at(m, n);
+  const lds_ptr xs = (lds_ptr)shared, xt = xs + at.xt, a = xs + at.a, b = xs + at.b;
+  const T *from = static_cast<const T *>(o.g) + matrix * o.g_matrix;
+  float v[8 * P];   // rows cols <= m n = 512 pairs, 8 P of them
+  double sum = 0.0;
+#pragma unroll
+  for (int u = 0; u < 8 * P; ++u) {
+    const int q = u * kSmallWg + (int)threadIdx.x, r = q / cols;
+    v[u] = q < rows * cols ? to_float(from[(long long)r * o.g_row + (q - r * cols)]) : 0.0f;
+  }
+  for (int q = threadIdx.x; q < at.a / 16; q += kSmallWg) *LDS(v4u, xs + q * 16) = v4u{0, 0, 0, 0};
+#pragma unroll
+  for (int u = 0; u < 8 * P; ++u) sum = sum + (double)v[u] * (double)v[u];
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) sum = sum + __shfl_xor(sum, d);
+  if (lane == 0) part[wave] = sum;
+  __syncthreads();
+  sum = 0.0;
+#pragma unroll
+  for (int w = 0; w < kSmallWaves; ++w) sum = sum + part[w];
+  const double inverse = 1.0 / (sqrt(sum) + o.eps) * (double)o.scale;
+#pragma unroll
+  for (int u = 0; u < 8 * P; ++u) {
+    const int q = u * kSmallWg + (int)threadIdx.x, r = q / cols, c = q - r * cols, xi = o.transposed ? c : r, xj = o.transposed ? r : c;
+    if (q < rows * cols) {
+      const float x = (float)((double)v[u] * inverse);
+      const _Float16 hi = (_Float16)x, lo = (_Float16)(x - (float)hi);
+      const lds_ptr p = small_place(xs, at.x_row, xi, xj), pt = small_place(xt, at.a_row, xj, xi);
+      *LDS(_Float16, p) = hi, *LDS(_Float16, p + 64) = lo;
+      *LDS(_Float16, pt) = hi, *LDS(_Float16, pt + 64) = lo;
+    }
+  }
+  __syncthreads();
+  const SmallPairs<P> square(wave, m / 16 * (m / 16) / 2, m / 16), wide(wave, m / 16 * (n / 16) / 2, n / 16);
+  for (int k = 0; k < o.steps; ++k) {
+    const StepFactors f = s.f[k];
+#pragma unroll
+    for (int u = 0; u < P; ++u)
+      if (u < square.mine) {
+        v4f c[2], d[2];
+        const int ia = square.ia[u], ib = square.ib[u];
+        small_sums<false>(xs, ia, xs, ib, at.x_row, n / 32, c, d);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) small_store(small_place(a, at.a_row, ia + i, ib + 16 * h + 4 * g), c[h] * f.a);
+      }
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < P; ++u)
+      if (u < square.mine) {
+        v4f c[2], d[2];
+        const int ia = square.ia[u], ib = square.ib[u];
+        small_sums<false>(a, ia, a, ib, at.a_row, m / 32, c, d);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const v4f was = small_load(small_place(a, at.a_row, ia + i, ib + 16 * h + 4 * g));
+          small_store(small_place(b, at.a_row, ia + i, ib + 16 * h + 4 * g), c[h] * f.b + was * f.b_extra);
+        }
+      }
+    __syncthreads();
+    v4f c[P][2], d[P][2];
+#pragma unroll
+    for (int u = 0; u < P; ++u)
+      if (u < wide.mine) {
+        const int ia = wide.ia[u], ib = wide.ib[u];
+        small_sums<true>(b, ia, xt, ib, at.a_row, m / 32, c[u], d[u]);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          c[u][h] = c[u][h] * f.x + small_load(small_place(xs, at.x_row, ia + i, ib + 16 * h + 4 * g)) * f.x_extra;
+          d[u][h] = d[u][h] * f.x + small_load(small_place(xt, at.a_row, ib + 16 * h + i, ia + 4 * g)) * f.x_extra;
+        }
+      }
+    const bool last = k + 1 == o.steps;
+    if (!last) __syncthreads();   // nobody reads X's transpose any more
+    T *to = static_cast<T *>(o.x) + matrix * o.x_matrix;
+#pragma unroll
+    for (int u = 0; u < P; ++u)
+      if (u < wide.mine)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int ia = wide.ia[u], ib = wide.ib[u] + 16 * h;
+          if (!last) {
+            small_store(small_place(xs, at.x_row, ia + i, ib + 4 * g), c[u][h]);
+            small_store(small_place(xt, at.a_row, ib + i, ia + 4 * g), d[u][h]);
+          } else {
+            const int r = (o.transposed ? ib : ia) + i, c0 = (o.transposed ? ia : ib) + 4 * g;
+            const v4f x = o.transposed ? d[u][h] : c[u][h];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (r < rows && c0 + e < cols) to[(long long)r * o.x_row + c0 + e] = from_float<T>(x[e]);
+          }
+        }
+    if (!last) __syncthreads();
+  }
+}
+
+constexpr int kMostSmall = 163840 - 128;   // bytes of shared memory, less the sums'
+
+// How many pairs of pieces of X a wave has where the matrices go into shared memory, otherwise 0.
+int small_pairs(const Orthogonal &o) {
+  if (o.steps < 1 || o.steps > kMostSmallSteps || o.m > 1024 || o.n > 1024 || SmallPlaces((int)o.m, (int)o.n).all > kMostSmall) return 0;
+  const int pairs = (int)(o.m * o.n / 512);
+  return pairs <= kSmallWaves ? 1 : pairs <= 2 * kSmallWaves ? 2 : pairs <= 5 * kSmallWaves ? 5 : 0;
+}
+
 constexpr int kCus = 256;
 
 enum Tile { kTile64, kTile128, kTile256 };
@@ -445,6 +629,7 @@ Layout layout_of(const Orthogonal &o) {
     at += (bytes + 255) & ~(size_t)255;
     return here;
   };
+  if (small_pairs(o)) return l;
   l.squares = take(sizeof(double) * (size_t)o.matrices * o.parts);
   if (o.steps > 0) {
     const size_t wide = (size_t)o.matrices * o.m * o.n * 4, square = (size_t)o.matrices * o.m * o.m * 4;
@@ -523,6 +708,32 @@ hipError_t launch_orthogonalize(const Orthogonal &call, void *workspace, hipStre
   double size = 1.0;
   int ex = exponent_for(size);
   o.scale = std::ldexp(1.0f, ex);
+  const auto factors = [&](int k) {   // of step k, and on to the next
+    const double next = largest(o.a, o.b, o.c, size);
+    const int ea = exponent_for(size * size), eb = exponent_for(largest_inner(o.b, o.c, size * size)), en = k + 1 < o.steps ? exponent_for(next) : 0;
+    const StepFactors f = {std::ldexp(1.0f, ea - 2 * ex), (float)std::ldexp(o.c, eb - 2 * ea), (float)std::ldexp(o.b, eb - ea), std::ldexp(1.0f, en - eb - ex),
+                           (float)std::ldexp(o.a, en - ex)};
+    size = next, ex = en;
+    return f;
+  };
+  if (const int pairs = small_pairs(o)) {
+    const int bytes = SmallPlaces((int)o.m, (int)o.n).all;
+    SmallOrthogonal small = {o, {}, 0};
+    for (int k = 0; k < o.steps; ++k) small.f[k] = factors(k);
+    in_launches(small, o.matrices, kSmallWg, [&](const SmallOrthogonal &part, unsigned x) {
+      const auto go = [&](auto t) {
+        typedef decltype(t) T;
+        // several workgroups a CU where they fit
+        if (pairs == 1 && bytes <= 40960 - 128) k_small<T, 1, 40960 - 128><<<dim3(x), kSmallWg, 0, s>>>(part);
+        else if (pairs == 1 && bytes <= 81920 - 128) k_small<T, 1, 81920 - 128><<<dim3(x), kSmallWg, 0, s>>>(part);
+        else if (pairs <= 2) k_small<T, 2, kMostSmall><<<dim3(x), kSmallWg, 0, s>>>(part);
+        else k_small<T, 5, kMostSmall><<<dim3(x), kSmallWg, 0, s>>>(part);
+      };
+      if (o.type == kF32) go(float());
+      else go(bf16());
+    });
+    return hipGetLastError();
+  }
   in_launches(o, o.matrices * o.parts, kWg, [&](const Orthogonal &part, unsigned x) {
     if (o.type == kF32) k_squares<float><<<dim3(x), kWg, 0, s>>>(part);
     else k_squares<bf16><<<dim3(x), kWg, 0, s>>>(part);
@@ -539,25 +750,20 @@ hipError_t launch_orthogonalize(const Orthogonal &call, void *workspace, hipStre
   });
   float *partial = reinterpret_cast<float *>(w + l.partial);
   for (int k = 0; k < o.steps; ++k) {
-    const double next = largest(o.a, o.b, o.c, size);
-    const int ea = exponent_for(size * size), eb = exponent_for(largest_inner(o.b, o.c, size * size)), en = exponent_for(next);
-    const bool last = k + 1 == o.steps;
-    char *xt = w + l.xt[k & 1];
+    const StepFactors f = factors(k);
     PairProduct p = shape_of(o, 0);   // A
     p.a = p.b = o.xs, p.out = p.out_t = w + l.a;
-    p.factor = std::ldexp(1.0f, ea - 2 * ex);
+    p.factor = f.a;
     launch_pairs(p, partial, s);
     p = shape_of(o, 1);               // B = b A + c A A
     p.a = p.b = p.e = w + l.a, p.out = p.out_t = w + l.b;
-    p.factor = (float)std::ldexp(o.c, eb - 2 * ea), p.extra = (float)std::ldexp(o.b, eb - ea);
+    p.factor = f.b, p.extra = f.b_extra;
     launch_pairs(p, partial, s);
     p = shape_of(o, 2);               // a X + B X
-    const int to = last ? 0 : en;
-    p.a = w + l.b, p.b = xt, p.e = o.xs, p.out = o.xs, p.out_t = w + l.xt[1 - (k & 1)];
-    p.factor = std::ldexp(1.0f, to - eb - ex), p.extra = (float)std::ldexp(o.a, to - ex);
-    if (last) p.x = o.x, p.x_matrix = o.x_matrix, p.x_row = o.x_row, p.x_rows = o.rows, p.x_cols = o.cols, p.x_transposed = o.transposed, p.type = o.type;
+    p.a = w + l.b, p.b = w + l.xt[k & 1], p.e = o.xs, p.out = o.xs, p.out_t = w + l.xt[1 - (k & 1)];
+    p.factor = f.x, p.extra = f.x_extra;
+    if (k + 1 == o.steps) p.x = o.x, p.x_matrix = o.x_matrix, p.x_row = o.x_row, p.x_rows = o.rows, p.x_cols = o.cols, p.x_transposed = o.transposed, p.type = o.type;
     launch_pairs(p, partial, s);
-    size = next, ex = en;
   }
   return hipGetLastError();
 }

@@ -88,6 +88,23 @@ def test_orthogonalize(m, n, dtype):
         assert mats.orthogonalize(g, steps=steps, out=g) is g and torch.equal(g, x)
 
 
+@pytest.mark.parametrize("m,n", SHAPES)
+def test_many_steps(m, n):
+    """More than are taken in one launch."""
+    g, gd = put(matrices(np.random.default_rng([m, n, 1]), 2, m, n), "f32")
+    check(mats.orthogonalize(g, steps=17, coefficients=(1.5, -0.5, 0.0)), gd, 17, (1.5, -0.5, 0.0), 1e-7, "f32")
+
+
+# the largest that stay in shared memory and the smallest that do not, both ways round, and batches of more matrices than the device holds at once
+@pytest.mark.parametrize("batch,m,n", [(1, 96, 96), (1, 97, 96), (1, 32, 512), (2, 544, 20), (1, 30, 545), (1, 64, 192), (3, 193, 64), (2000, 17, 40), (600, 64, 64), (300, 96, 70)])
+def test_at_the_border_of_shared_memory(batch, m, n):
+    g, gd = put(matrices(np.random.default_rng([m, n, 2]), batch, m, n), "f32")
+    x = mats.orthogonalize(g)
+    for k in {0, batch // 2, batch - 1}:
+        check(x[k], gd[k], 5, Q, 1e-7, "f32")
+    assert torch.equal(mats.orthogonalize(g[batch - 1]), x[batch - 1])
+
+
 @pytest.mark.parametrize("coefficients,steps", [((1.5, -0.5, 0.0), 8), ((2.0, -1.5, 0.5), 6), ((1.0, 0.0, 0.0), 4), ((0.0, 0.0, 0.0), 2), ((3.0, 1.0, 0.0), 3), ((0.0, 0.0, 1.0), 2),
                                                 ((-2.0, 1.5, -0.5), 5), ((1e-3, 1e-4, 1e-4), 3), ((100.0, -20.0, 3.0), 2)])
 def test_other_polynomials(coefficients, steps):

@@ -166,9 +166,11 @@ def test_arguments_that_python_refuses(lib):
 
 
 def test_bounded_polynomials_are_taken_for_any_number_of_steps(lib):
+    wide = dict(rows=300, cols=400, gr=400, gm=120000, xr=400, xm=120000)
     for steps in (0, 1, 1000, 2**31 - 1):
-        assert lib.qoda_orthogonalize_workspace_bytes(orthogonalize(steps=steps)[1]) > 0
-    assert lib.qoda_orthogonalize_workspace_bytes(orthogonalize(a=10.0, b=0.0, c=0.0, steps=12)[1]) > 0
-    name, args = orthogonalize()
+        assert lib.qoda_orthogonalize_workspace_bytes(orthogonalize(steps=steps, **wide)[1]) > 0
+    assert lib.qoda_orthogonalize_workspace_bytes(orthogonalize(a=10.0, b=0.0, c=0.0, steps=12, **wide)[1]) > 0
+    assert lib.qoda_orthogonalize_workspace_bytes(orthogonalize()[1]) == 0          # small ones stay in shared memory
+    name, args = orthogonalize(**wide)
     need = lib.qoda_orthogonalize_workspace_bytes(args)
     assert call(lib, name, args, A, need - 1) == qoda.EINVAL and "workspace" in lib.qoda_operator_error().decode()
