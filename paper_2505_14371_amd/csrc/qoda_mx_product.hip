@@ -193,7 +193,7 @@ __global__ void __launch_bounds__(64 * WM * WN, BM == 128 ? 2 : 1) k_mx_product(
   });
 }
 
-// Up to 16 rows of x, plain ones rounded here: b is read once, and that is the time.  A workgroup takes 32 rows of b, its NW waves the steps in turn; a
+// Up to 16 rows of x, plain ones rounded here: b is read once, and that is the time.  A workgroup takes 32 rows of b, its NW waves the half steps in turn; a
 // lane's block of x is 32 adjacent entries, so that its scale needs no other lane.
 template <class T, int FORM, int NW, bool PLAIN>
 __global__ void __launch_bounds__(64 * NW) k_mx_few_rows(MxProduct m) {
@@ -211,58 +211,54 @@ __global__ void __launch_bounds__(64 * NW) k_mx_few_rows(MxProduct m) {
   }
   const u8 *sb = m.b_scales + (long long)(j0 / 64) * 256 + lane * 4 + (j0 & 32 ? 2 : 0);
   const u8 *a = PLAIN ? nullptr : m.a + (long long)(i < p.m ? i : 0) * row_bytes + g * 16;
-  const u8 *sa = PLAIN ? nullptr : m.a_scales + scale_place(i, g);
+  const u8 *sa = PLAIN ? nullptr : m.a_scales + scale_place(i, g);   // up to 16 rows: one group
   const T *x = static_cast<const T *>(m.x) + (long long)(i < p.m ? i : 0) * m.ldx;
   v4f c[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
-  for (int t0 = wave; t0 < m.steps; t0 += NW * kAhead) {
-    v4u fb[kAhead][2][2], fa[kAhead][2];
-    u32 qb[kAhead][2], qa[kAhead][2];
+  const int halves = 2 * m.steps;
+  for (int t0 = wave; t0 < halves; t0 += NW * kAhead) {
+    v4u fb[kAhead][2], fa[kAhead];
+    u32 qb[kAhead], qa[kAhead];
+    Eight<T> e[PLAIN ? kAhead : 1][4];
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
       const int t = t0 + u * NW;
-      if (t < m.steps)
+      if (t < halves) {
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-#pragma unroll
-          for (int h = 0; h < 2; ++h) __builtin_memcpy(&fb[u][s][h], b[h] + (long long)t * 128 + s * 64, 16);
-          unsigned short w;
-          __builtin_memcpy(&w, sb + (2ll * t + s) * groups * 256, 2);
-          qb[u][s] = w;
-          if constexpr (!PLAIN) {
-            __builtin_memcpy(&fa[u][s], a + (long long)t * 128 + s * 64, 16);
-            qa[u][s] = sa[(2ll * t + s) * 256];   // up to 16 rows: one group
-          }
-        }
-    }
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      const int t = t0 + u * NW;
-      if (t >= m.steps) break;
-#pragma unroll
-      for (int s = 0; s < 2; ++s) {
+        for (int h = 0; h < 2; ++h) __builtin_memcpy(&fb[u][h], b[h] + (long long)t * 64, 16);
+        unsigned short w;
+        __builtin_memcpy(&w, sb + (long long)t * groups * 256, 2);
+        qb[u] = w;
         if constexpr (PLAIN) {
-          const long long l = (long long)t * kMxStep + s * 128 + g * 32;
-          Eight<T> e[4];
-          u32 most = 0;
+          const long long l = (long long)t * 128 + g * 32;
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
             const long long left = p.k - l - 8 * k;
-            e[k].load(x + l + 8 * k, i < p.m ? (left < 8 ? (int)left : 8) : 0);
+            e[u][k].load(x + l + 8 * k, i < p.m ? (left < 8 ? (int)left : 8) : 0);
           }
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const u32 one = most_of(e[k]);
-            most = most > one ? most : one;
-          }
-          qa[u][s] = scale_byte(most, false);
-#pragma unroll
-          for (int k = 0; k < 4; ++k) fa[u][s][k] = qa[u][s] == 255u ? 0u : codes_nearest(e[k], scale_of(qa[u][s]));
-        } else if (i >= p.m) {
-          fa[u][s] = v4u{0, 0, 0, 0};
+        } else {
+          __builtin_memcpy(&fa[u], a + (long long)t * 64, 16);
+          qa[u] = sa[(long long)t * 256];
         }
-        c[0] = multiply_blocks<0, 0>(fb[u][s][0], fa[u][s], c[0], qb[u][s], qa[u][s]);
-        c[1] = multiply_blocks<1, 0>(fb[u][s][1], fa[u][s], c[1], qb[u][s], qa[u][s]);
       }
+    }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      if (t0 + u * NW >= halves) break;
+      if constexpr (PLAIN) {
+        u32 most = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const u32 one = most_of(e[u][k]);
+          most = most > one ? most : one;
+        }
+        qa[u] = scale_byte(most, false);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) fa[u][k] = qa[u] == 255u ? 0u : codes_nearest(e[u][k], scale_of(qa[u]));
+      } else if (i >= p.m) {
+        fa[u] = v4u{0, 0, 0, 0};
+      }
+      c[0] = multiply_blocks<0, 0>(fb[u][0], fa[u], c[0], qb[u], qa[u]);
+      c[1] = multiply_blocks<1, 0>(fb[u][1], fa[u], c[1], qb[u], qa[u]);
     }
   }
   part[wave][0][lane] = c[0];
@@ -294,40 +290,52 @@ struct Plan {
 
 constexpr int kCus = 256;
 
-// What a cut would take, in us: the matrix cores' rate in whole tiles, a step's least time, a tile's start and end, the join of splits.
-double time_of(const Product &p, int bm, int bn, int a_cu, double rate, long long tiles, int steps, int splits) {
+// What a cut would take, in us, from what was measured: the matrix cores' rate in whole tiles of a size, the time of a step in a workgroup that is alone on its CU, what a
+// tile's end reads and writes at the rate of memory (half of it is hidden where a CU holds several workgroups), and the join of splits.  Measured and
+// estimated: 16384 x 2048 over 8192 with dropout and residual by 256 168 and 175, by 128 185 and 199; 8192 x 8192 over 2048 through gelu' by 256 157 and 142, by
+// 128 142 and 132; 64 x 64 over 16384 in 8 parts 9.5 and 15.
+struct Kind {
+  Tile tile;
+  int side, a_cu;
+  double rate, least;
+};
+constexpr Kind kKinds[] = {{kTile64, 64, 4, 2000e12, 0.45}, {kTile128, 128, 2, 3100e12, 0.6}, {kTile256, 256, 1, 3800e12, 1.3}};
+
+double time_of(const Product &p, const Kind &kind, long long tiles, int steps, int splits) {
   const int steps_each = (steps + splits - 1) / splits;
-  const double one = 2.0 * bm * bn * kMxStep / (rate / kCus) * 1e6;
+  const double one = 2.0 * kind.side * kind.side * kMxStep / (kind.rate / kCus) * 1e6;
   long long left = tiles * splits;
   double us = 0.0;
   while (left > 0) {
-    const long long now = left < (long long)a_cu * kCus ? left : (long long)a_cu * kCus, rounds = left / now;
-    const int sharing = (int)((now + kCus - 1) / kCus);
-    const double step = sharing * one;
-    us += (double)rounds * (2.0 + steps_each * (step > 0.4 ? step : 0.4));
+    const long long now = left < (long long)kind.a_cu * kCus ? left : (long long)kind.a_cu * kCus, rounds = left / now;
+    const double step = (double)((now + kCus - 1) / kCus) * one;
+    us += (double)rounds * (2.0 + steps_each * (step > kind.least ? step : kind.least));
     left -= rounds * now;
   }
-  if (splits > 1) us += 5.0 + 0.4 * splits + (double)splits * p.m * p.n * 8.0 / 4e6;
-  return us;
+  const double entry = p.form == kProductColumns || p.type == kF32 ? 4.0 : 2.0, moved = 1.0 + (p.pre ? 1.0 : 0.0) + (p.extra || p.accumulate ? 1.0 : 0.0);
+  const double end = (double)p.m * p.n * entry * moved / 5e6;
+  if (splits > 1) return us + 5.0 + 0.4 * splits + (double)splits * p.m * p.n * 8.0 / 4e6 + end;
+  return us + (kind.a_cu == 1 ? end : 0.5 * end);
 }
+
+bool few_rows(const Product &p) { return p.form != kProductColumns && p.m <= 16; }
 
 Plan plan_of(const MxProduct &m) {
   const Product &p = m.p;
   Plan q = {};
   q.splits = 1;
   if (p.m == 0 || p.n == 0) return q;
-  if (mx_takes_plain_rows(p)) {
+  if (few_rows(p)) {
     q.tile = kFewRows, q.tiles_m = 1, q.tiles_n = (p.n + 31) / 32;
     return q;
   }
-  const struct { Tile tile; int side, a_cu; double rate; } cuts[] = {{kTile64, 64, 2, 1500e12}, {kTile128, 128, 2, 2500e12}, {kTile256, 256, 1, 3500e12}};
   const int steps = m.steps > 0 ? m.steps : 1;
   double least = 0.0;
   int side = 0;
-  for (const auto &c : cuts) {
+  for (const Kind &c : kKinds) {
     const long long n = ((p.m + c.side - 1ll) / c.side) * ((p.n + c.side - 1ll) / c.side);
     for (int splits = 1; splits == 1 || (splits <= 64 && splits * 2 <= steps && n * splits <= c.a_cu * kCus); ++splits) {
-      const double us = time_of(p, c.side, c.side, c.a_cu, c.rate, n, steps, splits);
+      const double us = time_of(p, c, n, steps, splits);
       if (least == 0.0 || us < least) least = us, q.tile = c.tile, q.splits = splits, side = c.side;
     }
   }
@@ -379,7 +387,9 @@ void launch(const MxProduct &m, const Plan &q, hipStream_t s) {
 
 }  // namespace
 
-bool mx_takes_plain_rows(const Product &p) { return p.form != kProductColumns && p.m <= 16; }
+// Every workgroup of k_mx_few_rows rounds all of x: 0.3 ns for each 32 rows of b and half step.  Where that is more than a launch's 3.5 us, x is rounded before: one
+// row, 8192 -> 50304, 71 us inside and 45 before; 2048 -> 8192 5.3 and 8.8.
+bool mx_takes_plain_rows(const Product &p) { return few_rows(p) && ((p.n + 31ll) / 32) * ((p.k + 127ll) / 128) <= 12000; }
 
 size_t mx_product_scratch(const MxProduct &m) {
   const Plan q = plan_of(m);

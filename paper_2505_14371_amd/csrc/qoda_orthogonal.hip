@@ -694,7 +694,7 @@ void orthogonal_sides(Orthogonal *o) {
   o->transposed = o->rows > o->cols;
   o->m = up32(o->transposed ? o->cols : o->rows), o->n = up32(o->transposed ? o->rows : o->cols);
   const long long eights = o->rows * ((o->cols + 7) / 8), parts = (eights + kWg * 8 - 1) / (kWg * 8);
-  o->parts = (int)(parts < 1 ? 1 : parts > 256 ? 256 : parts);
+  o->parts = (int)(parts < 1 ? 1 : parts > 1024 ? 1024 : parts);
 }
 
 size_t orthogonal_scratch(const Orthogonal &o) { return layout_of(o).all; }

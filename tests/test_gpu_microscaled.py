@@ -135,7 +135,7 @@ def matrix(rng, rows, cols, dtype="f32", pad=0):
 
 PRODUCTS = [(0, 5, 7), (5, 0, 7), (20, 0, 7), (5, 7, 0), (1, 1, 1), (1, 64, 256), (1, 513, 130), (2, 7, 3), (3, 33, 257), (5, 200, 410), (16, 64, 64), (17, 65, 33),
             (33, 410, 100), (64, 64, 128), (65, 129, 127), (127, 40, 129), (128, 256, 128), (130, 31, 258), (257, 96, 255), (256, 128, 256),
-            (300, 520, 264), (513, 72, 520), (1024, 64, 8), (7, 2100, 410), (40, 4100, 24), (700, 24, 1000), (9, 300, 40000)]
+            (300, 520, 264), (513, 72, 520), (1024, 64, 8), (7, 2100, 410), (40, 4100, 24), (700, 24, 1000), (9, 300, 40000), (2, 2000, 30000)]
 
 
 @pytest.mark.parametrize("plain", [True, False])
