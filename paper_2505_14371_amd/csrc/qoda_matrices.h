@@ -57,15 +57,15 @@ struct SmallOrthogonal {
   long long first;
 };
 
-// out = a b^T factor + e extra of matrices of pairs, a [m][k], b [n][k], e and out [m][n], out_t [n][m] the transpose of out; x: where the result goes
+// out = a b^T factor + e extra + e2 extra2 of matrices of pairs, a [m][k], b [n][k], e, e2 (each may be null) and out [m][n], out_t [n][m] the transpose of out; x: where the result goes
 // instead, in the caller's type.  symmetric: m = n and out = out_t, of which the tiles above the diagonal are computed.
 struct PairProduct {
   int symmetric, type, x_transposed;
   long long matrices, m, n, k;
-  const void *a, *b, *e;
+  const void *a, *b, *e, *e2;
   void *out, *out_t, *x;
   long long x_matrix, x_row, x_rows, x_cols;
-  float factor, extra;
+  float factor, extra, extra2;
   float *partial;   // of split sums: [splits][matrices][m][n]
   long long first;
 };

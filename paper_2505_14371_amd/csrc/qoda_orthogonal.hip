@@ -125,20 +125,21 @@ __global__ void __launch_bounds__(kWg) k_start(Orthogonal o, long long tiles_r, 
   }
 }
 
-// What becomes of eight sums adjacent in a row: v = sums * factor + what E has there * extra, which is then stored as T's or as pairs.
+// What becomes of eight sums adjacent in a row: v = sums * factor + what E and E2 have there * extra and extra2, which is then stored as T's or as pairs.
 struct Place {
   const PairProduct &p;
   long long matrix;
+  __device__ __forceinline__ void add(const void *e, float extra, int i, int j, float (&v)[8]) const {
+    float was[8];
+    load_pairs(pair_place(const_cast<char *>(static_cast<const char *>(e) + matrix * p.m * p.n * 4), p.n, i, j), was);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = __builtin_fmaf(was[e], extra, v[e]);
+  }
   __device__ __forceinline__ void finish(int i, int j, float (&v)[8]) const {
-    if (p.e) {
-      float was[8];
-      load_pairs(pair_place(const_cast<char *>(static_cast<const char *>(p.e) + matrix * p.m * p.n * 4), p.n, i, j), was);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = __builtin_fmaf(was[e], p.extra, v[e] * p.factor);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = v[e] * p.factor;
-    }
+    for (int e = 0; e < 8; ++e) v[e] = v[e] * p.factor;
+    if (p.e) add(p.e, p.extra, i, j, v);
+    if (p.e2) add(p.e2, p.extra2, i, j, v);
   }
   template <class T>
   __device__ __forceinline__ void plain(long long i, long long j, const float (&v)[8]) const {
@@ -555,6 +556,7 @@ enum Tile { kTile64, kTile128, kTile256 };
 struct Cut {
   Tile tile;
   int side, splits, steps_each;
+  double us;   // estimated
 };
 
 long long tiles_of(const PairProduct &p, int side) {
@@ -582,7 +584,7 @@ Cut cut_of(const PairProduct &p) {
         left -= rounds * now;
       }
       if (splits > 1) us += 5.0 + (double)splits * p.matrices * p.m * p.n * (p.symmetric ? 4.0 : 8.0) / 4e6;
-      if (least == 0.0 || us < least) least = us, best = {c.tile, c.side, splits, each};
+      if (least == 0.0 || us < least) least = us, best = {c.tile, c.side, splits, each, us};
     }
   }
   best.splits = (steps + best.steps_each - 1) / best.steps_each;
@@ -597,8 +599,7 @@ void launch_tiles(const PairProduct &p, const Cut &c, hipStream_t s) {
   });
 }
 
-void launch_pairs(PairProduct p, float *partial, hipStream_t s) {
-  const Cut c = cut_of(p);
+void launch_pairs(PairProduct p, const Cut &c, float *partial, hipStream_t s) {
   p.partial = c.splits > 1 ? partial : nullptr;
   switch (c.tile) {
     case kTile64: launch_tiles<64, 2, 2>(p, c, s); break;
@@ -618,8 +619,23 @@ PairProduct shape_of(const Orthogonal &o, int which) {
   return p;
 }
 
+// Two steps can be taken at once, from step k on: with A of X and B = b A + c A A the next step's A is (a + B) A (a + B) = N B + a^2 A, N = B A + 2 a A, and
+// both steps are X <- a^2 X + R X with R = B' B + a B' + a B, B' of that A.  Three symmetric products of [m][m] in the place of A from X and one of
+// B X: 9 of 26 m^3 less where n = 4 m.  A's rounding errors then count (a + b s^2 + ..)^2 times, 12 times where singular values are small, beside those of X itself.
+// For fp32 the last two steps are taken so, whose errors no later step multiplies; for bf16, whose store rounds 2^13 times as much, all but the first.
+struct Cuts {   // of a step's products
+  Cut c[3];
+  explicit Cuts(const Orthogonal &o) {
+    for (int w = 0; w < 3; ++w) c[w] = cut_of(shape_of(o, w));
+  }
+  bool two_at_once(const Orthogonal &o, int k) const {
+    if (o.steps - k < 2 || (o.type == kF32 ? o.steps - k != 2 : k == 0 || (o.steps - k) % 2 != 0)) return false;
+    return c[0].us + c[2].us > 3.0 * (c[1].us + 1.5);
+  }
+};
+
 struct Layout {   // of the workspace, in bytes
-  size_t squares, xs, xt[2], a, b, partial, all;
+  size_t squares, xs, xt[2], a, b, c, d, partial, all;
 };
 Layout layout_of(const Orthogonal &o) {
   Layout l = {};
@@ -635,10 +651,12 @@ Layout layout_of(const Orthogonal &o) {
     const size_t wide = (size_t)o.matrices * o.m * o.n * 4, square = (size_t)o.matrices * o.m * o.m * 4;
     l.xs = take(wide), l.xt[0] = take(wide), l.xt[1] = take(wide);
     l.a = take(square), l.b = take(square);
+    const Cuts cuts(o);
+    if (o.steps > 1 && cuts.two_at_once(o, o.steps - 2)) l.c = take(square), l.d = take(square);
     size_t most = 0;
     for (int w = 0; w < 3; ++w) {
       const PairProduct p = shape_of(o, w);
-      const Cut c = cut_of(p);
+      const Cut &c = cuts.c[w];
       const size_t bytes = c.splits > 1 ? (size_t)c.splits * p.matrices * p.m * p.n * 4 : 0;
       most = bytes > most ? bytes : most;
     }
@@ -749,21 +767,50 @@ hipError_t launch_orthogonalize(const Orthogonal &call, void *workspace, hipStre
     }
   });
   float *partial = reinterpret_cast<float *>(w + l.partial);
-  for (int k = 0; k < o.steps; ++k) {
-    const StepFactors f = factors(k);
+  if (o.steps == 0) return hipGetLastError();
+  const Cuts cuts(o);
+  const auto square = [&](size_t a, size_t b, size_t out, double factor, size_t e, double extra, size_t e2 = 0, double extra2 = 0.0) {   // symmetric; 0: no such matrix
+    PairProduct p = shape_of(o, 1);
+    p.a = w + a, p.b = w + b, p.out = p.out_t = w + out;
+    p.factor = (float)factor;
+    if (e) p.e = w + e, p.extra = (float)extra;
+    if (e2) p.e2 = w + e2, p.extra2 = (float)extra2;
+    launch_pairs(p, cuts.c[1], partial, s);
+  };
+  int turn = 0;
+  for (int k = 0; k < o.steps;) {
+    const bool twice = cuts.two_at_once(o, k);
+    const bool last = k + (twice ? 2 : 1) == o.steps;
+    const auto two = [](int e) { return std::ldexp(1.0, e); };
+    const double inner = largest_inner(o.b, o.c, size * size), next = largest(o.a, o.b, o.c, size);
+    const int ea = exponent_for(size * size), eb = exponent_for(inner);
     PairProduct p = shape_of(o, 0);   // A
     p.a = p.b = o.xs, p.out = p.out_t = w + l.a;
-    p.factor = f.a;
-    launch_pairs(p, partial, s);
-    p = shape_of(o, 1);               // B = b A + c A A
-    p.a = p.b = p.e = w + l.a, p.out = p.out_t = w + l.b;
-    p.factor = f.b, p.extra = f.b_extra;
-    launch_pairs(p, partial, s);
-    p = shape_of(o, 2);               // a X + B X
-    p.a = w + l.b, p.b = w + l.xt[k & 1], p.e = o.xs, p.out = o.xs, p.out_t = w + l.xt[1 - (k & 1)];
-    p.factor = f.x, p.extra = f.x_extra;
-    if (k + 1 == o.steps) p.x = o.x, p.x_matrix = o.x_matrix, p.x_row = o.x_row, p.x_rows = o.rows, p.x_cols = o.cols, p.x_transposed = o.transposed, p.type = o.type;
-    launch_pairs(p, partial, s);
+    p.factor = (float)two(ea - 2 * ex);
+    launch_pairs(p, cuts.c[0], partial, s);
+    square(l.a, l.a, l.b, o.c * two(eb - 2 * ea), l.a, o.b * two(eb - ea));   // B
+    size_t by = l.b;
+    int ey = eb;
+    double own = o.a;
+    if (twice) {
+      const double inner2 = largest_inner(o.b, o.c, next * next);
+      const int en = exponent_for(size * size * (inner + 2.0 * std::fabs(o.a))), ea2 = exponent_for(next * next), eb2 = exponent_for(inner2);
+      ey = exponent_for(inner2 * inner + std::fabs(o.a) * (inner2 + inner));
+      square(l.b, l.a, l.c, two(en - eb - ea), l.a, 2.0 * o.a * two(en - ea));                                       // N
+      square(l.c, l.b, l.d, two(ea2 - en - eb), l.a, o.a * o.a * two(ea2 - ea));                                     // the next step's A
+      square(l.d, l.d, l.c, o.c * two(eb2 - 2 * ea2), l.d, o.b * two(eb2 - ea2));                                    // B'
+      square(l.c, l.b, l.d, two(ey - eb2 - eb), l.c, o.a * two(ey - eb2), l.b, o.a * two(ey - eb));                  // R
+      by = l.d, own = o.a * o.a;
+    }
+    const double then = twice ? largest(o.a, o.b, o.c, next) : next;
+    const int to = last ? 0 : exponent_for(then);
+    p = shape_of(o, 2);               // a X + B X, or a^2 X + R X
+    p.a = w + by, p.b = w + l.xt[turn], p.e = o.xs, p.out = o.xs, p.out_t = w + l.xt[1 - turn];
+    p.factor = (float)two(to - ey - ex), p.extra = (float)(own * two(to - ex));
+    if (last) p.x = o.x, p.x_matrix = o.x_matrix, p.x_row = o.x_row, p.x_rows = o.rows, p.x_cols = o.cols, p.x_transposed = o.transposed, p.type = o.type;
+    launch_pairs(p, cuts.c[2], partial, s);
+    size = then, ex = to, turn = 1 - turn;
+    k += twice ? 2 : 1;
   }
   return hipGetLastError();
 }
