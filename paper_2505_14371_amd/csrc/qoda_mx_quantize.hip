@@ -51,7 +51,10 @@ __global__ void __launch_bounds__(2048 / U) k_mx_rows(MxRounding a, long long gr
     if constexpr (STOCHASTIC) {
       float f[8];
       v[u].get(f);
-      codes = codes_stochastic(f, byte, (u32)r, (u32)(c0 >> 3), a);
+      u32 x[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = __float_as_uint(f[j]);
+      codes = codes_stochastic(x, byte, (u32)r, (u32)(c0 >> 3), a);
     } else {
       codes = codes_nearest(v[u], scale_of(byte));
     }
@@ -116,10 +119,10 @@ __global__ void __launch_bounds__(kWg) k_mx_columns(MxRounding a, long long grou
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       if constexpr (STOCHASTIC) {
-        float f[8];
+        u32 x[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) f[j] = __uint_as_float(v[8 * e + j].bits(h));
-        codes[e] = codes_stochastic(f, byte, (u32)(c0 + h), (u32)(r0 >> 3) + e, a);
+        for (int j = 0; j < 8; ++j) x[j] = v[8 * e + j].bits(h);
+        codes[e] = codes_stochastic(x, byte, (u32)(c0 + h), (u32)(r0 >> 3) + e, a);
       } else {
         Eight<T> f;
 #pragma unroll
