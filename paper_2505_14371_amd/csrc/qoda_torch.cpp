@@ -316,23 +316,32 @@ struct MatrixCalls {
 // use_matrices(addresses): the calls above, in their order.
 PyObject *use_matrices(PyObject *, PyObject *addresses) { return used(addresses, &matrix_calls, sizeof matrix_calls, "use_matrices(addresses)"); }
 
-// A microscaled matrix, as (codes, scales, rows, columns): the caller's class has looked at their shapes.
+// A microscaled matrix, as (codes, scales, rows, columns): the caller's class has looked at their shapes; scales None: they lie behind the codes.
 struct Mx {
-  const at::Tensor &codes, &scales;
+  const at::Tensor &codes;
   int64_t rows, cols;
-  Mx(PyObject *o, int64_t device) : codes(tensor(part(o, 0))), scales(tensor(part(o, 1))), rows(number<int64_t>(part(o, 2))), cols(number<int64_t>(part(o, 3))) {
-    if (!codes.is_cuda() || codes.get_device() != device || !scales.is_cuda() || scales.get_device() != device) throw Unknown();
+  void *scales;
+  Mx(PyObject *o, int64_t device) : codes(tensor(part(o, 0))), rows(number<int64_t>(part(o, 2))), cols(number<int64_t>(part(o, 3))) {
+    if (!codes.is_cuda() || codes.get_device() != device) throw Unknown();
+    if (part(o, 1) == Py_None) {
+      scales = static_cast<char *>(codes.data_ptr()) + code_bytes(rows, cols);
+    } else {
+      const at::Tensor &t = tensor(part(o, 1));
+      if (!t.is_cuda() || t.get_device() != device) throw Unknown();
+      scales = t.data_ptr();
+    }
   }
+  static int64_t code_bytes(int64_t rows, int64_t cols) { return rows * ((cols + 255) / 256 * 128); }
   static PyObject *part(PyObject *o, Py_ssize_t i) {
     if (!PyTuple_CheckExact(o) || PyTuple_GET_SIZE(o) != 4) throw Unknown();
     return PyTuple_GET_ITEM(o, i);
   }
-  qoda_mx as_is() const { return {codes.data_ptr(), scales.data_ptr()}; }
+  qoda_mx as_is() const { return {codes.data_ptr(), scales}; }
 };
 
 at::Tensor bytes_of(const at::Tensor &like, at::IntArrayRef sizes) { return at::empty(sizes, like.options().dtype(at::kByte)); }
 
-// (device, stream, x, transposed, stochastic, seed, offset): (codes, scales)
+// (device, stream, x, transposed, stochastic, seed, offset): (codes and scales, None, rows, columns)
 PyObject *microscale(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
   return answered(args, nargs, 7, [&](int64_t device, void *stream) {
     if (!matrix_calls.quantize) throw Unknown();
@@ -341,10 +350,13 @@ PyObject *microscale(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
     const bool transposed = truth(args[3]);
     const int64_t rows = transposed ? x.cols : x.rows, cols = transposed ? x.rows : x.cols, steps = (cols + 255) / 256;
     if (rows > QODA_MAX_SIDE || cols > QODA_MAX_SIDE) throw Unknown();
-    const at::Tensor codes = bytes_of(x.t, {rows, 128 * steps}), scales = bytes_of(x.t, {2 * steps, (rows + 63) / 64, 256});
-    const qoda_mx_quantize_args a = {x.dtype, transposed, truth(args[4]), x.rows, x.cols, matrix(args[2], x, x.rows, x.cols), {codes.data_ptr(), scales.data_ptr()},
-                                     number<uint64_t>(args[5]), number<uint64_t>(args[6])};
-    return outcome(matrix_calls.quantize(&a, stream), {codes, scales});
+    const int64_t codes = Mx::code_bytes(rows, cols), scales = (rows + 63) / 64 * 512 * steps;
+    const at::Tensor q = bytes_of(x.t, {codes + scales});
+    const qoda_mx_quantize_args a = {x.dtype, transposed, truth(args[4]), x.rows, x.cols, matrix(args[2], x, x.rows, x.cols),
+                                     {q.data_ptr(), static_cast<char *>(q.data_ptr()) + codes}, number<uint64_t>(args[5]), number<uint64_t>(args[6])};
+    const int rc = matrix_calls.quantize(&a, stream);
+    if (rc != QODA_OK) return PyLong_FromLong(rc);
+    return Py_BuildValue("(NOLL)", THPVariable_Wrap(q), Py_None, (long long)rows, (long long)cols);
   });
 }
 

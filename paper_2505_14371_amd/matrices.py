@@ -79,6 +79,12 @@ def _shapes(rows: int, cols: int):
     return (rows, 128 * steps), (2 * steps, -(-rows // 64), 256)
 
 
+def _bytes(t, shape, name: str) -> torch.Tensor:
+    if not isinstance(t, torch.Tensor) or t.dtype is not torch.uint8 or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"Microscaled: {name} are a contiguous uint8 tensor of shape {shape}")
+    return t
+
+
 class Microscaled:
     """A matrix of rows x cols in four bits, rounded by ``microscale`` or laid out by the caller as include/qoda_matrices.h says: ``codes`` and ``scales``
     are contiguous uint8 tensors on one device, [rows, 128 s] and [2 s, rows / 64 rounded up, 256], s = cols / 256 rounded up."""
@@ -86,15 +92,27 @@ class Microscaled:
     __slots__ = ("_parts",)
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, rows: int, cols: int):
-        for t, shape, name in zip((codes, scales), _shapes(rows, cols), ("codes", "scales")):
-            if not isinstance(t, torch.Tensor) or t.dtype != torch.uint8 or tuple(t.shape) != shape or not t.is_contiguous():
-                raise ValueError(f"Microscaled: {name} of {rows} rows and {cols} columns are a contiguous uint8 tensor of shape {shape}")
+        self._parts = (_bytes(codes, (rows, (cols + 255) // 256 * 128), "codes"), _bytes(scales, ((cols + 255) // 256 * 2, (rows + 63) // 64, 256), "scales"), rows, cols)
         if codes.device != scales.device:
             raise ValueError("Microscaled: codes and scales are on different devices")
-        self._parts = (codes, scales, rows, cols)
 
-    codes = property(lambda self: self._parts[0])
-    scales = property(lambda self: self._parts[1])
+    @property
+    def codes(self) -> torch.Tensor:
+        return self._apart()[0]
+
+    @property
+    def scales(self) -> torch.Tensor:
+        return self._apart()[1]
+
+    def _apart(self):
+        """(codes, scales, rows, columns), where one tensor holds both so far."""
+        both, scales, rows, cols = self._parts
+        if scales is None:
+            of_codes, of_scales = _shapes(rows, cols)
+            n = of_codes[0] * of_codes[1]
+            self._parts = (both[:n].view(of_codes), both[n:].view(of_scales), rows, cols)
+        return self._parts
+
     rows = property(lambda self: self._parts[2])
     cols = property(lambda self: self._parts[3])
     shape = property(lambda self: torch.Size(self._parts[2:]))
@@ -105,7 +123,7 @@ class Microscaled:
         if stream is not None:
             with _on(stream):
                 return self.values(dtype)
-        if _is_native():
+        if _native is not None or _is_native():
             out = ops._looked_at(_native.mx_values, self._parts, _bf16(dtype))
             if out is not None:
                 return out
@@ -117,6 +135,9 @@ class Microscaled:
 
     def __repr__(self) -> str:
         return f"Microscaled({self.rows} x {self.cols}, {self.device})"
+
+
+_new = object.__new__
 
 
 def _bf16(dtype):
@@ -147,10 +168,10 @@ def _type(dtype, name: str) -> int:
 
 
 def _current(q: Microscaled, name: str) -> None:
-    if not q.codes.is_cuda:
+    if q.device.type != "cuda":
         raise ValueError(f"{name}: a CUDA tensor is wanted")
-    if q.codes.get_device() != torch.cuda.current_device():
-        raise ValueError(f"{name}: the matrix is on device {q.codes.get_device()}, the current device is {torch.cuda.current_device()}")
+    if q.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name}: the matrix is on {q.device}, the current device is {torch.cuda.current_device()}")
 
 
 def _microscaled(q, name: str, rows: int, cols: int, device) -> Microscaled:
@@ -181,14 +202,13 @@ def microscale(x, *, transposed=False, rounding="nearest", seed=0, offset=0, str
     if stream is not None:
         with _on(stream):
             return microscale(x, transposed=transposed, rounding=rounding, seed=seed, offset=offset)
-    if not isinstance(rounding, str) or rounding not in ROUNDINGS:
+    if rounding.__class__ is not str or rounding not in ROUNDINGS:
         raise ValueError(f"rounding {rounding!r}: one of {', '.join(ROUNDINGS)}")
-    if _is_native():
+    if _native is not None or _is_native():
         out = ops._looked_at(_native.microscale, x, transposed, rounding == "stochastic", seed, offset)
         if out is not None:
-            rows, cols = x.numel() // x.shape[-1] if x.shape[-1] else ops._rows(x), x.shape[-1]
-            q = Microscaled.__new__(Microscaled)
-            q._parts = (*out, cols, rows) if transposed else (*out, rows, cols)
+            q = _new(Microscaled)
+            q._parts = out
             return q
     if ops._followed((x,)):
         raise RuntimeError("microscale: rounding has no derivative, and nothing is recorded for torch's differentiation; x.detach() is rounded")
@@ -224,7 +244,7 @@ def mx_linear(x, weight, bias=None, residual=None, *, activation="none", p=0.0, 
     if stream is not None:
         with _on(stream):
             return mx_linear(x, weight, bias, residual, activation=activation, p=p, seed=seed, offset=offset, keep_pre=keep_pre, dtype=dtype)
-    if _is_native():
+    if _native is not None or _is_native():
         first, bf16 = _plain_or_parts(x, dtype)
         out = ops._looked_at(_native.mx_linear, first, _parts(weight), bias, residual, ops._number(activation), p, seed, offset, keep_pre, bf16)
         if out is not None:
@@ -253,7 +273,7 @@ def mx_linear_input_grad(dz, weight_t, *, pre=None, activation="none", p=0.0, se
     if stream is not None:
         with _on(stream):
             return mx_linear_input_grad(dz, weight_t, pre=pre, activation=activation, p=p, seed=seed, offset=offset, residual=residual, dtype=dtype)
-    if _is_native():
+    if _native is not None or _is_native():
         first, bf16 = _plain_or_parts(dz, dtype)
         out = ops._looked_at(_native.mx_linear_input_grad, first, _parts(weight_t), pre, ops._number(activation), p, seed, offset, residual, bf16)
         if out is not None:
@@ -278,7 +298,7 @@ def mx_linear_weight_grad(dz_t, x_t, dweight=None, dbias=None, *, bias=True, acc
     if stream is not None:
         with _on(stream):
             return mx_linear_weight_grad(dz_t, x_t, dweight, dbias, bias=bias, accumulate=accumulate)
-    if _is_native() and type(dz_t) is Microscaled and type(x_t) is Microscaled and dz_t.codes.is_cuda and not (accumulate and (dweight is None or (bias and dbias is None))):
+    if _is_native() and type(dz_t) is Microscaled and type(x_t) is Microscaled and dz_t._parts[0].is_cuda and not (accumulate and (dweight is None or (bias and dbias is None))):
         if dweight is None:
             dweight = torch.empty((dz_t.rows, x_t.rows), dtype=torch.float32, device=dz_t.device)
         if dbias is None and bias:
@@ -325,7 +345,7 @@ def orthogonalize(g, *, steps=5, coefficients=QUINTIC, eps=1e-7, out=None, strea
         with _on(stream):
             return orthogonalize(g, steps=steps, coefficients=coefficients, eps=eps, out=out)
     a, b, c = coefficients
-    if _is_native():
+    if _native is not None or _is_native():
         x = ops._looked_at(_native.orthogonalize, g, steps, a, b, c, eps, out)
         if x is not None:
             return x
