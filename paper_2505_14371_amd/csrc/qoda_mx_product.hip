@@ -62,7 +62,7 @@ struct Scales {
 };
 
 template <class T, int FORM, int BM, int BN, int WM, int WN>
-__global__ void __launch_bounds__(64 * WM * WN, BM == 128 ? 2 : 1) k_mx_product(MxProduct m, int tiles_m, int tiles_n, int steps_each) {
+__global__ void __launch_bounds__(64 * WM * WN, 2) k_mx_product(MxProduct m, int tiles_m, int tiles_n, int steps_each) {
   constexpr int WG = 64 * WM * WN, FM = BM / WM / 16, FN = BN / WN / 16, QM = (FM + 3) / 4, QN = (FN + 3) / 4;
   static_assert(FM % 2 == 0 && FN % 2 == 0 && (FM == 2 || FM % 4 == 0) && (FN == 2 || FN % 4 == 0) && WG >= 256, "what the scales' order knows");
   typedef Operand<bf16, true, 1, BM, WG, true> A;   // in words of 16 bits: four codes

@@ -176,13 +176,13 @@ __device__ __forceinline__ v4f multiply_halves(v4u b, v4u a, v4f c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, b), __builtin_bit_cast(v8h, a), c, 0, 0, 0);
 }
 
-// c = a b^T of matrices of pairs, [m][k] and [n][k].
-template <int BM, int BN, int WM, int WN>
-__global__ void __launch_bounds__(64 * WM * WN, BM == 128 ? 2 : 1) k_pair_product(PairProduct p, int tiles_m, int tiles_n, int steps_each) {
+// c = a b^T of matrices of pairs, [m][k] and [n][k].  S: steps in shared memory, of which one is multiplied and the others are on their way.
+template <int BM, int BN, int WM, int WN, int S>
+__global__ void __launch_bounds__(64 * WM * WN, 2) k_pair_product(PairProduct p, int tiles_m, int tiles_n, int steps_each) {
   constexpr int WG = 64 * WM * WN, FM = BM / WM / 16, FN = BN / WN / 32, kSide = BM / WM < 64 ? BM / WM : 64, kRow = kSide + 4;
   typedef Operand<bf16, true, 0, BM, WG, true> A;   // entries of 16 bits: 32 high parts and their 32 low parts are a step
   typedef Operand<bf16, true, 1, BN, WG, true> B;
-  constexpr int kTiles = 2 * (BM + BN) * kStepBytes;
+  constexpr int kTiles = S * (BM + BN) * kStepBytes;
   static_assert(WM * WN * 32 * kRow * 4 <= kTiles, "the transposing end fits");
   __shared__ __align__(16) char shared[kTiles];
 
@@ -237,18 +237,21 @@ __global__ void __launch_bounds__(64 * WM * WN, BM == 128 ? 2 : 1) k_pair_produc
   // holds, and not used.  (With branches the compiler kept copies of the sums.)
   PiecesA a_hi, a_lo;
   PiecesB b_hi, b_lo;
-  request(0, 0);
-  if (steps > 1) request(1, kBuffer);
-  arrived();
+  constexpr int kLoads = A::kMine + B::kMine;
+  const auto behind = [&](int t) { return steps - 1 - t < S - 2 ? steps - 1 - t : S - 2; };   // steps behind step t that are on their way
+#pragma unroll
+  for (int t = 0; t < S; ++t)
+    if (t < steps) request(t, t * kBuffer);
+  arrived_but<kLoads, S - 2>(behind(0));
   read_a(a_hi, 0, 0);
   read_b(b_hi, 0, 0);
   for (int t = 0; t < steps; ++t) {
     read_b(b_lo, now, 1);
     read_a(a_lo, now, 1);
     multiply_all(a_hi, b_hi);
-    arrived();   // the next step is there, and nobody reads this one any more
-    if (t + 2 < steps) request(t + 2, now);
-    now = kBuffer - now;
+    arrived_but<kLoads, S - 2>(behind(t + 1));   // the next step is there, and nobody reads this one any more
+    if (t + S < steps) request(t + S, now);
+    now = now == (S - 1) * kBuffer ? 0 : now + kBuffer;
     multiply_all(a_hi, b_lo);
     read_a(a_hi, now, 0);
     multiply_all(a_lo, b_hi);
@@ -552,7 +555,7 @@ int small_pairs(const Orthogonal &o) {
 
 constexpr int kCus = 256;
 
-enum Tile { kTile64, kTile128, kTile256 };
+enum Tile { kTile64Ahead, kTile64, kTile128, kTile256 };
 struct Cut {
   Tile tile;
   int side, splits, steps_each;
@@ -564,26 +567,38 @@ long long tiles_of(const PairProduct &p, int side) {
   return (p.symmetric ? a * (a + 1) / 2 : a * b) * p.matrices;
 }
 
-// The cut with the least estimated time: a tile's rate, its start and end, the join of splits.
+// The cut with the least estimated time, from what was measured: a tile's rate (products of numbers) without its end, the least time of a step, a tile's start, what the
+// ends read and write at the rate of memory (half of it is hidden where a CU holds several workgroups), and the join of splits.  Tiles of 64 with a third step on
+// its way take 0.3 us a step where a CU has one of them (1024 x 1024 over 1024, symmetric: 12.6 us; 18.6 with two steps), but where it has several they have less
+// room (2048 x 2048 over 2048: 45 us, 38).  Measured and estimated, us: 2048 x 8192 over 2048 by 256 182 and 186, by 128 194 and 196; 16 times 416 x 2112 over 416 by 64 70
+// and 68; 2048 x 2048 over 8192, symmetric, in 7 parts of 256 115 and 103.
+struct Kind {
+  Tile tile;
+  int side, a_cu;
+  double rate, least;
+};
+constexpr Kind kKinds[] = {{kTile64Ahead, 64, 1, 310e12, 0.3}, {kTile64, 64, 4, 310e12, 0.5}, {kTile128, 128, 2, 400e12, 0.6}, {kTile256, 256, 1, 480e12, 1.7}};
+
 Cut cut_of(const PairProduct &p) {
   const int steps = (int)(p.k / 32);
-  const struct { Tile tile; int side, a_cu; double rate; } cuts[] = {{kTile64, 64, 4, 300e12}, {kTile128, 128, 2, 380e12}, {kTile256, 256, 1, 420e12}};
   Cut best = {};
   double least = 0.0;
-  for (const auto &c : cuts) {
-    const long long tiles = tiles_of(p, c.side);
-    for (int splits = 1; splits == 1 || (splits <= 16 && splits * 4 <= steps && tiles * splits <= (long long)c.a_cu * kCus); ++splits) {
+  const double entries = (double)p.matrices * p.m * p.n * (p.symmetric ? 0.5 : 1.0), end = entries * (p.symmetric ? 8.0 : 12.0) / 5e6;
+  for (const Kind &c : kKinds) {
+    const long long tiles = tiles_of(p, c.side), room = (long long)c.a_cu * kCus;
+    if (c.tile == kTile64Ahead && tiles > room) continue;
+    for (int splits = 1; splits == 1 || (splits <= 16 && splits * 4 <= steps && tiles * splits <= room); ++splits) {
       const int each = (steps + splits - 1) / splits;
       const double one = 2.0 * c.side * c.side * 32.0 / (c.rate / kCus) * 1e6;
       long long left = tiles * splits;
       double us = 0.0;
       while (left > 0) {
-        const long long now = left < (long long)c.a_cu * kCus ? left : (long long)c.a_cu * kCus, rounds = left / now;
+        const long long now = left < room ? left : room, rounds = left / now;
         const double step = (double)((now + kCus - 1) / kCus) * one;
-        us += (double)rounds * (3.0 + each * (step > 0.3 ? step : 0.3));
+        us += (double)rounds * (3.0 + each * (step > c.least ? step : c.least));
         left -= rounds * now;
       }
-      if (splits > 1) us += 5.0 + (double)splits * p.matrices * p.m * p.n * (p.symmetric ? 4.0 : 8.0) / 4e6;
+      us += splits > 1 ? 5.0 + (double)splits * entries * 8.0 / 4e6 + end : c.a_cu == 1 ? end : 0.5 * end;
       if (least == 0.0 || us < least) least = us, best = {c.tile, c.side, splits, each, us};
     }
   }
@@ -591,20 +606,21 @@ Cut cut_of(const PairProduct &p) {
   return best;
 }
 
-template <int SIDE, int WM, int WN>
+template <int SIDE, int WM, int WN, int S>
 void launch_tiles(const PairProduct &p, const Cut &c, hipStream_t s) {
   const int tm = (int)((p.m + SIDE - 1) / SIDE), tn = (int)((p.n + SIDE - 1) / SIDE);
   in_launches(p, tiles_of(p, SIDE), 64 * WM * WN, [&](const PairProduct &part, unsigned x) {
-    k_pair_product<SIDE, SIDE, WM, WN><<<dim3(x, (unsigned)c.splits), 64 * WM * WN, 0, s>>>(part, tm, tn, c.steps_each);
+    k_pair_product<SIDE, SIDE, WM, WN, S><<<dim3(x, (unsigned)c.splits), 64 * WM * WN, 0, s>>>(part, tm, tn, c.steps_each);
   });
 }
 
 void launch_pairs(PairProduct p, const Cut &c, float *partial, hipStream_t s) {
   p.partial = c.splits > 1 ? partial : nullptr;
   switch (c.tile) {
-    case kTile64: launch_tiles<64, 2, 2>(p, c, s); break;
-    case kTile128: launch_tiles<128, 2, 2>(p, c, s); break;
-    case kTile256: launch_tiles<256, 2, 4>(p, c, s); break;
+    case kTile64Ahead: launch_tiles<64, 2, 2, 3>(p, c, s); break;
+    case kTile64: launch_tiles<64, 2, 2, 2>(p, c, s); break;
+    case kTile128: launch_tiles<128, 2, 2, 2>(p, c, s); break;
+    case kTile256: launch_tiles<256, 2, 4, 2>(p, c, s); break;
   }
   if (c.splits > 1)
     in_launches(p, tiles_of(p, 64), kWg, [&](const PairProduct &part, unsigned x) { k_pair_join<<<dim3(x), kWg, 0, s>>>(part, c.splits); });
