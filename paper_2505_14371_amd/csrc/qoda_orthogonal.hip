@@ -187,11 +187,11 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_pair_product(PairProduct p,
   __shared__ __align__(16) char shared[kTiles];
 
   const int each = p.symmetric ? tiles_m * (tiles_m + 1) / 2 : tiles_m * tiles_n;
-  const long long id = p.first + blockIdx.x;
+  const long long id = xcd_run(p.first + blockIdx.x, p.matrices * each);   // an XCD has whole matrices, or runs of a matrix's tiles
   const int matrix = __builtin_amdgcn_readfirstlane((int)(id / each)), in = (int)(id - (long long)matrix * each);
   int tm, tn;
   if (p.symmetric) upper_tile(in, tm, tn);
-  else tile_of(in, tiles_m, tiles_n, tm, tn);
+  else band_tile(in, tiles_m, tiles_n, tm, tn);
   tm = __builtin_amdgcn_readfirstlane(tm), tn = __builtin_amdgcn_readfirstlane(tn);
   const int i0 = tm * BM, j0 = tn * BN;
   const int all = (int)(p.k / 32), step0 = (int)blockIdx.y * steps_each, steps = all - step0 < steps_each ? all - step0 : steps_each;
@@ -555,7 +555,7 @@ int small_pairs(const Orthogonal &o) {
 
 constexpr int kCus = 256;
 
-enum Tile { kTile64Ahead, kTile64, kTile128, kTile256 };
+enum Tile { kTile64Ahead, kTile64, kTile96Ahead, kTile128, kTile256 };
 struct Cut {
   Tile tile;
   int side, splits, steps_each;
@@ -569,15 +569,16 @@ long long tiles_of(const PairProduct &p, int side) {
 
 // The cut with the least estimated time, from what was measured: a tile's rate (products of numbers) without its end, the least time of a step, a tile's start, what the
 // ends read and write at the rate of memory (half of it is hidden where a CU holds several workgroups), and the join of splits.  Tiles of 64 with a third step on
-// its way take 0.3 us a step where a CU has one of them (1024 x 1024 over 1024, symmetric: 12.6 us; 18.6 with two steps), but where it has several they have less
-// room (2048 x 2048 over 2048: 45 us, 38).  Measured and estimated, us: 2048 x 8192 over 2048 by 256 182 and 186, by 128 194 and 196; 16 times 416 x 2112 over 416 by 64 70
-// and 68; 2048 x 2048 over 8192, symmetric, in 7 parts of 256 115 and 103.
+// its way take 0.3 us a step where a CU has one of them (1024 x 1024 over 1024, symmetric: 12.6 us; 17.8 with two steps), but where it has more than two they
+// have less room (2048 x 8192 over 2048: 235 us, 227); tiles of 96 fill the device once where those of 64 are more (2048 x 2048 over 2048, symmetric: 36 us, 39).
+// Measured and estimated, us: 2048 x 8192 over 2048 by 256 182 and 186, by 128 195 and 211; 16 times 416 x 2112 over 416 by 64 71 and 71; 2048 x 2048 over 8192,
+// symmetric, in 7 parts of 256 115 and 103.
 struct Kind {
   Tile tile;
   int side, a_cu;
   double rate, least;
 };
-constexpr Kind kKinds[] = {{kTile64Ahead, 64, 1, 310e12, 0.3}, {kTile64, 64, 4, 310e12, 0.5}, {kTile128, 128, 2, 400e12, 0.6}, {kTile256, 256, 1, 480e12, 1.7}};
+constexpr Kind kKinds[] = {{kTile64Ahead, 64, 2, 310e12, 0.3}, {kTile64, 64, 4, 310e12, 0.5}, {kTile96Ahead, 96, 1, 400e12, 0.55}, {kTile128, 128, 2, 370e12, 0.6}, {kTile256, 256, 1, 480e12, 1.7}};
 
 Cut cut_of(const PairProduct &p) {
   const int steps = (int)(p.k / 32);
@@ -586,7 +587,7 @@ Cut cut_of(const PairProduct &p) {
   const double entries = (double)p.matrices * p.m * p.n * (p.symmetric ? 0.5 : 1.0), end = entries * (p.symmetric ? 8.0 : 12.0) / 5e6;
   for (const Kind &c : kKinds) {
     const long long tiles = tiles_of(p, c.side), room = (long long)c.a_cu * kCus;
-    if (c.tile == kTile64Ahead && tiles > room) continue;
+    if ((c.tile == kTile64Ahead || c.tile == kTile96Ahead) && tiles > room) continue;
     for (int splits = 1; splits == 1 || (splits <= 16 && splits * 4 <= steps && tiles * splits <= room); ++splits) {
       const int each = (steps + splits - 1) / splits;
       const double one = 2.0 * c.side * c.side * 32.0 / (c.rate / kCus) * 1e6;
@@ -619,6 +620,7 @@ void launch_pairs(PairProduct p, const Cut &c, float *partial, hipStream_t s) {
   switch (c.tile) {
     case kTile64Ahead: launch_tiles<64, 2, 2, 3>(p, c, s); break;
     case kTile64: launch_tiles<64, 2, 2, 2>(p, c, s); break;
+    case kTile96Ahead: launch_tiles<96, 2, 3, 3>(p, c, s); break;
     case kTile128: launch_tiles<128, 2, 2, 2>(p, c, s); break;
     case kTile256: launch_tiles<256, 2, 4, 2>(p, c, s); break;
   }

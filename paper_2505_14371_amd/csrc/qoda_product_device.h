@@ -66,7 +66,7 @@ struct Operand {
   static constexpr int kMine = N * 8 / WG;                      // chunks that a thread moves
   static_assert(N * 8 % WG == 0, "whole chunks a thread");
   static constexpr bool kPower = (N & (N - 1)) == 0;
-  static_assert(kPower || (N % 64 == 0 && SIDE == 0 && sizeof(T) == 2), "what piece() knows");
+  static_assert(ROWS || kPower || (N % 64 == 0 && SIDE == 0 && sizeof(T) == 2), "what piece() knows");
 
   const T *base;     // entry (first, 0)
   long long ld;
@@ -291,15 +291,18 @@ __device__ __forceinline__ void by_activation(int a, F &&f) {
 // Workgroups go to the eight XCDs in turn, and each XCD has a cache of its own: an XCD gets a run of tiles that are adjacent in c, column by
 // column in bands of kBand rows of tiles, so that what its workgroups load at one time are few rows of a and few of b.
 constexpr int kXcds = 8, kBand = 8;
-__device__ __forceinline__ void tile_of(int id, int tiles_m, int tiles_n, int &tm, int &tn) {
-  const int total = tiles_m * tiles_n, x = id % kXcds, q = id / kXcds;
-  const int each = total / kXcds, more = total % kXcds;
-  const int at = x * each + (x < more ? x : more) + q;
+template <class I>
+__device__ __forceinline__ I xcd_run(I id, I total) {   // the place in that order of workgroup `id`
+  const I x = id % kXcds, q = id / kXcds, each = total / kXcds, more = total % kXcds;
+  return x * each + (x < more ? x : more) + q;
+}
+__device__ __forceinline__ void band_tile(int at, int tiles_m, int tiles_n, int &tm, int &tn) {
   const int band = at / (kBand * tiles_n), in = at - band * kBand * tiles_n;
   const int rows = tiles_m - band * kBand < kBand ? tiles_m - band * kBand : kBand;
   tm = band * kBand + in % rows;
   tn = in / rows;
 }
+__device__ __forceinline__ void tile_of(int id, int tiles_m, int tiles_n, int &tm, int &tn) { band_tile(xcd_run(id, tiles_m * tiles_n), tiles_m, tiles_n, tm, tn); }
 
 // The splits' sums added up in their order, and finished.
 template <class T, int FORM>

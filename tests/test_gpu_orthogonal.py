@@ -150,7 +150,7 @@ def test_what_lies_between_rows_and_matrices_is_left_alone():
 
 
 # tiles of every size, sums split along l, both ways round; against 64 bits on the GPU
-LARGER = [(1, 700, 1500), (1, 1600, 600), (2, 1000, 1000), (16, 410, 2100), (1, 2048, 2048), (1, 100, 20000), (40, 200, 180)]
+LARGER = [(1, 700, 1500), (1, 1600, 600), (2, 1000, 1000), (16, 410, 2100), (1, 2048, 2048), (1, 100, 20000), (40, 200, 180), (1, 1950, 1970), (15, 400, 1300)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])

@@ -53,7 +53,7 @@ def test_tiles(kernels):
             assert int(m.group(2)) == side and scratch == 0, name
             assert fit(waves, registers, shared) >= (1 if steps == "3" else A_CU[side]), (name, registers, shared)
             seen += 1
-    assert seen == 3 * 5 + 4
+    assert seen == 3 * 5 + 5
 
 
 def test_the_other_kernels_keep_nothing_in_scratch_memory(kernels):
