@@ -40,10 +40,11 @@ template <int N>
 struct Scales {
   static constexpr int kHalf = N * 4;      // bytes of half a step
   const u8 *base;
-  long long groups;
-  int first, last;                         // groups of 64 rows
+  long long groups;                        // of 64 rows
+  int last;                                // of them, from the tile's first on
   __device__ __forceinline__ void start(const u8 *p, long long rows, int row) {
-    base = p, groups = (rows + 63) / 64, first = row / 64, last = (int)groups - 1;
+    groups = (rows + 63) / 64, last = (int)groups - 1 - row / 64;
+    base = p + (long long)(row / 64) * 256;
   }
   // Half s of a step, by a wave: 16 bytes a lane.
 #pragma clang diagnostic push
@@ -51,7 +52,7 @@ struct Scales {
   __device__ __forceinline__ void direct(long long step, int s, lds_ptr to) const {
     const int lane = threadIdx.x & 63;
     if (lane >= kHalf / 16) return;
-    const int group = first + lane / 16;   // beyond the last rows: scales of sums that are not stored
+    const int group = lane / 16;   // beyond the last rows: scales of sums that are not stored
     const u8 *p = base + (2 * step + s) * groups * 256;
     const u32 offset = (u32)(group < last ? group : last) * 256u + (lane & 15) * 16;
     const u32 at = __builtin_amdgcn_readfirstlane((u32)(uintptr_t)to + s * kHalf);

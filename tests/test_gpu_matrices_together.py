@@ -235,6 +235,22 @@ def test_more_than_2_31_entries():
     assert torch.equal(y[-100:], mats.mx_linear(a[-100:], w)) and torch.equal(y[:100], mats.mx_linear(a[:100], w))
 
 
+def test_more_than_2_30_rows():
+    """Scales lie 256 bytes for 64 rows: those of the last rows are more than 2^32 bytes behind the first."""
+    rows = 2**30 + 200
+    x = torch.empty((rows, 1), dtype=torch.bfloat16, device="cuda").normal_()
+    w = mats.microscale(torch.tensor([[1.0], [2.0], [-0.5]], device="cuda"))
+    q = mats.microscale(x)
+    y = mats.mx_linear(q, w)
+    assert torch.equal(y[-300:], mats.mx_linear(x[-300:], w)) and torch.equal(y[:300], mats.mx_linear(x[:300], w))
+    few = mats.mx_linear(w, q, dtype=torch.bfloat16)           # the many rows as the second operand, three of the first
+    assert torch.equal(few[:, -300:], y[-300:].t()) and torch.equal(few[:, :300], y[:300].t())
+    del few, y
+    wide = mats.mx_linear(mats.microscale(torch.randn(20, 1, device="cuda")), q, dtype=torch.bfloat16)
+    assert torch.isfinite(wide[:, -300:]).all()
+    assert torch.equal(q.values(torch.bfloat16)[-300:], mats.microscale(x[-300:]).values(torch.bfloat16))
+
+
 def test_an_update_of_more_than_2_31_entries():
     m, n = 32800, 66000
     g = torch.randn((m, n), device="cuda")
