@@ -177,7 +177,7 @@ int orthogonal_of(const qoda_orthogonalize_args *a, Orthogonal *o) {
   if (!a) return fail(QODA_EINVAL, "%s: null arguments", call);
   TRY(check_type(call, a->dtype));
   TRY(check_sides(call, a->matrices, a->rows, a->cols));
-  if (a->steps < 0) return fail(QODA_EINVAL, "%s: %d steps", call, a->steps);
+  if (a->steps < 0 || a->steps > QODA_MAX_STEPS) return fail(QODA_EINVAL, "%s: %d steps, which are not in [0, %d]", call, a->steps, QODA_MAX_STEPS);
   if (!(a->eps >= 0.0) || !std::isfinite(a->eps)) return fail(QODA_EINVAL, "%s: eps = %g", call, a->eps);
   if (!std::isfinite(a->a) || !std::isfinite(a->b) || !std::isfinite(a->c) || !orthogonal_bounded(a->a, a->b, a->c, a->steps))
     return fail(QODA_EINVAL, "%s: %d steps with the coefficients %g, %g, %g may leave 2^40", call, a->steps, a->a, a->b, a->c);

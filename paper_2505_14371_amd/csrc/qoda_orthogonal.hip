@@ -724,7 +724,6 @@ bool orthogonal_bounded(double a, double b, double c, int steps) {
     if (largest_inner(b, c, s * s) > kMost) return false;
     s = largest(a, b, c, s);
     if (!(s <= kMost)) return false;
-    if (k > 200) return true;   // the bound does not grow any more, or has long been left
   }
   return true;
 }

@@ -102,7 +102,7 @@ REFUSED = [
     (input_grad(wc=0), "wt is null"), (input_grad(dx=0), "dx is null"), (input_grad(dxs=1), "dx has a stride"), (input_grad(r=A, rs=2), "residual has a stride"), (input_grad(p=-0.1), "p = "),
     (weight_grad(rows=BIG), "sums over"), (weight_grad(rows=-1), "size"), (weight_grad(dc=0), "dzt is null"), (weight_grad(xsc=0), "xt is null"), (weight_grad(xc=A + 8), "16 bytes"),
     (weight_grad(dw=0), "dw is null"), (weight_grad(dw=A + 2), "dw is not aligned"), (weight_grad(dws=7), "stride of 7"), (weight_grad(db=A + 1), "dbias is not aligned"),
-    (orthogonalize(dtype=7), "dtype 7"), (orthogonalize(steps=-1), "-1 steps"), (orthogonalize(n=-1), "size"), (orthogonalize(eps=-1e-9), "eps"), (orthogonalize(eps=NAN), "eps"), (orthogonalize(eps=INF), "eps"),
+    (orthogonalize(dtype=7), "dtype 7"), (orthogonalize(steps=-1), "-1 steps"), (orthogonalize(steps=1001), "1001 steps"), (orthogonalize(steps=1000, a=1.03, b=0.0, c=0.0), "2^40"), (orthogonalize(n=-1), "size"), (orthogonalize(eps=-1e-9), "eps"), (orthogonalize(eps=NAN), "eps"), (orthogonalize(eps=INF), "eps"),
     (orthogonalize(a=NAN), "coefficients"), (orthogonalize(b=INF), "coefficients"), (orthogonalize(a=1e13), "2^40"), (orthogonalize(a=10.0, b=0.0, c=0.0, steps=13), "2^40"),
     (orthogonalize(b=1e30, c=-1e30), "2^40"), (orthogonalize(g=0), "g is null"), (orthogonalize(x=0), "x is null"), (orthogonalize(g=A + 2), "g is not aligned"), (orthogonalize(xr=5), "strides of x"),
     (orthogonalize(gm=23), "strides of g"), (orthogonalize(gm=-24), "strides of g"), (orthogonalize(rows=(1 << 17) + 1, cols=(1 << 17) + 1, gr=1 << 18, gm=1 << 36, xr=1 << 18, xm=1 << 36), "sides"),
@@ -165,9 +165,9 @@ def test_arguments_that_python_refuses(lib):
         mats.microscale(torch.zeros(3, 4, requires_grad=True))
 
 
-def test_bounded_polynomials_are_taken_for_any_number_of_steps(lib):
+def test_bounded_polynomials_are_taken(lib):
     wide = dict(rows=300, cols=400, gr=400, gm=120000, xr=400, xm=120000)
-    for steps in (0, 1, 1000, 2**31 - 1):
+    for steps in (0, 1, 1000):
         assert lib.qoda_orthogonalize_workspace_bytes(orthogonalize(steps=steps, **wide)[1]) > 0
     assert lib.qoda_orthogonalize_workspace_bytes(orthogonalize(a=10.0, b=0.0, c=0.0, steps=12, **wide)[1]) > 0
     assert lib.qoda_orthogonalize_workspace_bytes(orthogonalize()[1]) == 0          # small ones stay in shared memory
