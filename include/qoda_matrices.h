@@ -98,11 +98,11 @@ int qoda_mx_linear(const qoda_mx_linear_args *a, void *workspace, size_t workspa
 int qoda_mx_linear_input_grad(const qoda_mx_linear_input_grad_args *a, void *workspace, size_t workspace_bytes, void *stream);
 int qoda_mx_linear_weight_grad(const qoda_mx_linear_weight_grad_args *a, void *workspace, size_t workspace_bytes, void *stream);
 
-/* x = the orthogonalised g, matrix by matrix of a batch: entry (n, i, j) is data[n * batch_stride + i * row_stride + j].
+/* x = the orthogonalised g, matrix by matrix of a batch: entry (n, i, j) is data[n * matrix + i * row + j].
  *   X_0 = g / (|g| + eps), |g| the root of the sum of squares;  A = X X^T,  X <- a X + (b A + c A A) X, steps times;
  * where g has more rows than columns X^T takes X's place, with the same result.  Accurate as fp32 products are: entries that the matrix cores take are
  * pairs of fp16 numbers, of 22 bits.  steps is at most QODA_MAX_STEPS, a, b, c are finite, and the singular values stay below 2^40 for every g (a bound from a, b and c; otherwise
- * QODA_EINVAL).  The smaller side is at most 2^17, the larger at most 2^22.  x may be g itself.  A matrix with an infinity or a NaN becomes NaN throughout, if steps > 0. */
+ * QODA_EINVAL; where the bound falls below 2^-40, digits are lost).  The smaller side is at most 2^17, the larger at most 2^22.  x may be g itself.  A matrix with an infinity or a NaN becomes NaN throughout, if steps > 0. */
 typedef struct {
   void *data;
   int64_t matrix, row; /* entries from one matrix, and from one row, to the next */

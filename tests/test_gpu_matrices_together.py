@@ -251,6 +251,26 @@ def test_more_than_2_30_rows():
     assert torch.equal(q.values(torch.bfloat16)[-300:], mats.microscale(x[-300:]).values(torch.bfloat16))
 
 
+@pytest.mark.parametrize("rows,dtype,turned", [(130, torch.float32, False), (130, torch.float32, True), (2048, torch.bfloat16, False)])
+def test_the_longest_side(rows, dtype, turned):
+    """2^22 columns of which 300 are not zero, the last ones among them: the update is that of these 300."""
+    cols = 2**22
+    gen = torch.Generator("cuda").manual_seed(rows)
+    few = torch.randn((rows, 300), device="cuda", generator=gen).to(dtype)
+    at = list(range(7, cols - 20000, 20971)) + list(range(cols - 100, cols))
+    g = torch.zeros((cols, rows) if turned else (rows, cols), dtype=dtype, device="cuda")
+    columns = g.t() if turned else g
+    assert len(at) == 300
+    for i, j in enumerate(at):
+        columns[:, j] = few[:, i]
+    mats.orthogonalize(g, steps=1, out=g)
+    got = torch.stack([columns[:, j] for j in at], 1)
+    want = mats.orthogonalize(few, steps=1)
+    # A's sums in another order, 2^-24 root(2 * 300), and two matrices' pairs of 2^-22, times |b| + 2 |c| = 9 and |X| = 1; each store at most half a step
+    assert (got.double() - want.double()).norm() <= 9 * (2.0**-24 * 600**0.5 + 2 * 2.0**-22) + torch.finfo(dtype).eps * 1.01 * want.double().norm()
+    assert torch.count_nonzero(g).item() <= few.numel()
+
+
 def test_an_update_of_more_than_2_31_entries():
     m, n = 32800, 66000
     g = torch.randn((m, n), device="cuda")
