@@ -313,3 +313,70 @@ def test_refusals(monkeypatch, look):
         y.sum().backward()
     with torch.no_grad():
         assert not mats.mx_linear(x, w).requires_grad and mats.microscale(x).shape == (20, 64)
+
+
+def called(name, args):
+    """A call of the C interface, its workspace full of NaN."""
+    lib, stream = mats._load(), torch.cuda.current_stream().cuda_stream
+    if name in ("mx_quantize", "mx_values"):
+        assert getattr(lib, "qoda_" + name)(args, stream) == 0
+        return
+    need = getattr(lib, f"qoda_{name}_workspace_bytes")(args)
+    assert need >= 0
+    work = torch.full((need + 16,), 255, dtype=torch.uint8, device="cuda")
+    assert getattr(lib, "qoda_" + name)(args, work.data_ptr() if need else None, need, stream) == 0
+    assert (work[need:] == 255).all()
+
+
+class Framed:
+    """A matrix inside a larger one: rows `pad` entries further apart than they are long, and entries before and behind that are to stay what they are."""
+
+    def __init__(self, rows, cols, dtype, pad):
+        self.store = torch.full((rows * (cols + pad) + 40,), 7.0, dtype=dtype, device="cuda")
+        self.t = self.store[pad: pad + rows * (cols + pad)].view(rows, cols + pad)[:, :cols]
+        self.at = (self.t.data_ptr(), cols + pad)
+
+    def taken(self):
+        got = self.t.clone()
+        self.t.fill_(7.0)
+        assert (self.store == 7.0).all()
+        return got
+
+
+@pytest.mark.parametrize("pad", [1, 3, 8])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("plain", [True, False])
+@pytest.mark.parametrize("rows,cin,cout", [(5, 300, 203), (70, 300, 203), (33, 8200, 61), (300, 260, 1030), (4000, 130, 2300)])
+def test_through_the_c_interface(rows, cin, cout, plain, dtype, pad):
+    """Outputs with strides of their own at any alignment, the residual in the output's memory, workspaces that hold anything."""
+    gen = torch.Generator("cuda").manual_seed(rows)
+    T, dt = TYPES[dtype], ops.DTYPES[TYPES[dtype]]
+    x, z, r, dz = (torch.randn(s, device="cuda", generator=gen).to(T) for s in ((rows, cin), (rows, cin), (rows, cout), (rows, cout)))
+    w, b = torch.randn((cout, cin), device="cuda", generator=gen), torch.randn(cout, device="cuda", generator=gen)
+    wq, wt, xq, dzq, xt, dzt = (mats.microscale(v, transposed=t) for v, t in ((w, 0), (w, 1), (x, 0), (dz, 0), (x, 1), (dz, 1)))
+    y, pre = Framed(rows, cout, T, pad), Framed(rows, cout, T, pad)
+    y.t.copy_(r)
+    called("mx_linear", mats._LINEAR.pack(dt, ops._number("gelu"), rows, cin, cout, *((x.data_ptr(), cin, 0, 0) if plain else (0, 0, *mats._mx(xq))), *mats._mx(wq), *y.at, *y.at, *pre.at,
+                                          b.data_ptr(), 0.1, 3, 4))
+    want, want_pre = mats.mx_linear(x if plain else xq, wq, b, r, activation="gelu", p=0.1, seed=3, offset=4, keep_pre=True, dtype=T)
+    assert torch.equal(y.taken(), want) and torch.equal(pre.taken(), want_pre)
+    dx = Framed(rows, cin, T, pad)
+    dx.t.copy_(x)
+    called("mx_linear_input_grad", mats._INPUT_GRAD.pack(dt, ops._number("silu"), rows, cin, cout, *((dz.data_ptr(), cout, 0, 0) if plain else (0, 0, *mats._mx(dzq))), *mats._mx(wt),
+                                                         z.data_ptr(), cin, *dx.at, *dx.at, 0.1, 3, 4))
+    assert torch.equal(dx.taken(), mats.mx_linear_input_grad(dz if plain else dzq, wt, pre=z, activation="silu", p=0.1, seed=3, offset=4, residual=x, dtype=T))
+    dw, db = Framed(cout, cin, torch.float32, pad), Framed(1, cout, torch.float32, pad)
+    dw.t.fill_(0.5), db.t.fill_(0.25)
+    called("mx_linear_weight_grad", mats._WEIGHT_GRAD.pack(1, rows, cin, cout, *mats._mx(dzt), *mats._mx(xt), *dw.at, db.at[0]))
+    want = mats.mx_linear_weight_grad(dzt, xt, torch.full((cout, cin), 0.5, device="cuda"), torch.full((cout,), 0.25, device="cuda"), accumulate=True)
+    assert torch.equal(dw.taken(), want[0]) and torch.equal(db.taken()[0], want[1])
+    v = Framed(rows, cin, T, pad)
+    called("mx_values", mats._VALUES.pack(dt, rows, cin, *mats._mx(xq), *v.at))
+    assert torch.equal(v.taken(), xq.values(T))
+    v.t.copy_(x)
+    for t in (0, 1):
+        q = mats.microscale(x, transposed=t, rounding="stochastic", seed=5, offset=6)
+        codes, scales = (torch.full((u.numel() + 64,), 99, dtype=torch.uint8, device="cuda") for u in (q.codes, q.scales))
+        called("mx_quantize", mats._QUANTIZE.pack(dt, t, 1, rows, cin, *v.at, codes.data_ptr(), scales.data_ptr(), 5, 6))
+        for got, u in ((codes, q.codes), (scales, q.scales)):
+            assert torch.equal(got[:u.numel()], u.flatten()) and (got[u.numel():] == 99).all()

@@ -186,3 +186,24 @@ def test_refusals():
             mats.orthogonalize(g, **bad)
     with pytest.raises(RuntimeError, match="differentiation"):
         mats.orthogonalize(g.clone().requires_grad_())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,rows,cols,pad", [(3, 20, 30, 1), (3, 30, 20, 3), (2, 150, 410, 1), (2, 410, 150, 3), (2, 700, 1300, 5), (1, 2048, 2048, 1), (1, 1030, 4100, 3)])
+@pytest.mark.parametrize("steps", [0, 1, 4, 5])
+def test_in_place_at_any_alignment(n, rows, cols, pad, steps, dtype):
+    """In g's memory, strided, through the C interface; the workspace holds NaN."""
+    T = TYPES[dtype]
+    store = torch.full((n * (rows * (cols + pad) + 7) + pad,), 7.0, dtype=T, device="cuda")
+    g = torch.as_strided(store, (n, rows, cols), (rows * (cols + pad) + 7, cols + pad, 1), pad)
+    g.copy_(torch.randn((n, rows, cols), device="cuda", generator=torch.Generator("cuda").manual_seed(cols)))
+    want = mats.orthogonalize(g.contiguous(), steps=steps)
+    at = (g.data_ptr(), g.stride(0), g.stride(1))
+    args = mats._ORTHOGONALIZE.pack({"f32": 0, "bf16": 1}[dtype], steps, n, rows, cols, *at, *at, *mats.QUINTIC, 1e-7)
+    lib = mats._load()
+    need = lib.qoda_orthogonalize_workspace_bytes(args)
+    work = torch.full((need + 16,), 255, dtype=torch.uint8, device="cuda")
+    assert lib.qoda_orthogonalize(args, work.data_ptr() if need else None, need, torch.cuda.current_stream().cuda_stream) == 0
+    assert torch.equal(g, want) and (work[need:] == 255).all()
+    g.fill_(7.0)
+    assert (store == 7.0).all()
