@@ -29,6 +29,7 @@ struct MxProduct {
   const void *x;
   long long ldx;
   int steps;                               // of 256 entries along the sum
+  float *row_sums;                         // of a, or null
   long long first;
 };
 
@@ -77,7 +78,6 @@ hipError_t launch_orthogonalize(const Orthogonal &o, void *workspace, hipStream_
 
 hipError_t launch_mx_quantize(const MxRounding &q, hipStream_t s);
 hipError_t launch_mx_values(const MxRounding &q, hipStream_t s);
-hipError_t launch_mx_row_sums(const u8 *codes, const u8 *scales, long long rows, long long cols, float *sums, bool accumulate, hipStream_t s);
 bool mx_takes_plain_rows(const Product &p);   // whether the product rounds plain rows itself
 size_t mx_product_scratch(const MxProduct &p);
 hipError_t launch_mx_product(const MxProduct &p, hipStream_t s);

@@ -125,6 +125,7 @@ int weight_grad_of(const qoda_mx_linear_weight_grad_args *a, MxProduct *m) {
   p->accumulate = a->accumulate != 0;
   operands(m, a->dzt, a->xt, a->rows);
   m->x = nullptr;
+  m->row_sums = a->dbias;
   return QODA_OK;
 }
 
@@ -142,7 +143,7 @@ int64_t scratch_of(const Args *a, int (*make)(const Args *, MxProduct *)) {
 }
 
 int run(const char *call, MxProduct *m, void *workspace, size_t bytes, void *stream) {
-  if (m->p.m == 0 || m->p.n == 0) return QODA_OK;
+  if (m->p.m == 0 || (m->p.n == 0 && !m->row_sums)) return QODA_OK;
   const size_t rounded = rounded_bytes(*m);
   TRY(check_workspace(call, workspace, bytes, rounded + mx_product_scratch(*m)));
   u8 *w = static_cast<u8 *>(workspace);
@@ -252,12 +253,9 @@ int qoda_mx_linear_input_grad(const qoda_mx_linear_input_grad_args *a, void *wor
 }
 
 int qoda_mx_linear_weight_grad(const qoda_mx_linear_weight_grad_args *a, void *workspace, size_t workspace_bytes, void *stream) {
-  const char *call = "qoda_mx_linear_weight_grad";
   MxProduct m;
   TRY(weight_grad_of(a, &m));
-  TRY(run(call, &m, workspace, workspace_bytes, stream));
-  if (!a->dbias || a->out == 0) return QODA_OK;
-  return done(call, launch_mx_row_sums(m.a, m.a_scales, a->out, a->rows, a->dbias, a->accumulate != 0, static_cast<hipStream_t>(stream)));
+  return run("qoda_mx_linear_weight_grad", &m, workspace, workspace_bytes, stream);
 }
 
 int64_t qoda_orthogonalize_workspace_bytes(const qoda_orthogonalize_args *a) {

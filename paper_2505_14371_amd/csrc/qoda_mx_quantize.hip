@@ -179,31 +179,6 @@ __global__ void __launch_bounds__(kWg) k_mx_values(MxRounding a, long long group
     }
 }
 
-// The sums of the rows of a microscaled matrix, a wave a row, in fp32.
-__global__ void __launch_bounds__(kWg) k_mx_row_sums(MxRounding a, long long groups, long long steps, float *sums, bool accumulate) {
-  const long long r = (a.first + blockIdx.x) * (kWg / 64) + (threadIdx.x >> 6);
-  if (r >= a.rows) return;
-  const int lane = threadIdx.x & 63;
-  float sum = 0.0f;
-  for (long long block = lane; block < steps * 8; block += 64) {
-    v4u codes;
-    __builtin_memcpy(&codes, a.codes + (r * steps * 8 + block) * 16, 16);
-    const u32 byte = a.scales[((block >> 2) * groups + (r >> 6)) * 256 + scale_place((int)(r & 63), (int)(block & 3))];
-    float part = 0.0f;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {   // exact: multiples of half a scale
-      float v[8];
-      values_of(codes[e], byte, v);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) part = part + v[j];
-    }
-    sum = sum + part;
-  }
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) sum = sum + __shfl_xor(sum, d);
-  if (lane == 0) sums[r] = accumulate ? sums[r] + sum : sum;
-}
-
 template <class T, bool STOCHASTIC>
 void launch_rounding(const MxRounding &q, hipStream_t s) {
   const long long rows = q.transposed ? q.cols : q.rows, along = q.transposed ? q.rows : q.cols;
@@ -231,17 +206,6 @@ hipError_t launch_mx_values(const MxRounding &q, hipStream_t s) {
   in_launches(q, groups * steps, kWg, [&](const MxRounding &part, unsigned grid) {
     if (q.type == kF32) k_mx_values<float><<<dim3(grid), kWg, 0, s>>>(part, groups, steps);
     else k_mx_values<bf16><<<dim3(grid), kWg, 0, s>>>(part, groups, steps);
-  });
-  return hipGetLastError();
-}
-
-hipError_t launch_mx_row_sums(const u8 *codes, const u8 *scales, long long rows, long long cols, float *sums, bool accumulate, hipStream_t s) {
-  MxRounding q = {};
-  q.rows = rows, q.cols = cols;
-  q.codes = const_cast<u8 *>(codes), q.scales = const_cast<u8 *>(scales);
-  const long long groups = mx_groups(rows), steps = mx_steps(cols);
-  in_launches(q, (rows + kWg / 64 - 1) / (kWg / 64), kWg, [&](const MxRounding &part, unsigned grid) {
-    k_mx_row_sums<<<dim3(grid), kWg, 0, s>>>(part, groups, steps, sums, accumulate);
   });
   return hipGetLastError();
 }

@@ -57,7 +57,7 @@ def test_tiles(kernels):
 
 
 def test_the_other_kernels_keep_nothing_in_scratch_memory(kernels):
-    names = [n for n in kernels if re.search(r"k_(mx_rows|mx_columns|mx_values|mx_row_sums|mx_few_rows|small|squares|start|pair_join)", n)]
+    names = [n for n in kernels if re.search(r"k_(mx_rows|mx_columns|mx_values|mx_few_rows|small|squares|start|pair_join)", n)]
     assert len(names) >= 20
     for name in names:
         assert kernels[name][1] == 0, name

@@ -104,17 +104,29 @@ def test_products(lib):
     assert short(launches(lib, "mx_linear", linear(1, 8192, 50304, plain=False))) == ["k_mx_few_rows"]
     assert short(launches(lib, "mx_linear", linear(3300, 410, 2100))) == ["k_mx_rows", "k_mx_product"]
     assert short(launches(lib, "mx_linear", linear(33, 8192, 2048, plain=False))) == ["k_mx_product", "k_join"]
-    assert short(launches(lib, "mx_linear_weight_grad", weight_grad(100000, 64, 64))) == ["k_mx_product", "k_join", "k_mx_row_sums"]
+    assert short(launches(lib, "mx_linear_weight_grad", weight_grad(100000, 64, 64))) == ["k_mx_product", "k_join"]
     assert short(launches(lib, "mx_linear_weight_grad", weight_grad(100000, 64, 64, bias=0))) == ["k_mx_product", "k_join"]
-    assert short(launches(lib, "mx_linear_weight_grad", weight_grad(0, 64, 64))) == ["k_mx_product", "k_mx_row_sums"]      # zeros
+    assert short(launches(lib, "mx_linear_weight_grad", weight_grad(0, 64, 64))) == ["k_mx_product"]      # zeros
+    def tiles_and_sums(rows, cin, cout, bias):
+        (kernel, workgroups, _), *_ = launches(lib, "mx_linear_weight_grad", weight_grad(rows, cin, cout, bias))
+        side, *_, wm, wn = map(int, re.match(r"k_mx_product<float,2,(\d+),(\d+),(\d+),(\d+)>", kernel).groups())
+        tiles = ceil(cout, side) * ceil(cin, side)
+        return workgroups - tiles, ceil(cout, wm * wn)
+    assert tiles_and_sums(300, 410, 2100, 0)[0] == 0
+    for sizes in ((300, 410, 2100), (0, 64, 70), (8192, 2048, 6144), (100, 0, 70)):      # sums of rows by workgroups behind the tiles', a row a wave
+        sums, rows = tiles_and_sums(*sizes, A)
+        assert sums == rows
+    sums, rows = tiles_and_sums(100000, 64, 64, A)                                         # ... of all the parts
+    assert 0 < sums < rows
+    assert launches(lib, "mx_linear_weight_grad", weight_grad(100, 0, 70, 0)) == launches(lib, "mx_linear_weight_grad", weight_grad(100, 70, 0)) == []
     assert launches(lib, "mx_linear", linear(5, 8, 0)) == launches(lib, "mx_linear", linear(0, 8, 5)) == []
     (kernel, workgroups, pieces), = launches(lib, "mx_linear", linear(1, 1, SIDE, plain=False))
     assert kernel.startswith("k_mx_few_rows<") and workgroups == ceil(SIDE, 32) and pieces > 1
     kernel, workgroups, pieces = launches(lib, "mx_linear", linear(SIDE, 1, 1, plain=False))[0]
     side = int(re.match(r"k_mx_product<\w+,0,(\d+),", kernel).group(1))
     assert workgroups == ceil(SIDE, side) and pieces > 1
-    got = launches(lib, "mx_linear_weight_grad", weight_grad(1, 1, SIDE))
-    assert got[-1][0] == "k_mx_row_sums" and got[-1][1] == ceil(SIDE, 4) and got[-1][2] > 1
+    sums, rows = tiles_and_sums(1, 1, SIDE, A)
+    assert sums == rows
 
 
 def test_orthogonalisation(lib):
