@@ -319,10 +319,12 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_pair_product(PairProduct p,
     }
 }
 
-// The splits' sums added up in their order, and finished: 64 x 64 entries a workgroup.
-__global__ void __launch_bounds__(kWg) k_pair_join(PairProduct p, int splits) {
-  __shared__ float tile[64][65];
-  const long long tiles_m = (p.m + 63) / 64, tiles_n = (p.n + 63) / 64, each = p.symmetric ? tiles_m * (tiles_m + 1) / 2 : tiles_m * tiles_n;
+// The splits' sums added up in their order, and finished: N x N entries a workgroup, N * 4 threads.  Of a symmetric product the entries of tiles above the diagonal and on
+// it are there, of the product's own tiles; the join's, which are taken whole, lie inside those where N divides their side.
+template <int N>
+__global__ void __launch_bounds__(N * 4) k_pair_join(PairProduct p, int splits) {
+  __shared__ float tile[N][N + 1];
+  const long long tiles_m = (p.m + N - 1) / N, tiles_n = (p.n + N - 1) / N, each = p.symmetric ? tiles_m * (tiles_m + 1) / 2 : tiles_m * tiles_n;
   const long long id = p.first + blockIdx.x, matrix = id / each;
   const int in = (int)(id - matrix * each);
   int tm, tn;
@@ -330,10 +332,10 @@ __global__ void __launch_bounds__(kWg) k_pair_join(PairProduct p, int splits) {
   else tm = (int)(in / tiles_n), tn = (int)(in - tm * tiles_n);
   const Place place{p, matrix};
   const bool columns = place.columns_wanted() && !(p.symmetric && tm == tn);
-  const int t = threadIdx.x, chunk = (t & 7) * 8;
+  const int t = threadIdx.x, chunk = t % (N / 8) * 8;
 #pragma unroll
-  for (int u = 0; u < 2; ++u) {
-    const int row = u * 32 + (t >> 3), i = tm * 64 + row, j = tn * 64 + chunk;
+  for (int u = 0; u < N / 32; ++u) {
+    const int row = u * 32 + t / (N / 8), i = tm * N + row, j = tn * N + chunk;
     float c[8] = {};
     if (i < p.m && j < p.n) {
       const float *from = p.partial + matrix * p.m * p.n + (long long)i * p.n + j;
@@ -362,12 +364,12 @@ __global__ void __launch_bounds__(kWg) k_pair_join(PairProduct p, int splits) {
   if (!columns) return;
   __syncthreads();
 #pragma unroll
-  for (int u = 0; u < 2; ++u) {
-    const int row = u * 32 + (t >> 3);
+  for (int u = 0; u < N / 32; ++u) {
+    const int row = u * 32 + t / (N / 8);
     float v[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = tile[chunk + e][row];
-    const int i = tm * 64 + chunk, j = tn * 64 + row;
+    const int i = tm * N + chunk, j = tn * N + row;
     if (i < p.m && j < p.n) place.column(i, j, v);
   }
 }
@@ -618,6 +620,11 @@ void launch_tiles(const PairProduct &p, const Cut &c, hipStream_t s) {
   });
 }
 
+template <int N>
+void launch_join(const PairProduct &p, const Cut &c, hipStream_t s) {
+  in_launches(p, tiles_of(p, N), N * 4, [&](const PairProduct &part, unsigned x) { k_pair_join<N><<<dim3(x), N * 4, 0, s>>>(part, c.splits); });
+}
+
 void launch_pairs(PairProduct p, const Cut &c, float *partial, hipStream_t s) {
   p.partial = c.splits > 1 ? partial : nullptr;
   switch (c.tile) {
@@ -627,8 +634,7 @@ void launch_pairs(PairProduct p, const Cut &c, float *partial, hipStream_t s) {
     case kTile128: launch_tiles<128, 2, 2, 2>(p, c, s); break;
     case kTile256: launch_tiles<256, 2, 4, 2>(p, c, s); break;
   }
-  if (c.splits > 1)
-    in_launches(p, tiles_of(p, 64), kWg, [&](const PairProduct &part, unsigned x) { k_pair_join<<<dim3(x), kWg, 0, s>>>(part, c.splits); });
+  if (c.splits > 1) c.side % 64 == 0 ? launch_join<64>(p, c, s) : launch_join<32>(p, c, s);
 }
 
 // The three products of a step, without their operands' places.

@@ -142,3 +142,33 @@ def test_orthogonalisation(lib):
     side = int(re.match(r"k_pair_product<(\d+),", got[2][0]).group(1))
     t = ceil(320, side)
     assert got[2][1] == (1 << 21) * t * (t + 1) // 2 and got[1][2] > 1
+
+
+def split_products(lib, *sizes):
+    """[(side of the tiles, side of the join's tiles, whether the product is symmetric)] of an update's products whose sums are split."""
+    got, out = launches(lib, "orthogonalize", orthogonalize(*sizes)), []
+    n, rows, cols = sizes[:3]
+    m = ceil(min(rows, cols), 32) * 32
+    for (kernel, workgroups, _), (join, joins, _) in zip(got, got[1:]):
+        if join.startswith("k_pair_join"):
+            side = int(re.match(r"k_pair_product<(\d+),", kernel).group(1))
+            of_join = int((re.search(r"<(\d+)>", join) or [0, 64])[1])
+            t, tj = ceil(m, side), ceil(m, of_join)
+            symmetric = workgroups == n * t * (t + 1) // 2
+            assert not symmetric or joins == n * tj * (tj + 1) // 2
+            out.append((side, of_join, symmetric))
+    return out
+
+
+# a batch's smaller side times the larger one, of which several take tiles of 96 with their sums in parts
+@pytest.mark.parametrize("sizes", [(3, 672, 4000), (1, 1440, 2176), (8, 480, 2048), (16, 288, 1500), (2, 544, 9000), (4, 576, 3100), (1, 672, 30000), (21, 288, 1200), (1, 2048, 8192), (1, 1000, 1000)])
+def test_a_join_takes_no_entry_of_a_symmetric_product_that_was_not_computed(lib, sizes):
+    """Of a symmetric product the tiles with row <= column are computed, and of the join's tiles those are finished whole: each has to lie in one of the product's."""
+    for side, of_join, symmetric in split_products(lib, *sizes):
+        assert not symmetric or side % of_join == 0, (side, of_join)
+
+
+def test_tiles_of_96_are_split(lib):
+    """That the sizes above reach them."""
+    for sizes in ((3, 672, 4000), (1, 1440, 2176)):
+        assert (96, 32, True) in split_products(lib, *sizes)
