@@ -698,15 +698,11 @@ double largest(double a, double b, double c, double most) {
   const auto at = [&](double s) { return std::fabs(s * (a + s * s * (b + s * s * c))); };
   double v = at(most);
   const double d = 9.0 * b * b - 20.0 * a * c;   // of the slope a + 3 b u + 5 c u^2, u = s^2
-  double roots[2];
-  int n = 0;
-  if (c != 0.0) {
-    if (d >= 0.0) roots[n++] = (-3.0 * b + std::sqrt(d)) / (10.0 * c), roots[n++] = (-3.0 * b - std::sqrt(d)) / (10.0 * c);
-  } else if (b != 0.0) {
-    roots[n++] = -a / (3.0 * b);
-  }
-  for (int i = 0; i < n; ++i)
-    if (roots[i] > 0.0 && roots[i] < most * most) v = std::fmax(v, at(std::sqrt(roots[i])));
+  if (!(d >= 0.0)) return v;
+  // its roots, without a difference of numbers that are nearly the same: next to c = 0 that would lose the one near -a / (3 b)
+  const double q = -0.5 * (3.0 * b + std::copysign(std::sqrt(d), b));
+  for (const double u : {q / (5.0 * c), a / q})   // infinite or no number where there is none
+    if (u > 0.0 && u < most * most) v = std::fmax(v, at(std::sqrt(u)));
   return v;
 }
 // ... and |b u + c u^2| for u in [0, most].
