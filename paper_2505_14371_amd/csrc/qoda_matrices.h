@@ -33,9 +33,10 @@ struct MxProduct {
   long long first;
 };
 
-// Matrices g [rows][cols]; X [m][n] is g or its transpose, m <= n, both sides filled up to multiples of 32.
+// Matrices g [rows][cols]; X [m][n] is g or its transpose, m <= n, both sides filled up to multiples of 32.  by_norm: how far X's numbers are from the bound on them is not known
+// before the call.
 struct Orthogonal {
-  int type, steps, transposed, parts;
+  int type, steps, transposed, parts, by_norm;
   long long matrices, rows, cols, m, n;
   const void *g;
   void *x;
@@ -44,6 +45,7 @@ struct Orthogonal {
   double *squares;   // [matrices][parts]
   void *xs, *xt;     // X and its transpose in pairs of fp16
   float scale;
+  float *scales;     // by_norm: [matrices][4], two factors of B and two of X
   long long first;
 };
 
@@ -67,11 +69,13 @@ struct PairProduct {
   void *out, *out_t, *x;
   long long x_matrix, x_row, x_rows, x_cols;
   float factor, extra, extra2;
-  float *partial;   // of split sums: [splits][matrices][m][n]
+  const float *scales;   // null, or of a product with partial sums: of every fourth matrix's place on, further factors of the sums and of e
+  float *partial;        // of split sums: [splits][matrices][m][n]
   long long first;
 };
 
 bool orthogonal_bounded(double a, double b, double c, int steps);
+bool orthogonal_by_norm(double a, double b, double c, int steps);
 void orthogonal_sides(Orthogonal *o);
 size_t orthogonal_scratch(const Orthogonal &o);
 hipError_t launch_orthogonalize(const Orthogonal &o, void *workspace, hipStream_t s);

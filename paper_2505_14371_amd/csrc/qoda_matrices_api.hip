@@ -194,6 +194,7 @@ int orthogonal_of(const qoda_orthogonalize_args *a, Orthogonal *o) {
   TRY(check_matrices(call, "x", a->x, a->matrices, a->rows, a->cols, e, &o->x_row, &o->x_matrix));
   o->g = a->g.data, o->x = a->x.data;
   o->a = a->a, o->b = a->b, o->c = a->c, o->eps = a->eps;
+  o->by_norm = orthogonal_by_norm(a->a, a->b, a->c, a->steps);
   orthogonal_sides(o);
   return QODA_OK;
 }

@@ -3,7 +3,9 @@
 // Small singular values grow by a in every step, and so do the errors of what they came from: sums of fp16 or bf16 products would leave them wrong in the
 // second digit.  A number is therefore a pair of fp16 numbers, high + low, of 22 bits, and a product three matrix instructions: high high, high low and
 // low high, summed in fp32.  Matrices are scaled by powers of two that the polynomial's bound on the singular values allows, so that the low parts are
-// no subnormal numbers where they matter.
+// no subnormal numbers where they matter: a number is held to 2^-22 of itself or 2^-41 of the bound.  Polynomials whose bound may be far above the numbers that are there (a
+// small or 0, or b s^3 and c s^5 growing) are taken by norm: in every step X and A are divided by what their norms are (at k_start_scales), which
+// takes longer: five steps of 8192 x 2048 2447 us, of 16 times 2100 x 410 1004, of 61 x 37 173.
 //
 // The work is done on X [m][n] with m <= n (g, or its transpose).  Every product is of rows with rows: X is kept beside its transpose, and A and
 // B = b A + c A A are symmetric, so that half of their tiles are computed and stored twice.  In memory 32 high parts of a row are followed by their low
@@ -73,13 +75,13 @@ __global__ void __launch_bounds__(kWg) k_squares(Orthogonal o) {
   if (threadIdx.x == 0) o.squares[id] = (part[0] + part[1]) + (part[2] + part[3]);
 }
 
-// 1 / (|g| + eps) of a matrix, from the parts' sums in their order.
-__device__ __forceinline__ double inverse_norm(const Orthogonal &o, long long matrix) {
+// |g| of a matrix, from the parts' sums in their order.
+__device__ __forceinline__ double norm_of(const double *squares, int parts, long long matrix) {
   double sum = 0.0;
-  for (int p = (int)(threadIdx.x & 63); p < o.parts; p += 64) sum = sum + o.squares[matrix * o.parts + p];
+  for (int p = (int)(threadIdx.x & 63); p < parts; p += 64) sum = sum + squares[matrix * parts + p];
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) sum = sum + __shfl_xor(sum, d);
-  return 1.0 / (sqrt(sum) + o.eps);
+  return sqrt(sum);
 }
 
 // X_0, scaled, and its transpose from g: 64 x 64 entries a workgroup, by way of shared memory.  STEPS false: nothing else is to be done, and x receives X_0.
@@ -88,7 +90,7 @@ __global__ void __launch_bounds__(kWg) k_start(Orthogonal o, long long tiles_r, 
   __shared__ float tile[64][65];
   const long long id = o.first + blockIdx.x, each = tiles_r * tiles_c, matrix = id / each, in = id - matrix * each;
   const long long r0 = in / tiles_c * 64, c0 = (in - in / tiles_c * tiles_c) * 64;
-  const double inverse = inverse_norm(o, matrix) * (STEPS ? (double)o.scale : 1.0);
+  const double inverse = 1.0 / (norm_of(o.squares, o.parts, matrix) + o.eps) * (STEPS ? (double)o.scale : 1.0);
   const T *g = static_cast<const T *>(o.g) + matrix * o.g_matrix;
   const int t = threadIdx.x, chunk = (t & 7) * 8;
 #pragma unroll
@@ -128,10 +130,27 @@ __global__ void __launch_bounds__(kWg) k_start(Orthogonal o, long long tiles_r, 
   }
 }
 
+// Of a step by norm: with n = |X|, Y = X / n, A' = Y Y^T, q = |A'| and A" = A' / q the next X is  n a Y + n^3 B' Y,  B' = q b A" + n^2 q^2 c A" A".  Y and A" are made from fp32 matrices by
+// k_start, so that what is held as pairs is near its bound whatever X's size, and |B'| <= |q b| + |n^2 q^2 c|, which a power of two brings below 2^15.  At first X = X_0.  A wave a matrix.
+__global__ void __launch_bounds__(kWg) k_start_scales(Orthogonal o, const double *squares_of_a, int parts_of_a, bool first) {
+  const long long matrix = (o.first + blockIdx.x) * (kWg / 64) + threadIdx.x / 64;
+  if (matrix >= o.matrices) return;
+  double n = norm_of(o.squares, o.parts, matrix);
+  const double q = norm_of(squares_of_a, parts_of_a, matrix);
+  if ((threadIdx.x & 63) != 0) return;
+  if (first) n = n / (n + o.eps);
+  const double b = o.b * q, c = o.c * (n * n * q * q), size = fabs(b) + fabs(c);
+  const int e = size > 0.0 && size < 1e300 ? 14 - ilogb(size) : 0;
+  float *s = o.scales + 4 * matrix;
+  s[0] = (float)ldexp(c, e), s[1] = (float)ldexp(b, e);
+  s[2] = (float)ldexp(n * n * n, -e), s[3] = (float)(n * o.a);
+}
+
 // What becomes of eight sums adjacent in a row: v = sums * factor + what E and E2 have there * extra and extra2, which is then stored as T's or as pairs.
 struct Place {
   const PairProduct &p;
   long long matrix;
+  const float *scales = nullptr;   // the matrix's own
   __device__ __forceinline__ void add(const void *e, float extra, int i, int j, float (&v)[8]) const {
     float was[8];
     load_pairs(pair_place(const_cast<char *>(static_cast<const char *>(e) + matrix * p.m * p.n * 4), p.n, i, j), was);
@@ -141,6 +160,13 @@ struct Place {
   __device__ __forceinline__ void finish(int i, int j, float (&v)[8]) const {
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = v[e] * p.factor;
+    if (scales) {   // one after the other: their product may be no normal number
+      float was[8] = {};
+      add(p.e, p.extra, i, j, was);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = __builtin_fmaf(was[e], scales[1], v[e] * scales[0]);
+      return;
+    }
     if (p.e) add(p.e, p.extra, i, j, v);
     if (p.e2) add(p.e2, p.extra2, i, j, v);
   }
@@ -330,7 +356,7 @@ __global__ void __launch_bounds__(N * 4) k_pair_join(PairProduct p, int splits) 
   int tm, tn;
   if (p.symmetric) upper_tile(in, tm, tn);
   else tm = (int)(in / tiles_n), tn = (int)(in - tm * tiles_n);
-  const Place place{p, matrix};
+  const Place place{p, matrix, p.scales ? p.scales + 4 * matrix : nullptr};
   const bool columns = place.columns_wanted() && !(p.symmetric && tm == tn);
   const int t = threadIdx.x, chunk = t % (N / 8) * 8;
 #pragma unroll
@@ -553,7 +579,7 @@ constexpr int kMostSmall = 163840 - 128;   // bytes of shared memory, less the s
 
 // How many pairs of pieces of X a wave has where the matrices go into shared memory, otherwise 0.
 int small_pairs(const Orthogonal &o) {
-  if (o.steps < 1 || o.steps > kMostSmallSteps || o.m > 1024 || o.n > 1024 || SmallPlaces((int)o.m, (int)o.n).all > kMostSmall) return 0;
+  if (o.by_norm || o.steps < 1 || o.steps > kMostSmallSteps || o.m > 1024 || o.n > 1024 || SmallPlaces((int)o.m, (int)o.n).all > kMostSmall) return 0;
   const int pairs = (int)(o.m * o.n / 512);
   return pairs <= kSmallWaves ? 1 : pairs <= 2 * kSmallWaves ? 2 : pairs <= 5 * kSmallWaves ? 5 : 0;
 }
@@ -626,7 +652,8 @@ void launch_join(const PairProduct &p, const Cut &c, hipStream_t s) {
 }
 
 void launch_pairs(PairProduct p, const Cut &c, float *partial, hipStream_t s) {
-  p.partial = c.splits > 1 ? partial : nullptr;
+  const bool joined = c.splits > 1 || p.scales;
+  p.partial = joined ? partial : nullptr;
   switch (c.tile) {
     case kTile64Ahead: launch_tiles<64, 2, 2, 3>(p, c, s); break;
     case kTile64: launch_tiles<64, 2, 2, 2>(p, c, s); break;
@@ -634,7 +661,7 @@ void launch_pairs(PairProduct p, const Cut &c, float *partial, hipStream_t s) {
     case kTile128: launch_tiles<128, 2, 2, 2>(p, c, s); break;
     case kTile256: launch_tiles<256, 2, 4, 2>(p, c, s); break;
   }
-  if (c.splits > 1) c.side % 64 == 0 ? launch_join<64>(p, c, s) : launch_join<32>(p, c, s);
+  if (joined) c.side % 64 == 0 ? launch_join<64>(p, c, s) : launch_join<32>(p, c, s);
 }
 
 // The three products of a step, without their operands' places.
@@ -642,7 +669,7 @@ PairProduct shape_of(const Orthogonal &o, int which) {
   PairProduct p = {};
   p.matrices = o.matrices;
   p.m = o.m, p.n = which == 2 ? o.n : o.m, p.k = which == 0 ? o.n : o.m;
-  p.symmetric = which != 2;
+  p.symmetric = which == 1 || (which == 0 && !o.by_norm);   // by norm A is an fp32 matrix, whose tiles are stored once
   return p;
 }
 
@@ -656,13 +683,19 @@ struct Cuts {   // of a step's products
     for (int w = 0; w < 3; ++w) c[w] = cut_of(shape_of(o, w));
   }
   bool two_at_once(const Orthogonal &o, int k) const {
-    if (o.steps - k < 2 || (o.type == kF32 ? o.steps - k != 2 : k == 0 || (o.steps - k) % 2 != 0)) return false;
+    if (o.by_norm || o.steps - k < 2 || (o.type == kF32 ? o.steps - k != 2 : k == 0 || (o.steps - k) % 2 != 0)) return false;
     return c[0].us + c[2].us > 3.0 * (c[1].us + 1.5);
   }
 };
 
+// How many workgroups sum up the squares of a matrix.
+int norm_parts(long long rows, long long cols) {
+  const long long eights = rows * ((cols + 7) / 8), parts = (eights + kWg * 8 - 1) / (kWg * 8);
+  return (int)(parts < 1 ? 1 : parts > 1024 ? 1024 : parts);
+}
+
 struct Layout {   // of the workspace, in bytes
-  size_t squares, xs, xt[2], a, b, c, d, partial, all;
+  size_t squares, squares_a, scales, xs, xt[2], a, b, c, d, x, partial, all;
 };
 Layout layout_of(const Orthogonal &o) {
   Layout l = {};
@@ -676,15 +709,22 @@ Layout layout_of(const Orthogonal &o) {
   l.squares = take(sizeof(double) * (size_t)o.matrices * o.parts);
   if (o.steps > 0) {
     const size_t wide = (size_t)o.matrices * o.m * o.n * 4, square = (size_t)o.matrices * o.m * o.m * 4;
-    l.xs = take(wide), l.xt[0] = take(wide), l.xt[1] = take(wide);
+    l.xs = take(wide), l.xt[0] = take(wide);
+    if (!o.by_norm) l.xt[1] = take(wide);
     l.a = take(square), l.b = take(square);
+    if (o.by_norm) {
+      const long long x = o.rows * o.cols, a = o.m * o.m;
+      l.squares_a = take(sizeof(double) * (size_t)o.matrices * norm_parts(o.m, o.m));
+      l.scales = take(sizeof(float) * 4 * (size_t)o.matrices);
+      l.x = take(sizeof(float) * (size_t)o.matrices * (x > a ? x : a));
+    }
     const Cuts cuts(o);
     if (o.steps > 1 && cuts.two_at_once(o, o.steps - 2)) l.c = take(square), l.d = take(square);
     size_t most = 0;
     for (int w = 0; w < 3; ++w) {
       const PairProduct p = shape_of(o, w);
       const Cut &c = cuts.c[w];
-      const size_t bytes = c.splits > 1 ? (size_t)c.splits * p.matrices * p.m * p.n * 4 : 0;
+      const size_t bytes = c.splits > 1 || (o.by_norm && w > 0) ? (size_t)c.splits * p.matrices * p.m * p.n * 4 : 0;
       most = bytes > most ? bytes : most;
     }
     l.partial = take(most);
@@ -730,12 +770,85 @@ bool orthogonal_bounded(double a, double b, double c, int steps) {
   return true;
 }
 
+// Whether the bound may be more than a few times what small singular values come to, |a| a step: pairs then lose digits of fp32's 24 (a matrix of 2^24 entries has some 2^-12
+// of its norm in each, 2^29 times what a pair is held to).  Polynomials that bring singular values towards 1 stay below |a|.
+bool orthogonal_by_norm(double a, double b, double c, int steps) {
+  constexpr double kTimes = 4.0, kSmall = 1.0 / (1 << 20);
+  double s = 1.0, small = 1.0;
+  for (int k = 0; k < steps; ++k) {
+    if (std::fabs(a) < kLeast || largest_inner(b, c, s * s) > kTimes * std::fabs(a)) return true;
+    s = largest(a, b, c, s), small *= std::fabs(a);
+    if (k + 1 < steps && (s > kTimes * small || s < kSmall)) return true;
+  }
+  return false;
+}
+
 void orthogonal_sides(Orthogonal *o) {
   o->transposed = o->rows > o->cols;
   o->m = up32(o->transposed ? o->cols : o->rows), o->n = up32(o->transposed ? o->rows : o->cols);
-  const long long eights = o->rows * ((o->cols + 7) / 8), parts = (eights + kWg * 8 - 1) / (kWg * 8);
-  o->parts = (int)(parts < 1 ? 1 : parts > 1024 ? 1024 : parts);
+  o->parts = norm_parts(o->rows, o->cols);
 }
+
+namespace {
+
+void launch_start(const Orthogonal &o, hipStream_t s) {
+  in_launches(o, o.matrices * o.parts, kWg, [&](const Orthogonal &part, unsigned x) {
+    if (o.type == kF32) k_squares<float><<<dim3(x), kWg, 0, s>>>(part);
+    else k_squares<bf16><<<dim3(x), kWg, 0, s>>>(part);
+  });
+  const long long tr = (o.rows + 63) / 64, tc = (o.cols + 63) / 64;
+  in_launches(o, o.matrices * tr * tc, kWg, [&](const Orthogonal &part, unsigned x) {
+    if (o.steps == 0) {
+      if (o.type == kF32) k_start<float, false><<<dim3(x), kWg, 0, s>>>(part, tr, tc);
+      else k_start<bf16, false><<<dim3(x), kWg, 0, s>>>(part, tr, tc);
+    } else {
+      if (o.type == kF32) k_start<float, true><<<dim3(x), kWg, 0, s>>>(part, tr, tc);
+      else k_start<bf16, true><<<dim3(x), kWg, 0, s>>>(part, tr, tc);
+    }
+  });
+}
+
+// All steps by norm.
+void launch_by_norm(const Orthogonal &o, const Layout &l, char *w, hipStream_t s) {
+  constexpr int kPower = 15;   // numbers of size 1 are held times 2^15
+  constexpr double kNothing = 1e-300;   // beside a norm: a matrix of zeros stays one
+  const float down = std::ldexp(1.0f, -kPower);
+  const Cuts cuts(o);
+  float *partial = reinterpret_cast<float *>(w + l.partial);
+  Orthogonal x = o, y, a = o;
+  x.scales = reinterpret_cast<float *>(w + l.scales);
+  a.type = kF32, a.transposed = 0, a.rows = a.cols = o.m, a.n = o.m;
+  a.g = w + l.x, a.g_row = o.m, a.g_matrix = o.m * o.m;
+  a.squares = reinterpret_cast<double *>(w + l.squares_a), a.parts = norm_parts(o.m, o.m);
+  a.xs = w + l.a, a.xt = w + l.b;   // its transpose, the same, is overwritten by B
+  a.eps = kNothing, a.scale = 1 << kPower;
+  for (int k = 0; k < o.steps; ++k) {
+    if (k > 0) x.g = w + l.x, x.type = kF32, x.g_row = o.cols, x.g_matrix = o.rows * o.cols;   // from the step before
+    y = x, y.eps = kNothing, y.scale = 1 << kPower;
+    launch_start(y, s);
+    PairProduct p = shape_of(o, 0);   // A'
+    p.a = p.b = o.xs;
+    p.factor = down * down;
+    p.x = w + l.x, p.x_row = p.x_rows = p.x_cols = o.m, p.x_matrix = o.m * o.m, p.type = kF32;
+    launch_pairs(p, cuts.c[0], partial, s);
+    launch_start(a, s);
+    in_launches(x, (o.matrices + kWg / 64 - 1) / (kWg / 64), kWg,
+                [&](const Orthogonal &part, unsigned grid) { k_start_scales<<<dim3(grid), kWg, 0, s>>>(part, a.squares, a.parts, k == 0); });
+    p = shape_of(o, 1);               // B'
+    p.a = p.b = p.e = w + l.a, p.out = p.out_t = w + l.b;
+    p.factor = down * down, p.extra = down, p.scales = x.scales;
+    launch_pairs(p, cuts.c[1], partial, s);
+    p = shape_of(o, 2);               // n a Y + n^3 B' Y
+    p.a = w + l.b, p.b = o.xt, p.e = o.xs;
+    p.factor = p.extra = down, p.scales = x.scales + 2;
+    const bool last = k + 1 == o.steps;
+    p.x = last ? o.x : w + l.x, p.x_matrix = last ? o.x_matrix : o.rows * o.cols, p.x_row = last ? o.x_row : o.cols, p.type = last ? o.type : kF32;
+    p.x_rows = o.rows, p.x_cols = o.cols, p.x_transposed = o.transposed;
+    launch_pairs(p, cuts.c[2], partial, s);
+  }
+}
+
+}  // namespace
 
 size_t orthogonal_scratch(const Orthogonal &o) { return layout_of(o).all; }
 
@@ -774,20 +887,11 @@ hipError_t launch_orthogonalize(const Orthogonal &call, void *workspace, hipStre
     });
     return hipGetLastError();
   }
-  in_launches(o, o.matrices * o.parts, kWg, [&](const Orthogonal &part, unsigned x) {
-    if (o.type == kF32) k_squares<float><<<dim3(x), kWg, 0, s>>>(part);
-    else k_squares<bf16><<<dim3(x), kWg, 0, s>>>(part);
-  });
-  const long long tr = (o.rows + 63) / 64, tc = (o.cols + 63) / 64;
-  in_launches(o, o.matrices * tr * tc, kWg, [&](const Orthogonal &part, unsigned x) {
-    if (o.steps == 0) {
-      if (o.type == kF32) k_start<float, false><<<dim3(x), kWg, 0, s>>>(part, tr, tc);
-      else k_start<bf16, false><<<dim3(x), kWg, 0, s>>>(part, tr, tc);
-    } else {
-      if (o.type == kF32) k_start<float, true><<<dim3(x), kWg, 0, s>>>(part, tr, tc);
-      else k_start<bf16, true><<<dim3(x), kWg, 0, s>>>(part, tr, tc);
-    }
-  });
+  if (o.by_norm) {
+    launch_by_norm(o, l, w, s);
+    return hipGetLastError();
+  }
+  launch_start(o, s);
   float *partial = reinterpret_cast<float *>(w + l.partial);
   if (o.steps == 0) return hipGetLastError();
   const Cuts cuts(o);

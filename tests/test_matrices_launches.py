@@ -172,3 +172,17 @@ def test_tiles_of_96_are_split(lib):
     """That the sizes above reach them."""
     for sizes in ((3, 672, 4000), (1, 1440, 2176)):
         assert (96, 32, True) in split_products(lib, *sizes)
+
+
+def test_orthogonalisation_by_norm(lib):
+    """Polynomials whose bound may be far above the singular values: norms of X and A in every step, whatever the size; a join of every product that has a matrix's own factors."""
+    step = ["k_squares<float>", "k_start<float,true>", "k_pair_product", "k_squares<float>", "k_start<float,true>", "k_start_scales", "k_pair_product", "k_pair_join", "k_pair_product", "k_pair_join"]
+    for n, rows, cols, dtype in ((3, 20, 30, 0), (1, 61, 37, 1), (40, 300, 410, 0)):
+        for co in ((0.0, 1.0, 0.0), (0.9, 0.9, 0.9), (1e-30, 1e-30, 0.0)):
+            args = mats._ORTHOGONALIZE.pack(dtype, 2, n, rows, cols, A, rows * cols, cols, A, rows * cols, cols, *co, 1e-7)
+            got = [k if k.startswith("k_s") else k.split("<")[0] for k, _, _ in launches(lib, "orthogonalize", args)]
+            first = [k.replace("float", "bf16") if dtype and at < 2 else k for at, k in enumerate(step)]
+            assert got == first + step, got
+    for co, steps in ((mats.QUINTIC, 5), (mats.QUINTIC, 1000), ((1.5, -0.5, 0.0), 100), ((2.0, -1.5, 0.5), 30), ((1.875, -1.25, 0.375), 30), ((1.0, 0.0, 0.0), 4), ((4.0848, -6.8946, 2.9270), 5)):
+        args = mats._ORTHOGONALIZE.pack(0, steps, 1, 300, 410, A, 0, 410, A, 0, 410, *co, 1e-7)          # the usual ones are not
+        assert "k_start_scales" not in [k for k, _, _ in launches(lib, "orthogonalize", args)], co

@@ -67,3 +67,9 @@ def test_polynomials_of_all_kinds(lib):
             assert taken(lib, (a, b, c), steps) == (v < 2.0**40), (a, b, c, steps, v)
             seen[int(v < 2.0**40)] += 1
     assert min(seen) > 70, seen
+
+
+def test_polynomials_that_the_gpu_tests_take(lib):
+    for co, steps in (((1.0, 10.0, 80.0), 2), ((0.9, 0.9, 0.9), 3), ((1.0, 1.0, 0.5), 3), ((0.0, 1.0, 0.0), 3), ((0.0, 0.0, 1.0), 2), ((0.5, 0.5, 0.0), 60), ((1e-30, 1e-30, 0.0), 1)):
+        assert taken(lib, co, steps), co
+    assert not taken(lib, (1.0, 1.0, 1.0), 3) and not taken(lib, (1.0, 100.0, 1000.0), 2)
