@@ -104,7 +104,8 @@ int qoda_mx_linear_weight_grad(const qoda_mx_linear_weight_grad_args *a, void *w
  * (a bound from a, b and c; otherwise QODA_EINVAL).  Accurate as fp32 products are: what the matrix cores take are pairs of fp16 numbers, 22 bits of a number or 2^-41 of a bound on it.
  * The bound is that of the polynomial where it stays near |a| a step, as for those that bring singular values towards 1; digits are then lost where |g| is less than 2^-8 eps.  For
  * others (a small or 0, or large singular values that grow faster than small ones) it is that of the norms that X and A have in each step, which takes longer.  The smaller side is at most
- * 2^17, the larger at most 2^22.  x may be g itself.  A matrix with an infinity or a NaN becomes NaN throughout, if steps > 0. */
+ * 2^17, the larger at most 2^22.  x may be g itself, with the same
+ * strides; where one lies in the other's entries otherwise, QODA_EINVAL.  A matrix with an infinity or a NaN becomes NaN throughout, if steps > 0. */
 typedef struct {
   void *data;
   int64_t matrix, row; /* entries from one matrix, and from one row, to the next */

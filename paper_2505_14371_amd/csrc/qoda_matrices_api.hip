@@ -4,6 +4,8 @@
 #include "qoda_matrices.h"
 #include "qoda_operators_checks.h"
 
+#include <cstdlib>
+
 using namespace qoda;
 
 namespace {
@@ -173,6 +175,31 @@ int check_matrices(const char *call, const char *name, const qoda_matrices &v, i
   return QODA_OK;
 }
 
+// Whether x is neither g itself nor apart from it: an entry of the one lies where another one of the other does.  Rows of one set are apart and in the order of their addresses.
+bool overlapping(const Orthogonal &o, size_t bytes) {
+  if (o.g == o.x && o.g_row == o.x_row && o.g_matrix == o.x_matrix) return false;
+  const long long off = ((intptr_t)o.x - (intptr_t)o.g) / (long long)bytes;   // of x's first entry from g's
+  const auto last = [&](long long matrix, long long row) { return (o.matrices - 1) * matrix + (o.rows - 1) * row + o.cols; };
+  if (off >= last(o.g_matrix, o.g_row) || -off >= last(o.x_matrix, o.x_row)) return false;
+  if (o.g_row == o.x_row && o.g_matrix == o.x_matrix) {   // the distances of matrices and of rows that come near `off`
+    const auto below = [](long long v, long long by) { return v >= 0 ? v / by : -((by - 1 - v) / by); };
+    const long long n0 = o.g_matrix ? below(off, o.g_matrix) : 0;
+    for (long long n = n0; n <= n0 + (o.g_matrix ? 1 : 0); ++n) {
+      const long long rest = off - n * o.g_matrix, i0 = below(rest, o.g_row);
+      for (long long i = i0; i <= i0 + 1; ++i)
+        if (n > -o.matrices && n < o.matrices && i > -o.rows && i < o.rows && std::llabs(rest - i * o.g_row) < o.cols) return true;
+    }
+    return false;
+  }
+  const long long rows = o.matrices * o.rows;
+  for (long long g = 0, x = 0; g < rows && x < rows;) {
+    const long long at = g / o.rows * o.g_matrix + g % o.rows * o.g_row, to = off + x / o.rows * o.x_matrix + x % o.rows * o.x_row;
+    if (at < to + o.cols && to < at + o.cols) return true;
+    at < to ? ++g : ++x;
+  }
+  return false;
+}
+
 int orthogonal_of(const qoda_orthogonalize_args *a, Orthogonal *o) {
   const char *call = "qoda_orthogonalize";
   if (!a) return fail(QODA_EINVAL, "%s: null arguments", call);
@@ -193,6 +220,7 @@ int orthogonal_of(const qoda_orthogonalize_args *a, Orthogonal *o) {
   TRY(check_matrices(call, "g", a->g, a->matrices, a->rows, a->cols, e, &o->g_row, &o->g_matrix));
   TRY(check_matrices(call, "x", a->x, a->matrices, a->rows, a->cols, e, &o->x_row, &o->x_matrix));
   o->g = a->g.data, o->x = a->x.data;
+  if (overlapping(*o, e)) return fail(QODA_EINVAL, "%s: x is neither g nor apart from it", call);
   o->a = a->a, o->b = a->b, o->c = a->c, o->eps = a->eps;
   o->by_norm = orthogonal_by_norm(a->a, a->b, a->c, a->steps);
   orthogonal_sides(o);

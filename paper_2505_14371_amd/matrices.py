@@ -340,7 +340,7 @@ def _matrices(t: torch.Tensor, like: torch.Tensor, name: str):
 
 def orthogonalize(g, *, steps=5, coefficients=QUINTIC, eps=1e-7, out=None, stream=None):
     """The matrices g [..., rows, columns] with their singular values brought towards 1: X = g / (|g| + eps), then ``steps`` times (1000 at most)
-    X <- a X + (b A + c A A) X with A = X X^T and (a, b, c) = coefficients.  Written to out, if given, which may be g; of g's type."""
+    X <- a X + (b A + c A A) X with A = X X^T and (a, b, c) = coefficients.  Written to out, if given, which may be g (or apart from it); of g's type."""
     if stream is not None:
         with _on(stream):
             return orthogonalize(g, steps=steps, coefficients=coefficients, eps=eps, out=out)
