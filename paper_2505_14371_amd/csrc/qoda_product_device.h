@@ -178,21 +178,15 @@ __device__ __forceinline__ void arrived() {
   __builtin_amdgcn_sched_barrier(0);
 }
 
-// ... behind which all but the last `left` steps' direct loads are done, of which each wave has LOADS a step; left is at most AHEAD.  Loads arrive in their
-// order.  (The branches are written out because the instruction takes a constant.)
+// ... behind which all but the last step's direct loads are done where `left` is more than 0 (then there are LOADS of them a wave), and with AHEAD = 0 always all.  Loads arrive in
+// their order.  (The branch is written out because the instruction takes a constant.)
 template <int LOADS, int AHEAD>
 __device__ __forceinline__ void arrived_but(int left) {
-  static_assert(AHEAD <= 2, "what is written out");
+  static_assert(AHEAD <= 1, "what is written out");
   if constexpr (AHEAD == 0) return arrived();
   __builtin_amdgcn_sched_barrier(0);
   left = __builtin_amdgcn_readfirstlane(left);
-  if constexpr (AHEAD == 1)
-    asm volatile("s_cmp_gt_i32 %0, 0\n\ts_cbranch_scc1 1f\n\ts_waitcnt vmcnt(0)\n1:\n\ts_waitcnt vmcnt(%1) lgkmcnt(0)" ::"s"(left), "n"(LOADS) : "memory", "scc");
-  if constexpr (AHEAD == 2)
-    asm volatile("s_cmp_gt_i32 %0, 0\n\ts_cbranch_scc1 1f\n\ts_waitcnt vmcnt(0)\n1:\n\ts_cmp_gt_i32 %0, 1\n\ts_cbranch_scc1 2f\n\ts_waitcnt vmcnt(%1)\n2:\n\t"
-                 "s_waitcnt vmcnt(%2) lgkmcnt(0)" ::"s"(left),
-                 "n"(LOADS), "n"(2 * LOADS)
-                 : "memory", "scc");
+  asm volatile("s_cmp_gt_i32 %0, 0\n\ts_cbranch_scc1 1f\n\ts_waitcnt vmcnt(0)\n1:\n\ts_waitcnt vmcnt(%1) lgkmcnt(0)" ::"s"(left), "n"(LOADS) : "memory", "scc");
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
   __builtin_amdgcn_sched_barrier(0);
