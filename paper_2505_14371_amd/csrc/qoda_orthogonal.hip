@@ -876,7 +876,7 @@ hipError_t launch_orthogonalize(const Orthogonal &call, void *workspace, hipStre
     in_launches(small, o.matrices, kSmallWg, [&](const SmallOrthogonal &part, unsigned x) {
       const auto go = [&](auto t) {
         typedef decltype(t) T;
-        // several workgroups a CU where they fit
+        // three workgroups a CU (by their registers) or two (by shared memory) where they fit
         if (pairs == 1 && bytes <= 40960 - 128) k_small<T, 1, 40960 - 128><<<dim3(x), kSmallWg, 0, s>>>(part);
         else if (pairs == 1 && bytes <= 81920 - 128) k_small<T, 1, 81920 - 128><<<dim3(x), kSmallWg, 0, s>>>(part);
         else if (pairs <= 2) k_small<T, 2, kMostSmall><<<dim3(x), kSmallWg, 0, s>>>(part);
