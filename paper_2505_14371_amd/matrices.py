@@ -13,8 +13,9 @@ scratch memory come from torch's allocator, on the stream that the call runs on 
     orthogonalize(g_w, out=g_w)                                                           # ... or its orthogonalised form
 
 An operand of a product has its blocks along what the product sums over, so that a matrix that is summed over both ways is rounded twice.  Plain
-rows in a product's first place are rounded to nearest inside the call; up to 16 of them take one launch.  ``activation``, ``p``, ``seed``, ``offset``, ``residual``, biases and gradients of parameters are as in ``operators``, and
-so is the refusal to be differentiated: outputs on tensors that require a gradient raise where torch asks for it.
+rows in a product's first place are rounded to nearest inside the call; up to 16 of them take one launch.  ``activation``, ``p``, ``seed``, ``offset``, ``residual``, biases and
+gradients of parameters are as in ``operators``.  Nothing is recorded for torch's differentiation, as there: outputs of ``mx_linear`` on tensors that require a gradient raise where torch asks
+for it, and tangents are refused; ``microscale`` and ``orthogonalize``, which have no gradient calls, refuse both at once; what the gradient calls return is plain.
 """
 from __future__ import annotations
 
