@@ -179,7 +179,7 @@ int check_matrices(const char *call, const char *name, const qoda_matrices &v, i
 bool overlapping(const Orthogonal &o, size_t bytes) {
   if (o.g == o.x && o.g_row == o.x_row && o.g_matrix == o.x_matrix) return false;
   const long long off = ((intptr_t)o.x - (intptr_t)o.g) / (long long)bytes;   // of x's first entry from g's
-  const auto last = [&](long long matrix, long long row) { return (o.matrices - 1) * matrix + (o.rows - 1) * row + o.cols; };
+  const auto last = [&](long long matrix, long long row) { return (__int128)(o.matrices - 1) * matrix + (o.rows - 1) * row + o.cols; };
   if (off >= last(o.g_matrix, o.g_row) || -off >= last(o.x_matrix, o.x_row)) return false;
   if (o.g_row == o.x_row && o.g_matrix == o.x_matrix) {   // the distances of matrices and of rows that come near `off`
     const auto below = [](long long v, long long by) { return v >= 0 ? v / by : -((by - 1 - v) / by); };
