@@ -7,10 +7,10 @@
 //
 // Both operands' pieces take every other four of eight rows: a lane then holds eight sums adjacent in a row of c.
 //
-// Measured: 16384 x 2048 over 8192 145 us (3.8 PFLOP/s), with dropout and residual 163; 8192 x 8192 over 2048 through gelu' 141; 6144 x 2048 over 8192 in fp32
-// 65.  With nothing loaded behind the first steps the first takes 121 us, and without reads of shared memory too 103: the matrix cores themselves reach 5.3
-// PFLOP/s.  Tiles of 256 take 1.8 us a step of 68 KB; tiles of 128, two a CU, are slower there (176) and faster where ends weigh more than steps, which they
-// overlap (2048 entries through gelu': 141 and 157).
+// Measured: 16384 x 2048 over 8192 135 to 145 us (3.8 to 4.1 PFLOP/s), with dropout and residual 151 to 163; 8192 x 8192 over 2048 through gelu' 142; 6144 x 2048 over 8192
+// in fp32 65.  With nothing loaded behind the first steps the first takes 121 us, and without reads of shared memory too 103, its start and end among them.  The
+// instruction by itself reaches 5.9 PFLOP/s on random codes (6.9 on zeros: power is the limit), the one of 32 x 32 x 64 6.7 (9.8).  Tiles of 256 take 1.8 us a step of
+// 68 KB; tiles of 128, two a CU, are slower there (176) and faster where ends weigh more than steps, which they overlap (2048 entries through gelu': 141 and 157).
 
 #include <utility>
 

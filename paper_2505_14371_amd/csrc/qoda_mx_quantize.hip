@@ -4,8 +4,8 @@
 // As it lies: eight entries a lane, 16 or 32 bytes, a block's largest magnitude joined over its four lanes.  Transposed: a lane takes two columns
 // of x over 32 rows, a block each, so that nothing is joined, and the codes pass through shared memory to be stored as rows.
 //
-// Measured, 16384 x 8192 of bf16 (268 MB, and 71 of codes and scales): to nearest 64 us as it lies (5.3 TB/s, memory) and 75 transposed, stochastically 88 and
-// 81 (arithmetic: the generator is twelve operations an entry and the code ten); values 55 to 61.  Of fp32 110 and 131, 117 and 132, values 152.
+// Measured, 16384 x 8192 of bf16 (268 MB, and 71 of codes and scales): to nearest 64 us as it lies (5.3 TB/s, memory) and 76 transposed, stochastically 84 to 105 and
+// 77 to 92, the first passes after idle ones the longest (arithmetic: the generator is twelve operations an entry and the code ten); values 55 to 63.  Of fp32 111 and 130, 111 and 132, values 152.
 
 #include "qoda_mx_device.h"
 

@@ -11,8 +11,8 @@
 // B = b A + c A A are symmetric, so that half of their tiles are computed and stored twice.  In memory 32 high parts of a row are followed by their low
 // parts, 128 bytes, which is a step along l in shared memory, as in qoda_linear.hip.  Sides are filled up to multiples of 32 with zeros.
 //
-// Measured, five steps: 8192 x 2048 of fp32 1473 us, of which A 4 times 98 and its join 16, the squares of 2048 8 times 38, the four products with X 178 each (375
-// TFLOP/s of numbers, 1130 of halves: the library's product of halves reaches 1154) and the start 55; 16 of 2100 x 410 495; 61 x 37 of bf16 19, all in one
+// Measured, five steps: 8192 x 2048 of fp32 1484 to 1550 us, of which A 4 times 98 and its join 16, the squares of 2048 8 times 38, the four products with X 178 each (375
+// TFLOP/s of numbers, 1130 of halves: the library's product of halves reaches 1154) and the start 55; 16 of 2100 x 410 471 to 523; 61 x 37 of bf16 19, all in one
 // launch.  Error against 64 bits of 8192 x 2048: 2.8e-6 (fp32 products 3.0e-6).
 
 #include <cmath>
