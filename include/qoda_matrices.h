@@ -100,12 +100,12 @@ int qoda_mx_linear_weight_grad(const qoda_mx_linear_weight_grad_args *a, void *w
 
 /* x = the orthogonalised g, matrix by matrix of a batch: entry (n, i, j) is data[n * matrix + i * row + j].
  *   X_0 = g / (|g| + eps), |g| the root of the sum of squares;  A = X X^T,  X <- a X + (b A + c A A) X, steps times;
- * where g has more rows than columns X^T takes X's place, with the same result.  steps is at most QODA_MAX_STEPS, a, b, c are finite, and the singular values stay below 2^40 for every g
- * (a bound from a, b and c; otherwise QODA_EINVAL).  Accurate as fp32 products are: what the matrix cores take are pairs of fp16 numbers, 22 bits of a number or 2^-41 of a bound on it.
- * The bound is that of the polynomial where it stays near |a| a step, as for those that bring singular values towards 1; digits are then lost where |g| is less than 2^-8 eps.  For
- * others (a small or 0, or large singular values that grow faster than small ones) it is that of the norms that X and A have in each step, which takes longer.  The smaller side is at most
- * 2^17, the larger at most 2^22.  x may be g itself, with the same
- * strides; where one lies in the other's entries otherwise, QODA_EINVAL.  A matrix with an infinity or a NaN becomes NaN throughout, if steps > 0. */
+ * where g has more rows than columns X^T takes X's place, with the same result.  steps is at most QODA_MAX_STEPS, a, b, c are finite, and the singular values stay
+ * below 2^40 for every g (a bound from a, b and c; otherwise QODA_EINVAL).  The smaller side is at most 2^17, the larger at most 2^22.  x may be g itself, with the
+ * same strides; where one lies in the other's entries otherwise, QODA_EINVAL.  A matrix with an infinity or a NaN becomes NaN throughout, if steps > 0.
+ * Accurate as fp32 products are: what the matrix cores take are pairs of fp16 numbers, 22 bits of a number or 2^-41 of a bound on it.  The bound is that of the
+ * polynomial where it stays near |a| a step, as for those that bring singular values towards 1; digits are then lost where |g| is less than 2^-8 eps.  For others (a
+ * small or 0, or large singular values that grow faster than small ones) it is that of the norms that X and A have in each step, which takes longer. */
 typedef struct {
   void *data;
   int64_t matrix, row; /* entries from one matrix, and from one row, to the next */
